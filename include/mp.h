@@ -405,6 +405,80 @@ int mp_attention_bwd_ldp(int n_seq, int n_heads, int seq_len, int d_head, const 
                          const mp_half* p, int ld_p, const mp_half* dctx, int ld_ctx, mp_half* dqkv, int ld_dqkv,
                          mp_stream stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Attention under a mask, for any length (Section 3.1 arithmetic: fp16 operands, fp32 sums; Section 3.2: the softmax is an
+ * fp32 part).  Scores and probabilities never reach memory, so no [length, length] tensor is kept.
+ *
+ * A mask is one interval of keys per query row: row r sees keys lo[r] <= c < hi[r], and nothing where lo[r] >= hi[r].  Documents
+ * packed side by side, causal order, prefixes that see themselves whole and sliding windows are all of this form.  It is prepared
+ * once per batch in `mask` (device, mp_attention_mask_bytes(rows_q) bytes, 16-byte aligned) and serves every layer and head.
+ * ------------------------------------------------------------------------------------------ */
+size_t mp_attention_mask_bytes(int rows_q); /* 0 for a negative number of rows */
+
+/* Mask of self-attention over `rows` rows that hold n_docs documents: document b has rows [doc_start[b], doc_start[b+1])
+ * (doc_start: device int32, n_docs + 1 values, ascending; empty documents are fine).  Rows of no document see nothing.
+ *   causal  nonzero: row r sees its document's rows up to r;  zero: the whole document.
+ *   prefix  device int32 [n_docs] or NULL: the first prefix[b] rows of document b are seen by all of it (causal only).
+ *   window  0: none; w > 0: of these, only rows closer than w (|r - c| < w).  Not together with prefix. */
+int mp_attention_mask_docs(int rows, int n_docs, const int32_t* doc_start, const int32_t* prefix, int causal, int window,
+                           void* mask, mp_stream stream);
+/* Mask from the intervals themselves: lo, hi device int32 [rows_q], cut to [0, rows_k]. */
+int mp_attention_mask_ranges(int rows_q, int rows_k, const int32_t* lo, const int32_t* hi, void* mask, mp_stream stream);
+
+/* q[rows_q, ld_q], k[rows_k, ld_k], v[rows_k, ld_v], ctx[rows_q, ld_ctx]: head h owns columns [h d_head, (h+1) d_head) of q and
+ * ctx; heads h n_kv_heads / n_heads (rounded down) share the columns of one key / value head.  The gradients have leading
+ * dimensions of their own.  A fused projection is three pointers into one matrix. */
+typedef struct mp_attn_desc {
+    int32_t rows_q, rows_k;
+    int32_t n_heads, n_kv_heads, d_head;  /* n_kv_heads divides n_heads; d_head a multiple of 8 up to 128 */
+    int32_t ld_q, ld_k, ld_v, ld_ctx;     /* multiples of 8, as are those of the gradients                */
+    int32_t ld_dq, ld_dk, ld_dv, ld_dctx;
+    float   alpha;                        /* > 0                                                          */
+    float   cap;                          /* 0: none                                                      */
+    int32_t reserved;                     /* 0                                                            */
+} mp_attn_desc;
+
+/*     t = alpha q k^T;   s = cap tanh(t / cap)  (cap > 0), else t;   s -= slopes[h] |r - c|  (slopes given)
+ *     p = softmax_fp32 of s over the keys that the row sees;   ctx = RNE16(p v);   lse = log(sum exp(s))
+ * slopes: device fp32 [n_heads] or NULL.  lse: device fp32 [n_heads, rows_q], kept for the backward call.  A row that sees nothing
+ * has ctx 0 and lse -inf.  Scores stay fp32; the exponentials enter the second product rounded to fp16, unnormalised (none is
+ * above 1, the row's largest is 1).
+ * What a row does not see does not reach it, NaN and infinities included; of a value row that holds one, those rows that see it get
+ * non-finite results.  All rows of ctx are written.  Any rows_k >= 0 and rows_q >= 0.
+ * 16-byte aligned matrices with leading dimensions in multiples of 8 and a d_head as above; otherwise MP_E_UNSUPPORTED. */
+int mp_attention_masked_fwd(const mp_attn_desc* desc /* host */, const void* mask, const mp_half* q, const mp_half* k,
+                            const mp_half* v, const float* slopes, mp_half* ctx, float* lse, mp_stream stream);
+
+/* Gradients of the above, from its inputs and results (delta = sum_d dctx ctx in fp32 from the stored ctx):
+ *     dp = dctx v^T,  ds = p (dp - delta) (1 - tanh(t / cap)^2)     (fp32, then rounded to fp16 as an operand)
+ *     dq = RNE16(alpha ds k),  dk = RNE16(alpha ds^T q),  dv = RNE16(p^T dctx),  dk and dv summed over the heads that share them.
+ * Every row of dq, dk and dv is written (0 where no pair is left).  The sums' order is fixed: two calls give the same bits.  None of
+ * the outputs may overlap an input.  ws: device, 16-byte aligned, mp_attention_masked_bwd_workspace_bytes(desc) bytes (0 for a
+ * description that the calls refuse). */
+size_t mp_attention_masked_bwd_workspace_bytes(const mp_attn_desc* desc /* host */);
+int mp_attention_masked_bwd(const mp_attn_desc* desc /* host */, const void* mask, const mp_half* q, const mp_half* k,
+                            const mp_half* v, const float* slopes, const mp_half* ctx, const float* lse, const mp_half* dctx,
+                            mp_half* dq, mp_half* dk, mp_half* dv, void* ws, size_t ws_bytes, mp_stream stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Embedding: rows of a table w[vocab, d] by token (the other end of the vocabulary projection).
+ * ------------------------------------------------------------------------------------------ */
+/* y[t] = RNE16(scale w[tokens[t]]); a token outside [0, vocab) gives a zero row.  w, y contiguous, at any element.  tokens: device
+ * int32 [rows]. */
+int mp_embedding_fwd(int rows, int vocab, int d, const int32_t* tokens, const mp_half* w, float scale, mp_half* y,
+                     mp_stream stream);
+
+/* dw[v] = RNE16(scale sum over t with tokens[t] = v of dy[t]): fp32 sums of the tokens sorted by value (of equal ones by
+ * position), in an order that the tokens alone decide.  Rows without a token are zero; tokens outside [0, vocab) are left out.
+ *   add   device fp16 [vocab, d] or NULL: a second gradient of the same table (a projection that shares it); then
+ *         dw = RNE16(RNE16(scale sum) + add), as if both had been stored.  dw may be add.
+ *   st    as for mp_gemm_bwd_dw.   dw may not overlap dy.
+ *   ws    device, 16-byte aligned, mp_embedding_bwd_workspace_bytes(rows, vocab, d) bytes.
+ * rows up to 2^24, vocab up to 2^21 - 1; otherwise MP_E_UNSUPPORTED. */
+size_t mp_embedding_bwd_workspace_bytes(int rows, int vocab, int d);
+int mp_embedding_bwd(int rows, int vocab, int d, const int32_t* tokens, const mp_half* dy, float scale, const mp_half* add,
+                     mp_half* dw, mp_scale_state* st, void* ws, size_t ws_bytes, mp_stream stream);
+
 /* LSTM cell, gate blocks ordered (i, f, g, o) in gates[B, 4H] (leading dimension ldg):
  *   c = sigma(f) c_prev + sigma(i) tanh(g)   (fp32, never rounded),  h = RNE16( sigma(o) tanh(c) ).
  * c_prev, c: device fp32 [B, H] contiguous.  h is written to h_out (ld ldh) and, if h_out2 != NULL,
@@ -519,7 +593,8 @@ int mp_mfma_sustained_rate(const mp_half* operands, size_t n_operands, float* si
  * Optimizer wrapper (Section 3.2) with the gradient inspection of Section 3.1 and the fp32-side
  * regulariser of Section 3.3.
  * ------------------------------------------------------------------------------------------ */
-enum { MP_OPT_SGD = 0, MP_OPT_ADAM = 1 };
+enum { MP_OPT_SGD = 0, MP_OPT_ADAM = 1,
+       MP_OPT_ADAMW = 2 /* Adam whose decay acts on the master itself, not through the moments */ };
 enum { MP_UPDATE_DEFAULT = 0,
        MP_UPDATE_PRECHECKED = 1 /* every gradient was produced by a call given `st`: skip the
                                    separate inspection pass and trust st->found_inf */ };
@@ -534,12 +609,13 @@ typedef struct mp_tensor_desc {
 } mp_tensor_desc;
 
 typedef struct mp_opt_cfg {
-    int32_t kind;         /* MP_OPT_SGD | MP_OPT_ADAM */
+    int32_t kind;         /* MP_OPT_SGD | MP_OPT_ADAM | MP_OPT_ADAMW */
     int32_t reserved;
     double  lr;           /* hyper-parameters are given in double; the kernel uses their fp32   */
     double  beta1, beta2; /* roundings, except that the bias corrections 1 - beta^t are formed  */
     double  eps;          /* in double from the double betas and then rounded to fp32           */
     double  weight_decay; /* L2 coefficient applied to the fp32 master: g += wd * w32           */
+                          /* (MP_OPT_ADAMW: w32 -= lr wd w32, lr wd formed in double)           */
 } mp_opt_cfg;
 
 /* One call covers every parameter tensor, because the skip decision is global.
@@ -550,6 +626,7 @@ typedef struct mp_opt_cfg {
  *            SGD : w32 -= lr g
  *            Adam: m = b1 m + (1-b1) g;  v = b2 v + (1-b2) g^2;  t = st->opt_step + 1
  *                  w32 -= lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
+ *            AdamW: g without wd * w32;  w32 -= (lr wd) w32;  then as Adam
  *            w16 = RNE16(w32)
  *            else nothing is written.
  * `tensors` is a host array of ntensors descriptors (device pointers inside), copied into kernel
@@ -565,6 +642,42 @@ int mp_unscale_check_update(const mp_tensor_desc* tensors /* host */, int ntenso
 size_t mp_update_counters_bytes(void);
 int mp_unscale_check_update_end(const mp_tensor_desc* tensors /* host array */, int ntensors, const mp_opt_cfg* cfg, mp_scale_state* st,
                                 int flags, const mp_mean_parts* parts, float* loss, int32_t* counters, mp_stream stream);
+
+/* ------------------------------------------------------------------------------------------
+ * The update with Adam's moments in 8 bits (4 bytes a parameter of state and traffic instead of 16): blocks of MP_STATE8_BLOCK
+ * consecutive elements of a tensor share one fp32 scale for m and one for v.
+ *     m = sm q |q| / 127^2,          q = -127 .. 127, sm the block's largest |m|
+ *     v = (sv (q / 255)^2)^2,        q = 0 .. 255,    sv the block's largest sqrt(v);  q = 0 only where v = 0
+ * The codes are even in sqrt(|m|) and in the fourth root of v, so that a value far below the block's largest keeps its magnitude
+ * (at a hundredth of the largest m a step is a sixth of the value).  New states are all zero bytes.
+ * ------------------------------------------------------------------------------------------ */
+#define MP_STATE8_BLOCK 256
+
+typedef struct mp_tensor_desc8 {
+    const mp_half* g16; /* device: as in mp_tensor_desc                             */
+    float*         w32;
+    mp_half*       w16;
+    int8_t*        m8;  /* device: codes of m                                       */
+    uint8_t*       v8;  /* device: codes of v                                       */
+    float*         ms;  /* device: scales, (n + MP_STATE8_BLOCK - 1) / MP_STATE8_BLOCK each */
+    float*         vs;
+    size_t         n;
+} mp_tensor_desc8;
+
+/* mp_unscale_check_update and mp_unscale_check_update_end for such tensors; cfg->kind is MP_OPT_ADAM or MP_OPT_ADAMW.  Per element
+ * in fp32, operation by operation, t = st->opt_step + 1, the coefficients formed in double and rounded:
+ *     Adam : g = float(g16) inv_scale + wd w32          AdamW : g = float(g16) inv_scale;  w32 -= (lr wd) w32
+ *     m = b1 (float(q |q|) (sm (1 / 127^2))) + (1 - b1) g,   r = float(q q) (sv (1 / 255^2)),   v = b2 (r r) + (1 - b2) (g g)
+ *     w32 -= ((lr / (1 - b1^t)) m) / (sqrt(v) (1 / sqrt(1 - b2^t)) + eps),   w16 = RNE16(w32)
+ *     sm = max |m|, sv = max sqrt(v) over the block;  codes: sqrt(|m| (127^2 / sm)) and sqrt(sqrt(v) (255^2 / sv)), rounded to
+ *     nearest even and cut to their range, the latter at least 1 where v > 0.  A scale of 2^-100 or less is stored as 0, with codes 0. */
+int mp_unscale_check_update8(const mp_tensor_desc8* tensors /* host */, int ntensors, const mp_opt_cfg* cfg /* host */,
+                             mp_scale_state* st, int flags, mp_stream stream);
+int mp_unscale_check_update8_end(const mp_tensor_desc8* tensors /* host */, int ntensors, const mp_opt_cfg* cfg, mp_scale_state* st,
+                                 int flags, const mp_mean_parts* parts, float* loss, int32_t* counters, mp_stream stream);
+/* The values that n codes stand for, in fp32 (either pair of outputs and codes may be NULL).  n counts from a block's first element. */
+int mp_state8_decode(size_t n, const int8_t* m8, const float* ms, const uint8_t* v8, const float* vs, float* m, float* v,
+                     mp_stream stream);
 
 #ifdef __cplusplus
 }

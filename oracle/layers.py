@@ -133,6 +133,83 @@ def attention_bwd(P: Policy, dctx, cache):
     return np.concatenate([_unheads(dq), _unheads(dk_), _unheads(dv)], axis=1)
 
 
+def attention_ranges(rows, doc_start, causal=False, prefix=None, window=0):
+    """Interval [lo, hi) of rows that each of `rows` rows sees: its document [doc_start[b], doc_start[b+1]); causal: up to itself,
+    and the document's first prefix[b] rows; window: of these the ones closer than `window`.  Rows of no document see nothing."""
+    lo, hi = np.zeros(rows, np.int64), np.zeros(rows, np.int64)
+    for b in range(len(doc_start) - 1):
+        for r in range(int(doc_start[b]), int(doc_start[b + 1])):
+            lo[r], hi[r] = doc_start[b], doc_start[b + 1]
+            if causal:
+                hi[r] = r + 1
+                if prefix is not None:
+                    hi[r] = max(r + 1, min(doc_start[b] + prefix[b], doc_start[b + 1]))
+            if window:
+                lo[r], hi[r] = max(lo[r], r - window + 1), min(hi[r], r + window)
+    return lo, hi
+
+
+def masked_attention_fwd(P: Policy, q, k, v, lo, hi, n_heads, n_kv_heads, cap=0.0, slopes=None):
+    """Attention where row r sees keys [lo[r], hi[r]); q[rows, h dk], k and v[keys, kv_heads dk], heads share key / value heads in
+    order.  t = q k^T / sqrt(dk), s = cap tanh(t / cap) if cap, s -= slopes[h] |r - c|; p = softmax(s) over what is seen;
+    ctx = store(p v), the scores and probabilities staying in the arithmetic type.  A row that sees nothing gives 0."""
+    g, dk = n_heads // n_kv_heads, q.shape[1] // n_heads
+    split = lambda t, n: t.reshape(t.shape[0], n, dk).transpose(1, 0, 2)  # noqa: E731
+    q3, k3, v3 = split(q, n_heads), np.repeat(split(k, n_kv_heads), g, 0), np.repeat(split(v, n_kv_heads), g, 0)
+    alpha = P.scalar(1.0 / np.sqrt(float(dk)))
+    c = np.arange(k.shape[0])[None, :]
+    seen = (c >= np.asarray(lo)[:, None]) & (c < np.asarray(hi)[:, None])
+    t = alpha * (q3 @ k3.transpose(0, 2, 1))
+    th = np.tanh(t / P.scalar(cap)) if cap else None
+    s = P.scalar(cap) * th if cap else t
+    if slopes is not None:
+        s = s - np.asarray(slopes, P.acc)[:, None, None] * np.abs(np.arange(q.shape[0])[:, None] - c).astype(P.acc)
+    s = np.where(seen, s, P.scalar(-np.inf))
+    top = s.max(-1, keepdims=True, initial=-np.inf)
+    e = np.where(seen, np.exp(s - np.where(np.isinf(top), P.scalar(0), top)), P.scalar(0))
+    total = e.sum(-1, keepdims=True, dtype=P.acc)
+    p = e / np.where(total == 0, P.scalar(1), total)
+    with np.errstate(divide="ignore"):
+        lse = (top + np.log(total))[..., 0]
+    ctx = P.store((p @ v3).transpose(1, 0, 2).reshape(q.shape))
+    return ctx, dict(q=q3, k=k3, v=v3, p=p, th=th, alpha=alpha, g=g, lse=lse, ctx=ctx)
+
+
+def masked_attention_bwd(P: Policy, dctx, cache):
+    """dp = dctx v^T, ds = p (dp - sum_d dctx ctx) (1 - tanh^2), dq = alpha ds k, dk = alpha ds^T q, dv = p^T dctx; dk and dv summed
+    over the heads that share them; each gradient a stored tensor.  Returns (dq, dk, dv)."""
+    q, k, v, p, alpha, g = (cache[n] for n in ("q", "k", "v", "p", "alpha", "g"))
+    h, rows, dk_ = q.shape
+    split = lambda t: t.reshape(rows, h, dk_).transpose(1, 0, 2)  # noqa: E731
+    do, ctx = split(dctx), split(cache["ctx"])
+    ds = p * (do @ v.transpose(0, 2, 1) - (do * ctx).sum(-1, keepdims=True, dtype=P.acc))
+    if cache["th"] is not None:
+        ds = ds * (P.scalar(1) - cache["th"] * cache["th"])
+    cache["ds"] = ds
+    shared = lambda t: t.reshape(h // g, g, t.shape[1], dk_).sum(1, dtype=P.acc)  # noqa: E731
+    flat = lambda t: t.transpose(1, 0, 2).reshape(t.shape[1], t.shape[0] * t.shape[2])  # noqa: E731
+    dq = P.store(flat(alpha * (ds @ k)))
+    dk = P.store(flat(shared(alpha * (ds.transpose(0, 2, 1) @ q))))
+    dv = P.store(flat(shared(p.transpose(0, 2, 1) @ do)))
+    return dq, dk, dv
+
+
+# ---------------------------------------------------------------- embedding
+def embedding_fwd(P: Policy, tokens, w, scale):
+    """y[t] = store(scale w[tokens[t]]); a token outside the table gives a zero row."""
+    there = (tokens >= 0) & (tokens < w.shape[0])
+    return P.store(np.where(there[:, None], P.scalar(scale) * w[np.where(there, tokens, 0)], P.scalar(0)))
+
+
+def embedding_bwd(P: Policy, tokens, dy, vocab, scale):
+    """dw[v] = store(scale sum of dy[t] over the tokens t that are v)."""
+    dw = np.zeros((vocab, dy.shape[1]), P.acc)
+    for t, v in enumerate(tokens):
+        if 0 <= v < vocab:
+            dw[v] += dy[t]
+    return P.store(P.scalar(scale) * dw)
+
+
 # ---------------------------------------------------------------- losses
 def mse_scaled(P: Policy, y, target, scale):
     """L = mean((y - target)^2) (arithmetic type, reported unscaled);

@@ -57,6 +57,7 @@ def unscale_check_update(P: Policy, tensors: List[Dict[str, np.ndarray]], opt, s
         SGD : w32 -= lr * g
         Adam: m = b1 m + (1-b1) g ; v = b2 v + (1-b2) g^2 ;  t = opt_step + 1
               w32 -= lr * (m / (1-b1^t)) / (sqrt(v / (1-b2^t)) + eps)
+        AdamW: g without the decay;  w32 -= (lr weight_decay) w32;  then as Adam
         w16 = store(w32)
     Scalars (1-b1, 1-b2, bias corrections) are formed in double and cast.
     """
@@ -65,18 +66,20 @@ def unscale_check_update(P: Policy, tensors: List[Dict[str, np.ndarray]], opt, s
     A = P.scalar
     inv_s = A(1) / A(st.scale)
     lr, wd = A(opt.lr), A(opt.weight_decay)
-    if opt.kind == "adam":
+    if opt.kind in ("adam", "adamw"):
         t = st.opt_step + 1
         b1, b2, eps = A(opt.beta1), A(opt.beta2), A(opt.eps)
         omb1, omb2 = A(1.0 - opt.beta1), A(1.0 - opt.beta2)
         bc1, bc2 = A(1.0 - float(opt.beta1) ** t), A(1.0 - float(opt.beta2) ** t)
     for tn in tensors:
         g = tn["g16"] * inv_s
-        if opt.weight_decay != 0.0:
+        if opt.kind == "adamw":
+            tn["w32"][...] = tn["w32"] - A(float(opt.lr) * float(opt.weight_decay)) * tn["w32"]
+        elif opt.weight_decay != 0.0:
             g = g + wd * tn["w32"]
         if opt.kind == "sgd":
             tn["w32"][...] = tn["w32"] - lr * g
-        elif opt.kind == "adam":
+        elif opt.kind in ("adam", "adamw"):
             tn["m"][...] = b1 * tn["m"] + omb1 * g
             tn["v"][...] = b2 * tn["v"] + omb2 * (g * g)
             mhat = tn["m"] / bc1
@@ -84,6 +87,66 @@ def unscale_check_update(P: Policy, tensors: List[Dict[str, np.ndarray]], opt, s
             tn["w32"][...] = tn["w32"] - lr * mhat / (np.sqrt(vhat) + eps)
         else:
             raise ValueError(opt.kind)
+        tn["w16"][...] = P.store(tn["w32"])
+    return 0
+
+
+STATE8_BLOCK = 256
+
+
+def _blocks(x, P: Policy):
+    x = np.asarray(x, P.acc).reshape(-1)
+    return np.concatenate([x, np.zeros(-x.size % STATE8_BLOCK, P.acc)]).reshape(-1, STATE8_BLOCK)
+
+
+def state8_decode(P: Policy, codes, scales, second):
+    """Values of 8-bit codes: m = sm q |q| / 127^2, and (second) v = (sv (q / 255)^2)^2; blocks of 256 elements share a scale."""
+    q, A = _blocks(codes, P), P.scalar
+    if second:
+        out = np.square((q * q) * (np.asarray(scales, P.acc) * A(1 / 65025.0))[:, None])
+    else:
+        out = (q * np.abs(q)) * (np.asarray(scales, P.acc) * A(1 / 16129.0))[:, None]
+    return out.reshape(-1)[:np.asarray(codes).size]
+
+
+def state8_encode(P: Policy, m, root):
+    """(m8, ms, v8, vs) of moments m and sqrt(v): scales are the blocks' largest |m| and sqrt(v) (0 up to 2^-100, codes 0), codes
+    rounded to nearest even in sqrt(|m|) and in the root of sqrt(v), the latter at least 1 where v > 0."""
+    A, n = P.scalar, np.asarray(m).size
+    mb, rb = _blocks(m, P), _blocks(root, P)
+
+    def fit(top, k):
+        ok = top > 2.0 ** -100
+        return np.where(ok, top, A(0)), np.where(ok, A(k) / np.where(ok, top, A(1)), A(0))[:, None]
+    ms, mf = fit(np.abs(mb).max(1), 16129.0)
+    vs, vf = fit(rb.max(1), 65025.0)
+    qm = np.minimum(np.rint(np.sqrt(np.abs(mb) * mf)), 127) * np.sign(mb)
+    qv = np.minimum(np.rint(np.sqrt(rb * vf)), 255)
+    qv = np.where((rb > 0) & (vf > 0), np.maximum(qv, 1), qv)
+    return qm.reshape(-1)[:n].astype(np.int8), ms, qv.reshape(-1)[:n].astype(np.uint8), vs
+
+
+def unscale_check_update8(P: Policy, tensors: List[Dict[str, np.ndarray]], opt, st: ScaleState) -> int:
+    """unscale_check_update with moments in 8 bits (keys m8, ms, v8, vs instead of m, v; opt.kind "adam" or "adamw"):
+        m = b1 decode(m8) + (1-b1) g,  v = b2 decode(v8) + (1-b2) g^2,
+        w32 -= ((lr / (1-b1^t)) m) / (sqrt(v) (1 / sqrt(1-b2^t)) + eps),  then the moments are encoded."""
+    if has_nonfinite(P, [t["g16"] for t in tensors]):
+        return 1
+    A, t = P.scalar, st.opt_step + 1
+    inv_s, b1, b2 = A(1) / A(st.scale), float(opt.beta1), float(opt.beta2)
+    rate, rbc2 = A(opt.lr / (1.0 - b1 ** t)), A(1.0 / np.sqrt(1.0 - b2 ** t))
+    for tn in tensors:
+        g, w = tn["g16"].reshape(-1) * inv_s, tn["w32"].reshape(-1)
+        if opt.kind == "adamw":
+            w = w - A(float(opt.lr) * float(opt.weight_decay)) * w
+        elif opt.weight_decay != 0.0:
+            g = g + A(opt.weight_decay) * w
+        m = A(b1) * state8_decode(P, tn["m8"], tn["ms"], False) + A(1.0 - b1) * g
+        v = A(b2) * state8_decode(P, tn["v8"], tn["vs"], True) + A(1.0 - b2) * (g * g)
+        root = np.sqrt(v)
+        w = w - (rate * m) / (root * rbc2 + A(opt.eps))
+        tn["w32"][...] = w.reshape(tn["w32"].shape)
+        tn["m8"][...], tn["ms"][...], tn["v8"][...], tn["vs"][...] = state8_encode(P, m, root)
         tn["w16"][...] = P.store(tn["w32"])
     return 0
 

@@ -11,7 +11,8 @@ MP_HISTORY = 4096
 MP_OK, MP_E_INVAL, MP_E_UNSUPPORTED, MP_E_WORKSPACE, MP_E_HIP = 0, -1, -2, -3, -4
 MP_SCALE_STATIC, MP_SCALE_BACKOFF = 0, 1
 MP_EPI_NONE, MP_EPI_BIAS, MP_EPI_BIAS_RELU = 0, 1, 2
-MP_OPT_SGD, MP_OPT_ADAM = 0, 1
+MP_OPT_SGD, MP_OPT_ADAM, MP_OPT_ADAMW = 0, 1, 2
+MP_STATE8_BLOCK = 256
 MP_UPDATE_DEFAULT, MP_UPDATE_PRECHECKED = 0, 1
 
 
@@ -54,6 +55,18 @@ class LstmLayerDesc(C.Structure):
 class TensorDesc(C.Structure):
     _fields_ = [("g16", C.c_void_p), ("w32", C.c_void_p), ("w16", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
                 ("n", C.c_size_t)]
+
+
+class TensorDesc8(C.Structure):
+    _fields_ = [("g16", C.c_void_p), ("w32", C.c_void_p), ("w16", C.c_void_p), ("m8", C.c_void_p), ("v8", C.c_void_p),
+                ("ms", C.c_void_p), ("vs", C.c_void_p), ("n", C.c_size_t)]
+
+
+class AttnDesc(C.Structure):
+    _fields_ = [("rows_q", C.c_int32), ("rows_k", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("d_head", C.c_int32),
+                ("ld_q", C.c_int32), ("ld_k", C.c_int32), ("ld_v", C.c_int32), ("ld_ctx", C.c_int32),
+                ("ld_dq", C.c_int32), ("ld_dk", C.c_int32), ("ld_dv", C.c_int32), ("ld_dctx", C.c_int32),
+                ("alpha", C.c_float), ("cap", C.c_float), ("reserved", C.c_int32)]
 
 
 class OptCfg(C.Structure):
@@ -107,6 +120,15 @@ SIGNATURES = {
     "mp_attention_bwd": (_I, [_I, _I, _I, _I, _P, _I, _F, _P, _P, _I, _P, _I, _P]),
     "mp_attention_fwd_ldp": (_I, [_I, _I, _I, _I, _P, _I, _F, _P, _I, _P, _I, _P]),
     "mp_attention_bwd_ldp": (_I, [_I, _I, _I, _I, _P, _I, _F, _P, _I, _P, _I, _P, _I, _P]),
+    "mp_attention_mask_bytes": (_SZ, [_I]),
+    "mp_attention_mask_docs": (_I, [_I, _I, _P, _P, _I, _I, _P, _P]),
+    "mp_attention_mask_ranges": (_I, [_I, _I, _P, _P, _P, _P]),
+    "mp_attention_masked_fwd": (_I, [C.POINTER(AttnDesc), _P, _P, _P, _P, _P, _P, _P, _P]),
+    "mp_attention_masked_bwd_workspace_bytes": (_SZ, [C.POINTER(AttnDesc)]),
+    "mp_attention_masked_bwd": (_I, [C.POINTER(AttnDesc), _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "mp_embedding_fwd": (_I, [_I, _I, _I, _P, _P, _F, _P, _P]),
+    "mp_embedding_bwd_workspace_bytes": (_SZ, [_I, _I, _I]),
+    "mp_embedding_bwd": (_I, [_I, _I, _I, _P, _P, _F, _P, _P, _P, _P, _SZ, _P]),
     "mp_lstm_cell_fwd": (_I, [_I, _I, _P, _I, _P, _P, _P, _I, _P, _I, _P]),
     "mp_lstm_cell_bwd": (_I, [_I, _I, _P, _I, _P, _P, _P, _I, _P, _I, _P, _P, _P]),
     "mp_lstm_layer_workspace_bytes": (_SZ, []),
@@ -122,6 +144,9 @@ SIGNATURES = {
     "mp_mfma_sustained_rate": (_I, [_P, _SZ, _P, _SZ, _I, _I, C.POINTER(C.c_double), _P]),
     "mp_unscale_check_update": (_I, [C.POINTER(TensorDesc), _I, C.POINTER(OptCfg), _P, _I, _P]),
     "mp_unscale_check_update_end": (_I, [C.POINTER(TensorDesc), _I, C.POINTER(OptCfg), _P, _I, C.POINTER(MeanParts), _P, _P, _P]),
+    "mp_unscale_check_update8": (_I, [C.POINTER(TensorDesc8), _I, C.POINTER(OptCfg), _P, _I, _P]),
+    "mp_unscale_check_update8_end": (_I, [C.POINTER(TensorDesc8), _I, C.POINTER(OptCfg), _P, _I, C.POINTER(MeanParts), _P, _P, _P]),
+    "mp_state8_decode": (_I, [_SZ, _P, _P, _P, _P, _P, _P, _P]),
     "mp_update_counters_bytes": (_SZ, []),
 }
 

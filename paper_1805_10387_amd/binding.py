@@ -282,6 +282,55 @@ def mp_attention_bwd_ldp(n_seq, n_heads, seq_len, d_head, qkv, ld_qkv, alpha, p,
                                          _p(dqkv), ld_dqkv, _stream()))
 
 
+def mp_attention_mask_bytes(rows_q: int) -> int:
+    return L.load().mp_attention_mask_bytes(rows_q)
+
+
+def mp_attention_mask_docs(rows, n_docs, doc_start, mask, prefix=None, causal=False, window=0):
+    _check(L.load().mp_attention_mask_docs(rows, n_docs, _p(doc_start), _p(prefix), int(causal), window, _p(mask), _stream()))
+
+
+def mp_attention_mask_ranges(rows_q, rows_k, lo, hi, mask):
+    _check(L.load().mp_attention_mask_ranges(rows_q, rows_k, _p(lo), _p(hi), _p(mask), _stream()))
+
+
+def attn_desc(rows_q, rows_k, n_heads, n_kv_heads, d_head, ld_q=None, ld_k=None, ld_v=None, ld_ctx=None, alpha=1.0, cap=0.0,
+              ld_dq=None, ld_dk=None, ld_dv=None, ld_dctx=None) -> L.AttnDesc:
+    """Leading dimensions: one matrix after the other where not given; the gradients' are their matrices' where not given."""
+    first = lambda *v: next(x for x in v if x is not None)  # noqa: E731
+    d = L.AttnDesc(rows_q, rows_k, n_heads, n_kv_heads, d_head)
+    d.ld_q, d.ld_ctx = first(ld_q, n_heads * d_head), first(ld_ctx, n_heads * d_head)
+    d.ld_k, d.ld_v = first(ld_k, n_kv_heads * d_head), first(ld_v, n_kv_heads * d_head)
+    d.ld_dq, d.ld_dk, d.ld_dv, d.ld_dctx = first(ld_dq, d.ld_q), first(ld_dk, d.ld_k), first(ld_dv, d.ld_v), first(ld_dctx, d.ld_ctx)
+    d.alpha, d.cap = alpha, cap
+    return d
+
+
+def mp_attention_masked_fwd(desc, mask, q, k, v, slopes, ctx, lse):
+    _check(L.load().mp_attention_masked_fwd(C.byref(desc), _p(mask), _p(q), _p(k), _p(v), _p(slopes), _p(ctx), _p(lse), _stream()))
+
+
+def mp_attention_masked_bwd_workspace_bytes(desc) -> int:
+    return L.load().mp_attention_masked_bwd_workspace_bytes(C.byref(desc))
+
+
+def mp_attention_masked_bwd(desc, mask, q, k, v, slopes, ctx, lse, dctx, dq, dk, dv, ws):
+    _check(L.load().mp_attention_masked_bwd(C.byref(desc), _p(mask), _p(q), _p(k), _p(v), _p(slopes), _p(ctx), _p(lse), _p(dctx), _p(dq),
+                                            _p(dk), _p(dv), _p(ws), _nbytes(ws), _stream()))
+
+
+def mp_embedding_fwd(rows, vocab, d, tokens, w, scale, y):
+    _check(L.load().mp_embedding_fwd(rows, vocab, d, _p(tokens), _p(w), scale, _p(y), _stream()))
+
+
+def mp_embedding_bwd_workspace_bytes(rows: int, vocab: int, d: int) -> int:
+    return L.load().mp_embedding_bwd_workspace_bytes(rows, vocab, d)
+
+
+def mp_embedding_bwd(rows, vocab, d, tokens, dy, scale, dw, add=None, st=None, ws=None):
+    _check(L.load().mp_embedding_bwd(rows, vocab, d, _p(tokens), _p(dy), scale, _p(add), _p(dw), _p(st), _p(ws), _nbytes(ws), _stream()))
+
+
 def mp_lstm_cell_fwd(B, H, gates, ldg, c_prev, c, h_out, ldh, h_out2=None, ldh2=0):
     _check(L.load().mp_lstm_cell_fwd(B, H, _p(gates), ldg, _p(c_prev), _p(c), _p(h_out), ldh, _p(h_out2), ldh2, _stream()))
 
@@ -352,7 +401,7 @@ def mp_mfma_sustained_rate(operands, sink, workgroups: int, iters: int) -> float
 # ------------------------------------------------------------------ optimizer wrapper
 def opt_cfg(kind: str, lr: float, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0) -> OptCfg:
     c = OptCfg()
-    c.kind = {"sgd": L.MP_OPT_SGD, "adam": L.MP_OPT_ADAM}[kind]
+    c.kind = {"sgd": L.MP_OPT_SGD, "adam": L.MP_OPT_ADAM, "adamw": L.MP_OPT_ADAMW}[kind]
     c.lr, c.beta1, c.beta2, c.eps, c.weight_decay = lr, beta1, beta2, eps, weight_decay
     return c
 
@@ -369,6 +418,29 @@ def tensor_list(entries: Sequence[dict]):
 
 def mp_unscale_check_update(tensors, ntensors: int, cfg: OptCfg, st, flags: int = L.MP_UPDATE_DEFAULT):
     _check(L.load().mp_unscale_check_update(tensors, ntensors, C.byref(cfg), _p(st), flags, _stream()))
+
+
+def tensor_list8(entries: Sequence[dict]):
+    """Host array of mp_tensor_desc8 from dicts of torch tensors {g16, w32, w16, m8, v8, ms, vs}."""
+    arr = (L.TensorDesc8 * len(entries))()
+    for i, e in enumerate(entries):
+        for k in ("g16", "w32", "w16", "m8", "v8", "ms", "vs"):
+            setattr(arr[i], k, _p(e[k]))
+        arr[i].n = e["w32"].numel()
+    return arr
+
+
+def mp_unscale_check_update8(tensors, ntensors: int, cfg: OptCfg, st, flags: int = L.MP_UPDATE_DEFAULT):
+    _check(L.load().mp_unscale_check_update8(tensors, ntensors, C.byref(cfg), _p(st), flags, _stream()))
+
+
+def mp_unscale_check_update8_end(tensors, ntensors: int, cfg: OptCfg, st, counters, flags: int = L.MP_UPDATE_DEFAULT, parts=None, loss=None):
+    _check(L.load().mp_unscale_check_update8_end(tensors, ntensors, C.byref(cfg), _p(st), flags, None if parts is None else C.byref(parts),
+                                                 _p(loss), _p(counters), _stream()))
+
+
+def mp_state8_decode(n, m8, ms, v8, vs, m, v):
+    _check(L.load().mp_state8_decode(n, _p(m8), _p(ms), _p(v8), _p(vs), _p(m), _p(v), _stream()))
 
 
 def mp_update_counters_bytes() -> int:

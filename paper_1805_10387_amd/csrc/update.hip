@@ -3,7 +3,7 @@
 // Both kernels of mp_unscale_check_update are pure streaming kernels bound by HBM:
 //   inspect : reads 2 B/parameter  (fp16 gradient bit test, one ballot per wave)
 //   update  : Adam reads g16 + w32 + m + v (14 B) and writes w32 + m + v + w16 (14 B) = 28 B/param,
-//             SGD reads 6 B and writes 6 B = 12 B/param,
+//             SGD reads 6 B and writes 6 B = 12 B/param; with moments in 8 bits Adam reads and writes 8 B each = 16 B/param,
 // with 16-byte accesses per lane, consecutive lanes on consecutive addresses.
 #include "mean.hpp"
 
@@ -117,22 +117,38 @@ struct UpdBatch {
     int                ntensors;
 };
 
+// The same with moments in 8 bits.
+struct UpdBatch8 {
+    const uint16_t*    g16[UPD_MAX_TENSORS];
+    float*             w32[UPD_MAX_TENSORS];
+    uint16_t*          w16[UPD_MAX_TENSORS];
+    int8_t*            m8[UPD_MAX_TENSORS];
+    uint8_t*           v8[UPD_MAX_TENSORS];
+    float*             ms[UPD_MAX_TENSORS];
+    float*             vs[UPD_MAX_TENSORS];
+    unsigned long long n[UPD_MAX_TENSORS];
+    int                chunk_start[UPD_MAX_TENSORS + 1];
+    unsigned           vec_ok;
+    int                ntensors;
+};
+
 struct UpdScalars {
-    float  lr, beta1, beta2, eps, wd, omb1, omb2;
-    double beta1d, beta2d;
+    float  lr, beta1, beta2, eps, wd, omb1, omb2, lrwd;
+    double lrd, beta1d, beta2d;
     int    kind;
 };
 
 // (entries past the last tensor hold the workgroup count: no branch, the whole table comes with a few scalar loads)
-__device__ __forceinline__ int find_tensor(const UpdBatch& b, int bid) {
+template <typename Batch>
+__device__ __forceinline__ int find_tensor(const Batch& b, int bid) {
     int t = 0;
 #pragma unroll
     for (int i = 1; i < UPD_MAX_TENSORS; ++i) t += bid >= b.chunk_start[i];
     return t;
 }
 
-template <int ITERS>
-__global__ __launch_bounds__(UPD_THREADS) void inspect_kernel(UpdBatch b, mp_scale_state* st) {
+template <int ITERS, typename Batch>
+__global__ __launch_bounds__(UPD_THREADS) void inspect_kernel(Batch b, mp_scale_state* st) {
     const int                 t   = find_tensor(b, blockIdx.x);
     const unsigned long long  n   = b.n[t];
     const unsigned long long  off = (unsigned long long)(blockIdx.x - b.chunk_start[t]) * (UPD_PIECE * ITERS);
@@ -160,21 +176,25 @@ __global__ __launch_bounds__(UPD_THREADS) void inspect_kernel(UpdBatch b, mp_sca
     }
 }
 
-// (1 - beta^t) in double by repeated squaring, rounded to fp32.
-__device__ __forceinline__ float bias_correction(double beta, int t) {
+// 1 - beta^t in double, by repeated squaring.
+__device__ __forceinline__ double bias_correction_double(double beta, int t) {
     double r = 1.0, p = beta;
     for (int e = t; e > 0; e >>= 1) {
         if (e & 1) r *= p;
         p *= p;
     }
-    return (float)(1.0 - r);
+    return 1.0 - r;
 }
+__device__ __forceinline__ float bias_correction(double beta, int t) { return (float)bias_correction_double(beta, t); }
 
 template <int KIND>
 __device__ __forceinline__ void update_one(float g16v, float& w, float& m, float& v, const UpdScalars& s,
                                            float inv_scale, float bc1, float bc2) {
     float g = g16v * inv_scale;
-    if (s.wd != 0.f) g = g + s.wd * w;
+    if (KIND == MP_OPT_ADAMW)
+        w = w - s.lrwd * w;
+    else if (s.wd != 0.f)
+        g = g + s.wd * w;
     if (KIND == MP_OPT_SGD) {
         w = w - s.lr * g;
     } else {
@@ -213,7 +233,7 @@ __device__ __forceinline__ void update_share(const UpdBatch& b, const UpdScalars
     auto   fetch = [&](unsigned long long i) {
         gq = __builtin_nontemporal_load(reinterpret_cast<const u32x2v*>(g16 + i));
         w0 = __builtin_nontemporal_load(reinterpret_cast<const f32x4v*>(w32 + i));
-        if (KIND == MP_OPT_ADAM) {
+        if (KIND != MP_OPT_SGD) {
             m0 = __builtin_nontemporal_load(reinterpret_cast<const f32x4v*>(mm + i));
             v0 = __builtin_nontemporal_load(reinterpret_cast<const f32x4v*>(vv + i));
         }
@@ -224,7 +244,7 @@ __device__ __forceinline__ void update_share(const UpdBatch& b, const UpdScalars
     if (st->found_inf != 0) return;  // overflow somewhere in this iteration: the whole step is skipped
     const float inv_scale = st->inv_scale;
     float       bc1 = 1.f, bc2 = 1.f;
-    if (KIND == MP_OPT_ADAM) {
+    if (KIND != MP_OPT_SGD) {
         const int k = st->opt_step + 1;
         bc1 = bias_correction(s.beta1d, k);
         bc2 = bias_correction(s.beta2d, k);
@@ -245,7 +265,7 @@ __device__ __forceinline__ void update_share(const UpdBatch& b, const UpdScalars
                 v0[k] = v;
             }
             __builtin_nontemporal_store(w0, reinterpret_cast<f32x4v*>(w32 + i));
-            if (KIND == MP_OPT_ADAM) {
+            if (KIND != MP_OPT_SGD) {
                 __builtin_nontemporal_store(m0, reinterpret_cast<f32x4v*>(mm + i));
                 __builtin_nontemporal_store(v0, reinterpret_cast<f32x4v*>(vv + i));
             }
@@ -256,13 +276,13 @@ __device__ __forceinline__ void update_share(const UpdBatch& b, const UpdScalars
         } else {
             for (unsigned long long j = i; j < n && j < i + UPD_VEC; ++j) {
                 float w = w32[j], m1 = 0.f, v1 = 0.f;
-                if (KIND == MP_OPT_ADAM) {
+                if (KIND != MP_OPT_SGD) {
                     m1 = mm[j];
                     v1 = vv[j];
                 }
                 update_one<KIND>(h2f(g16[j]), w, m1, v1, s, inv_scale, bc1, bc2);
                 w32[j] = w;
-                if (KIND == MP_OPT_ADAM) {
+                if (KIND != MP_OPT_SGD) {
                     mm[j] = m1;
                     vv[j] = v1;
                 }
@@ -272,8 +292,144 @@ __device__ __forceinline__ void update_share(const UpdBatch& b, const UpdScalars
     }
 }
 
+// ------------------------------------------------------------------ moments in 8 bits
+// The values that codes stand for (m = sm q |q| / 127^2, sqrt(v) = sv (q / 255)^2; the integer products are exact) and back.
+constexpr float STATE8_LEAST = 0x1p-100f;   // scales up to this are 0: their reciprocals would leave the range
+__device__ __forceinline__ float decode_m(int q, float ms) { return (float)(q * abs(q)) * (ms * (1.f / 16129.f)); }
+__device__ __forceinline__ float decode_r(int q, float vs) { return (float)(q * q) * (vs * (1.f / 65025.f)); }
+__device__ __forceinline__ int   encode_m(float m, float fit) {
+    const int q = (int)fminf(rintf(sqrtf(fabsf(m) * fit)), 127.f);
+    return m < 0.f ? -q : q;
+}
+__device__ __forceinline__ int encode_r(float r, float fit) {
+    const int q = (int)fminf(rintf(sqrtf(r * fit)), 255.f);
+    return r > 0.f && fit > 0.f && q == 0 ? 1 : q;
+}
+
+// As above; a wave's 64 x 4 elements are one block of codes, whose scales are the wave's maxima.
 template <int KIND, int ITERS>
-__global__ __launch_bounds__(UPD_THREADS) void update_kernel(UpdBatch b, UpdScalars s, const mp_scale_state* st) {
+__device__ __forceinline__ void update_share(const UpdBatch8& b, const UpdScalars& s, const mp_scale_state* st) {
+    static_assert(64 * UPD_VEC == MP_STATE8_BLOCK, "a wave takes one block of codes at a time");
+    const int                t   = find_tensor(b, blockIdx.x);
+    const unsigned long long n   = b.n[t];
+    const unsigned long long off = (unsigned long long)(blockIdx.x - b.chunk_start[t]) * (UPD_PIECE * ITERS);
+    const bool               vec = (b.vec_ok >> t) & 1u;
+    if (st->found_inf != 0) return;
+    const float  inv_scale = st->inv_scale;
+    const int    step      = st->opt_step + 1;
+    const float  rate      = (float)(s.lrd / bias_correction_double(s.beta1d, step));
+    const float  rbc2      = (float)(1.0 / sqrt(bias_correction_double(s.beta2d, step)));
+#pragma unroll 1
+    for (int it = 0; it < ITERS; ++it) {
+        const unsigned long long first = off + (unsigned long long)(it * UPD_THREADS + (threadIdx.x & ~63)) * UPD_VEC;
+        if (first >= n) break;   // (the same for the whole wave)
+        const unsigned long long i     = first + (threadIdx.x & 63) * UPD_VEC;
+        const unsigned long long block = first / MP_STATE8_BLOCK;
+        const float              ms0 = b.ms[t][block], vs0 = b.vs[t][block];
+        float                    g[4], w[4], m[4], r[4];
+        const bool               four = vec && i + UPD_VEC <= n;
+        if (four) {
+            const u32x2v gq = __builtin_nontemporal_load(reinterpret_cast<const u32x2v*>(b.g16[t] + i));
+            const f32x4v wq = __builtin_nontemporal_load(reinterpret_cast<const f32x4v*>(b.w32[t] + i));
+            const int      mq = __builtin_nontemporal_load(reinterpret_cast<const int*>(b.m8[t] + i));
+            const unsigned vq = __builtin_nontemporal_load(reinterpret_cast<const unsigned*>(b.v8[t] + i));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                g[k] = h2f((uint16_t)(gq[k / 2] >> (16 * (k & 1))));
+                w[k] = wq[k];
+                m[k] = decode_m((mq << (24 - 8 * k)) >> 24, ms0);
+                r[k] = decode_r((vq >> (8 * k)) & 255u, vs0);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const bool in = i + k < n;
+                g[k] = in ? h2f(b.g16[t][i + k]) : 0.f;
+                w[k] = in ? b.w32[t][i + k] : 0.f;
+                m[k] = in ? decode_m(b.m8[t][i + k], ms0) : 0.f;
+                r[k] = in ? decode_r(b.v8[t][i + k], vs0) : 0.f;
+            }
+        }
+        float mtop = 0.f, rtop = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float gk = g[k] * inv_scale;
+            if (KIND == MP_OPT_ADAMW)
+                w[k] = w[k] - s.lrwd * w[k];
+            else if (s.wd != 0.f && i + k < n)
+                gk = gk + s.wd * w[k];
+            m[k]          = s.beta1 * m[k] + s.omb1 * gk;
+            const float v = s.beta2 * (r[k] * r[k]) + s.omb2 * (gk * gk);
+            r[k]          = sqrtf(v);
+            w[k]          = w[k] - (rate * m[k]) / (r[k] * rbc2 + s.eps);
+            mtop          = fmaxf(mtop, fabsf(m[k]));
+            rtop          = fmaxf(rtop, r[k]);
+        }
+        mtop = wave_max(mtop);
+        rtop = wave_max(rtop);
+        const float mfit = mtop > STATE8_LEAST ? 16129.f / mtop : 0.f, rfit = rtop > STATE8_LEAST ? 65025.f / rtop : 0.f;
+        if ((threadIdx.x & 63) == 0) {
+            b.ms[t][block] = mfit > 0.f ? mtop : 0.f;
+            b.vs[t][block] = rfit > 0.f ? rtop : 0.f;
+        }
+        if (four) {
+            unsigned mq = 0, vq = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                mq |= (unsigned)(encode_m(m[k], mfit) & 255) << (8 * k);
+                vq |= (unsigned)encode_r(r[k], rfit) << (8 * k);
+            }
+            __builtin_nontemporal_store(f32x4v{w[0], w[1], w[2], w[3]}, reinterpret_cast<f32x4v*>(b.w32[t] + i));
+            __builtin_nontemporal_store((int)mq, reinterpret_cast<int*>(b.m8[t] + i));
+            __builtin_nontemporal_store(vq, reinterpret_cast<unsigned*>(b.v8[t] + i));
+            u32x2v hq;
+            hq.x = (unsigned)f2h(w[0]) | ((unsigned)f2h(w[1]) << 16);
+            hq.y = (unsigned)f2h(w[2]) | ((unsigned)f2h(w[3]) << 16);
+            *reinterpret_cast<u32x2v*>(b.w16[t] + i) = hq;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (i + k >= n) break;
+                b.w32[t][i + k] = w[k];
+                b.m8[t][i + k]  = (int8_t)encode_m(m[k], mfit);
+                b.v8[t][i + k]  = (uint8_t)encode_r(r[k], rfit);
+                b.w16[t][i + k] = f2h(w[k]);
+            }
+        }
+    }
+}
+
+__global__ __launch_bounds__(UPD_THREADS) void state8_decode_kernel(size_t n, const int8_t* __restrict__ m8, const float* __restrict__ ms,
+                                                                    const uint8_t* __restrict__ v8, const float* __restrict__ vs, float* __restrict__ m,
+                                                                    float* __restrict__ v, bool vec) {
+    const size_t i = ((size_t)blockIdx.x * UPD_THREADS + threadIdx.x) * UPD_VEC;
+    if (i >= n) return;
+    if (vec && i + UPD_VEC <= n) {
+        if (m) {
+            const int   q = __builtin_nontemporal_load(reinterpret_cast<const int*>(m8 + i));
+            const float k = ms[i / MP_STATE8_BLOCK];
+            __builtin_nontemporal_store(f32x4v{decode_m(q << 24 >> 24, k), decode_m(q << 16 >> 24, k), decode_m(q << 8 >> 24, k), decode_m(q >> 24, k)},
+                                        reinterpret_cast<f32x4v*>(m + i));
+        }
+        if (v) {
+            const unsigned q = __builtin_nontemporal_load(reinterpret_cast<const unsigned*>(v8 + i));
+            const float    k = vs[i / MP_STATE8_BLOCK];
+            const float    a = decode_r(q & 255u, k), b = decode_r(q >> 8 & 255u, k), c = decode_r(q >> 16 & 255u, k), d = decode_r(q >> 24, k);
+            __builtin_nontemporal_store(f32x4v{a * a, b * b, c * c, d * d}, reinterpret_cast<f32x4v*>(v + i));
+        }
+        return;
+    }
+    for (size_t j = i; j < n && j < i + UPD_VEC; ++j) {
+        if (m) m[j] = decode_m(m8[j], ms[j / MP_STATE8_BLOCK]);
+        if (v) {
+            const float r = decode_r(v8[j], vs[j / MP_STATE8_BLOCK]);
+            v[j]          = r * r;
+        }
+    }
+}
+
+template <int KIND, int ITERS, typename Batch>
+__global__ __launch_bounds__(UPD_THREADS) void update_kernel(Batch b, UpdScalars s, const mp_scale_state* st) {
     update_share<KIND, ITERS>(b, s, st);
 }
 
@@ -289,8 +445,8 @@ struct UpdEnd {
     float*        loss;
     int*          counters;   // [UPD_END_GROUPS + 1][UPD_END_LINE]
 };
-template <int KIND, int ITERS>
-__global__ __launch_bounds__(UPD_THREADS) void update_end_kernel(UpdBatch b, UpdScalars s, mp_scale_state* st, UpdEnd end) {
+template <int KIND, int ITERS, typename Batch>
+__global__ __launch_bounds__(UPD_THREADS) void update_end_kernel(Batch b, UpdScalars s, mp_scale_state* st, UpdEnd end) {
     static_assert(UPD_THREADS == MEAN_THREADS, "one workgroup size");
     __shared__ int last;
     update_share<KIND, ITERS>(b, s, st);
@@ -315,30 +471,43 @@ __global__ __launch_bounds__(UPD_THREADS) void update_end_kernel(UpdBatch b, Upd
 }
 
 // *ended: in: whether to end the iteration too, out: whether that was done (`end`)
-template <int ITERS>
-static int launch_update(const std::vector<UpdBatch>& batches, const UpdScalars& s, mp_scale_state* st, bool inspect, const UpdEnd& end, bool* ended,
+template <int KIND, int ITERS, typename Batch>
+static int launch_update(const std::vector<Batch>& batches, const UpdScalars& s, mp_scale_state* st, bool inspect, const UpdEnd& end, bool* ended,
                          hipStream_t hs) {
     const bool with_end = *ended && !batches.empty() && batches.back().chunk_start[batches.back().ntensors] <= UPD_END_WGS;
     *ended = with_end;
     if (inspect) {
-        for (const UpdBatch& b : batches) {
-            hipLaunchKernelGGL(inspect_kernel<ITERS>, dim3(b.chunk_start[b.ntensors]), dim3(UPD_THREADS), 0, hs, b, st);
+        for (const Batch& b : batches) {
+            hipLaunchKernelGGL((inspect_kernel<ITERS, Batch>), dim3(b.chunk_start[b.ntensors]), dim3(UPD_THREADS), 0, hs, b, st);
             MP_LAUNCH_CHECK("mp_unscale_check_update(inspect)");
         }
     }
-    for (const UpdBatch& b : batches) {
-        if (with_end && &b == &batches.back()) {
-            if (s.kind == MP_OPT_ADAM)
-                hipLaunchKernelGGL((update_end_kernel<MP_OPT_ADAM, ITERS>), dim3(b.chunk_start[b.ntensors]), dim3(UPD_THREADS), 0, hs, b, s, st, end);
-            else
-                hipLaunchKernelGGL((update_end_kernel<MP_OPT_SGD, ITERS>), dim3(b.chunk_start[b.ntensors]), dim3(UPD_THREADS), 0, hs, b, s, st, end);
-        } else if (s.kind == MP_OPT_ADAM)
-            hipLaunchKernelGGL((update_kernel<MP_OPT_ADAM, ITERS>), dim3(b.chunk_start[b.ntensors]), dim3(UPD_THREADS), 0, hs, b, s, st);
+    for (const Batch& b : batches) {
+        if (with_end && &b == &batches.back())
+            hipLaunchKernelGGL((update_end_kernel<KIND, ITERS, Batch>), dim3(b.chunk_start[b.ntensors]), dim3(UPD_THREADS), 0, hs, b, s, st, end);
         else
-            hipLaunchKernelGGL((update_kernel<MP_OPT_SGD, ITERS>), dim3(b.chunk_start[b.ntensors]), dim3(UPD_THREADS), 0, hs, b, s, st);
+            hipLaunchKernelGGL((update_kernel<KIND, ITERS, Batch>), dim3(b.chunk_start[b.ntensors]), dim3(UPD_THREADS), 0, hs, b, s, st);
         MP_LAUNCH_CHECK("mp_unscale_check_update(update)");
     }
     return MP_OK;
+}
+
+// What the two kinds of tensors do not share: the moments.
+static bool has_moments(const mp_tensor_desc& d) { return d.m && d.v; }
+static bool has_moments(const mp_tensor_desc8& d) { return d.m8 && d.v8 && d.ms && d.vs; }
+static bool moments_at_element(const mp_tensor_desc&) { return true; }
+static bool moments_at_element(const mp_tensor_desc8& d) { return ((reinterpret_cast<uintptr_t>(d.ms) | reinterpret_cast<uintptr_t>(d.vs)) & 3) == 0; }
+static bool moments_aligned(const mp_tensor_desc& d) { return aligned16(d.m) && aligned16(d.v); }
+static bool moments_aligned(const mp_tensor_desc8& d) { return ((reinterpret_cast<uintptr_t>(d.m8) | reinterpret_cast<uintptr_t>(d.v8)) & 3) == 0; }
+static void set_moments(UpdBatch& b, int k, const mp_tensor_desc& d) {
+    b.m[k] = d.m;
+    b.v[k] = d.v;
+}
+static void set_moments(UpdBatch8& b, int k, const mp_tensor_desc8& d) {
+    b.m8[k] = d.m8;
+    b.v8[k] = d.v8;
+    b.ms[k] = d.ms;
+    b.vs[k] = d.vs;
 }
 
 }  // namespace mp
@@ -382,20 +551,21 @@ extern "C" int mp_loss_scale_update_mean(mp_scale_state* st, const mp_mean_parts
 }
 
 // *ended: see launch_update
-static int unscale_check_update(const mp_tensor_desc* tensors, int ntensors, const mp_opt_cfg* cfg, mp_scale_state* st, int flags,
+template <typename Batch, typename Desc>
+static int unscale_check_update(const Desc* tensors, int ntensors, const mp_opt_cfg* cfg, mp_scale_state* st, int flags,
                                 const UpdEnd& end, bool* ended, mp_stream stream) {
     MP_REQUIRE(st != nullptr && cfg != nullptr, "mp_unscale_check_update: st / cfg is NULL");
     MP_REQUIRE(ntensors >= 0 && (ntensors == 0 || tensors != nullptr), "mp_unscale_check_update: bad tensor list");
-    MP_REQUIRE(cfg->kind == MP_OPT_SGD || cfg->kind == MP_OPT_ADAM, "mp_unscale_check_update: bad optimizer kind %d",
-               cfg->kind);
+    MP_REQUIRE(cfg->kind == MP_OPT_ADAM || cfg->kind == MP_OPT_ADAMW || (cfg->kind == MP_OPT_SGD && std::is_same<Desc, mp_tensor_desc>::value),
+               "mp_unscale_check_update: bad optimizer kind %d", cfg->kind);
     MP_REQUIRE((flags & ~MP_UPDATE_PRECHECKED) == 0, "mp_unscale_check_update: unknown flags 0x%x", flags);
     for (int i = 0; i < ntensors; ++i) {
-        const mp_tensor_desc& d = tensors[i];
+        const Desc& d = tensors[i];
         if (d.n == 0) continue;
         MP_REQUIRE(d.g16 && d.w32 && d.w16, "mp_unscale_check_update: tensor %d has a NULL g16/w32/w16", i);
-        MP_REQUIRE(cfg->kind != MP_OPT_ADAM || (d.m && d.v), "mp_unscale_check_update: tensor %d lacks Adam moments", i);
+        MP_REQUIRE(cfg->kind == MP_OPT_SGD || has_moments(d), "mp_unscale_check_update: tensor %d lacks Adam moments", i);
         MP_REQUIRE((reinterpret_cast<uintptr_t>(d.g16) & 1) == 0 && (reinterpret_cast<uintptr_t>(d.w16) & 1) == 0 &&
-                       (reinterpret_cast<uintptr_t>(d.w32) & 3) == 0,
+                       (reinterpret_cast<uintptr_t>(d.w32) & 3) == 0 && moments_at_element(d),
                    "mp_unscale_check_update: tensor %d is not element-aligned", i);
         MP_REQUIRE(d.n < (1ull << 40), "mp_unscale_check_update: tensor %d too large", i);
     }
@@ -409,6 +579,8 @@ static int unscale_check_update(const mp_tensor_desc* tensors, int ntensors, con
     s.wd     = (float)cfg->weight_decay;
     s.omb1   = (float)(1.0 - cfg->beta1);
     s.omb2   = (float)(1.0 - cfg->beta2);
+    s.lrwd   = (float)(cfg->lr * cfg->weight_decay);
+    s.lrd    = cfg->lr;
     s.beta1d = cfg->beta1;
     s.beta2d = cfg->beta2;
 
@@ -416,20 +588,20 @@ static int unscale_check_update(const mp_tensor_desc* tensors, int ntensors, con
     for (int i = 0; i < ntensors; ++i) total += (long long)tensors[i].n;
     const int             iters = upd_iters(total);
     const long long       chunk = (long long)UPD_PIECE * iters;
-    std::vector<UpdBatch> batches;
-    UpdBatch              cur;
-    cur = UpdBatch{};
+    std::vector<Batch>    batches;
+    Batch                 cur;
+    cur = Batch{};
     long long chunks = 0;
     auto      flush  = [&]() {
         if (cur.ntensors > 0) {
             for (int k = cur.ntensors; k <= UPD_MAX_TENSORS; ++k) cur.chunk_start[k] = (int)chunks;
             batches.push_back(cur);
         }
-        cur = UpdBatch{};
+        cur = Batch{};
         chunks = 0;
     };
     for (int i = 0; i < ntensors; ++i) {
-        const mp_tensor_desc& d = tensors[i];
+        const Desc& d = tensors[i];
         if (d.n == 0) continue;
         const long long c = ((long long)d.n + chunk - 1) / chunk;
         if (cur.ntensors == UPD_MAX_TENSORS || chunks + c > 0x3FFFFFFF) flush();
@@ -437,41 +609,77 @@ static int unscale_check_update(const mp_tensor_desc* tensors, int ntensors, con
         cur.g16[k]  = d.g16;
         cur.w32[k]  = d.w32;
         cur.w16[k]  = d.w16;
-        cur.m[k]    = d.m;
-        cur.v[k]    = d.v;
+        set_moments(cur, k, d);
         cur.n[k]    = d.n;
         cur.chunk_start[k] = (int)chunks;
         const bool ok = aligned16(d.g16) && aligned16(d.w32) && aligned16(d.w16) &&
-                        (cfg->kind != MP_OPT_ADAM || (aligned16(d.m) && aligned16(d.v)));
+                        (cfg->kind == MP_OPT_SGD || moments_aligned(d));
         if (ok) cur.vec_ok |= (1u << k);
         chunks += c;
     }
     flush();
 
     const bool inspect = !(flags & MP_UPDATE_PRECHECKED);
-    switch (iters) {
-        case 1: return launch_update<1>(batches, s, st, inspect, end, ended, as_stream(stream));
-        case 2: return launch_update<2>(batches, s, st, inspect, end, ended, as_stream(stream));
-        case 4: return launch_update<4>(batches, s, st, inspect, end, ended, as_stream(stream));
-        default: return launch_update<8>(batches, s, st, inspect, end, ended, as_stream(stream));
-    }
+    const auto launch  = [&](auto kind) {
+        constexpr int KIND = decltype(kind)::value;
+        switch (iters) {
+            case 1: return launch_update<KIND, 1>(batches, s, st, inspect, end, ended, as_stream(stream));
+            case 2: return launch_update<KIND, 2>(batches, s, st, inspect, end, ended, as_stream(stream));
+            case 4: return launch_update<KIND, 4>(batches, s, st, inspect, end, ended, as_stream(stream));
+            default: return launch_update<KIND, 8>(batches, s, st, inspect, end, ended, as_stream(stream));
+        }
+    };
+    if (cfg->kind == MP_OPT_ADAMW) return launch(std::integral_constant<int, MP_OPT_ADAMW>{});
+    if constexpr (std::is_same<Desc, mp_tensor_desc>::value)
+        if (cfg->kind == MP_OPT_SGD) return launch(std::integral_constant<int, MP_OPT_SGD>{});
+    return launch(std::integral_constant<int, MP_OPT_ADAM>{});
 }
 
 extern "C" int mp_unscale_check_update(const mp_tensor_desc* tensors, int ntensors, const mp_opt_cfg* cfg,
                                        mp_scale_state* st, int flags, mp_stream stream) {
     bool ended = false;
-    return unscale_check_update(tensors, ntensors, cfg, st, flags, UpdEnd{}, &ended, stream);
+    return unscale_check_update<UpdBatch>(tensors, ntensors, cfg, st, flags, UpdEnd{}, &ended, stream);
 }
 
 extern "C" size_t mp_update_counters_bytes(void) { return (UPD_END_GROUPS + 1) * UPD_END_LINE * sizeof(int); }
 
-extern "C" int mp_unscale_check_update_end(const mp_tensor_desc* tensors, int ntensors, const mp_opt_cfg* cfg, mp_scale_state* st,
-                                           int flags, const mp_mean_parts* parts, float* loss, int32_t* counters, mp_stream stream) {
+extern "C" int mp_unscale_check_update8(const mp_tensor_desc8* tensors, int ntensors, const mp_opt_cfg* cfg, mp_scale_state* st, int flags,
+                                        mp_stream stream) {
+    bool ended = false;
+    return unscale_check_update<UpdBatch8>(tensors, ntensors, cfg, st, flags, UpdEnd{}, &ended, stream);
+}
+
+template <typename Batch, typename Desc>
+static int unscale_check_update_end(const Desc* tensors, int ntensors, const mp_opt_cfg* cfg, mp_scale_state* st, int flags,
+                                    const mp_mean_parts* parts, float* loss, int32_t* counters, mp_stream stream) {
     MP_REQUIRE(counters != nullptr && (reinterpret_cast<uintptr_t>(counters) & 3) == 0, "mp_unscale_check_update_end: counters NULL or not 4-byte aligned");
     MP_REQUIRE(parts == nullptr || (parts->part && parts->n > 0 && loss), "mp_unscale_check_update_end: parts without partial sums or loss");
     const UpdEnd end{parts ? *parts : mp_mean_parts{}, loss, counters};
     bool      ended = true;
-    const int rc    = unscale_check_update(tensors, ntensors, cfg, st, flags, end, &ended, stream);
+    const int rc    = unscale_check_update<Batch>(tensors, ntensors, cfg, st, flags, end, &ended, stream);
     if (rc != MP_OK || ended) return rc;
     return parts ? mp_loss_scale_update_mean(st, parts, loss, stream) : mp_loss_scale_update(st, stream);
+}
+
+extern "C" int mp_unscale_check_update_end(const mp_tensor_desc* tensors, int ntensors, const mp_opt_cfg* cfg, mp_scale_state* st,
+                                           int flags, const mp_mean_parts* parts, float* loss, int32_t* counters, mp_stream stream) {
+    return unscale_check_update_end<UpdBatch>(tensors, ntensors, cfg, st, flags, parts, loss, counters, stream);
+}
+
+extern "C" int mp_unscale_check_update8_end(const mp_tensor_desc8* tensors, int ntensors, const mp_opt_cfg* cfg, mp_scale_state* st, int flags,
+                                            const mp_mean_parts* parts, float* loss, int32_t* counters, mp_stream stream) {
+    return unscale_check_update_end<UpdBatch8>(tensors, ntensors, cfg, st, flags, parts, loss, counters, stream);
+}
+
+extern "C" int mp_state8_decode(size_t n, const int8_t* m8, const float* ms, const uint8_t* v8, const float* vs, float* m, float* v, mp_stream stream) {
+    MP_REQUIRE(n < (1ull << 40), "mp_state8_decode: too large");
+    MP_REQUIRE((!m || (m8 && ms)) && (!v || (v8 && vs)), "mp_state8_decode: an output without its codes and scales");
+    const uintptr_t words = reinterpret_cast<uintptr_t>(m) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(ms) | reinterpret_cast<uintptr_t>(vs);
+    MP_REQUIRE((words & 3) == 0, "mp_state8_decode: outputs or scales are not element-aligned");
+    if (n == 0 || (!m && !v)) return MP_OK;
+    const bool vec = ((reinterpret_cast<uintptr_t>(m8) | reinterpret_cast<uintptr_t>(v8)) & 3) == 0 && aligned16(m) && aligned16(v);
+    hipLaunchKernelGGL(state8_decode_kernel, dim3((unsigned)((n + UPD_PIECE - 1) / UPD_PIECE)), dim3(UPD_THREADS), 0, as_stream(stream), n, m8, ms, v8, vs, m,
+                       v, vec);
+    MP_LAUNCH_CHECK("mp_state8_decode");
+    return MP_OK;
 }

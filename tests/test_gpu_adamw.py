@@ -1,0 +1,163 @@
+"""AdamW, and moments in 8 bits, through the C ABI against the oracle.  The update is stated operation by operation in fp32, every
+operation correctly rounded on both sides, except that the oracle's NumPy and the device may form the double coefficients an ulp of a
+double apart, which moves their fp32 rounding rarely and then by 2^-24: codes, scales and moments are compared bit by bit (they
+use no such coefficient), masters to 2^-22 of the master and of the step."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+import paper_1805_10387_amd as mp
+from paper_1805_10387_amd import _lib as ML
+import mp_inputs as I
+from oracle import MIXED
+from oracle import optimizer as O
+from oracle.numerics import half_bits
+from gpu_util import *
+
+S16 = MIXED.store
+SIZES = [8192 * 3 + 5, 1, 7, 255, 256, 257, 4096, 100000, 33] + [64] * 40      # > 32 tensors: several launches
+
+
+def tensors8(sizes, seed):
+    r = np.random.default_rng(seed)
+    out = []
+    for n in sizes:
+        b = (n + 255) // 256
+        size = np.repeat(np.exp(2 * r.standard_normal(b)), 256)[:n]
+        w = (0.05 * r.standard_normal(n)).astype(np.float32)
+        m8, ms, v8, vs = O.state8_encode(MIXED, (1e-2 * size * r.standard_normal(n)).astype(np.float32),
+                                         (1e-2 * size * np.abs(r.standard_normal(n))).astype(np.float32))
+        out.append(dict(g16=S16(size * r.standard_normal(n)), w32=w, w16=S16(w), m8=m8, ms=ms.astype(np.float32), v8=v8, vs=vs.astype(np.float32)))
+    return out
+
+
+def to_device(t, skew=0):
+    def put(x, kind):
+        y = torch.empty(x.size + 16, dtype=kind, device="cuda")
+        y[skew:skew + x.size] = torch.from_numpy(np.ascontiguousarray(x.astype(dict(g16=np.float16, w16=np.float16).get(k, x.dtype)))).cuda()
+        return y[skew:skew + x.size]
+    kinds = dict(g16=torch.float16, w16=torch.float16, w32=torch.float32, m8=torch.int8, v8=torch.uint8, ms=torch.float32, vs=torch.float32)
+    out = {}
+    for k in t:
+        out[k] = put(t[k], kinds[k])
+    return out
+
+
+def state(scale, step):
+    st = mp.scale_state_alloc()
+    mp.mp_scale_state_init(st, ML.MP_SCALE_BACKOFF, scale, 3)
+    st[8] = step
+    return st
+
+
+def same(a, b):
+    return np.array_equal(a.cpu().numpy().view(np.uint8), np.ascontiguousarray(b).view(np.uint8))
+
+
+@pytest.mark.parametrize("kind", ["adam", "adamw"])
+@pytest.mark.parametrize("step,wd,skew", [(0, 0.0, 0), (1, 1e-2, 0), (57, 0.1, 1), (3, 0.3, 4)])
+def test_update8_matches_the_oracle(kind, step, wd, skew):
+    host = tensors8(SIZES, step)
+    dev, before = [to_device(t, skew) for t in host], [t["w32"].copy() for t in host]
+    cfg, st = I.OptCfg(kind=kind, lr=1e-3, weight_decay=wd), state(2.0 ** 7, step)
+    assert O.unscale_check_update8(MIXED, host, cfg, O.ScaleState(scale=2.0 ** 7, opt_step=step)) == 0
+    mp.mp_unscale_check_update8(mp.tensor_list8(dev), len(dev), mp.opt_cfg(kind, 1e-3, weight_decay=wd), st)
+    for h, d, w0 in zip(host, dev, before):
+        for k in ("m8", "v8", "ms", "vs"):
+            assert same(d[k], h[k]), (k, h["w32"].size)
+        got = np32(d["w32"]).astype(np.float64)
+        assert np.all(np.abs(got - h["w32"]) <= 2.0 ** -22 * (np.abs(h["w32"]) + np.abs(h["w32"] - w0)))
+        assert np.array_equal(bits(d["w16"]), half_bits(S16(np32(d["w32"]))))
+        m, v = empty32(h["w32"].size), empty32(h["w32"].size)
+        mp.mp_state8_decode(m.numel(), d["m8"], d["ms"], d["v8"], d["vs"], m, v)
+        assert same(m, O.state8_decode(MIXED, h["m8"], h["ms"], False)) and same(v, O.state8_decode(MIXED, h["v8"], h["vs"], True))
+
+
+@pytest.mark.parametrize("step,wd", [(0, 0.0), (57, 0.1)])
+def test_adamw_with_ordinary_moments(step, wd):
+    r = np.random.default_rng(step)
+    host = [dict(g16=S16(100 * r.standard_normal(n)), w32=(0.05 * r.standard_normal(n)).astype(np.float32), w16=np.zeros(n, np.float32),
+                 m=(0.01 * r.standard_normal(n)).astype(np.float32), v=(1e-4 * np.abs(r.standard_normal(n))).astype(np.float32)) for n in SIZES]
+    dev = [dict(g16=h16(t["g16"]), w32=f32(t["w32"]), w16=h16(t["w16"]), m=f32(t["m"]), v=f32(t["v"])) for t in host]
+    before = [t["w32"].copy() for t in host]
+    assert O.unscale_check_update(MIXED, host, I.OptCfg(kind="adamw", lr=1e-3, weight_decay=wd), O.ScaleState(scale=2.0 ** 7, opt_step=step)) == 0
+    mp.mp_unscale_check_update(mp.tensor_list(dev), len(dev), mp.opt_cfg("adamw", 1e-3, weight_decay=wd), state(2.0 ** 7, step))
+    for h, d, w0 in zip(host, dev, before):
+        assert same(d["m"], h["m"]) and same(d["v"], h["v"])
+        assert np.all(np.abs(np32(d["w32"]).astype(np.float64) - h["w32"]) <= 2.0 ** -22 * (np.abs(h["w32"]) + np.abs(h["w32"] - w0)))
+        assert np.array_equal(bits(d["w16"]), half_bits(S16(np32(d["w32"]))))
+
+
+@pytest.mark.parametrize("n", [2048 * 1024 - 2, 2048 * 1024 + 5, 2 * 2048 * 1024 + 1023, 4 * 2048 * 1024 + 4])
+def test_update8_workgroup_shares(n):
+    """Around the lines where a workgroup takes 1, 2, 4 or 8 pieces: every element and every block once."""
+    host = tensors8([n - 1500, 1500], 2)
+    dev = [to_device(t) for t in host]
+    O.unscale_check_update8(MIXED, host, I.OptCfg(kind="adamw", lr=1e-3), O.ScaleState(scale=2.0 ** 7, opt_step=5))
+    mp.mp_unscale_check_update8(mp.tensor_list8(dev), 2, mp.opt_cfg("adamw", 1e-3), state(2.0 ** 7, 5))
+    for h, d in zip(host, dev):
+        assert all(same(d[k], h[k]) for k in ("m8", "v8", "ms", "vs"))
+
+
+@pytest.mark.parametrize("bad", [np.inf, np.nan])
+@pytest.mark.parametrize("where", [(0, 0), (7, 99999), (48, 63)])
+def test_update8_skips_where_a_gradient_overflowed(bad, where):
+    host = tensors8(SIZES, 3)
+    host[where[0]]["g16"][where[1]] = bad
+    dev, st = [to_device(t) for t in host], state(2.0 ** 15, 4)
+    counters = mp.update_counters_alloc()
+    mp.mp_unscale_check_update8_end(mp.tensor_list8(dev), len(dev), mp.opt_cfg("adamw", 1e-3, weight_decay=0.1), st, counters)
+    s = mp.scale_state_read(st)
+    assert (s.scale, s.opt_step, s.skipped_steps, s.found_inf) == (2.0 ** 14, 4, 1, 0) and int(counters.abs().sum()) == 0
+    for t, d in zip(host, dev):
+        assert all(same(d[k], t[k]) for k in ("m8", "v8", "ms", "vs", "w32"))
+        assert np.array_equal(bits(d["w16"]), half_bits(t["w16"]))
+
+
+def test_blocks_of_zeros_and_of_tiny_moments():
+    """New states are zero bytes; a block without gradients stays so; moments so small that their scale is at the edge become 0 and
+    nothing becomes NaN."""
+    n = 256 * 4
+    g = np.zeros(n)
+    g[256:512] = 6e-8                       # fp16's smallest
+    g[512:768] = 6e4
+    g[768] = 1.0
+    host = [dict(g16=S16(g), w32=np.ones(n, np.float32), w16=np.ones(n, np.float32), m8=np.zeros(n, np.int8), v8=np.zeros(n, np.uint8),
+                 ms=np.zeros(4, np.float32), vs=np.zeros(4, np.float32))]
+    dev, st = [to_device(host[0])], state(2.0 ** 24, 0)
+    O.unscale_check_update8(MIXED, host, I.OptCfg(kind="adamw", lr=1e-2), O.ScaleState(scale=2.0 ** 24))
+    mp.mp_unscale_check_update8(mp.tensor_list8(dev), 1, mp.opt_cfg("adamw", 1e-2), st)
+    assert all(same(dev[0][k], host[0][k]) for k in ("m8", "v8", "ms", "vs"))
+    w = np32(dev[0]["w32"])
+    # (the smallest gradients, 2^-48: a step of at most lr 2^-48 / eps = 3.6e-9, less than half a unit of fp32 below 1)
+    assert np.all(np.isfinite(w)) and np.all(w[:512] == 1) and np.all(w[769:] == 1) and np.all(w[512:769] < 1)
+
+
+def test_captured_iterations_with_the_end_of_the_iteration():
+    """Update and scale update captured; each replay against the oracle's own next step, bit by bit in the codes."""
+    host = tensors8([5000, 300], 8)
+    for t in host:
+        for k in ("m8", "v8", "ms", "vs"):
+            t[k][...] = 0
+    dev, st, counters = [to_device(t) for t in host], state(2.0 ** 7, 0), mp.update_counters_alloc()
+    lst, cfg, ost = mp.tensor_list8(dev), mp.opt_cfg("adamw", 1e-3, weight_decay=0.1), O.ScaleState(scale=2.0 ** 7, growth_interval=3)
+    ocfg = I.OptCfg(kind="adamw", lr=1e-3, weight_decay=0.1)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mp.mp_unscale_check_update8_end(lst, 2, cfg, st, counters)
+    r = np.random.default_rng(1)
+    for step in range(5):
+        for t, d in zip(host, dev):
+            t["g16"][...] = S16(r.standard_normal(t["g16"].size))
+            d["g16"].copy_(h16(t["g16"]))
+        if step == 2:
+            dev[1]["g16"][7] = float("inf")
+            host[1]["g16"][7] = np.inf
+        graph.replay()
+        O.loss_scale_update(ost, O.unscale_check_update8(MIXED, host, ocfg, ost))
+        s = mp.scale_state_read(st)
+        assert (s.scale, s.opt_step, s.skipped_steps) == (ost.scale, ost.opt_step, ost.skipped_steps)
+        for t, d in zip(host, dev):
+            assert all(same(d[k], t[k]) for k in ("m8", "v8", "ms", "vs")), step

@@ -1,0 +1,132 @@
+"""Embedding lookup and its gradient through the C ABI against the oracle.
+
+Forward is one fp32 product and one rounding: equal bits.  Backward: at most half a step of the result (2^-11), and of the sum of n rows
+n 2^-24 times the sum of their magnitudes; with a second gradient one more rounding of each of the two values."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+import paper_1805_10387_amd as mp
+from paper_1805_10387_amd import _lib as ML
+from oracle import FP64, MIXED
+from oracle import layers as L
+from oracle.numerics import half_bits
+from gpu_util import *
+
+S16 = MIXED.store
+
+
+def tokens_of(kind, rows, vocab, r):
+    if kind == "spread":
+        return r.integers(0, vocab, rows)
+    if kind == "zipf":
+        return np.minimum((vocab ** r.random(rows)).astype(np.int64) - 1, vocab - 1)
+    if kind == "same":
+        return np.full(rows, vocab - 1)
+    if kind == "pads":                                   # half of them no token at all
+        return np.where(r.random(rows) < 0.5, r.choice([-1, vocab, 2 ** 31 - 1, -2 ** 31], rows), r.integers(0, vocab, rows))
+    if kind == "none":
+        return np.full(rows, -1)
+    return np.arange(rows) % vocab                       # "in turn"
+
+
+def place(x, skew):
+    """The array on the device, `skew` elements behind a 16-byte boundary."""
+    t = torch.empty(x.size + 16, dtype=torch.float16, device="cuda")
+    t[skew:skew + x.size] = h16(x).view(-1)
+    return t[skew:skew + x.size].view(x.shape)
+
+
+def check(rows, vocab, d, kind, scale=1.5, add=False, skew=0, seed=0):
+    r = np.random.default_rng(seed + rows + vocab + d)
+    tok = tokens_of(kind, rows, vocab, r).astype(np.int32)
+    w, dy, second = S16(r.standard_normal((vocab, d))), S16(r.standard_normal((rows, d))), S16(r.standard_normal((vocab, d)))
+    tokens, y = i32(tok), place(np.full((rows, d), 7.0), skew)
+    mp.mp_embedding_fwd(rows, vocab, d, tokens, place(w, skew), scale, y)
+    assert np.array_equal(bits(y), half_bits(L.embedding_fwd(MIXED, tok, w, scale))), "forward"
+    dw, ws = place(np.full((vocab, d), 7.0), skew), torch.empty(mp.mp_embedding_bwd_workspace_bytes(rows, vocab, d), dtype=torch.uint8, device="cuda")
+    mp.mp_embedding_bwd(rows, vocab, d, tokens, place(dy, skew), scale, dw, ws=ws)
+    ok = (tok >= 0) & (tok < vocab)
+    ref, mag, n = np.zeros((vocab, d)), np.zeros((vocab, d)), np.zeros(vocab)
+    np.add.at(ref, tok[ok], scale * dy[ok].astype(np.float64))
+    np.add.at(mag, tok[ok], scale * np.abs(dy[ok]).astype(np.float64))
+    np.add.at(n, tok[ok], 1)
+    bound = 2.0 ** -11 * np.abs(ref) + (n[:, None] + 2) * 2.0 ** -24 * mag + 2.0 ** -25
+    assert np.all(np.abs(np32(dw) - ref) <= bound), "backward"
+    assert torch.all(dw[torch.from_numpy(n == 0).cuda()] == 0)
+    again = torch.empty_like(dw)
+    mp.mp_embedding_bwd(rows, vocab, d, tokens, place(dy, skew), scale, again, ws=ws)
+    assert torch.equal(again, dw), "two calls"
+    if add:
+        other, tied = place(second, skew), place(second, skew)
+        mp.mp_embedding_bwd(rows, vocab, d, tokens, place(dy, skew), scale, again, add=other, ws=ws)
+        mp.mp_embedding_bwd(rows, vocab, d, tokens, place(dy, skew), scale, tied, add=tied, ws=ws)
+        assert np.array_equal(bits(again), half_bits(S16(np32(dw) + second))), "with a second gradient"
+        assert torch.equal(again, tied), "in place"
+
+
+@pytest.mark.parametrize("kind", ["spread", "zipf", "same", "pads", "none", "in turn"])
+@pytest.mark.parametrize("rows", [1, 31, 32, 33, 64, 65, 500, 2047, 2048, 2049, 5000])
+def test_row_counts(rows, kind):
+    check(rows, 97, 24, kind, add=True)
+
+
+@pytest.mark.parametrize("d,skew", [(1, 0), (7, 0), (8, 0), (8, 1), (24, 3), (64, 0), (192, 4), (515, 0), (512, 0), (520, 0), (1024, 1), (1032, 0)])
+def test_widths_and_alignments(d, skew):
+    check(300, 61, d, "zipf", scale=d ** 0.5, add=True, skew=skew)
+
+
+@pytest.mark.parametrize("rows,vocab", [(40, 1), (3, 30000), (5000, 30000), (65536, 100), (65537, 3), (70000, 2 ** 21 - 1), (140000, 50000)])
+def test_many_tokens_and_words(rows, vocab):
+    """Up to several levels of merging, the largest vocabulary."""
+    check(rows, vocab, 2 if vocab < 2 ** 20 else 1, "zipf")
+    check(rows, vocab, 1, "same")
+
+
+def test_no_rows():
+    dw, ws = torch.full((5, 8), 7.0, dtype=torch.float16, device="cuda"), torch.empty(1024, dtype=torch.uint8, device="cuda")
+    mp.mp_embedding_bwd(0, 5, 8, None, None, 1.0, dw, ws=ws)
+    assert torch.all(dw == 0)
+    mp.mp_embedding_fwd(0, 5, 8, None, dw, 1.0, None)
+
+
+@pytest.mark.parametrize("d", [8, 9])
+def test_overflow_is_flagged_and_kept(d):
+    """A sum beyond fp16 is an infinity in its own row and sets the flag; a clean gradient does not.  A sum over several chunks, and
+    an infinite second gradient of an absent word, too."""
+    st, ws = mp.scale_state_alloc(), torch.empty(mp.mp_embedding_bwd_workspace_bytes(300, 7, d), dtype=torch.uint8, device="cuda")
+    for rows, value, add, want in ((4, 1.0, None, 0), (4, 30000.0, None, 1), (300, 300.0, None, 1), (4, 1.0, 1.0, 0), (4, 1.0, np.inf, 1)):
+        mp.mp_scale_state_init(st, ML.MP_SCALE_BACKOFF, 2.0 ** 15, 10)
+        dw, tok = empty16(7, d), i32(np.full(rows, 3))
+        second = None if add is None else torch.zeros(7, d, dtype=torch.float16, device="cuda")
+        if add is not None:
+            second[6, d - 1] = add
+        mp.mp_embedding_bwd(rows, 7, d, tok, torch.full((rows, d), value, dtype=torch.float16, device="cuda"), 1.0, dw, add=second, st=st, ws=ws)
+        assert mp.scale_state_read(st).found_inf == want, (rows, value, add)
+        assert torch.all(torch.isfinite(dw[[0, 1, 2, 4, 5]]))
+        assert torch.all(torch.isinf(dw[3])) == (value * rows > 65519)
+
+
+def test_captured_and_replayed_with_other_tokens():
+    rows, vocab, d = 3000, 500, 64
+    r = np.random.default_rng(1)
+    dy, w, tokens = h16(S16(r.standard_normal((rows, d)))), h16(S16(r.standard_normal((vocab, d)))), i32(np.zeros(rows))
+    out = [[empty16(rows, d), empty16(vocab, d), torch.empty(mp.mp_embedding_bwd_workspace_bytes(rows, vocab, d), dtype=torch.uint8, device="cuda")]
+           for _ in range(2)]
+
+    def both(o):
+        mp.mp_embedding_fwd(rows, vocab, d, tokens, w, 2.0, o[0])
+        mp.mp_embedding_bwd(rows, vocab, d, tokens, dy, 2.0, o[1], ws=o[2])
+    both(out[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both(out[0])
+    for kind in ("zipf", "same", "pads", "spread"):
+        tokens.copy_(i32(tokens_of(kind, rows, vocab, r)))
+        graph.replay()
+        both(out[1])
+        torch.cuda.synchronize()
+        assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1]), kind
