@@ -431,7 +431,7 @@ int mp_attention_mask_ranges(int rows_q, int rows_k, const int32_t* lo, const in
 typedef struct mp_attn_desc {
     int32_t rows_q, rows_k;
     int32_t n_heads, n_kv_heads, d_head;  /* n_kv_heads divides n_heads; d_head a multiple of 8 up to 128 */
-    int32_t ld_q, ld_k, ld_v, ld_ctx;     /* multiples of 8, as are those of the gradients                */
+    int32_t ld_q, ld_k, ld_v, ld_ctx;     /* multiples of 8 below 2^22, as are those of the gradients     */
     int32_t ld_dq, ld_dk, ld_dv, ld_dctx;
     float   alpha;                        /* > 0                                                          */
     float   cap;                          /* 0: none                                                      */
@@ -445,7 +445,7 @@ typedef struct mp_attn_desc {
  * above 1, the row's largest is 1).
  * What a row does not see does not reach it, NaN and infinities included; of a value row that holds one, those rows that see it get
  * non-finite results.  All rows of ctx are written.  Any rows_k >= 0 and rows_q >= 0.
- * 16-byte aligned matrices with leading dimensions in multiples of 8 and a d_head as above; otherwise MP_E_UNSUPPORTED. */
+ * 16-byte aligned matrices with leading dimensions and a d_head as above; otherwise MP_E_UNSUPPORTED. */
 int mp_attention_masked_fwd(const mp_attn_desc* desc /* host */, const void* mask, const mp_half* q, const mp_half* k,
                             const mp_half* v, const float* slopes, mp_half* ctx, float* lse, mp_stream stream);
 

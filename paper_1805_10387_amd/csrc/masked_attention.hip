@@ -26,7 +26,7 @@ constexpr int   MA_THREADS = 256;
 constexpr int   MA_Q       = 128;   // queries of a workgroup, 32 a wave (dk/dv: keys)
 constexpr int   MA_K       = 64;    // keys of a tile (dk/dv: queries)
 constexpr float LOG2E      = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr float P_SCALE    = 1024.f;  // dv's probabilities: of 10^5 keys one has 10^-5, which fp16 has to three digits only
+constexpr float P_LOG2 = 10.f, P_SCALE = 1024.f;  // dv's probabilities: of 10^5 keys one has 10^-5, which fp16 has to three digits only
 
 struct AttnArgs {
     const uint16_t *q, *k, *v, *ctx, *dctx;
@@ -34,9 +34,10 @@ struct AttnArgs {
     float*          lse;                 // forward: out
     const float *   lse_in, *slopes;
     float *         lse2, *delta;        // backward: [n_heads, rows_pad]
+    float*          part;                // dk and dv of a part of a group's heads: [kv_heads * parts, rows_k, 2, d]
     const int2*     range;
     const int4*     tile;
-    int             rows_q, rows_k, heads, group, d, rows_pad;
+    int             rows_q, rows_k, heads, group, part_heads, d, rows_pad;
     int             ld_q, ld_k, ld_v, ld_ctx, ld_dq, ld_dk, ld_dv, ld_dctx;
     float           alpha, cap;
 };
@@ -68,8 +69,8 @@ __global__ __launch_bounds__(64) void mask_kernel(int rows, int rows_k, int n_do
             }
         }
         if (lo >= hi) lo = hi = 0;
-        range[r] = make_int2(lo, hi);
     }
+    range[r]        = make_int2(lo, hi);  // (of the last 64 rows all)
     const bool some = lo < hi;
     int        a = some ? lo : INT_MAX, b = some ? hi : 0, c = some ? lo : INT_MAX, d = some ? hi : 0;
 #pragma unroll
@@ -83,76 +84,30 @@ __global__ __launch_bounds__(64) void mask_kernel(int rows, int rows_k, int n_do
 }
 
 // ------------------------------------------------------------------------------------------------ scores
-// Base-2 scores of a block of accumulators; lanes own one index, registers the other (`at0` + 8 (r / 4) + r % 4).
-// th (backward): tanh of the capped score.
-template <bool GENERAL>
-__device__ __forceinline__ void scores(const AttnArgs& a, f32x16& s, float slope2, int dist0, f32x16* th = nullptr) {
-    if (!GENERAL) {
+// What is done to q k^T: nothing but the scale (to base 2: one factor beside the exponential's), a distance bias, or a cap with a bias
+// that may be 0.
+enum { PLAIN = 0, BIAS = 1, CAP = 2 };
+// Base-2 scores in place.  Lanes own one index, registers the other; dist: query less key (or the reverse) at register 0.  th: tanh of the
+// capped score, for the backward pass.
+template <int MODE>
+__device__ __forceinline__ void scores(const AttnArgs& a, f32x16& s, float slope2, int dist, f32x16* th = nullptr) {
+    if (MODE == PLAIN) return;
+    const float k = MODE == CAP ? a.alpha / a.cap * (2.f * LOG2E) : a.alpha * LOG2E, c = a.cap * LOG2E, at = (float)dist;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] *= a.alpha * LOG2E;
-        return;
-    }
-    if (a.cap > 0.f) {
-        // tanh(x) = 1 - 2 / (exp(2x) + 1): an absolute error of 1e-7, which is what counts for a score
-        const float k = a.alpha / a.cap * (2.f * LOG2E), c = a.cap * LOG2E;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
+    for (int r = 0; r < 16; ++r) {
+        if (MODE == CAP) {
+            // tanh(x) = 1 - 2 / (exp(2x) + 1): an absolute error of 1e-7, which is what counts for a score
             const float t = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[r] * k) + 1.f), 1.f);
             if (th) (*th)[r] = t;
             s[r] = c * t;
+        } else {
+            s[r] *= k;
         }
-    } else {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] *= a.alpha * LOG2E;
-    }
-    if (a.slopes) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = fmaf(-slope2, (float)abs(dist0 + 8 * (r >> 2) + (r & 3)), s[r]);
+        s[r] = fmaf(-slope2, fabsf(at + (float)(8 * (r >> 2) + (r & 3))), s[r]);
     }
 }
 
-// ------------------------------------------------------------------------------------------------ staging
-// ROWS rows of a matrix from `row0` on, columns [0, d), into registers; rows outside [0, rows) and columns from d on are zero.
-template <int D, int ROWS>
-struct Stage {
-    static constexpr int ROWB = D <= 64 ? 128 : 256, C = ROWB / 16, N = ROWS * C / MA_THREADS;
-    u32x4m               r[N];
-    __device__ __forceinline__ void load(const uint16_t* M, int ld, int row0, int rows, int d) {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int v = threadIdx.x + MA_THREADS * j, row = row0 + v / C, col = (v % C) * 8;
-            r[j]        = u32x4m{0u, 0u, 0u, 0u};
-            if (row < rows && col < d) r[j] = *reinterpret_cast<const u32x4m*>(M + (long long)row * ld + col);
-        }
-    }
-    __device__ __forceinline__ void store(char* X) const {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int v = threadIdx.x + MA_THREADS * j;
-            *reinterpret_cast<u32x4m*>(LdsTile<ROWB>::piece(X, v / C, v % C)) = r[j];
-        }
-    }
-    // Zeroes non-finite elements; bad (may be null): per row, NaN if it had one, else 0.
-    __device__ __forceinline__ void clean(float* bad) {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            bool any = false;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const unsigned x = r[j][w];
-                const bool     l = (x & 0x7C00u) == 0x7C00u, h = (x & 0x7C000000u) == 0x7C000000u;
-                r[j][w]          = x & ((l ? 0u : 0xFFFFu) | (h ? 0u : 0xFFFF0000u));
-                any |= l | h;
-            }
-            if (bad) {  // the C pieces of a row are with C neighbouring lanes
-                const unsigned long long m    = __ballot(any);
-                const int                lane = threadIdx.x & 63, first = lane / C * C;
-                if (lane == first) bad[(threadIdx.x + MA_THREADS * j) / C] = (m >> first) & ((1ull << C) - 1) ? NAN : 0.f;
-            }
-        }
-    }
-};
-
+// ------------------------------------------------------------------------------------------------ tiles
 __device__ __forceinline__ f32x16 zero16() { return f32x16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}; }
 
 // Rows of a result tile D[i = column][j = row], scaled, to memory: this lane's row, 16-byte pieces.
@@ -170,151 +125,255 @@ __device__ __forceinline__ void store_rows(uint16_t* row, const f32x16 (&o)[DT],
         }
 }
 
-// What the keys of 128 queries are: of the workgroup and of this wave's 32.
+// What 128 queries see: of the workgroup, of this wave's 32 and of this lane's.
 struct QueryRange {
-    int lo, hi;                        // this lane's query
-    int wlo, whi, wlo_max, whi_min;    // the wave's
-    int glo, ghi, glo_max, ghi_min;    // the workgroup's
-};
-__device__ __forceinline__ QueryRange query_range(const AttnArgs& a, int m, int m0) {
-    QueryRange x;
-    const int2 r = m < a.rows_q ? a.range[m] : make_int2(0, 0);
-    x.lo         = max(r.x, 0);
-    x.hi         = min(r.y, a.rows_k);
-    if (x.lo >= x.hi) x.lo = x.hi = 0;
-    const bool some = x.lo < x.hi;
-    x.wlo = some ? x.lo : INT_MAX, x.whi = some ? x.hi : 0, x.wlo_max = some ? x.lo : INT_MAX, x.whi_min = some ? x.hi : 0;
+    int lo, hi;
+    int wlo, whi, wlo_max, whi_min;
+    int glo, ghi, glo_max, ghi_min;
+    __device__ __forceinline__ QueryRange(const AttnArgs& a, int m0, int m) {
+        const int2 v = m < a.rows_q ? a.range[m] : make_int2(0, 0);
+        lo           = max(v.x, 0);
+        hi           = min(v.y, a.rows_k);
+        if (lo >= hi) lo = hi = 0;
+        int p = lo < hi ? lo : INT_MAX, q = hi, r = p, t = hi;
 #pragma unroll
-    for (int s = 1; s < 32; s *= 2) {
-        x.wlo     = min(x.wlo, __shfl_xor(x.wlo, s, 64));
-        x.whi     = max(x.whi, __shfl_xor(x.whi, s, 64));
-        x.wlo_max = max(x.wlo_max, __shfl_xor(x.wlo_max, s, 64));
-        x.whi_min = min(x.whi_min, __shfl_xor(x.whi_min, s, 64));
+        for (int s = 1; s < 32; s *= 2) {
+            p = min(p, __shfl_xor(p, s, 64));
+            q = max(q, __shfl_xor(q, s, 64));
+            r = max(r, __shfl_xor(r, s, 64));
+            t = min(t, __shfl_xor(t, s, 64));
+        }
+        wlo = __builtin_amdgcn_readfirstlane(p), whi = __builtin_amdgcn_readfirstlane(q);
+        wlo_max = __builtin_amdgcn_readfirstlane(r), whi_min = __builtin_amdgcn_readfirstlane(t);
+        int4 x = a.tile[m0 / 64];
+        if (m0 + 64 < a.rows_q) {
+            const int4 y = a.tile[m0 / 64 + 1];
+            x            = make_int4(min(x.x, y.x), max(x.y, y.y), max(x.z, y.z), min(x.w, y.w));
+        } else {
+            x.z = INT_MAX;  // rows behind the last one: not whole
+        }
+        glo = __builtin_amdgcn_readfirstlane(max(x.x, 0)), ghi = __builtin_amdgcn_readfirstlane(min(x.y, a.rows_k));
+        glo_max = __builtin_amdgcn_readfirstlane(x.z), ghi_min = __builtin_amdgcn_readfirstlane(x.w);
     }
-    x.wlo     = __builtin_amdgcn_readfirstlane(x.wlo);
-    x.whi     = __builtin_amdgcn_readfirstlane(x.whi);
-    x.wlo_max = __builtin_amdgcn_readfirstlane(x.wlo_max);
-    x.whi_min = __builtin_amdgcn_readfirstlane(x.whi_min);
-    int4 t    = a.tile[m0 / 64];
-    if (m0 + 64 < a.rows_q) {
-        const int4 u = a.tile[m0 / 64 + 1];
-        t            = make_int4(min(t.x, u.x), max(t.y, u.y), max(t.z, u.z), min(t.w, u.w));
-    } else {
-        t.z = INT_MAX;  // rows behind the last one: not whole
-    }
-    x.glo = max(t.x, 0), x.ghi = min(t.y, a.rows_k), x.glo_max = t.z, x.ghi_min = t.w;
-    return x;
-}
+    __device__ __forceinline__ bool whole(int kb) const { return glo_max <= kb && ghi_min >= kb + MA_K; }
+    __device__ __forceinline__ bool none(int kb) const { return wlo >= kb + MA_K || whi <= kb; }
+    __device__ __forceinline__ bool all(int kb) const { return wlo_max <= kb && whi_min >= kb + MA_K; }
+};
 
-// ------------------------------------------------------------------------------------------------ forward
-template <int D, bool GENERAL>
-__global__ __launch_bounds__(MA_THREADS, 2) void masked_fwd_kernel(AttnArgs a) {
-    constexpr int KK = D / 16, DT = D / 32;
-    typedef Stage<D, MA_K>        St;
-    typedef LdsTile<St::ROWB>     Tile;
-    __shared__ __align__(16) char Ks[MA_K * St::ROWB], Vs[MA_K * St::ROWB];
-    __shared__ float              bad[MA_K];
-
-    const int tiles = (a.rows_q + MA_Q - 1) / MA_Q;
-    const int h = blockIdx.x % a.heads, qt = tiles - 1 - blockIdx.x / a.heads, kvh = h / a.group;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hf = lane >> 5;
-    const int m0 = qt * MA_Q, m = m0 + 32 * wave + (lane & 31);
-    const QueryRange x = query_range(a, m, m0);
-    const uint16_t*  K = a.k + kvh * a.d;
-    const uint16_t*  V = a.v + kvh * a.d;
-
-    f16x8 qf[KK];
+// This lane's row of a matrix as second operands (zeros outside).
+template <int KK>
+__device__ __forceinline__ void row_frags(f16x8 (&f)[KK], const uint16_t* row, int d, int hf) {
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
         u32x4m p = {0u, 0u, 0u, 0u};
-        if (m < a.rows_q && 16 * kk + 8 * hf < a.d) p = *reinterpret_cast<const u32x4m*>(a.q + (long long)m * a.ld_q + h * a.d + 16 * kk + 8 * hf);
-        qf[kk] = frag8(p);
+        if (row && 16 * kk + 8 * hf < d) p = *reinterpret_cast<const u32x4m*>(row + 16 * kk + 8 * hf);
+        f[kk] = frag8(p);
     }
-    const float slope2 = GENERAL && a.slopes ? a.slopes[h] * LOG2E : 0.f;
-    f32x16      o[DT];
+}
+// Fragments have come from memory here: otherwise the first use of them in a loop would wait for every load in flight, in each turn.
+template <int KK>
+__device__ __forceinline__ void settle(f16x8 (&f)[KK]) {
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(f[kk]));
+}
+
+__device__ __forceinline__ f32x16 mma(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f16x8  words(const unsigned (&w)[8], int e) { return frag8(u32x4m{w[e], w[e + 1], w[e + 2], w[e + 3]}); }
+// A barrier behind which the loads of every wave have arrived.
+__device__ __forceinline__ void arrive() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+__device__ __forceinline__ void step() { __builtin_amdgcn_sched_barrier(0); }
+
+// ------------------------------------------------------------------------------------------------ forward
+constexpr float LAZY = 8.f;  // the maximum that exponentials refer to follows when it is 2^8 behind
+
+// The scores of a tile take the registers of the one before as soon as its exponentials leave them, half by half: matrix and vector
+// instructions of one wave run side by side, and there is room for a second wave.
+template <int D, int MODE>
+__global__ __launch_bounds__(MA_THREADS, D <= 64 ? 2 : 1) void masked_fwd_kernel(AttnArgs a) {
+    constexpr int KK = D / 16, DT = D / 32, ROWB = D <= 64 ? 128 : 256;
+    typedef TileLoad<ROWB, 4>     Load;
+    typedef LdsTile<ROWB>         Tile;
+    __shared__ __align__(256) char Ks[2][MA_K * ROWB], Vs[2][MA_K * ROWB];
+    __shared__ __align__(16) float bad[MA_K];
+
+    const int tiles = (a.rows_q + MA_Q - 1) / MA_Q;
+    const int h = blockIdx.x % a.heads, qt = tiles - 1 - blockIdx.x / a.heads, kvh = h / a.group;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hf = lane >> 5;
+    const int m0 = qt * MA_Q, m = m0 + 32 * wave + (lane & 31);
+    const QueryRange x(a, m0, m);
+    const uint16_t*  K = a.k + kvh * a.d;
+    const uint16_t*  V = a.v + kvh * a.d;
+    Load             lk, lv;
+    lk.init(a.ld_k, a.d, wave, lane);
+    lv.init(a.ld_v, a.d, wave, lane);
+    if (x.glo < x.ghi) {
+        lk.issue(K, a.ld_k, x.glo, a.rows_k, a.d, Ks[0], wave);
+        lv.issue(V, a.ld_v, x.glo, a.rows_k, a.d, Vs[0], wave);
+    }
+    f16x8 qf[KK];
+    row_frags<KK>(qf, m < a.rows_q ? a.q + (long long)m * a.ld_q + h * a.d : nullptr, a.d, hf);
+    const float slope2 = MODE && a.slopes ? a.slopes[h] * LOG2E : 0.f;
+    const float c      = MODE ? 1.f : a.alpha * LOG2E;  // scores to base 2
+    f32x16      o[DT], s[2];
+    float       ref = -INFINITY, sum = 0.f, top = -INFINITY;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) o[dt] = zero16();
-    float mx = -INFINITY, sum = 0.f;
+    settle<KK>(qf);
 
-    St rk, rv;
-    if (x.glo < x.ghi) {
-        rk.load(K, a.ld_k, x.glo, a.rows_k, a.d);
-        rv.load(V, a.ld_v, x.glo, a.rows_k, a.d);
+    const unsigned at_k = lds_address(Ks) + Tile::plain(lane), at_v = lds_address(Vs) + Tile::across(lane);
+    constexpr unsigned SIZE = MA_K * ROWB;
+    const auto score = [&](f32x16(&to)[2], int kb, int t, unsigned X) {  // 32 keys of tile kb
+        to[t] = zero16();
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+            to[t] = mma(Tile::frag(X, 32 * t, kk), qf[kk], to[t]);
+            if (kk % 4 == 3) step();
+        }
+        scores<MODE>(a, to[t], slope2, kb + 32 * t + 4 * hf - m);
+    };
+    const auto highest = [&](const f32x16(&of)[2]) {
+        float v = of[0][0];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) v = fmaxf(v, of[t][r]);
+        return join_halves(v, [](float p, float q) { return fmaxf(p, q); }) * c;
+    };
+    unsigned   pk[2][8];
+    float      base = 0.f;
+    const auto follow = [&]() {  // the reference, where a query's maximum has left it behind
+        const bool late = top > ref + LAZY;
+        if (__any(late)) {  // (each query by itself: its bits do not depend on its neighbours)
+            const float fix = late ? __builtin_amdgcn_exp2f(ref - top) : 1.f;
+            ref             = late ? top : ref;
+            sum *= fix;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[dt][r] *= fix;
+        }
+        base = ref == -INFINITY ? 0.f : ref;  // (nothing seen yet: exp(-inf - 0) = 0)
+    };
+    const auto weights = [&](int t, int first, int last) {
+#pragma unroll
+        for (int e = first; e < last; ++e) {
+            const float p0 = __builtin_amdgcn_exp2f(fmaf(s[t][2 * e], c, -base)), p1 = __builtin_amdgcn_exp2f(fmaf(s[t][2 * e + 1], c, -base));
+            sum += p0 + p1;
+            pk[t][e] = pack_f16(p0, p1);
+        }
+    };
+    const auto values = [&](int t, unsigned X) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[dt] = mma(Tile::frag_t(X, 32 * t + 16 * u, dt), words(pk[t], 4 * u), o[dt]);
+            step();
+        }
+    };
+
+    int        b = 0, kb = x.glo;
+    const auto turn = [&]() {  // the values of this tile and the keys of the next are there, and every wave is done with those before
+        arrive();
+        if (kb + 2 * MA_K < x.ghi) lk.issue(K, a.ld_k, kb + 2 * MA_K, a.rows_k, a.d, Ks[b], wave);
+        if (kb + MA_K < x.ghi) lv.issue(V, a.ld_v, kb + MA_K, a.rows_k, a.d, Vs[b ^ 1], wave);
+    };
+    const auto fast = [&]() { return x.whole(kb) && kb + MA_K < x.ghi && !x.none(kb + MA_K); };
+    if (kb < x.ghi) {
+        arrive();
+        if (kb + MA_K < x.ghi) lk.issue(K, a.ld_k, kb + MA_K, a.rows_k, a.d, Ks[1], wave);
+        if (!x.none(kb)) {
+            score(s, kb, 0, at_k);
+            score(s, kb, 1, at_k);
+            top = highest(s);
+        }
     }
-    for (int kb = x.glo; kb < x.ghi; kb += MA_K) {
-        const bool whole = x.glo_max <= kb && x.ghi_min >= kb + MA_K;
-        __syncthreads();  // every wave is done with the tile before
-        if (!whole) rv.clean(bad);
-        rk.store(Ks);
-        rv.store(Vs);
-        __syncthreads();
-        if (kb + MA_K < x.ghi) {
-            rk.load(K, a.ld_k, kb + MA_K, a.rows_k, a.d);
-            rv.load(V, a.ld_v, kb + MA_K, a.rows_k, a.d);
-        }
-        if (x.wlo >= kb + MA_K || x.whi <= kb) continue;  // nothing for this wave
-        f32x16 s[2];
+    for (; kb < x.ghi; kb += MA_K, b ^= 1) {
+        turn();
+        while (fast()) {
+            // Steps, each the products of fragments that were read during the one before: values of 32 keys, scores of the 32 keys of the
+            // next tile that take their registers, and the same of the other 32.
+            constexpr int PARTS = D > 64 ? 2 : 1, PER = KK / PARTS, STEPS = 4 * PARTS;
+            f16x8         F[2][PER];
+            const unsigned xk = at_k + (b ^ 1) * SIZE, xv = at_v + b * SIZE;
+            const auto    read = [&](int i) {
+                const int t = i / PARTS >> 1, part = i % PARTS;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            s[t] = zero16();
-#pragma unroll
-            for (int kk = 0; kk < KK; ++kk)
-                s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(Tile::frag(Ks, 32 * t + (lane & 31), kk, hf), qf[kk], s[t], 0, 0, 0);
-            scores<GENERAL>(a, s[t], slope2, kb + 32 * t + 4 * hf - m);
-        }
-        if (!whole) {  // (also where this wave's own queries see all of it: values were zeroed)
-            const bool     mine = x.wlo_max <= kb && x.whi_min >= kb + MA_K;
-            const int      n0   = kb + 4 * hf - x.lo;
-            const unsigned len  = x.hi - x.lo;
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int n = 32 * t + 8 * (r >> 2) + (r & 3);
-                    s[t][r] += bad[n + 4 * hf];
-                    if (!mine) s[t][r] = (unsigned)(n0 + n) < len ? s[t][r] : -INFINITY;
+                for (int j = 0; j < PER; ++j) {
+                    const int w = (part * PER + j) / DT, dt = (part * PER + j) % DT;
+                    F[i & 1][j] = i / PARTS & 1 ? Tile::frag(xk, 32 * t, part * PER + j) : Tile::frag_t(xv, 32 * t + 16 * w, dt);
                 }
-        }
-        float top = mx;
+            };
+            const auto multiply = [&](int i) {
+                const int t = i / PARTS >> 1, part = i % PARTS;
+                if ((i / PARTS & 1) && part == 0) s[t] = zero16();
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+                for (int j = 0; j < PER; ++j) {
+                    const int w = (part * PER + j) / DT, dt = (part * PER + j) % DT;
+                    if (i / PARTS & 1) s[t] = mma(F[i & 1][j], qf[part * PER + j], s[t]);
+                    else o[dt] = mma(F[i & 1][j], words(pk[t], 4 * w), o[dt]);
+                }
+            };
+            read(0);
+            follow();
+            weights(0, 0, 8);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
-        top              = join_halves(top, [](float p, float q) { return fmaxf(p, q); });
-        const float base = top == -INFINITY ? 0.f : top;  // (nothing seen yet: exp(-inf - 0) = 0)
-        const float fix  = __builtin_amdgcn_exp2f(mx - base);
-        mx               = top;
-        sum *= fix;
-        unsigned pk[2][8];
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float p0 = __builtin_amdgcn_exp2f(s[t][2 * e] - base), p1 = __builtin_amdgcn_exp2f(s[t][2 * e + 1] - base);
-                sum += p0 + p1;
-                pk[t][e] = pack_f16(p0, p1);
+            for (int i = 0; i < STEPS; ++i) {
+                step();
+                if (i + 1 < STEPS) read(i + 1);
+                multiply(i);
+                if (i < 2 * PARTS) weights(1, 4 * i / PARTS, 4 * (i + 1) / PARTS);
+                if (i == 2 * PARTS) scores<MODE>(a, s[0], slope2, kb + MA_K + 4 * hf - m);
             }
+            scores<MODE>(a, s[1], slope2, kb + MA_K + 32 + 4 * hf - m);
+            top = highest(s);
+            kb += MA_K, b ^= 1;
+            turn();
+        }
+        const bool whole = x.whole(kb), more = kb + MA_K < x.ghi;
+        if (!whole) {
+            Load::clean(Vs[b], bad, wave, lane);
+            lds_barrier();
+        }
+        if (!x.none(kb)) {
+            if (!whole) {  // (also where this wave's own queries see all of it: values were zeroed)
+                const bool     mine = x.all(kb);
+                const int      n0   = kb + 4 * hf - x.lo;
+                const unsigned len  = x.hi - x.lo;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
+                for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) o[dt][r] *= fix;
+                    for (int r = 0; r < 16; ++r) {
+                        const int n = 32 * t + 8 * (r >> 2) + (r & 3);
+                        s[t][r] += bad[n + 4 * hf];
+                        if (!mine) s[t][r] = (unsigned)(n0 + n) < len ? s[t][r] : -INFINITY;
+                        if (r % 8 == 7) step();
+                    }
+                top = highest(s);
+            }
+            follow();
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(Tile::frag_t(Vs, 32 * dt, 32 * t + 16 * u + 4 * hf, lane),
-                                                                   frag8(u32x4m{pk[t][4 * u], pk[t][4 * u + 1], pk[t][4 * u + 2], pk[t][4 * u + 3]}),
-                                                                   o[dt], 0, 0, 0);
+            for (int t = 0; t < 2; ++t) {
+                weights(t, 0, 8);
+                step();
+                values(t, at_v + b * SIZE);
+            }
+        }
+        if (more && !x.none(kb + MA_K)) {
+            step();
+            score(s, kb + MA_K, 0, at_k + (b ^ 1) * SIZE);
+            score(s, kb + MA_K, 1, at_k + (b ^ 1) * SIZE);
+            top = highest(s);
         }
     }
     sum = join_halves(sum, [](float p, float q) { return p + q; });
-    if (m < a.rows_q && hf == 0) a.lse[(long long)h * a.rows_q + m] = sum == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * LN2;
+    if (m < a.rows_q && hf == 0) a.lse[(long long)h * a.rows_q + m] = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * LN2;
     store_rows<DT>(m < a.rows_q ? a.out + (long long)m * a.ld_ctx + h * a.d : nullptr, o, sum == 0.f ? 0.f : 1.f / sum, a.d, hf);
 }
 
 // ------------------------------------------------------------------------------------------------ backward
 // Row statistics: lse in base 2 (+inf where a row sees nothing: its probabilities are then 0; NaN where it or delta is not a number
-// to go by) and delta.  16 lanes a (row, head) pair.
+// to go by) less log2 of P_SCALE, and delta / P_SCALE, so that p comes out times P_SCALE and ds = p (dp / P_SCALE - delta) as it is.
+// 16 lanes a (row, head) pair.
 __global__ __launch_bounds__(MA_THREADS) void masked_stats_kernel(AttnArgs a) {
     const long long pair = (long long)blockIdx.x * (MA_THREADS / 16) + (threadIdx.x >> 4);
     const int       row = (int)(pair / a.heads), h = (int)(pair - (long long)row * a.heads), c = (threadIdx.x & 15) * 8;
@@ -338,38 +397,37 @@ __global__ __launch_bounds__(MA_THREADS) void masked_stats_kernel(AttnArgs a) {
         else if (!(fabsf(l) < INFINITY && fabsf(s) < INFINITY))
             l = NAN, s = 0.f;
     }
-    a.lse2[(long long)h * a.rows_pad + row]  = l;
-    a.delta[(long long)h * a.rows_pad + row] = s;
+    a.lse2[(long long)h * a.rows_pad + row]  = l - P_LOG2;
+    a.delta[(long long)h * a.rows_pad + row] = s * (1.f / P_SCALE);
 }
 
-// dq of 128 queries: the forward kernel's walk over the keys.
-template <int D, bool GENERAL>
-__global__ __launch_bounds__(MA_THREADS, 2) void masked_dq_kernel(AttnArgs a) {
-    constexpr int KK = D / 16, DT = D / 32;
-    typedef Stage<D, MA_K>        St;
-    typedef LdsTile<St::ROWB>     Tile;
-    __shared__ __align__(16) char Ks[MA_K * St::ROWB], Vs[MA_K * St::ROWB];
+// dq of 128 queries, 32 of them a wave.
+template <int D, int MODE>
+__global__ __launch_bounds__(MA_THREADS, D <= 64 ? 2 : 1) void masked_dq_kernel(AttnArgs a) {
+    constexpr int KK = D / 16, DT = D / 32, ROWB = D <= 64 ? 128 : 256;
+    typedef TileLoad<ROWB, 4>     Load;
+    typedef LdsTile<ROWB>         Tile;
+    __shared__ __align__(256) char Ks[2][MA_K * ROWB], Vs[2][MA_K * ROWB];
 
     const int tiles = (a.rows_q + MA_Q - 1) / MA_Q;
     const int h = blockIdx.x % a.heads, qt = tiles - 1 - blockIdx.x / a.heads, kvh = h / a.group;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hf = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hf = lane >> 5;
     const int m0 = qt * MA_Q, m = m0 + 32 * wave + (lane & 31);
-    const QueryRange x = query_range(a, m, m0);
+    const QueryRange x(a, m0, m);
     const uint16_t*  K = a.k + kvh * a.d;
     const uint16_t*  V = a.v + kvh * a.d;
-
-    f16x8 qf[KK], gf[KK];
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-        u32x4m p = {0u, 0u, 0u, 0u}, g = p;
-        if (m < a.rows_q && 16 * kk + 8 * hf < a.d) {
-            p = *reinterpret_cast<const u32x4m*>(a.q + (long long)m * a.ld_q + h * a.d + 16 * kk + 8 * hf);
-            g = *reinterpret_cast<const u32x4m*>(a.dctx + (long long)m * a.ld_dctx + h * a.d + 16 * kk + 8 * hf);
-        }
-        qf[kk] = frag8(p);
-        gf[kk] = frag8(g);
+    Load             lk, lv;
+    lk.init(a.ld_k, a.d, wave, lane);
+    lv.init(a.ld_v, a.d, wave, lane);
+    if (x.glo < x.ghi) {
+        lk.issue(K, a.ld_k, x.glo, a.rows_k, a.d, Ks[0], wave);
+        lv.issue(V, a.ld_v, x.glo, a.rows_k, a.d, Vs[0], wave);
     }
-    const float slope2 = GENERAL && a.slopes ? a.slopes[h] * LOG2E : 0.f;
+    f16x8 qf[KK], gf[KK];
+    row_frags<KK>(qf, m < a.rows_q ? a.q + (long long)m * a.ld_q + h * a.d : nullptr, a.d, hf);
+    row_frags<KK>(gf, m < a.rows_q ? a.dctx + (long long)m * a.ld_dctx + h * a.d : nullptr, a.d, hf);
+    const float slope2 = MODE && a.slopes ? a.slopes[h] * LOG2E : 0.f;
+    const float c      = MODE ? 1.f : a.alpha * LOG2E;
     float       lse2 = INFINITY, delta = 0.f;
     if (m < a.rows_q) {
         lse2  = a.lse2[(long long)h * a.rows_pad + m];
@@ -378,60 +436,98 @@ __global__ __launch_bounds__(MA_THREADS, 2) void masked_dq_kernel(AttnArgs a) {
     f32x16 o[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) o[dt] = zero16();
+    settle<KK>(qf);
+    settle<KK>(gf);
+    asm volatile("" : "+v"(lse2), "+v"(delta));
+    const unsigned     at_k = lds_address(Ks) + Tile::plain(lane), at_v = lds_address(Vs) + Tile::plain(lane), at_t = lds_address(Ks) + Tile::across(lane);
+    constexpr unsigned SIZE = MA_K * ROWB;
 
-    St rk, rv;
-    if (x.glo < x.ghi) {
-        rk.load(K, a.ld_k, x.glo, a.rows_k, a.d);
-        rv.load(V, a.ld_v, x.glo, a.rows_k, a.d);
-    }
-    for (int kb = x.glo; kb < x.ghi; kb += MA_K) {
-        const bool whole = x.glo_max <= kb && x.ghi_min >= kb + MA_K;
-        __syncthreads();
-        if (!whole) {
-            rk.clean(nullptr);
-            rv.clean(nullptr);
-        }
-        rk.store(Ks);
-        rv.store(Vs);
-        __syncthreads();
+    int b = 0;
+    for (int kb = x.glo; kb < x.ghi; kb += MA_K, b ^= 1) {
+        arrive();
         if (kb + MA_K < x.ghi) {
-            rk.load(K, a.ld_k, kb + MA_K, a.rows_k, a.d);
-            rv.load(V, a.ld_v, kb + MA_K, a.rows_k, a.d);
+            lk.issue(K, a.ld_k, kb + MA_K, a.rows_k, a.d, Ks[b ^ 1], wave);
+            lv.issue(V, a.ld_v, kb + MA_K, a.rows_k, a.d, Vs[b ^ 1], wave);
         }
-        if (x.wlo >= kb + MA_K || x.whi <= kb) continue;
-        const bool     mine = x.wlo_max <= kb && x.whi_min >= kb + MA_K;
-        const int      n0   = kb + 4 * hf - x.lo;
-        const unsigned len  = x.hi - x.lo;
-        unsigned       ds[2][8];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            f32x16 s = zero16(), dp = zero16(), th;
-#pragma unroll
-            for (int kk = 0; kk < KK; ++kk) {
-                s  = __builtin_amdgcn_mfma_f32_32x32x16_f16(Tile::frag(Ks, 32 * t + (lane & 31), kk, hf), qf[kk], s, 0, 0, 0);
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_f16(Tile::frag(Vs, 32 * t + (lane & 31), kk, hf), gf[kk], dp, 0, 0, 0);
-            }
-            scores<GENERAL>(a, s, slope2, kb + 32 * t + 4 * hf - m, &th);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                float p = __builtin_amdgcn_exp2f(s[r] - lse2);
-                if (!mine) p = (unsigned)(n0 + 32 * t + 8 * (r >> 2) + (r & 3)) < len ? p : 0.f;
-                float d = p * (dp[r] - delta);
-                if (GENERAL && a.cap > 0.f) d *= fmaf(-th[r], th[r], 1.f);
-                s[r] = d;
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) ds[t][e] = pack_f16(s[2 * e], s[2 * e + 1]);
+        if (!x.whole(kb)) {
+            Load::clean(Ks[b], nullptr, wave, lane);
+            Load::clean(Vs[b], nullptr, wave, lane);
+            lds_barrier();
         }
+        if (x.none(kb)) continue;
+        const auto work = [&](auto masked) {
+            constexpr bool MASKED = decltype(masked)::value;
+            const int      n0     = kb + 4 * hf - x.lo;
+            const unsigned len    = x.hi - x.lo;
+            const unsigned xk = at_k + b * SIZE, xv = at_v + b * SIZE, xt = at_t + b * SIZE;
+            f32x16         s[2], dp[2], th[2];
+            unsigned       ds[2][8];
+            // Steps as in the kernel of dk and dv: scores and dp of 32 keys (u), of the other 32, dq of the first, of the other.
+            constexpr int PP = D / 32, GP = D == 128 ? 2 : 1, PER = 2 * DT / GP, STEPS = 2 * PP + 2 * GP;
+            f16x8         F[2][PER > 4 ? PER : 4];
+            const auto    read = [&](int i) {
+                if (i < 2 * PP) {
+                    const int u = i / PP, part = i % PP;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
+                    for (int j = 0; j < 2; ++j) {
+                        F[i & 1][2 * j]     = Tile::frag(xk, 32 * u, 2 * part + j);
+                        F[i & 1][2 * j + 1] = Tile::frag(xv, 32 * u, 2 * part + j);
+                    }
+                } else {
+                    const int u = (i - 2 * PP) / GP, part = (i - 2 * PP) % GP;
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+                    for (int j = 0; j < PER; ++j) {
+                        const int w = (part * PER + j) / DT, dt = (part * PER + j) % DT;
+                        F[i & 1][j] = Tile::frag_t(xt, 32 * u + 16 * w, dt);
+                    }
+                }
+            };
+            const auto multiply = [&](int i) {
+                if (i < 2 * PP) {
+                    const int u = i / PP, part = i % PP;
+                    if (part == 0) s[u] = dp[u] = zero16();
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
-                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(Tile::frag_t(Ks, 32 * dt, 32 * t + 16 * u + 4 * hf, lane),
-                                                                   frag8(u32x4m{ds[t][4 * u], ds[t][4 * u + 1], ds[t][4 * u + 2], ds[t][4 * u + 3]}),
-                                                                   o[dt], 0, 0, 0);
+                    for (int j = 0; j < 2; ++j) {
+                        s[u]  = mma(F[i & 1][2 * j], qf[2 * part + j], s[u]);
+                        dp[u] = mma(F[i & 1][2 * j + 1], gf[2 * part + j], dp[u]);
+                    }
+                } else {
+                    const int u = (i - 2 * PP) / GP, part = (i - 2 * PP) % GP;
+#pragma unroll
+                    for (int j = 0; j < PER; ++j) {
+                        const int w = (part * PER + j) / DT, dt = (part * PER + j) % DT;
+                        o[dt] = mma(F[i & 1][j], words(ds[u], 4 * w), o[dt]);
+                    }
+                }
+            };
+            const auto weights = [&](int u, int first, int last) {  // ds of pairs of keys
+                if (MODE && first == 0) scores<MODE>(a, s[u], slope2, kb + 32 * u + 4 * hf - m, &th[u]);
+#pragma unroll
+                for (int e = first; e < last; ++e) {
+                    float d[2];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const int r = 2 * e + y;
+                        float     p = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -lse2));  // (times P_SCALE)
+                        if (MASKED) p = (unsigned)(n0 + 32 * u + 8 * (r >> 2) + (r & 3)) < len ? p : 0.f;
+                        d[y] = p * fmaf(dp[u][r], 1.f / P_SCALE, -delta);
+                        if (MODE == CAP) d[y] *= fmaf(-th[u][r], th[u][r], 1.f);
+                    }
+                    ds[u][e] = pack_f16(d[0], d[1]);
+                }
+            };
+            read(0);
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                step();
+                if (i + 1 < STEPS) read(i + 1);
+                multiply(i);
+                if (i >= PP && i < 2 * PP) weights(0, 8 * (i - PP) / PP, 8 * (i - PP + 1) / PP);
+                if (i >= 2 * PP && i < 2 * PP + GP) weights(1, 8 * (i - 2 * PP) / GP, 8 * (i - 2 * PP + 1) / GP);
+            }
+        };
+        if (x.all(kb)) work(std::false_type{});
+        else work(std::true_type{});
     }
     // (a row that sees nothing may hold anything in q and dctx, and 0 x NaN has reached its sums)
     if (x.lo >= x.hi) {
@@ -441,130 +537,217 @@ __global__ __launch_bounds__(MA_THREADS, 2) void masked_dq_kernel(AttnArgs a) {
     store_rows<DT>(m < a.rows_q ? a.dq + (long long)m * a.ld_dq + h * a.d : nullptr, o, a.alpha, a.d, hf);
 }
 
-// dk and dv of 128 keys: 32 of them a wave, over the tiles of 64 queries that see any of them, head by head.
-template <int D, bool GENERAL>
-__global__ __launch_bounds__(MA_THREADS, 1) void masked_dkv_kernel(AttnArgs a) {
-    constexpr int KK = D / 16, DT = D / 32;
-    typedef Stage<D, MA_K>        St;
-    typedef LdsTile<St::ROWB>     Tile;
-    __shared__ __align__(16) char Qs[MA_K * St::ROWB], Gs[MA_K * St::ROWB];
-    __shared__ __align__(16) float lse2[MA_K], delta[MA_K];
-    __shared__ __align__(16) int   los[MA_K], lens[MA_K];
+// dk and dv of 128 keys, 32 of them a wave, over the tiles of 64 queries that see any of them, head by head: of all heads that share
+// the keys, or (PART) of a.part_heads of them, whose sums the join kernel adds up.
+template <int D, int MODE>
+__global__ __launch_bounds__(MA_THREADS, D <= 64 && MODE == PLAIN ? 2 : 1) void masked_dkv_kernel(AttnArgs a) {
+    constexpr int KK = D / 16, DT = D / 32, ROWB = D <= 64 ? 128 : 256;
+    typedef TileLoad<ROWB, 4> Load;
+    typedef LdsTile<ROWB>     Tile;
+    struct Stats {
+        float lse2[MA_K], delta[MA_K];
+        int2  range[2 * MA_K];  // (a wave's load is twice as long)
+    };
+    __shared__ __align__(256) char Qs[2][MA_K * ROWB], Gs[2][MA_K * ROWB];
+    __shared__ __align__(16) Stats stats[2];
 
-    const int kv_heads = a.heads / a.group, kvh = blockIdx.x % kv_heads, kt = blockIdx.x / kv_heads;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hf = lane >> 5;
+    const int kv_heads = a.heads / a.group, parts = a.group / a.part_heads, per = kv_heads * parts;
+    const int id = blockIdx.x % per, kvh = id / parts, h0 = kvh * a.group + id % parts * a.part_heads, kt = blockIdx.x / per;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hf = lane >> 5;
     const int k0 = kt * MA_Q, n0 = k0 + 32 * wave, n = n0 + (lane & 31);
-    const int qtiles = (a.rows_q + MA_K - 1) / MA_K;
+    const int qtiles = a.rows_pad / MA_K;
 
-    f16x8 kf[KK], vf[KK];
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-        u32x4m p = {0u, 0u, 0u, 0u}, g = p;
-        if (n < a.rows_k && 16 * kk + 8 * hf < a.d) {
-            p = *reinterpret_cast<const u32x4m*>(a.k + (long long)n * a.ld_k + kvh * a.d + 16 * kk + 8 * hf);
-            g = *reinterpret_cast<const u32x4m*>(a.v + (long long)n * a.ld_v + kvh * a.d + 16 * kk + 8 * hf);
+    // the tiles to come, one by one
+    int                h = h0, base = -64, q0 = 0;
+    int4               bounds = make_int4(0, 0, 0, 0), t4 = bounds;
+    unsigned long long todo = 0;
+    const auto         advance = [&]() {
+        while (todo == 0) {
+            base += 64;
+            if (base >= qtiles) {
+                base = 0;
+                if (++h >= h0 + a.part_heads) return false;
+            }
+            bounds = base + lane < qtiles ? a.tile[base + lane] : make_int4(INT_MAX, 0, INT_MAX, 0);
+            todo   = __ballot(bounds.x < k0 + MA_Q && bounds.y > k0);  // (the same in every wave)
         }
-        kf[kk] = frag8(p);
-        vf[kk] = frag8(g);
-    }
+        const int i = __builtin_ctzll(todo);
+        todo &= todo - 1;
+        q0 = (base + i) * MA_K;
+        t4 = make_int4(__builtin_amdgcn_readlane(bounds.x, i), __builtin_amdgcn_readlane(bounds.y, i), __builtin_amdgcn_readlane(bounds.z, i),
+                       __builtin_amdgcn_readlane(bounds.w, i));
+        return true;
+    };
+    Load lq, lg;
+    lq.init(a.ld_q, a.d, wave, lane);
+    lg.init(a.ld_dctx, a.d, wave, lane);
+    const auto issue = [&](int b) {
+        lq.issue(a.q + h * a.d, a.ld_q, q0, a.rows_q, a.d, Qs[b], wave);
+        lg.issue(a.dctx + h * a.d, a.ld_dctx, q0, a.rows_q, a.d, Gs[b], wave);
+        const long long at = (long long)h * a.rows_pad + q0;
+        if (wave == 0) load_words(a.lse2 + at, stats[b].lse2, lane);
+        if (wave == 1) load_words(a.delta + at, stats[b].delta, lane);
+        if (wave == 2) load_ranges(a.range + q0, stats[b].range, lane);
+    };
+    bool more = advance();
+    if (more) issue(0);
+    f16x8 kf[KK], vf[KK];
+    row_frags<KK>(kf, n < a.rows_k ? a.k + (long long)n * a.ld_k + kvh * a.d : nullptr, a.d, hf);
+    row_frags<KK>(vf, n < a.rows_k ? a.v + (long long)n * a.ld_v + kvh * a.d : nullptr, a.d, hf);
     f32x16 dk[DT], dv[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) dk[dt] = dv[dt] = zero16();
+    settle<KK>(kf);
+    settle<KK>(vf);
+    const float c = MODE ? 1.f : a.alpha * LOG2E;
 
-    St rq, rg;
-    for (int h = kvh * a.group; h < (kvh + 1) * a.group; ++h) {
-        const uint16_t* Q      = a.q + h * a.d;
-        const uint16_t* G      = a.dctx + h * a.d;
-        const float     slope2 = GENERAL && a.slopes ? a.slopes[h] * LOG2E : 0.f;
-        for (int base = 0; base < qtiles; base += 64) {
-            int4 mine = make_int4(INT_MAX, 0, INT_MAX, 0);
-            if (base + lane < qtiles) mine = a.tile[base + lane];
-            unsigned long long todo = __ballot(mine.x < k0 + MA_Q && mine.y > k0);  // (the same in every wave)
-            bool               have = false;
-            while (todo) {
-                const int i = __builtin_ctzll(todo);
-                todo &= todo - 1;
-                const int q0 = (base + i) * MA_K;
-                if (!have) {
-                    rq.load(Q, a.ld_q, q0, a.rows_q, a.d);
-                    rg.load(G, a.ld_dctx, q0, a.rows_q, a.d);
-                }
-                const int4 t4 = make_int4(__builtin_amdgcn_readlane(mine.x, i), __builtin_amdgcn_readlane(mine.y, i),
-                                          __builtin_amdgcn_readlane(mine.z, i), __builtin_amdgcn_readlane(mine.w, i));
-                const bool whole = t4.z <= k0 && t4.w >= k0 + MA_Q && q0 + MA_K <= a.rows_q;
-                __syncthreads();
-                if (!whole) {
-                    rq.clean(nullptr);
-                    rg.clean(nullptr);
-                }
-                rq.store(Qs);
-                rg.store(Gs);
-                if (threadIdx.x < MA_K) {
-                    const int  m = q0 + threadIdx.x;
-                    const int2 r = m < a.rows_q ? a.range[m] : make_int2(0, 0);
-                    los[threadIdx.x]   = r.x;
-                    lens[threadIdx.x]  = max(r.y - r.x, 0);
-                    lse2[threadIdx.x]  = a.lse2[(long long)h * a.rows_pad + m];
-                    delta[threadIdx.x] = a.delta[(long long)h * a.rows_pad + m];
-                }
-                __syncthreads();
-                have = todo != 0;
-                if (have) {
-                    const int next = (base + __builtin_ctzll(todo)) * MA_K;
-                    rq.load(Q, a.ld_q, next, a.rows_q, a.d);
-                    rg.load(G, a.ld_dctx, next, a.rows_q, a.d);
-                }
-                if (t4.x >= n0 + 32 || t4.y <= n0) continue;
-                const bool all = t4.z <= n0 && t4.w >= n0 + 32 && q0 + MA_K <= a.rows_q;
+    const unsigned     at_q = lds_address(Qs) + Tile::plain(lane), at_g = lds_address(Gs) + Tile::plain(lane);
+    const unsigned     at_tq = lds_address(Qs) + Tile::across(lane), at_tg = lds_address(Gs) + Tile::across(lane);
+    constexpr unsigned SIZE = MA_K * ROWB;
+    for (int b = 0; more; b ^= 1) {
+        const int  m0 = q0, head = h;
+        const int4 t  = t4;
+        arrive();
+        more = advance();
+        if (more) issue(b ^ 1);
+        if (!(t.z <= k0 && t.w >= k0 + MA_Q)) {
+            Load::clean(Qs[b], nullptr, wave, lane);
+            Load::clean(Gs[b], nullptr, wave, lane);
+            lds_barrier();
+        }
+        if (t.x >= n0 + 32 || t.y <= n0) continue;
+        const float slope2 = MODE && a.slopes ? a.slopes[head] * LOG2E : 0.f;
+        const unsigned xq = at_q + b * SIZE, xg = at_g + b * SIZE, tq = at_tq + b * SIZE, tg = at_tg + b * SIZE;
+        // which of this lane's 16 queries of each half see its key
+        unsigned   seen[2] = {0xFFFFu, 0xFFFFu};
+        const bool all     = t.z <= n0 && t.w >= n0 + 32;
+        if (!all) {
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    f32x16 s = zero16(), dp = zero16(), th;
+            for (int u = 0; u < 2; ++u) {
+                seen[u] = 0;
 #pragma unroll
-                    for (int kk = 0; kk < KK; ++kk) {
-                        s  = __builtin_amdgcn_mfma_f32_32x32x16_f16(Tile::frag(Qs, 32 * t + (lane & 31), kk, hf), kf[kk], s, 0, 0, 0);
-                        dp = __builtin_amdgcn_mfma_f32_32x32x16_f16(Tile::frag(Gs, 32 * t + (lane & 31), kk, hf), vf[kk], dp, 0, 0, 0);
-                    }
-                    scores<GENERAL>(a, s, slope2, q0 + 32 * t + 4 * hf - n, &th);
-                    unsigned pk[8], dsk[8];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int   i0 = 32 * t + 8 * e + 4 * hf;
-                        const f32x4 l4 = *reinterpret_cast<const f32x4*>(lse2 + i0), d4 = *reinterpret_cast<const f32x4*>(delta + i0);
-                        float       p[4], d[4];
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const int r = 4 * e + c;
-                            p[c]        = __builtin_amdgcn_exp2f(s[r] - l4[c]);
-                            d[c]        = p[c] * (dp[r] - d4[c]);
-                            if (GENERAL && a.cap > 0.f) d[c] *= fmaf(-th[r], th[r], 1.f);
-                            if (!all) {  // (this lane's key may be one that holds anything)
-                                const bool seen = (unsigned)(n - los[i0 + c]) < (unsigned)lens[i0 + c];
-                                p[c]            = seen ? p[c] : 0.f;
-                                d[c]            = seen ? d[c] : 0.f;
-                            }
-                        }
-                        pk[2 * e]      = pack_f16(p[0] * P_SCALE, p[1] * P_SCALE);
-                        pk[2 * e + 1]  = pack_f16(p[2] * P_SCALE, p[3] * P_SCALE);
-                        dsk[2 * e]     = pack_f16(d[0], d[1]);
-                        dsk[2 * e + 1] = pack_f16(d[2], d[3]);
-                    }
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            const int i0 = 32 * t + 16 * u + 4 * hf;
-                            dv[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(Tile::frag_t(Gs, 32 * dt, i0, lane),
-                                                                            frag8(u32x4m{pk[4 * u], pk[4 * u + 1], pk[4 * u + 2], pk[4 * u + 3]}), dv[dt], 0, 0, 0);
-                            dk[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(Tile::frag_t(Qs, 32 * dt, i0, lane),
-                                                                            frag8(u32x4m{dsk[4 * u], dsk[4 * u + 1], dsk[4 * u + 2], dsk[4 * u + 3]}), dk[dt], 0, 0, 0);
-                        }
+                for (int r = 0; r < 16; ++r) {
+                    const int2 g = stats[b].range[32 * u + 8 * (r >> 2) + 4 * hf + (r & 3)];
+                    seen[u] |= (unsigned)(n - g.x) < (unsigned)(g.y - g.x) ? 1u << r : 0u;
+                    if ((r & 7) == 7) step();
                 }
             }
         }
+        const auto work = [&](auto masked) {
+            constexpr bool MASKED = decltype(masked)::value;
+            f32x16         s[2], dp[2], th[2];
+            unsigned       pk[2][8], dsk[2][8];
+            // Steps, each the products of fragments that were read during the one before: scores and dp of 32 queries (u), the same of
+            // the other 32, dv and dk of the first, of the other; what lies between products of one u rides beside those of the other.
+            constexpr int PARTS = D / 32, CK = KK / PARTS, PAIRS = 2 * DT / PARTS, STEPS = 4 * PARTS;
+            static_assert(KK % PARTS == 0 && 2 * DT % PARTS == 0, "whole parts");
+            f16x8      F[2][2 * (CK > PAIRS ? CK : PAIRS)];
+            const auto read = [&](int i) {
+                const int u = i / PARTS & 1, part = i % PARTS;
+                if (i < 2 * PARTS) {
+#pragma unroll
+                    for (int j = 0; j < CK; ++j) {
+                        F[i & 1][2 * j]     = Tile::frag(xq, 32 * u, part * CK + j);
+                        F[i & 1][2 * j + 1] = Tile::frag(xg, 32 * u, part * CK + j);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < PAIRS; ++j) {
+                        const int w = (part * PAIRS + j) / DT, dt = (part * PAIRS + j) % DT;
+                        F[i & 1][2 * j]     = Tile::frag_t(tg, 32 * u + 16 * w, dt);
+                        F[i & 1][2 * j + 1] = Tile::frag_t(tq, 32 * u + 16 * w, dt);
+                    }
+                }
+            };
+            const auto multiply = [&](int i) {
+                const int u = i / PARTS & 1, part = i % PARTS;
+                if (i < 2 * PARTS) {
+                    if (part == 0) s[u] = dp[u] = zero16();
+#pragma unroll
+                    for (int j = 0; j < CK; ++j) {
+                        s[u]  = mma(F[i & 1][2 * j], kf[part * CK + j], s[u]);
+                        dp[u] = mma(F[i & 1][2 * j + 1], vf[part * CK + j], dp[u]);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < PAIRS; ++j) {
+                        const int e = (part * PAIRS + j) / DT * 4, dt = (part * PAIRS + j) % DT;
+                        dv[dt] = mma(F[i & 1][2 * j], words(pk[u], e), dv[dt]);
+                        dk[dt] = mma(F[i & 1][2 * j + 1], words(dsk[u], e), dk[dt]);
+                    }
+                }
+            };
+            const auto weights = [&](int u, int part) {  // probabilities and ds
+                if (MODE && part == 0) scores<MODE>(a, s[u], slope2, m0 + 32 * u + 4 * hf - n, &th[u]);
+#pragma unroll
+                for (int e = 4 * part / PARTS; e < 4 * (part + 1) / PARTS; ++e) {
+                    const int   i0 = 32 * u + 8 * e + 4 * hf;
+                    const f32x4 l4 = *reinterpret_cast<const f32x4*>(stats[b].lse2 + i0), d4 = *reinterpret_cast<const f32x4*>(stats[b].delta + i0);
+                    float       p[4], d[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int r = 4 * e + x;
+                        p[x]        = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -l4[x]));  // (P_SCALE is in it)
+                        d[x]        = p[x] * fmaf(dp[u][r], 1.f / P_SCALE, -d4[x]);
+                        if (MODE == CAP) d[x] *= fmaf(-th[u][r], th[u][r], 1.f);
+                        if (MASKED) {  // (this lane's key may be one that holds anything)
+                            const int keep = (int)(seen[u] << (31 - r)) >> 31;
+                            p[x]           = __builtin_bit_cast(float, __builtin_bit_cast(int, p[x]) & keep);
+                            d[x]           = __builtin_bit_cast(float, __builtin_bit_cast(int, d[x]) & keep);
+                        }
+                    }
+                    pk[u][2 * e]      = pack_f16(p[0], p[1]);
+                    pk[u][2 * e + 1]  = pack_f16(p[2], p[3]);
+                    dsk[u][2 * e]     = pack_f16(d[0], d[1]);
+                    dsk[u][2 * e + 1] = pack_f16(d[2], d[3]);
+                }
+            };
+            read(0);
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                step();
+                if (i + 1 < STEPS) read(i + 1);
+                multiply(i);
+                if (i >= PARTS && i < 3 * PARTS) weights(i / PARTS - 1, i % PARTS);
+            }
+        };
+        if (all) work(std::false_type{});
+        else work(std::true_type{});
     }
-    const bool in = n < a.rows_k;
-    store_rows<DT>(in ? a.dv + (long long)n * a.ld_dv + kvh * a.d : nullptr, dv, 1.f / P_SCALE, a.d, hf);
-    store_rows<DT>(in ? a.dk + (long long)n * a.ld_dk + kvh * a.d : nullptr, dk, a.alpha, a.d, hf);
+    if (a.part_heads == a.group) {
+        const bool in = n < a.rows_k;
+        store_rows<DT>(in ? a.dv + (long long)n * a.ld_dv + kvh * a.d : nullptr, dv, 1.f / P_SCALE, a.d, hf);
+        store_rows<DT>(in ? a.dk + (long long)n * a.ld_dk + kvh * a.d : nullptr, dk, a.alpha, a.d, hf);
+    } else if (n < a.rows_k) {
+        float* to = a.part + ((long long)id * a.rows_k + n) * 2 * a.d;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int col = 32 * dt + 8 * e + 4 * hf;
+                if (col < a.d) {
+                    *reinterpret_cast<f32x4*>(to + col)       = f32x4{dk[dt][4 * e], dk[dt][4 * e + 1], dk[dt][4 * e + 2], dk[dt][4 * e + 3]};
+                    *reinterpret_cast<f32x4*>(to + a.d + col) = f32x4{dv[dt][4 * e], dv[dt][4 * e + 1], dv[dt][4 * e + 2], dv[dt][4 * e + 3]};
+                }
+            }
+    }
+}
+
+// Sums of the parts of a key / value head, in order: 4 columns a thread.
+__global__ __launch_bounds__(MA_THREADS) void masked_join_kernel(AttnArgs a) {
+    const int       kv_heads = a.heads / a.group, parts = a.group / a.part_heads, per = a.d / 4;
+    const long long i = (long long)blockIdx.x * MA_THREADS + threadIdx.x, row = i / per / kv_heads;
+    if (row >= a.rows_k) return;
+    const int kvh = (int)(i / per % kv_heads), col = (int)(i % per) * 4;
+    f32x4     dk = {0.f, 0.f, 0.f, 0.f}, dv = dk;
+    for (int p = 0; p < parts; ++p) {
+        const float* from = a.part + ((long long)(kvh * parts + p) * a.rows_k + row) * 2 * a.d + col;
+        dk += *reinterpret_cast<const f32x4*>(from);
+        dv += *reinterpret_cast<const f32x4*>(from + a.d);
+    }
+    const float k = a.alpha, v = 1.f / P_SCALE;
+    *reinterpret_cast<u32x2m*>(a.dk + row * a.ld_dk + kvh * a.d + col) = u32x2m{pack_f16(dk[0] * k, dk[1] * k), pack_f16(dk[2] * k, dk[3] * k)};
+    *reinterpret_cast<u32x2m*>(a.dv + row * a.ld_dv + kvh * a.d + col) = u32x2m{pack_f16(dv[0] * v, dv[1] * v), pack_f16(dv[2] * v, dv[3] * v)};
 }
 
 // ------------------------------------------------------------------------------------------------ entry points
@@ -587,8 +770,8 @@ static int check_desc(const char* who, const mp_attn_desc* d) {
     MP_REQUIRE(((long long)d->rows_q + MA_Q) / MA_Q * d->n_heads < (1ll << 31) && ((long long)d->rows_k + MA_Q) / MA_Q * d->n_heads < (1ll << 31),
                "%s: too many rows and heads", who);
     MP_REQUIRE(d->ld_q >= w && d->ld_k >= wk && d->ld_v >= wk && d->ld_ctx >= w, "%s: a leading dimension is smaller than its rows", who);
-    if ((d->ld_q | d->ld_k | d->ld_v | d->ld_ctx) & 7) {
-        set_error("%s: leading dimensions must be multiples of 8", who);
+    if (((d->ld_q | d->ld_k | d->ld_v | d->ld_ctx) & 7) || (d->ld_q | d->ld_k | d->ld_v | d->ld_ctx) >= (1 << 22)) {
+        set_error("%s: leading dimensions must be multiples of 8 below 2^22", who);
         return MP_E_UNSUPPORTED;
     }
     return MP_OK;
@@ -602,7 +785,8 @@ static int check_aligned(const char* who, std::initializer_list<const void*> ps)
     return MP_OK;
 }
 static AttnArgs attn_args(const mp_attn_desc* d, const void* mask, const float* slopes) {
-    AttnArgs a = {};
+    AttnArgs a   = {};
+    a.part_heads = d->n_heads / d->n_kv_heads;
     a.slopes   = slopes;
     a.range    = static_cast<const int2*>(mask);
     a.tile     = reinterpret_cast<const int4*>(static_cast<const char*>(mask) + mask_rows_bytes(d->rows_q));
@@ -613,22 +797,16 @@ static AttnArgs attn_args(const mp_attn_desc* d, const void* mask, const float* 
     a.alpha = d->alpha, a.cap = d->cap;
     return a;
 }
-// The kernel of the head size (rounded up to a multiple of 32) and of plain or general scores.
-#define MA_LAUNCH(kernel, grid, a, hs)                                                                       \
-    do {                                                                                                     \
-        const bool general = (a).cap > 0.f || (a).slopes;                                                    \
-        const dim3 g((unsigned)(grid)), b(MA_THREADS);                                                       \
-        switch (((a).d + 31) / 32 * 2 + general) {                                                           \
-            case 2: hipLaunchKernelGGL((kernel<32, false>), g, b, 0, hs, a); break;                          \
-            case 3: hipLaunchKernelGGL((kernel<32, true>), g, b, 0, hs, a); break;                           \
-            case 4: hipLaunchKernelGGL((kernel<64, false>), g, b, 0, hs, a); break;                          \
-            case 5: hipLaunchKernelGGL((kernel<64, true>), g, b, 0, hs, a); break;                           \
-            case 6: hipLaunchKernelGGL((kernel<96, false>), g, b, 0, hs, a); break;                          \
-            case 7: hipLaunchKernelGGL((kernel<96, true>), g, b, 0, hs, a); break;                           \
-            case 8: hipLaunchKernelGGL((kernel<128, false>), g, b, 0, hs, a); break;                         \
-            default: hipLaunchKernelGGL((kernel<128, true>), g, b, 0, hs, a); break;                         \
-        }                                                                                                    \
-    } while (0)
+// The kernel of the head size (rounded up to a multiple of 32) and of what is done to the scores.
+#define MA_CASE(kernel, D, M, grid, a, hs) \
+    case D / 32 * 3 + M: hipLaunchKernelGGL((kernel<D, M>), dim3((unsigned)(grid)), dim3(MA_THREADS), 0, hs, a); break
+#define MA_CASES(kernel, D, grid, a, hs) \
+    MA_CASE(kernel, D, PLAIN, grid, a, hs); MA_CASE(kernel, D, BIAS, grid, a, hs); MA_CASE(kernel, D, CAP, grid, a, hs)
+#define MA_LAUNCH(kernel, grid, a, hs)                                                          \
+    switch (((a).d + 31) / 32 * 3 + ((a).cap > 0.f ? CAP : (a).slopes ? BIAS : PLAIN)) {        \
+        MA_CASES(kernel, 32, grid, a, hs); MA_CASES(kernel, 64, grid, a, hs);                   \
+        MA_CASES(kernel, 96, grid, a, hs); MA_CASES(kernel, 128, grid, a, hs);                  \
+    }
 
 }  // namespace mp
 
@@ -682,9 +860,21 @@ extern "C" int mp_attention_masked_fwd(const mp_attn_desc* desc, const void* mas
     return MP_OK;
 }
 
+// How many of the heads that share keys a workgroup of dk and dv takes: all of them where that gives every compute unit two workgroups
+// (their sums then stay in registers), else one, with sums in fp32 through memory.
+static int part_heads(const mp_attn_desc* d) {
+    const int group = d->n_heads / d->n_kv_heads;
+    return (long long)((d->rows_k + MA_Q - 1) / MA_Q) * d->n_kv_heads >= 512 ? group : 1;
+}
+static size_t stats_bytes(const mp_attn_desc* d) { return (size_t)rows64(d->rows_q) * 64 * d->n_heads * 2 * sizeof(float); }
+static size_t parts_bytes(const mp_attn_desc* d) {
+    const int group = d->n_heads / d->n_kv_heads;
+    return group == part_heads(d) ? 0 : (size_t)d->n_heads * d->rows_k * 2 * d->d_head * sizeof(float);
+}
+
 extern "C" size_t mp_attention_masked_bwd_workspace_bytes(const mp_attn_desc* desc) {
     if (check_desc("mp_attention_masked_bwd_workspace_bytes", desc) != MP_OK) return 0;
-    return (size_t)rows64(desc->rows_q) * 64 * desc->n_heads * 2 * sizeof(float) + 256;
+    return stats_bytes(desc) + parts_bytes(desc) + 256;
 }
 
 extern "C" int mp_attention_masked_bwd(const mp_attn_desc* desc, const void* mask, const mp_half* q, const mp_half* k, const mp_half* v,
@@ -696,8 +886,8 @@ extern "C" int mp_attention_masked_bwd(const mp_attn_desc* desc, const void* mas
     const mp_attn_desc& d = *desc;
     const int           w = d.n_heads * d.d_head, wk = d.n_kv_heads * d.d_head;
     MP_REQUIRE(d.ld_dq >= w && d.ld_dk >= wk && d.ld_dv >= wk && d.ld_dctx >= w, "%s: a leading dimension is smaller than its rows", who);
-    if ((d.ld_dq | d.ld_dk | d.ld_dv | d.ld_dctx) & 7) {
-        set_error("%s: leading dimensions must be multiples of 8", who);
+    if (((d.ld_dq | d.ld_dk | d.ld_dv | d.ld_dctx) & 7) || (d.ld_dq | d.ld_dk | d.ld_dv | d.ld_dctx) >= (1 << 22)) {
+        set_error("%s: leading dimensions must be multiples of 8 below 2^22", who);
         return MP_E_UNSUPPORTED;
     }
     if (d.rows_q == 0 && d.rows_k == 0) return MP_OK;
@@ -713,6 +903,8 @@ extern "C" int mp_attention_masked_bwd(const mp_attn_desc* desc, const void* mas
     a.q = q, a.k = k, a.v = v, a.ctx = ctx, a.lse_in = lse, a.dctx = dctx, a.dq = dq, a.dk = dk, a.dv = dv;
     a.lse2  = static_cast<float*>(ws);
     a.delta = a.lse2 + (size_t)a.rows_pad * a.heads;
+    a.part  = a.delta + (size_t)a.rows_pad * a.heads;
+    a.part_heads = part_heads(desc);
     if (d.rows_q > 0) {
         const long long pairs = (long long)a.rows_pad * a.heads, per = MA_THREADS / 16;
         hipLaunchKernelGGL(masked_stats_kernel, dim3((unsigned)((pairs + per - 1) / per)), dim3(MA_THREADS), 0, hs, a);
@@ -721,8 +913,13 @@ extern "C" int mp_attention_masked_bwd(const mp_attn_desc* desc, const void* mas
         MP_LAUNCH_CHECK(who);
     }
     if (d.rows_k > 0) {
-        MA_LAUNCH(masked_dkv_kernel, (long long)((d.rows_k + MA_Q - 1) / MA_Q) * d.n_kv_heads, a, hs);
+        MA_LAUNCH(masked_dkv_kernel, (long long)((d.rows_k + MA_Q - 1) / MA_Q) * (d.n_heads / a.part_heads), a, hs);
         MP_LAUNCH_CHECK(who);
+        if (a.part_heads < a.group) {
+            const long long quads = (long long)d.rows_k * d.n_kv_heads * (d.d_head / 4);
+            hipLaunchKernelGGL(masked_join_kernel, dim3((unsigned)((quads + MA_THREADS - 1) / MA_THREADS)), dim3(MA_THREADS), 0, hs, a);
+            MP_LAUNCH_CHECK(who);
+        }
     }
     return MP_OK;
 }
