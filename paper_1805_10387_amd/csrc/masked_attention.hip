@@ -14,7 +14,7 @@
 // What is hidden must not be felt, though 0 x NaN is NaN: scores of hidden pairs are replaced, not added to; and in tiles that are
 // not whole, non-finite elements of the matrices that a zero probability would multiply are zeroed on their way into LDS.
 // Those that are visible still show: forward by a NaN score in their place, backward because a query that sees one has a non-finite
-// lse or delta, and its lse is made a NaN.
+// lse or delta, and its lse is made so low that its probabilities are infinite.
 #include "attn_lds.hpp"
 
 #include <limits.h>
@@ -26,6 +26,7 @@ constexpr int   MA_THREADS = 256;
 constexpr int   MA_Q       = 128;   // queries of a workgroup, 32 a wave (dk/dv: keys)
 constexpr int   MA_K       = 64;    // keys of a tile (dk/dv: queries)
 constexpr float LOG2E      = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float POISON = -3e38f;
 constexpr float P_LOG2 = 10.f, P_SCALE = 1024.f;  // dv's probabilities: of 10^5 keys one has 10^-5, which fp16 has to three digits only
 
 struct AttnArgs {
@@ -152,7 +153,8 @@ struct QueryRange {
         } else {
             x.z = INT_MAX;  // rows behind the last one: not whole
         }
-        glo = __builtin_amdgcn_readfirstlane(max(x.x, 0)), ghi = __builtin_amdgcn_readfirstlane(min(x.y, a.rows_k));
+        // (where nothing is seen, x.x is the largest number there is, and tiles are counted on from glo)
+        glo = __builtin_amdgcn_readfirstlane(min(max(x.x, 0), a.rows_k)), ghi = __builtin_amdgcn_readfirstlane(min(x.y, a.rows_k));
         glo_max = __builtin_amdgcn_readfirstlane(x.z), ghi_min = __builtin_amdgcn_readfirstlane(x.w);
     }
     __device__ __forceinline__ bool whole(int kb) const { return glo_max <= kb && ghi_min >= kb + MA_K; }
@@ -186,62 +188,85 @@ __device__ __forceinline__ void step() { __builtin_amdgcn_sched_barrier(0); }
 // ------------------------------------------------------------------------------------------------ forward
 constexpr float LAZY = 8.f;  // the maximum that exponentials refer to follows when it is 2^8 behind
 
-// The scores of a tile take the registers of the one before as soon as its exponentials leave them, half by half: matrix and vector
-// instructions of one wave run side by side, and there is room for a second wave.
-template <int D, int MODE>
-__global__ __launch_bounds__(MA_THREADS, D <= 64 ? 2 : 1) void masked_fwd_kernel(AttnArgs a) {
+// 128 queries a workgroup, 32 a wave.  SPLIT: so many teams of four waves share the workgroup's tiles of keys in turn, each with buffers and
+// sums of its own, and are joined at the end.
+template <int D, int MODE, int SPLIT>
+__global__ __launch_bounds__(256 * SPLIT, 2) void masked_fwd_kernel(AttnArgs a) {
     constexpr int KK = D / 16, DT = D / 32, ROWB = D <= 64 ? 128 : 256;
-    typedef TileLoad<ROWB, 4>     Load;
-    typedef LdsTile<ROWB>         Tile;
-    __shared__ __align__(256) char Ks[2][MA_K * ROWB], Vs[2][MA_K * ROWB];
-    __shared__ __align__(16) float bad[MA_K];
+    constexpr unsigned SIZE = MA_K * ROWB;
+    typedef TileLoad<ROWB, 4> Load;
+    typedef LdsTile<ROWB>     Tile;
+    __shared__ __align__(256) char tiles_of[SPLIT][2][2][SIZE];  // keys, values of two tiles
+    __shared__ __align__(16) float bads[SPLIT][MA_K];
 
     const int tiles = (a.rows_q + MA_Q - 1) / MA_Q;
     const int h = blockIdx.x % a.heads, qt = tiles - 1 - blockIdx.x / a.heads, kvh = h / a.group;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hf = lane >> 5;
+    const int lane = threadIdx.x & 63, wave8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = wave8 & 3, team = wave8 >> 2, hf = lane >> 5;
     const int m0 = qt * MA_Q, m = m0 + 32 * wave + (lane & 31);
     const QueryRange x(a, m0, m);
     const uint16_t*  K = a.k + kvh * a.d;
     const uint16_t*  V = a.v + kvh * a.d;
+    float*           bad = bads[team];
     Load             lk, lv;
     lk.init(a.ld_k, a.d, wave, lane);
     lv.init(a.ld_v, a.d, wave, lane);
-    if (x.glo < x.ghi) {
-        lk.issue(K, a.ld_k, x.glo, a.rows_k, a.d, Ks[0], wave);
-        lv.issue(V, a.ld_v, x.glo, a.rows_k, a.d, Vs[0], wave);
+    if (x.glo + MA_K * team < x.ghi) {
+        lk.issue(K, a.ld_k, x.glo + MA_K * team, a.rows_k, a.d, tiles_of[team][0][0], wave);
+        lv.issue(V, a.ld_v, x.glo + MA_K * team, a.rows_k, a.d, tiles_of[team][0][1], wave);
     }
     f16x8 qf[KK];
     row_frags<KK>(qf, m < a.rows_q ? a.q + (long long)m * a.ld_q + h * a.d : nullptr, a.d, hf);
     const float slope2 = MODE && a.slopes ? a.slopes[h] * LOG2E : 0.f;
     const float c      = MODE ? 1.f : a.alpha * LOG2E;  // scores to base 2
-    f32x16      o[DT], s[2];
-    float       ref = -INFINITY, sum = 0.f, top = -INFINITY;
+    f32x16      o[DT];
+    float       ref = -INFINITY, sum = 0.f;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) o[dt] = zero16();
     settle<KK>(qf);
+    const unsigned at_k = lds_address(tiles_of[team][0][0]) + Tile::plain(lane), at_v = lds_address(tiles_of[team][0][1]) + Tile::across(lane);
 
-    const unsigned at_k = lds_address(Ks) + Tile::plain(lane), at_v = lds_address(Vs) + Tile::across(lane);
-    constexpr unsigned SIZE = MA_K * ROWB;
-    const auto score = [&](f32x16(&to)[2], int kb, int t, unsigned X) {  // 32 keys of tile kb
-        to[t] = zero16();
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-            to[t] = mma(Tile::frag(X, 32 * t, kk), qf[kk], to[t]);
-            if (kk % 4 == 3) step();
+    int b = 0;
+    for (int k0 = x.glo; k0 < x.ghi; k0 += MA_K * SPLIT, b ^= 1) {
+        const int kb = k0 + MA_K * team, next = kb + MA_K * SPLIT;
+        arrive();
+        if (next < x.ghi) {
+            lk.issue(K, a.ld_k, next, a.rows_k, a.d, tiles_of[team][b ^ 1][0], wave);
+            lv.issue(V, a.ld_v, next, a.rows_k, a.d, tiles_of[team][b ^ 1][1], wave);
         }
-        scores<MODE>(a, to[t], slope2, kb + 32 * t + 4 * hf - m);
-    };
-    const auto highest = [&](const f32x16(&of)[2]) {
-        float v = of[0][0];
+        const bool whole = x.whole(kb);
+        if (!(x.whole(k0) && (SPLIT == 1 || x.whole(k0 + MA_K * (SPLIT - 1))))) {
+            if (!whole && kb < x.ghi) Load::clean(tiles_of[team][b][1], bad, wave, lane);
+            lds_barrier();
+        }
+        if (x.none(kb)) continue;
+        const unsigned xk = at_k + b * 2 * SIZE, xv = at_v + b * 2 * SIZE;
+        f32x16         s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            s[t] = zero16();
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) s[t] = mma(Tile::frag(xk, 32 * t, kk), qf[kk], s[t]);
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) scores<MODE>(a, s[t], slope2, kb + 32 * t + 4 * hf - m);
+        if (!whole) {  // (also where this wave's queries see all of it: values were zeroed)
+            const int      n0  = kb + 4 * hf - x.lo;
+            const unsigned len = x.hi - x.lo;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int   n = 32 * t + 8 * (r >> 2) + (r & 3);
+                    const float v = s[t][r] + bad[n + 4 * hf];
+                    s[t][r]       = (unsigned)(n0 + n) < len ? v : -INFINITY;
+                }
+        }
+        float top = s[0][0];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) v = fmaxf(v, of[t][r]);
-        return join_halves(v, [](float p, float q) { return fmaxf(p, q); }) * c;
-    };
-    unsigned   pk[2][8];
-    float      base = 0.f;
-    const auto follow = [&]() {  // the reference, where a query's maximum has left it behind
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
+        top             = join_halves(top, [](float p, float q) { return fmaxf(p, q); }) * c;
         const bool late = top > ref + LAZY;
         if (__any(late)) {  // (each query by itself: its bits do not depend on its neighbours)
             const float fix = late ? __builtin_amdgcn_exp2f(ref - top) : 1.f;
@@ -252,127 +277,53 @@ __global__ __launch_bounds__(MA_THREADS, D <= 64 ? 2 : 1) void masked_fwd_kernel
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[dt][r] *= fix;
         }
-        base = ref == -INFINITY ? 0.f : ref;  // (nothing seen yet: exp(-inf - 0) = 0)
-    };
-    const auto weights = [&](int t, int first, int last) {
+        const float base = ref == -INFINITY ? 0.f : ref;  // (nothing seen yet: exp(-inf - 0) = 0)
 #pragma unroll
-        for (int e = first; e < last; ++e) {
-            const float p0 = __builtin_amdgcn_exp2f(fmaf(s[t][2 * e], c, -base)), p1 = __builtin_amdgcn_exp2f(fmaf(s[t][2 * e + 1], c, -base));
-            sum += p0 + p1;
-            pk[t][e] = pack_f16(p0, p1);
-        }
-    };
-    const auto values = [&](int t, unsigned X) {
+        for (int t = 0; t < 2; ++t) {
+            unsigned pk[8];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) o[dt] = mma(Tile::frag_t(X, 32 * t + 16 * u, dt), words(pk[t], 4 * u), o[dt]);
-            step();
-        }
-    };
-
-    int        b = 0, kb = x.glo;
-    const auto turn = [&]() {  // the values of this tile and the keys of the next are there, and every wave is done with those before
-        arrive();
-        if (kb + 2 * MA_K < x.ghi) lk.issue(K, a.ld_k, kb + 2 * MA_K, a.rows_k, a.d, Ks[b], wave);
-        if (kb + MA_K < x.ghi) lv.issue(V, a.ld_v, kb + MA_K, a.rows_k, a.d, Vs[b ^ 1], wave);
-    };
-    const auto fast = [&]() { return x.whole(kb) && kb + MA_K < x.ghi && !x.none(kb + MA_K); };
-    if (kb < x.ghi) {
-        arrive();
-        if (kb + MA_K < x.ghi) lk.issue(K, a.ld_k, kb + MA_K, a.rows_k, a.d, Ks[1], wave);
-        if (!x.none(kb)) {
-            score(s, kb, 0, at_k);
-            score(s, kb, 1, at_k);
-            top = highest(s);
-        }
-    }
-    for (; kb < x.ghi; kb += MA_K, b ^= 1) {
-        turn();
-        while (fast()) {
-            // Steps, each the products of fragments that were read during the one before: values of 32 keys, scores of the 32 keys of the
-            // next tile that take their registers, and the same of the other 32.
-            constexpr int PARTS = D > 64 ? 2 : 1, PER = KK / PARTS, STEPS = 4 * PARTS;
-            f16x8         F[2][PER];
-            const unsigned xk = at_k + (b ^ 1) * SIZE, xv = at_v + b * SIZE;
-            const auto    read = [&](int i) {
-                const int t = i / PARTS >> 1, part = i % PARTS;
-#pragma unroll
-                for (int j = 0; j < PER; ++j) {
-                    const int w = (part * PER + j) / DT, dt = (part * PER + j) % DT;
-                    F[i & 1][j] = i / PARTS & 1 ? Tile::frag(xk, 32 * t, part * PER + j) : Tile::frag_t(xv, 32 * t + 16 * w, dt);
-                }
-            };
-            const auto multiply = [&](int i) {
-                const int t = i / PARTS >> 1, part = i % PARTS;
-                if ((i / PARTS & 1) && part == 0) s[t] = zero16();
-#pragma unroll
-                for (int j = 0; j < PER; ++j) {
-                    const int w = (part * PER + j) / DT, dt = (part * PER + j) % DT;
-                    if (i / PARTS & 1) s[t] = mma(F[i & 1][j], qf[part * PER + j], s[t]);
-                    else o[dt] = mma(F[i & 1][j], words(pk[t], 4 * w), o[dt]);
-                }
-            };
-            read(0);
-            follow();
-            weights(0, 0, 8);
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                step();
-                if (i + 1 < STEPS) read(i + 1);
-                multiply(i);
-                if (i < 2 * PARTS) weights(1, 4 * i / PARTS, 4 * (i + 1) / PARTS);
-                if (i == 2 * PARTS) scores<MODE>(a, s[0], slope2, kb + MA_K + 4 * hf - m);
+            for (int e = 0; e < 8; ++e) {
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(s[t][2 * e], c, -base)), p1 = __builtin_amdgcn_exp2f(fmaf(s[t][2 * e + 1], c, -base));
+                sum += p0 + p1;
+                pk[e] = pack_f16(p0, p1);
             }
-            scores<MODE>(a, s[1], slope2, kb + MA_K + 32 + 4 * hf - m);
-            top = highest(s);
-            kb += MA_K, b ^= 1;
-            turn();
-        }
-        const bool whole = x.whole(kb), more = kb + MA_K < x.ghi;
-        if (!whole) {
-            Load::clean(Vs[b], bad, wave, lane);
-            lds_barrier();
-        }
-        if (!x.none(kb)) {
-            if (!whole) {  // (also where this wave's own queries see all of it: values were zeroed)
-                const bool     mine = x.all(kb);
-                const int      n0   = kb + 4 * hf - x.lo;
-                const unsigned len  = x.hi - x.lo;
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int n = 32 * t + 8 * (r >> 2) + (r & 3);
-                        s[t][r] += bad[n + 4 * hf];
-                        if (!mine) s[t][r] = (unsigned)(n0 + n) < len ? s[t][r] : -INFINITY;
-                        if (r % 8 == 7) step();
-                    }
-                top = highest(s);
-            }
-            follow();
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                weights(t, 0, 8);
-                step();
-                values(t, at_v + b * SIZE);
-            }
-        }
-        if (more && !x.none(kb + MA_K)) {
-            step();
-            score(s, kb + MA_K, 0, at_k + (b ^ 1) * SIZE);
-            score(s, kb + MA_K, 1, at_k + (b ^ 1) * SIZE);
-            top = highest(s);
+                for (int dt = 0; dt < DT; ++dt) o[dt] = mma(Tile::frag_t(xv, 32 * t + 16 * u, dt), words(pk, 4 * u), o[dt]);
         }
     }
     sum = join_halves(sum, [](float p, float q) { return p + q; });
+    if constexpr (SPLIT > 1) {  // the second team's sums to the first, through the tiles' LDS
+        static_assert(sizeof(tiles_of) >= (16 * DT + 2) * 256 * sizeof(float), "the sums fit");
+        float* const ex = reinterpret_cast<float*>(tiles_of) + (threadIdx.x & 255);
+        lds_barrier();
+        if (team == 1) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) ex[256 * (16 * dt + r)] = o[dt][r];
+            ex[256 * (16 * DT)]     = ref;
+            ex[256 * (16 * DT + 1)] = sum;
+        }
+        lds_barrier();
+        if (team == 1) return;
+        const float ref1 = ex[256 * (16 * DT)], top = fmaxf(ref, ref1);
+        const float f0 = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - top), f1 = ref1 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref1 - top);
+        sum = sum * f0 + ex[256 * (16 * DT + 1)] * f1;
+        ref = top;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[dt][r] = o[dt][r] * f0 + ex[256 * (16 * dt + r)] * f1;
+    }
     if (m < a.rows_q && hf == 0) a.lse[(long long)h * a.rows_q + m] = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * LN2;
     store_rows<DT>(m < a.rows_q ? a.out + (long long)m * a.ld_ctx + h * a.d : nullptr, o, sum == 0.f ? 0.f : 1.f / sum, a.d, hf);
 }
 
 // ------------------------------------------------------------------------------------------------ backward
-// Row statistics: lse in base 2 (+inf where a row sees nothing: its probabilities are then 0; NaN where it or delta is not a number
-// to go by) less log2 of P_SCALE, and delta / P_SCALE, so that p comes out times P_SCALE and ds = p (dp / P_SCALE - delta) as it is.
+// Row statistics: lse in base 2 (+inf where a row sees nothing: its probabilities are then 0; POISON where it or delta is not a number
+// to go by: a visible score's probability is then infinite, and that of a hidden one, exp(-inf - POISON), still 0) less log2 of P_SCALE, and delta / P_SCALE, so that p comes out times P_SCALE and ds = p (dp / P_SCALE - delta) as it is.
 // 16 lanes a (row, head) pair.
 __global__ __launch_bounds__(MA_THREADS) void masked_stats_kernel(AttnArgs a) {
     const long long pair = (long long)blockIdx.x * (MA_THREADS / 16) + (threadIdx.x >> 4);
@@ -395,7 +346,7 @@ __global__ __launch_bounds__(MA_THREADS) void masked_stats_kernel(AttnArgs a) {
         if (max(r.x, 0) >= min(r.y, a.rows_k) || l == -INFINITY)
             l = INFINITY, s = 0.f;
         else if (!(fabsf(l) < INFINITY && fabsf(s) < INFINITY))
-            l = NAN, s = 0.f;
+            l = POISON, s = 0.f;
     }
     a.lse2[(long long)h * a.rows_pad + row]  = l - P_LOG2;
     a.delta[(long long)h * a.rows_pad + row] = s * (1.f / P_SCALE);
@@ -455,79 +406,82 @@ __global__ __launch_bounds__(MA_THREADS, D <= 64 ? 2 : 1) void masked_dq_kernel(
             lds_barrier();
         }
         if (x.none(kb)) continue;
-        const auto work = [&](auto masked) {
-            constexpr bool MASKED = decltype(masked)::value;
-            const int      n0     = kb + 4 * hf - x.lo;
-            const unsigned len    = x.hi - x.lo;
-            const unsigned xk = at_k + b * SIZE, xv = at_v + b * SIZE, xt = at_t + b * SIZE;
-            f32x16         s[2], dp[2], th[2];
-            unsigned       ds[2][8];
-            // Steps as in the kernel of dk and dv: scores and dp of 32 keys (u), of the other 32, dq of the first, of the other.
-            constexpr int PP = D / 32, GP = D == 128 ? 2 : 1, PER = 2 * DT / GP, STEPS = 2 * PP + 2 * GP;
-            f16x8         F[2][PER > 4 ? PER : 4];
-            const auto    read = [&](int i) {
-                if (i < 2 * PP) {
-                    const int u = i / PP, part = i % PP;
+        const bool     all    = x.all(kb);
+        const int      n0     = kb + 4 * hf - x.lo;
+        const unsigned len    = x.hi - x.lo;
+        const unsigned xk = at_k + b * SIZE, xv = at_v + b * SIZE, xt = at_t + b * SIZE;
+        f32x16         s[2], dp[2], th[2];
+        unsigned       ds[2][8];
+        // Steps as in the kernel of dk and dv: scores and dp of 32 keys (u), of the other 32, dq of the first, of the other.
+        constexpr int PP = D / 32, GP = D == 128 ? 2 : 1, PER = 2 * DT / GP, STEPS = 2 * PP + 2 * GP;
+        f16x8         F[2][PER > 4 ? PER : 4];
+        const auto    read = [&](int i) {
+            if (i < 2 * PP) {
+                const int u = i / PP, part = i % PP;
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        F[i & 1][2 * j]     = Tile::frag(xk, 32 * u, 2 * part + j);
-                        F[i & 1][2 * j + 1] = Tile::frag(xv, 32 * u, 2 * part + j);
-                    }
-                } else {
-                    const int u = (i - 2 * PP) / GP, part = (i - 2 * PP) % GP;
-#pragma unroll
-                    for (int j = 0; j < PER; ++j) {
-                        const int w = (part * PER + j) / DT, dt = (part * PER + j) % DT;
-                        F[i & 1][j] = Tile::frag_t(xt, 32 * u + 16 * w, dt);
-                    }
+                for (int j = 0; j < 2; ++j) {
+                    F[i & 1][2 * j]     = Tile::frag(xk, 32 * u, 2 * part + j);
+                    F[i & 1][2 * j + 1] = Tile::frag(xv, 32 * u, 2 * part + j);
                 }
-            };
-            const auto multiply = [&](int i) {
-                if (i < 2 * PP) {
-                    const int u = i / PP, part = i % PP;
-                    if (part == 0) s[u] = dp[u] = zero16();
+            } else {
+                const int u = (i - 2 * PP) / GP, part = (i - 2 * PP) % GP;
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        s[u]  = mma(F[i & 1][2 * j], qf[2 * part + j], s[u]);
-                        dp[u] = mma(F[i & 1][2 * j + 1], gf[2 * part + j], dp[u]);
-                    }
-                } else {
-                    const int u = (i - 2 * PP) / GP, part = (i - 2 * PP) % GP;
-#pragma unroll
-                    for (int j = 0; j < PER; ++j) {
-                        const int w = (part * PER + j) / DT, dt = (part * PER + j) % DT;
-                        o[dt] = mma(F[i & 1][j], words(ds[u], 4 * w), o[dt]);
-                    }
+                for (int j = 0; j < PER; ++j) {
+                    const int w = (part * PER + j) / DT, dt = (part * PER + j) % DT;
+                    F[i & 1][j] = Tile::frag_t(xt, 32 * u + 16 * w, dt);
                 }
-            };
-            const auto weights = [&](int u, int first, int last) {  // ds of pairs of keys
-                if (MODE && first == 0) scores<MODE>(a, s[u], slope2, kb + 32 * u + 4 * hf - m, &th[u]);
-#pragma unroll
-                for (int e = first; e < last; ++e) {
-                    float d[2];
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const int r = 2 * e + y;
-                        float     p = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -lse2));  // (times P_SCALE)
-                        if (MASKED) p = (unsigned)(n0 + 32 * u + 8 * (r >> 2) + (r & 3)) < len ? p : 0.f;
-                        d[y] = p * fmaf(dp[u][r], 1.f / P_SCALE, -delta);
-                        if (MODE == CAP) d[y] *= fmaf(-th[u][r], th[u][r], 1.f);
-                    }
-                    ds[u][e] = pack_f16(d[0], d[1]);
-                }
-            };
-            read(0);
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                step();
-                if (i + 1 < STEPS) read(i + 1);
-                multiply(i);
-                if (i >= PP && i < 2 * PP) weights(0, 8 * (i - PP) / PP, 8 * (i - PP + 1) / PP);
-                if (i >= 2 * PP && i < 2 * PP + GP) weights(1, 8 * (i - 2 * PP) / GP, 8 * (i - 2 * PP + 1) / GP);
             }
         };
-        if (x.all(kb)) work(std::false_type{});
-        else work(std::true_type{});
+        const auto multiply = [&](int i) {
+            if (i < 2 * PP) {
+                const int u = i / PP, part = i % PP;
+                if (part == 0) s[u] = dp[u] = zero16();
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    s[u]  = mma(F[i & 1][2 * j], qf[2 * part + j], s[u]);
+                    dp[u] = mma(F[i & 1][2 * j + 1], gf[2 * part + j], dp[u]);
+                }
+            } else {
+                const int u = (i - 2 * PP) / GP, part = (i - 2 * PP) % GP;
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    const int w = (part * PER + j) / DT, dt = (part * PER + j) % DT;
+                    o[dt] = mma(F[i & 1][j], words(ds[u], 4 * w), o[dt]);
+                }
+            }
+        };
+        const auto weights = [&](int u, int first, int last) {  // ds of pairs of keys
+#pragma unroll
+            for (int e = first; e < last; ++e) {
+                float d[2];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const int   r = 2 * e + y;
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -lse2));  // (times P_SCALE)
+                    d[y] = p * fmaf(dp[u][r], 1.f / P_SCALE, -delta);
+                    if (MODE == CAP) d[y] *= fmaf(-th[u][r], th[u][r], 1.f);
+                }
+                ds[u][e] = pack_f16(d[0], d[1]);
+            }
+        };
+        const auto prepare = [&](int u) {
+            scores<MODE>(a, s[u], slope2, kb + 32 * u + 4 * hf - m, &th[u]);
+            if (!all) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[u][r] = (unsigned)(n0 + 32 * u + 8 * (r >> 2) + (r & 3)) < len ? s[u][r] : -INFINITY;
+            }
+        };
+        read(0);
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            if (i == PP) prepare(0);
+            if (i == 2 * PP) prepare(1);
+            step();
+            if (i + 1 < STEPS) read(i + 1);
+            multiply(i);
+            if (i >= PP && i < 2 * PP) weights(0, 8 * (i - PP) / PP, 8 * (i - PP + 1) / PP);
+            if (i >= 2 * PP && i < 2 * PP + GP) weights(1, 8 * (i - 2 * PP) / GP, 8 * (i - 2 * PP + 1) / GP);
+        }
     }
     // (a row that sees nothing may hold anything in q and dctx, and 0 x NaN has reached its sums)
     if (x.lo >= x.hi) {
@@ -604,6 +558,7 @@ __global__ __launch_bounds__(MA_THREADS, D <= 64 && MODE == PLAIN ? 2 : 1) void 
     const unsigned     at_q = lds_address(Qs) + Tile::plain(lane), at_g = lds_address(Gs) + Tile::plain(lane);
     const unsigned     at_tq = lds_address(Qs) + Tile::across(lane), at_tg = lds_address(Gs) + Tile::across(lane);
     constexpr unsigned SIZE = MA_K * ROWB;
+    bool               ever = false;  // (the other half of the wave has the other queries)
     for (int b = 0; more; b ^= 1) {
         const int  m0 = q0, head = h;
         const int4 t  = t4;
@@ -633,86 +588,89 @@ __global__ __launch_bounds__(MA_THREADS, D <= 64 && MODE == PLAIN ? 2 : 1) void 
                 }
             }
         }
-        const auto work = [&](auto masked) {
-            constexpr bool MASKED = decltype(masked)::value;
-            f32x16         s[2], dp[2], th[2];
-            unsigned       pk[2][8], dsk[2][8];
-            // Steps, each the products of fragments that were read during the one before: scores and dp of 32 queries (u), the same of
-            // the other 32, dv and dk of the first, of the other; what lies between products of one u rides beside those of the other.
-            constexpr int PARTS = D / 32, CK = KK / PARTS, PAIRS = 2 * DT / PARTS, STEPS = 4 * PARTS;
-            static_assert(KK % PARTS == 0 && 2 * DT % PARTS == 0, "whole parts");
-            f16x8      F[2][2 * (CK > PAIRS ? CK : PAIRS)];
-            const auto read = [&](int i) {
-                const int u = i / PARTS & 1, part = i % PARTS;
-                if (i < 2 * PARTS) {
+        ever |= (seen[0] | seen[1]) != 0;
+        f32x16         s[2], dp[2], th[2];
+        unsigned       pk[2][8], dsk[2][8];
+        // Steps, each the products of fragments that were read during the one before: scores and dp of 32 queries (u), the same of
+        // the other 32, dv and dk of the first, of the other; what lies between products of one u rides beside those of the other.
+        constexpr int PARTS = D / 32, CK = KK / PARTS, PAIRS = 2 * DT / PARTS, STEPS = 4 * PARTS;
+        static_assert(KK % PARTS == 0 && 2 * DT % PARTS == 0, "whole parts");
+        f16x8      F[2][2 * (CK > PAIRS ? CK : PAIRS)];
+        const auto read = [&](int i) {
+            const int u = i / PARTS & 1, part = i % PARTS;
+            if (i < 2 * PARTS) {
 #pragma unroll
-                    for (int j = 0; j < CK; ++j) {
-                        F[i & 1][2 * j]     = Tile::frag(xq, 32 * u, part * CK + j);
-                        F[i & 1][2 * j + 1] = Tile::frag(xg, 32 * u, part * CK + j);
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < PAIRS; ++j) {
-                        const int w = (part * PAIRS + j) / DT, dt = (part * PAIRS + j) % DT;
-                        F[i & 1][2 * j]     = Tile::frag_t(tg, 32 * u + 16 * w, dt);
-                        F[i & 1][2 * j + 1] = Tile::frag_t(tq, 32 * u + 16 * w, dt);
-                    }
+                for (int j = 0; j < CK; ++j) {
+                    F[i & 1][2 * j]     = Tile::frag(xq, 32 * u, part * CK + j);
+                    F[i & 1][2 * j + 1] = Tile::frag(xg, 32 * u, part * CK + j);
                 }
-            };
-            const auto multiply = [&](int i) {
-                const int u = i / PARTS & 1, part = i % PARTS;
-                if (i < 2 * PARTS) {
-                    if (part == 0) s[u] = dp[u] = zero16();
+            } else {
 #pragma unroll
-                    for (int j = 0; j < CK; ++j) {
-                        s[u]  = mma(F[i & 1][2 * j], kf[part * CK + j], s[u]);
-                        dp[u] = mma(F[i & 1][2 * j + 1], vf[part * CK + j], dp[u]);
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < PAIRS; ++j) {
-                        const int e = (part * PAIRS + j) / DT * 4, dt = (part * PAIRS + j) % DT;
-                        dv[dt] = mma(F[i & 1][2 * j], words(pk[u], e), dv[dt]);
-                        dk[dt] = mma(F[i & 1][2 * j + 1], words(dsk[u], e), dk[dt]);
-                    }
+                for (int j = 0; j < PAIRS; ++j) {
+                    const int w = (part * PAIRS + j) / DT, dt = (part * PAIRS + j) % DT;
+                    F[i & 1][2 * j]     = Tile::frag_t(tg, 32 * u + 16 * w, dt);
+                    F[i & 1][2 * j + 1] = Tile::frag_t(tq, 32 * u + 16 * w, dt);
                 }
-            };
-            const auto weights = [&](int u, int part) {  // probabilities and ds
-                if (MODE && part == 0) scores<MODE>(a, s[u], slope2, m0 + 32 * u + 4 * hf - n, &th[u]);
-#pragma unroll
-                for (int e = 4 * part / PARTS; e < 4 * (part + 1) / PARTS; ++e) {
-                    const int   i0 = 32 * u + 8 * e + 4 * hf;
-                    const f32x4 l4 = *reinterpret_cast<const f32x4*>(stats[b].lse2 + i0), d4 = *reinterpret_cast<const f32x4*>(stats[b].delta + i0);
-                    float       p[4], d[4];
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int r = 4 * e + x;
-                        p[x]        = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -l4[x]));  // (P_SCALE is in it)
-                        d[x]        = p[x] * fmaf(dp[u][r], 1.f / P_SCALE, -d4[x]);
-                        if (MODE == CAP) d[x] *= fmaf(-th[u][r], th[u][r], 1.f);
-                        if (MASKED) {  // (this lane's key may be one that holds anything)
-                            const int keep = (int)(seen[u] << (31 - r)) >> 31;
-                            p[x]           = __builtin_bit_cast(float, __builtin_bit_cast(int, p[x]) & keep);
-                            d[x]           = __builtin_bit_cast(float, __builtin_bit_cast(int, d[x]) & keep);
-                        }
-                    }
-                    pk[u][2 * e]      = pack_f16(p[0], p[1]);
-                    pk[u][2 * e + 1]  = pack_f16(p[2], p[3]);
-                    dsk[u][2 * e]     = pack_f16(d[0], d[1]);
-                    dsk[u][2 * e + 1] = pack_f16(d[2], d[3]);
-                }
-            };
-            read(0);
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                step();
-                if (i + 1 < STEPS) read(i + 1);
-                multiply(i);
-                if (i >= PARTS && i < 3 * PARTS) weights(i / PARTS - 1, i % PARTS);
             }
         };
-        if (all) work(std::false_type{});
-        else work(std::true_type{});
+        const auto multiply = [&](int i) {
+            const int u = i / PARTS & 1, part = i % PARTS;
+            if (i < 2 * PARTS) {
+                if (part == 0) s[u] = dp[u] = zero16();
+#pragma unroll
+                for (int j = 0; j < CK; ++j) {
+                    s[u]  = mma(F[i & 1][2 * j], kf[part * CK + j], s[u]);
+                    dp[u] = mma(F[i & 1][2 * j + 1], vf[part * CK + j], dp[u]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < PAIRS; ++j) {
+                    const int e = (part * PAIRS + j) / DT * 4, dt = (part * PAIRS + j) % DT;
+                    dv[dt] = mma(F[i & 1][2 * j], words(pk[u], e), dv[dt]);
+                    dk[dt] = mma(F[i & 1][2 * j + 1], words(dsk[u], e), dk[dt]);
+                }
+            }
+        };
+        const auto weights = [&](int u, int part) {  // probabilities and ds
+#pragma unroll
+            for (int e = 4 * part / PARTS; e < 4 * (part + 1) / PARTS; ++e) {
+                const int   i0 = 32 * u + 8 * e + 4 * hf;
+                const f32x4 l4 = *reinterpret_cast<const f32x4*>(stats[b].lse2 + i0), d4 = *reinterpret_cast<const f32x4*>(stats[b].delta + i0);
+                float       p[4], d[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int r = 4 * e + x;
+                    p[x]        = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -l4[x]));  // (P_SCALE is in it)
+                    d[x]        = p[x] * fmaf(dp[u][r], 1.f / P_SCALE, -d4[x]);
+                    if (MODE == CAP) d[x] *= fmaf(-th[u][r], th[u][r], 1.f);
+                }
+                pk[u][2 * e]      = pack_f16(p[0], p[1]);
+                pk[u][2 * e + 1]  = pack_f16(p[2], p[3]);
+                dsk[u][2 * e]     = pack_f16(d[0], d[1]);
+                dsk[u][2 * e + 1] = pack_f16(d[2], d[3]);
+            }
+        };
+        const auto prepare = [&](int u) {
+            scores<MODE>(a, s[u], slope2, m0 + 32 * u + 4 * hf - n, &th[u]);
+            if (!all) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[u][r] = seen[u] >> r & 1 ? s[u][r] : -INFINITY;
+            }
+        };
+        read(0);
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            if (i == PARTS) prepare(0);
+            if (i == 2 * PARTS) prepare(1);
+            step();
+            if (i + 1 < STEPS) read(i + 1);
+            multiply(i);
+            if (i >= PARTS && i < 3 * PARTS) weights(i / PARTS - 1, i % PARTS);
+        }
+    }
+    if (!(__ballot(ever) >> (lane & 31) & 0x100000001ull)) {  // (a key that nobody sees may hold anything, and 0 x NaN has reached its sums)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) dk[dt] = dv[dt] = zero16();
     }
     if (a.part_heads == a.group) {
         const bool in = n < a.rows_k;
@@ -798,14 +756,13 @@ static AttnArgs attn_args(const mp_attn_desc* d, const void* mask, const float* 
     return a;
 }
 // The kernel of the head size (rounded up to a multiple of 32) and of what is done to the scores.
-#define MA_CASE(kernel, D, M, grid, a, hs) \
-    case D / 32 * 3 + M: hipLaunchKernelGGL((kernel<D, M>), dim3((unsigned)(grid)), dim3(MA_THREADS), 0, hs, a); break
-#define MA_CASES(kernel, D, grid, a, hs) \
-    MA_CASE(kernel, D, PLAIN, grid, a, hs); MA_CASE(kernel, D, BIAS, grid, a, hs); MA_CASE(kernel, D, CAP, grid, a, hs)
-#define MA_LAUNCH(kernel, grid, a, hs)                                                          \
-    switch (((a).d + 31) / 32 * 3 + ((a).cap > 0.f ? CAP : (a).slopes ? BIAS : PLAIN)) {        \
-        MA_CASES(kernel, 32, grid, a, hs); MA_CASES(kernel, 64, grid, a, hs);                   \
-        MA_CASES(kernel, 96, grid, a, hs); MA_CASES(kernel, 128, grid, a, hs);                  \
+#define MA_CASE(D, M, kernel, threads, grid, a, hs, ...) \
+    case D / 32 * 3 + M: hipLaunchKernelGGL((kernel<D, M, ##__VA_ARGS__>), dim3((unsigned)(grid)), dim3(threads), 0, hs, a); break
+#define MA_CASES(D, ...) MA_CASE(D, PLAIN, __VA_ARGS__); MA_CASE(D, BIAS, __VA_ARGS__); MA_CASE(D, CAP, __VA_ARGS__)
+#define MA_LAUNCH(kernel, threads, grid, a, ...)                                                                  \
+    switch (((a).d + 31) / 32 * 3 + ((a).cap > 0.f ? CAP : (a).slopes ? BIAS : PLAIN)) {                          \
+        MA_CASES(32, kernel, threads, grid, a, __VA_ARGS__); MA_CASES(64, kernel, threads, grid, a, __VA_ARGS__);  \
+        MA_CASES(96, kernel, threads, grid, a, __VA_ARGS__); MA_CASES(128, kernel, threads, grid, a, __VA_ARGS__); \
     }
 
 }  // namespace mp
@@ -855,7 +812,11 @@ extern "C" int mp_attention_masked_fwd(const mp_attn_desc* desc, const void* mas
     if (rc) return rc;
     AttnArgs a = attn_args(desc, mask, slopes);
     a.q = q, a.k = k, a.v = v, a.out = ctx, a.lse = lse;
-    MA_LAUNCH(masked_fwd_kernel, (long long)((desc->rows_q + MA_Q - 1) / MA_Q) * desc->n_heads, a, as_stream(stream));
+    const long long wgs = (long long)((desc->rows_q + MA_Q - 1) / MA_Q) * desc->n_heads;
+    if (wgs >= 1024)
+        MA_LAUNCH(masked_fwd_kernel, 256, wgs, a, as_stream(stream), 1)
+    else
+        MA_LAUNCH(masked_fwd_kernel, 512, wgs, a, as_stream(stream), 2)
     MP_LAUNCH_CHECK(who);
     return MP_OK;
 }
@@ -909,11 +870,11 @@ extern "C" int mp_attention_masked_bwd(const mp_attn_desc* desc, const void* mas
         const long long pairs = (long long)a.rows_pad * a.heads, per = MA_THREADS / 16;
         hipLaunchKernelGGL(masked_stats_kernel, dim3((unsigned)((pairs + per - 1) / per)), dim3(MA_THREADS), 0, hs, a);
         MP_LAUNCH_CHECK(who);
-        MA_LAUNCH(masked_dq_kernel, (long long)((d.rows_q + MA_Q - 1) / MA_Q) * d.n_heads, a, hs);
+        MA_LAUNCH(masked_dq_kernel, MA_THREADS, (long long)((d.rows_q + MA_Q - 1) / MA_Q) * d.n_heads, a, hs);
         MP_LAUNCH_CHECK(who);
     }
     if (d.rows_k > 0) {
-        MA_LAUNCH(masked_dkv_kernel, (long long)((d.rows_k + MA_Q - 1) / MA_Q) * (d.n_heads / a.part_heads), a, hs);
+        MA_LAUNCH(masked_dkv_kernel, MA_THREADS, (long long)((d.rows_k + MA_Q - 1) / MA_Q) * (d.n_heads / a.part_heads), a, hs);
         MP_LAUNCH_CHECK(who);
         if (a.part_heads < a.group) {
             const long long quads = (long long)d.rows_k * d.n_kv_heads * (d.d_head / 4);
