@@ -85,27 +85,28 @@ __global__ __launch_bounds__(64) void mask_kernel(int rows, int rows_k, int n_do
 }
 
 // ------------------------------------------------------------------------------------------------ scores
-// What is done to q k^T: nothing but the scale (to base 2: one factor beside the exponential's), a distance bias, or a cap with a bias
-// that may be 0.
+// What is done to q k^T: nothing but the scale (to base 2: one factor beside the exponential's), a distance bias, a cap, or both.
 enum { PLAIN = 0, BIAS = 1, CAP = 2 };
-// Base-2 scores in place.  Lanes own one index, registers the other; dist: query less key (or the reverse) at register 0.  th: tanh of the
-// capped score, for the backward pass.
+// Base-2 scores in place.  Lanes own one index, registers the other; dist: query less key (or the reverse) at register 0.
 template <int MODE>
-__device__ __forceinline__ void scores(const AttnArgs& a, f32x16& s, float slope2, int dist, f32x16* th = nullptr) {
+__device__ __forceinline__ void scores(const AttnArgs& a, f32x16& s, float slope2, int dist) {
     if (MODE == PLAIN) return;
-    const float k = MODE == CAP ? a.alpha / a.cap * (2.f * LOG2E) : a.alpha * LOG2E, c = a.cap * LOG2E, at = (float)dist;
+    const float k = MODE & CAP ? a.alpha / a.cap * (2.f * LOG2E) : a.alpha * LOG2E, c = a.cap * LOG2E, at = (float)dist;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-        if (MODE == CAP) {
-            // tanh(x) = 1 - 2 / (exp(2x) + 1): an absolute error of 1e-7, which is what counts for a score
-            const float t = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[r] * k) + 1.f), 1.f);
-            if (th) (*th)[r] = t;
-            s[r] = c * t;
-        } else {
-            s[r] *= k;
-        }
-        s[r] = fmaf(-slope2, fabsf(at + (float)(8 * (r >> 2) + (r & 3))), s[r]);
+        // tanh(x) = 1 - 2 / (exp(2x) + 1): an absolute error of 1e-7, which is what counts for a score
+        if (MODE & CAP) s[r] = c * fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[r] * k) + 1.f), 1.f);
+        else s[r] *= k;
+        if (MODE & BIAS) s[r] = fmaf(-slope2, fabsf(at + (float)(8 * (r >> 2) + (r & 3))), s[r]);
     }
+}
+// d s / d (alpha q k^T) = 1 - tanh^2, out of the score itself (which is cheaper than a register that keeps tanh); 0 for a hidden one's -inf.
+template <int MODE>
+__device__ __forceinline__ float fade(const AttnArgs& a, float s, float slope2, float dist) {
+    if (!(MODE & CAP)) return 1.f;
+    if (MODE & BIAS) s = fmaf(slope2, fabsf(dist), s);
+    const float t = s * (1.f / (a.cap * LOG2E));
+    return fmaxf(fmaf(-t, t, 1.f), 0.f);
 }
 
 // ------------------------------------------------------------------------------------------------ tiles
@@ -322,47 +323,21 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void masked_fwd_kernel(AttnArgs a) 
 }
 
 // ------------------------------------------------------------------------------------------------ backward
-// Row statistics: lse in base 2 (+inf where a row sees nothing: its probabilities are then 0; POISON where it or delta is not a number
-// to go by: a visible score's probability is then infinite, and that of a hidden one, exp(-inf - POISON), still 0) less log2 of P_SCALE, and delta / P_SCALE, so that p comes out times P_SCALE and ds = p (dp / P_SCALE - delta) as it is.
-// 16 lanes a (row, head) pair.
-__global__ __launch_bounds__(MA_THREADS) void masked_stats_kernel(AttnArgs a) {
-    const long long pair = (long long)blockIdx.x * (MA_THREADS / 16) + (threadIdx.x >> 4);
-    const int       row = (int)(pair / a.heads), h = (int)(pair - (long long)row * a.heads), c = (threadIdx.x & 15) * 8;
-    if (row >= a.rows_pad) return;
-    float s = 0.f;
-    if (row < a.rows_q && c < a.d) {
-        const f16x8 p = *reinterpret_cast<const f16x8*>(a.ctx + (long long)row * a.ld_ctx + h * a.d + c);
-        const f16x8 g = *reinterpret_cast<const f16x8*>(a.dctx + (long long)row * a.ld_dctx + h * a.d + c);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s = fmaf((float)p[i], (float)g[i], s);
-    }
-#pragma unroll
-    for (int i = 1; i < 16; i *= 2) s += __shfl_xor(s, i, 64);
-    if (threadIdx.x & 15) return;
-    float l = INFINITY;
-    if (row < a.rows_q) {
-        const int2 r = a.range[row];
-        l            = a.lse_in[(long long)h * a.rows_q + row] * LOG2E;
-        if (max(r.x, 0) >= min(r.y, a.rows_k) || l == -INFINITY)
-            l = INFINITY, s = 0.f;
-        else if (!(fabsf(l) < INFINITY && fabsf(s) < INFINITY))
-            l = POISON, s = 0.f;
-    }
-    a.lse2[(long long)h * a.rows_pad + row]  = l - P_LOG2;
-    a.delta[(long long)h * a.rows_pad + row] = s * (1.f / P_SCALE);
-}
-
-// dq of 128 queries, 32 of them a wave.
-template <int D, int MODE>
-__global__ __launch_bounds__(MA_THREADS, D <= 64 ? 2 : 1) void masked_dq_kernel(AttnArgs a) {
-    constexpr int KK = D / 16, DT = D / 32, ROWB = D <= 64 ? 128 : 256;
-    typedef TileLoad<ROWB, 4>     Load;
-    typedef LdsTile<ROWB>         Tile;
-    __shared__ __align__(256) char Ks[2][MA_K * ROWB], Vs[2][MA_K * ROWB];
+// dq of 128 queries, 32 of them a wave; teams as in the forward kernel.  Leaves the rows' statistics for the kernel of dk and dv: lse in base 2
+// (+inf where a row sees nothing: its probabilities are then 0; POISON where it or delta is not a number to go by: a visible score's
+// probability is then infinite, and that of a hidden one, exp(-inf - POISON), still 0) less log2 of P_SCALE, and delta / P_SCALE, so
+// that p comes out times P_SCALE and ds = p (dp / P_SCALE - delta) as it is.
+template <int D, int MODE, int SPLIT>
+__global__ __launch_bounds__(256 * SPLIT, 2) void masked_dq_kernel(AttnArgs a) {
+    constexpr int      KK = D / 16, DT = D / 32, ROWB = D <= 64 ? 128 : 256;
+    constexpr unsigned SIZE = MA_K * ROWB;
+    typedef TileLoad<ROWB, 4> Load;
+    typedef LdsTile<ROWB>     Tile;
+    __shared__ __align__(256) char tiles_of[SPLIT][2][2][SIZE];  // keys, values of two tiles
 
     const int tiles = (a.rows_q + MA_Q - 1) / MA_Q;
     const int h = blockIdx.x % a.heads, qt = tiles - 1 - blockIdx.x / a.heads, kvh = h / a.group;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hf = lane >> 5;
+    const int lane = threadIdx.x & 63, wave8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = wave8 & 3, team = wave8 >> 2, hf = lane >> 5;
     const int m0 = qt * MA_Q, m = m0 + 32 * wave + (lane & 31);
     const QueryRange x(a, m0, m);
     const uint16_t*  K = a.k + kvh * a.d;
@@ -370,9 +345,9 @@ __global__ __launch_bounds__(MA_THREADS, D <= 64 ? 2 : 1) void masked_dq_kernel(
     Load             lk, lv;
     lk.init(a.ld_k, a.d, wave, lane);
     lv.init(a.ld_v, a.d, wave, lane);
-    if (x.glo < x.ghi) {
-        lk.issue(K, a.ld_k, x.glo, a.rows_k, a.d, Ks[0], wave);
-        lv.issue(V, a.ld_v, x.glo, a.rows_k, a.d, Vs[0], wave);
+    if (x.glo + MA_K * team < x.ghi) {
+        lk.issue(K, a.ld_k, x.glo + MA_K * team, a.rows_k, a.d, tiles_of[team][0][0], wave);
+        lv.issue(V, a.ld_v, x.glo + MA_K * team, a.rows_k, a.d, tiles_of[team][0][1], wave);
     }
     f16x8 qf[KK], gf[KK];
     row_frags<KK>(qf, m < a.rows_q ? a.q + (long long)m * a.ld_q + h * a.d : nullptr, a.d, hf);
@@ -381,8 +356,24 @@ __global__ __launch_bounds__(MA_THREADS, D <= 64 ? 2 : 1) void masked_dq_kernel(
     const float c      = MODE ? 1.f : a.alpha * LOG2E;
     float       lse2 = INFINITY, delta = 0.f;
     if (m < a.rows_q) {
-        lse2  = a.lse2[(long long)h * a.rows_pad + m];
-        delta = a.delta[(long long)h * a.rows_pad + m];
+        lse2 = a.lse_in[(long long)h * a.rows_q + m] * LOG2E;
+        f16x8 cf[KK];
+        row_frags<KK>(cf, a.ctx + (long long)m * a.ld_ctx + h * a.d, a.d, hf);
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) delta = fmaf((float)cf[kk][i], (float)gf[kk][i], delta);
+    }
+    delta = join_halves(delta, [](float p, float q) { return p + q; });
+    if (x.lo >= x.hi || lse2 == -INFINITY)
+        lse2 = INFINITY, delta = 0.f;
+    else if (!(fabsf(lse2) < INFINITY && fabsf(delta) < INFINITY))
+        lse2 = POISON, delta = 0.f;
+    lse2 -= P_LOG2;
+    delta *= 1.f / P_SCALE;
+    if (team == 0 && hf == 0 && m < a.rows_pad) {
+        a.lse2[(long long)h * a.rows_pad + m]  = lse2;
+        a.delta[(long long)h * a.rows_pad + m] = delta;
     }
     f32x16 o[DT];
 #pragma unroll
@@ -390,27 +381,30 @@ __global__ __launch_bounds__(MA_THREADS, D <= 64 ? 2 : 1) void masked_dq_kernel(
     settle<KK>(qf);
     settle<KK>(gf);
     asm volatile("" : "+v"(lse2), "+v"(delta));
-    const unsigned     at_k = lds_address(Ks) + Tile::plain(lane), at_v = lds_address(Vs) + Tile::plain(lane), at_t = lds_address(Ks) + Tile::across(lane);
-    constexpr unsigned SIZE = MA_K * ROWB;
+    const unsigned at_k = lds_address(tiles_of[team][0][0]) + Tile::plain(lane), at_v = lds_address(tiles_of[team][0][1]) + Tile::plain(lane);
+    const unsigned at_t = lds_address(tiles_of[team][0][0]) + Tile::across(lane);
 
     int b = 0;
-    for (int kb = x.glo; kb < x.ghi; kb += MA_K, b ^= 1) {
+    for (int k0 = x.glo; k0 < x.ghi; k0 += MA_K * SPLIT, b ^= 1) {
+        const int kb = k0 + MA_K * team, next = kb + MA_K * SPLIT;
         arrive();
-        if (kb + MA_K < x.ghi) {
-            lk.issue(K, a.ld_k, kb + MA_K, a.rows_k, a.d, Ks[b ^ 1], wave);
-            lv.issue(V, a.ld_v, kb + MA_K, a.rows_k, a.d, Vs[b ^ 1], wave);
+        if (next < x.ghi) {
+            lk.issue(K, a.ld_k, next, a.rows_k, a.d, tiles_of[team][b ^ 1][0], wave);
+            lv.issue(V, a.ld_v, next, a.rows_k, a.d, tiles_of[team][b ^ 1][1], wave);
         }
-        if (!x.whole(kb)) {
-            Load::clean(Ks[b], nullptr, wave, lane);
-            Load::clean(Vs[b], nullptr, wave, lane);
+        if (!(x.whole(k0) && (SPLIT == 1 || x.whole(k0 + MA_K * (SPLIT - 1))))) {
+            if (!x.whole(kb) && kb < x.ghi) {
+                Load::clean(tiles_of[team][b][0], nullptr, wave, lane);
+                Load::clean(tiles_of[team][b][1], nullptr, wave, lane);
+            }
             lds_barrier();
         }
         if (x.none(kb)) continue;
         const bool     all    = x.all(kb);
         const int      n0     = kb + 4 * hf - x.lo;
         const unsigned len    = x.hi - x.lo;
-        const unsigned xk = at_k + b * SIZE, xv = at_v + b * SIZE, xt = at_t + b * SIZE;
-        f32x16         s[2], dp[2], th[2];
+        const unsigned xk = at_k + b * 2 * SIZE, xv = at_v + b * 2 * SIZE, xt = at_t + b * 2 * SIZE;
+        f32x16         s[2], dp[2];
         unsigned       ds[2][8];
         // Steps as in the kernel of dk and dv: scores and dp of 32 keys (u), of the other 32, dq of the first, of the other.
         constexpr int PP = D / 32, GP = D == 128 ? 2 : 1, PER = 2 * DT / GP, STEPS = 2 * PP + 2 * GP;
@@ -459,13 +453,13 @@ __global__ __launch_bounds__(MA_THREADS, D <= 64 ? 2 : 1) void masked_dq_kernel(
                     const int   r = 2 * e + y;
                     const float p = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -lse2));  // (times P_SCALE)
                     d[y] = p * fmaf(dp[u][r], 1.f / P_SCALE, -delta);
-                    if (MODE == CAP) d[y] *= fmaf(-th[u][r], th[u][r], 1.f);
+                    if (MODE & CAP) d[y] *= fade<MODE>(a, s[u][r], slope2, (float)(kb + 32 * u + 4 * hf - m + 8 * (r >> 2) + (r & 3)));
                 }
                 ds[u][e] = pack_f16(d[0], d[1]);
             }
         };
         const auto prepare = [&](int u) {
-            scores<MODE>(a, s[u], slope2, kb + 32 * u + 4 * hf - m, &th[u]);
+            scores<MODE>(a, s[u], slope2, kb + 32 * u + 4 * hf - m);
             if (!all) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[u][r] = (unsigned)(n0 + 32 * u + 8 * (r >> 2) + (r & 3)) < len ? s[u][r] : -INFINITY;
@@ -483,6 +477,23 @@ __global__ __launch_bounds__(MA_THREADS, D <= 64 ? 2 : 1) void masked_dq_kernel(
             if (i >= 2 * PP && i < 2 * PP + GP) weights(1, 8 * (i - 2 * PP) / GP, 8 * (i - 2 * PP + 1) / GP);
         }
     }
+    if constexpr (SPLIT > 1) {  // the second team's sums to the first, through the tiles' LDS
+        static_assert(sizeof(tiles_of) >= 16 * DT * 256 * sizeof(float), "the sums fit");
+        float* const ex = reinterpret_cast<float*>(tiles_of) + (threadIdx.x & 255);
+        lds_barrier();
+        if (team == 1) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) ex[256 * (16 * dt + r)] = o[dt][r];
+        }
+        lds_barrier();
+        if (team == 1) return;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[dt][r] += ex[256 * (16 * dt + r)];
+    }
     // (a row that sees nothing may hold anything in q and dctx, and 0 x NaN has reached its sums)
     if (x.lo >= x.hi) {
 #pragma unroll
@@ -494,7 +505,7 @@ __global__ __launch_bounds__(MA_THREADS, D <= 64 ? 2 : 1) void masked_dq_kernel(
 // dk and dv of 128 keys, 32 of them a wave, over the tiles of 64 queries that see any of them, head by head: of all heads that share
 // the keys, or (PART) of a.part_heads of them, whose sums the join kernel adds up.
 template <int D, int MODE>
-__global__ __launch_bounds__(MA_THREADS, D <= 64 && MODE == PLAIN ? 2 : 1) void masked_dkv_kernel(AttnArgs a) {
+__global__ __launch_bounds__(MA_THREADS, D <= 64 ? 2 : 1) void masked_dkv_kernel(AttnArgs a) {
     constexpr int KK = D / 16, DT = D / 32, ROWB = D <= 64 ? 128 : 256;
     typedef TileLoad<ROWB, 4> Load;
     typedef LdsTile<ROWB>     Tile;
@@ -589,7 +600,7 @@ __global__ __launch_bounds__(MA_THREADS, D <= 64 && MODE == PLAIN ? 2 : 1) void 
             }
         }
         ever |= (seen[0] | seen[1]) != 0;
-        f32x16         s[2], dp[2], th[2];
+        f32x16         s[2], dp[2];
         unsigned       pk[2][8], dsk[2][8];
         // Steps, each the products of fragments that were read during the one before: scores and dp of 32 queries (u), the same of
         // the other 32, dv and dk of the first, of the other; what lies between products of one u rides beside those of the other.
@@ -642,7 +653,7 @@ __global__ __launch_bounds__(MA_THREADS, D <= 64 && MODE == PLAIN ? 2 : 1) void 
                     const int r = 4 * e + x;
                     p[x]        = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -l4[x]));  // (P_SCALE is in it)
                     d[x]        = p[x] * fmaf(dp[u][r], 1.f / P_SCALE, -d4[x]);
-                    if (MODE == CAP) d[x] *= fmaf(-th[u][r], th[u][r], 1.f);
+                    if (MODE & CAP) d[x] *= fade<MODE>(a, s[u][r], slope2, (float)(m0 + 32 * u + 4 * hf - n + 8 * e + x));
                 }
                 pk[u][2 * e]      = pack_f16(p[0], p[1]);
                 pk[u][2 * e + 1]  = pack_f16(p[2], p[3]);
@@ -651,7 +662,7 @@ __global__ __launch_bounds__(MA_THREADS, D <= 64 && MODE == PLAIN ? 2 : 1) void 
             }
         };
         const auto prepare = [&](int u) {
-            scores<MODE>(a, s[u], slope2, m0 + 32 * u + 4 * hf - n, &th[u]);
+            scores<MODE>(a, s[u], slope2, m0 + 32 * u + 4 * hf - n);
             if (!all) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[u][r] = seen[u] >> r & 1 ? s[u][r] : -INFINITY;
@@ -757,10 +768,10 @@ static AttnArgs attn_args(const mp_attn_desc* d, const void* mask, const float* 
 }
 // The kernel of the head size (rounded up to a multiple of 32) and of what is done to the scores.
 #define MA_CASE(D, M, kernel, threads, grid, a, hs, ...) \
-    case D / 32 * 3 + M: hipLaunchKernelGGL((kernel<D, M, ##__VA_ARGS__>), dim3((unsigned)(grid)), dim3(threads), 0, hs, a); break
-#define MA_CASES(D, ...) MA_CASE(D, PLAIN, __VA_ARGS__); MA_CASE(D, BIAS, __VA_ARGS__); MA_CASE(D, CAP, __VA_ARGS__)
+    case D / 32 * 4 + M: hipLaunchKernelGGL((kernel<D, M, ##__VA_ARGS__>), dim3((unsigned)(grid)), dim3(threads), 0, hs, a); break
+#define MA_CASES(D, ...) MA_CASE(D, PLAIN, __VA_ARGS__); MA_CASE(D, BIAS, __VA_ARGS__); MA_CASE(D, CAP, __VA_ARGS__); MA_CASE(D, CAP + BIAS, __VA_ARGS__)
 #define MA_LAUNCH(kernel, threads, grid, a, ...)                                                                  \
-    switch (((a).d + 31) / 32 * 3 + ((a).cap > 0.f ? CAP : (a).slopes ? BIAS : PLAIN)) {                          \
+    switch (((a).d + 31) / 32 * 4 + ((a).cap > 0.f ? CAP : 0) + ((a).slopes ? BIAS : 0)) {                          \
         MA_CASES(32, kernel, threads, grid, a, __VA_ARGS__); MA_CASES(64, kernel, threads, grid, a, __VA_ARGS__);  \
         MA_CASES(96, kernel, threads, grid, a, __VA_ARGS__); MA_CASES(128, kernel, threads, grid, a, __VA_ARGS__); \
     }
@@ -867,10 +878,11 @@ extern "C" int mp_attention_masked_bwd(const mp_attn_desc* desc, const void* mas
     a.part  = a.delta + (size_t)a.rows_pad * a.heads;
     a.part_heads = part_heads(desc);
     if (d.rows_q > 0) {
-        const long long pairs = (long long)a.rows_pad * a.heads, per = MA_THREADS / 16;
-        hipLaunchKernelGGL(masked_stats_kernel, dim3((unsigned)((pairs + per - 1) / per)), dim3(MA_THREADS), 0, hs, a);
-        MP_LAUNCH_CHECK(who);
-        MA_LAUNCH(masked_dq_kernel, MA_THREADS, (long long)((d.rows_q + MA_Q - 1) / MA_Q) * d.n_heads, a, hs);
+        const long long wgs = (long long)((d.rows_q + MA_Q - 1) / MA_Q) * d.n_heads;
+        if (wgs >= 1024)
+            MA_LAUNCH(masked_dq_kernel, 256, wgs, a, hs, 1)
+        else
+            MA_LAUNCH(masked_dq_kernel, 512, wgs, a, hs, 2)
         MP_LAUNCH_CHECK(who);
     }
     if (d.rows_k > 0) {
