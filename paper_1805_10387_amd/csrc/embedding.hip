@@ -19,8 +19,15 @@ constexpr int EMB_THREADS = 256;
 constexpr int SORT_RUN    = 2048;   // 11 bits of position beside 21 bits of token
 constexpr int SORT_BITS   = 11;
 constexpr int MERGE_RUNS  = 32;
-constexpr int EMB_CHUNK   = 32;
+constexpr int EMB_CHUNK   = 8;
 constexpr int FILL_WGS    = 2048;
+
+// What the lanes of this wave wrote to LDS is there for its other lanes.
+__device__ __forceinline__ void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 // The product rounded to fp32 before it is rounded to fp16: the compiler else makes one instruction of the two in some places,
 // which rounds once (an element in 10^4 differs, and a call with `add` from one without).
@@ -30,49 +37,92 @@ __device__ __forceinline__ float scaled(float x, float scale) {
     return x;
 }
 
-// VEC elements of a row (8: one 16-byte access, 1: any alignment)
-template <int VEC>
-struct Part {
-    float x[VEC];
-    __device__ __forceinline__ void load(const uint16_t* p) {
-        if (VEC == 8) {
-            const u32x4e q = *reinterpret_cast<const u32x4e*>(p);
+// 8 elements of a row that may begin at any element.  A load asks for the four words, or five, that hold them: a word is the least that
+// memory serves at its full rate.
+typedef u32x4e   u32x4e_any __attribute__((aligned(2)));
+typedef u32x4e   u32x4e_word __attribute__((aligned(4)));
+typedef f32x4    f32x4_word __attribute__((aligned(4)));
+struct Words {
+    unsigned v[5];
+    int      odd;
+    __device__ __forceinline__ Words() {}
+    __device__ __forceinline__ explicit Words(const uint16_t* p) {
+        odd               = (int)(reinterpret_cast<uintptr_t>(p) >> 1) & 1;
+        const unsigned* q = reinterpret_cast<const unsigned*>(p - odd);
+        const u32x4e    w = *reinterpret_cast<const u32x4e_word*>(q);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) x[i] = h2f((uint16_t)(q[i / 2] >> (16 * (i & 1))));
-        } else {
-            x[0] = h2f(*p);
+        for (int k = 0; k < 4; ++k) v[k] = w[k];
+        v[4] = q[3 + odd];
+    }
+    __device__ __forceinline__ Words(const uint16_t* p, int n) {  // the first n, the others 0
+        odd = 0;
+#pragma unroll
+        for (int k = 0; k < 5; ++k) v[k] = (2 * k < n ? p[2 * k] : 0u) | (2 * k + 1 < n ? (unsigned)p[2 * k + 1] << 16 : 0u);
+    }
+};
+struct Part {
+    float x[8];
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = 0.f;
+    }
+    __device__ __forceinline__ void load(const uint16_t* p) { set(Words(p)); }
+    __device__ __forceinline__ void set(const Words& w) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const unsigned v = __builtin_amdgcn_alignbit(w.v[k + 1], w.v[k], 16 * w.odd);
+            x[2 * k]         = h2f((uint16_t)v);
+            x[2 * k + 1]     = h2f((uint16_t)(v >> 16));
         }
     }
-    __device__ __forceinline__ void store(uint16_t* p) const {
-        if (VEC == 8) {
+    __device__ __forceinline__ void store(uint16_t* p, int first, int end) const {  // elements first .. end-1
+        if (end - first == 8) {
             u32x4e q;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) q[i] = (unsigned)f2h(x[2 * i]) | ((unsigned)f2h(x[2 * i + 1]) << 16);
-            *reinterpret_cast<u32x4e*>(p) = q;
+            for (int k = 0; k < 4; ++k) q[k] = (unsigned)f2h(x[2 * k]) | ((unsigned)f2h(x[2 * k + 1]) << 16);
+            *reinterpret_cast<u32x4e_any*>(p) = q;
         } else {
-            *p = f2h(x[0]);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k >= first && k < end) p[k] = f2h(x[k]);
         }
     }
 };
 
 // ------------------------------------------------------------------------------------------------ forward
-template <int VEC>
-__global__ __launch_bounds__(EMB_THREADS) void embedding_fwd_kernel(long long pieces, int per_row, int vocab, int d, const int* __restrict__ tokens,
-                                                                    const uint16_t* __restrict__ w, float scale, uint16_t* __restrict__ y) {
-    for (long long i = (long long)blockIdx.x * EMB_THREADS + threadIdx.x; i < pieces; i += (long long)gridDim.x * EMB_THREADS) {
-        const int t = (int)(i / per_row), c = (int)(i - (long long)t * per_row) * VEC;
-        const int v = tokens[t];
-        Part<VEC> p;
-        if ((unsigned)v < (unsigned)vocab) {
-            p.load(w + (long long)v * d + c);
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) p.x[k] = scaled(p.x[k], scale);
-        } else {
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) p.x[k] = 0.f;
-        }
-        p.store(y + (long long)t * d + c);
+// A thread has one piece of 8 columns of a row, the rows' pieces one behind the other.  The last piece of a row of 8 or more is its last 8
+// columns, which may repeat some of the piece before it; only its own (from `skip`) are stored.  TINY: rows of fewer.
+struct Piece {
+    long long row;
+    int       col, skip, end;
+    __device__ Piece(int d, int pieces) {
+        const long long base = (long long)blockIdx.x * EMB_THREADS;  // (one long division a workgroup)
+        const long long r    = base / pieces;
+        const unsigned  i    = (unsigned)(base - r * pieces) + threadIdx.x, down = i / (unsigned)pieces;
+        const int       first = (int)(i - down * (unsigned)pieces) * 8;
+        row                   = r + down;
+        col                   = max(min(first, d - 8), 0);
+        skip                  = first - col;
+        end                   = min(d - col, 8);
     }
+};
+template <bool TINY>
+__device__ __forceinline__ Words load_piece(const uint16_t* p, const Piece& at) {
+    return TINY ? Words(p, at.end) : Words(p);
+}
+
+template <bool TINY>
+__global__ __launch_bounds__(EMB_THREADS) void embedding_fwd_kernel(int rows, int vocab, int d, int pieces, const int* __restrict__ tokens,
+                                                                    const uint16_t* __restrict__ w, float scale, uint16_t* __restrict__ y) {
+    const Piece at(d, pieces);
+    if (at.row >= rows) return;
+    const int v = tokens[at.row];
+    Part      p;
+    p.zero();
+    if ((unsigned)v < (unsigned)vocab) p.set(load_piece<TINY>(w + (long long)v * d + at.col, at));
+#pragma unroll
+    for (int k = 0; k < 8; ++k) p.x[k] = scaled(p.x[k], scale);
+    p.store(y + at.row * d + at.col, at.skip, at.end);
 }
 
 // ------------------------------------------------------------------------------------------------ sort
@@ -111,16 +161,24 @@ __global__ __launch_bounds__(1024) void embedding_sort_kernel(int rows, int voca
         s[i] = key;
     }
     __syncthreads();
-    for (int k = 2; k <= SORT_RUN; k *= 2)
+    int most = 2;  // (what lies behind the last key is the largest)
+    while (most < SORT_RUN && most < rows - base) most *= 2;
+    // Bitonic.  A thread's two elements of a step lie in its wave's 128 for distances up to 64: LDS serves a wave in order, so only
+    // larger distances need the workgroup.
+    for (int k = 2; k <= most; k *= 2)
         for (int j = k / 2; j > 0; j /= 2) {
+            if (j >= 128) __syncthreads();
+            else wave_order();
             const int      a = 2 * threadIdx.x - (threadIdx.x & (j - 1)), b = a + j;
             const unsigned x = s[a], y = s[b];
             if ((x > y) == ((a & k) == 0)) {
                 s[a] = y;
                 s[b] = x;
             }
-            __syncthreads();
+            if (j >= 128) __syncthreads();
+            else wave_order();
         }
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int i = threadIdx.x + 1024 * j;
@@ -128,137 +186,196 @@ __global__ __launch_bounds__(1024) void embedding_sort_kernel(int rows, int voca
     }
 }
 
-// Groups of MERGE_RUNS sorted runs of `run` keys into one each.  All keys differ.
-__global__ __launch_bounds__(EMB_THREADS) void embedding_merge_kernel(int rows, long long run, const u64* __restrict__ in, u64* __restrict__ out) {
-    const long long p = (long long)blockIdx.x * EMB_THREADS + threadIdx.x;
-    if (p >= rows) return;
-    const u64       key   = in[p];
-    const long long group = p / (run * MERGE_RUNS) * (run * MERGE_RUNS), own = p / run * run;
-    long long       at    = group + (p - own);
-    const long long end   = min((long long)rows, group + run * MERGE_RUNS);
-    for (long long r = group; r < end; r += run) {
-        if (r == own) continue;
-        int a = 0, b = (int)min(run, end - r);  // keys below `key` in that run
-        while (a < b) {
-            const int c = (a + b) >> 1;
-            if (in[r + c] < key) a = c + 1; else b = c;
+// Groups of MERGE_RUNS sorted runs of `run` keys (a power of two) into one each: a key's place is the number of smaller ones, run by run
+// (all keys differ).  A workgroup places MERGE_KEYS neighbours of one run.  What lies between the first and the last of them in the other
+// runs, about as many keys of each, goes through LDS and is searched there; a search of each key in memory takes ten times as long.
+constexpr int MERGE_KEYS = 256, MERGE_THREADS = 1024, MERGE_TILE = 8192;
+__global__ __launch_bounds__(MERGE_THREADS) void embedding_merge_kernel(int rows, int run, const u64* __restrict__ in, u64* __restrict__ out) {
+    __shared__ unsigned tile[MERGE_TILE];                              // tokens
+    __shared__ int      low[MERGE_RUNS], before[MERGE_RUNS + 1], smaller[MERGE_KEYS];
+    const int       tid = threadIdx.x, mine = tid % MERGE_KEYS, share = tid / MERGE_KEYS;
+    const long long p0 = (long long)blockIdx.x * MERGE_KEYS, group = p0 / ((long long)run * MERGE_RUNS) * run * MERGE_RUNS;
+    const long long p1   = min((long long)rows, p0 + MERGE_KEYS);
+    const int       own  = (int)((p0 - group) / run);
+    const u64       key  = in[min(p0 + mine, p1 - 1)], head = in[p0], tail = in[p1 - 1];
+    const unsigned  t    = (unsigned)(key >> 32);
+    {  // 32 lanes to a run look at 32 places of it at a time
+        const int       r = tid / 32, lane = tid % 32, half = (tid & 32);
+        const long long start = group + (long long)r * run;
+        const int       len   = r == own ? 0 : (int)max(0ll, min((long long)run, rows - start));
+        int             lo = 0, hi = 0;
+        for (int width = run;;) {
+            const int  part = max(width / 32, 1);
+            const int  a = lo + (lane + 1) * part - 1, b = hi + (lane + 1) * part - 1;
+            const bool in_width = (lane + 1) * part <= width;
+            const u64  less_a = __ballot(in_width && a < len && in[start + min(a, max(len - 1, 0))] < head);
+            const u64  less_b = __ballot(in_width && b < len && in[start + min(b, max(len - 1, 0))] < tail);
+            lo += part * __popc((unsigned)(less_a >> half));
+            hi += part * __popc((unsigned)(less_b >> half));
+            if (part == 1) break;
+            width = part;
         }
-        at += a;
+        if (lane == 0) {
+            low[r]    = lo;
+            before[r] = hi - lo;
+        }
     }
-    out[at] = key;
+    __syncthreads();
+    if (tid < 64) {  // before[r]: keys of the windows in front of run r's
+        const int n = tid < MERGE_RUNS ? before[tid] : 0;
+        int       sum = n;
+        for (int j = 1; j < MERGE_RUNS; j *= 2) {
+            const int x = __shfl_up(sum, j);
+            if (tid >= j) sum += x;
+        }
+        int lows = tid < MERGE_RUNS ? low[tid] : 0;
+        for (int j = 1; j < 64; j *= 2) lows += __shfl_xor(lows, j);
+        if (tid < MERGE_RUNS) before[tid] = sum - n;
+        if (tid == MERGE_RUNS - 1) before[MERGE_RUNS] = sum;
+        for (int i = tid; i < MERGE_KEYS; i += 64) smaller[i] = lows;
+    }
+    __syncthreads();
+    const int all = before[MERGE_RUNS];
+    int       count = 0;
+    for (int base = 0; base < all; base += MERGE_TILE) {
+        const int here = min(all - base, MERGE_TILE);
+        for (int i = tid; i < here; i += MERGE_THREADS) {
+            int r = 0;
+#pragma unroll
+            for (int step = MERGE_RUNS / 2; step > 0; step /= 2)
+                if (before[r + step] <= base + i) r += step;
+            tile[i] = (unsigned)(in[group + (long long)r * run + low[r] + (base + i - before[r])] >> 32);
+        }
+        __syncthreads();
+        for (int r = share; r < MERGE_RUNS; r += MERGE_THREADS / MERGE_KEYS) {
+            const int      a = max(before[r] - base, 0), len = min(before[r + 1] - base, here) - a;
+            const unsigned than = t + (r < own ? 1 : 0);  // equal tokens of an earlier run come first
+            int            n = 0;
+            if (len > 0)
+                for (int step = 1 << (31 - __clz(len)); step > 0; step /= 2) {
+                    const int next = n + step;
+                    if (next <= len && tile[a + next - 1] < than) n = next;
+                }
+            count += n;
+        }
+        __syncthreads();
+    }
+    if (count) atomicAdd(&smaller[mine], count);
+    __syncthreads();
+    if (tid < MERGE_KEYS && p0 + tid < p1) out[group + (p0 - group) % run + tid + smaller[tid]] = key;
 }
 
 // ------------------------------------------------------------------------------------------------ sums
-// A group of `lanes` lanes (a power of two) has one chunk of sorted positions and `lanes` x VEC columns.
-template <int VEC>
-struct SumAt {
-    long long chunk, p0, p1;
-    int       col;
-    bool      in;
-    __device__ SumAt(int rows, int d, int lanes, int blocks) {
-        const long long id = ((long long)blockIdx.x * EMB_THREADS + threadIdx.x) / lanes;
-        chunk              = id / blocks;
-        col                = ((int)(id - chunk * blocks) * lanes + (int)(threadIdx.x & (lanes - 1))) * VEC;
-        p0                 = chunk * EMB_CHUNK;
-        p1                 = min((long long)rows, p0 + EMB_CHUNK);
-        in                 = p0 < rows && col < d;
-    }
-};
 __device__ __forceinline__ unsigned token_of(u64 k) { return (unsigned)(k >> 32); }
 
-template <int VEC>
-__device__ __forceinline__ bool finish_row(const float (&sum)[VEC], float scale, uint16_t* dw, const uint16_t* add) {
-    Part<VEC> r, a;
-    if (add) a.load(add);
+template <bool TINY>
+__device__ __forceinline__ bool finish_row(const Part& sum, float scale, uint16_t* dw, const uint16_t* add, const Piece& at) {
+    Part r, a;
+    if (add) a.set(load_piece<TINY>(add, at));
     bool bad = false;
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-        r.x[k] = scaled(sum[k], scale);
+    for (int k = 0; k < 8; ++k) {
+        r.x[k] = scaled(sum.x[k], scale);
         if (add) r.x[k] = round16(r.x[k]) + a.x[k];
-        bad |= half_nonfinite(f2h(r.x[k]));
+        bad |= k >= at.skip && half_nonfinite(f2h(r.x[k]));
     }
-    r.store(dw);
+    r.store(dw, at.skip, at.end);
     return bad;
 }
+__device__ __forceinline__ void store_part(float* o, const Part& s) {
+    *reinterpret_cast<f32x4_word*>(o)     = f32x4{s.x[0], s.x[1], s.x[2], s.x[3]};
+    *reinterpret_cast<f32x4_word*>(o + 4) = f32x4{s.x[4], s.x[5], s.x[6], s.x[7]};
+}
 
-template <int VEC>
-__global__ __launch_bounds__(EMB_THREADS) void embedding_sum_kernel(int rows, int vocab, int d, int lanes, int blocks, const u64* __restrict__ keys,
-                                                                    const uint16_t* __restrict__ dy, float scale, const uint16_t* add,
-                                                                    uint16_t* dw, float* __restrict__ part, mp_scale_state* st) {
-    const SumAt<VEC> at(rows, d, lanes, blocks);
-    bool             bad = false;
-    if (at.in) {
-        unsigned prev  = at.p0 > 0 ? token_of(keys[at.p0 - 1]) : 0xFFFFFFFFu;  // token of the open sum
-        bool     whole = false;                                               // whether that began in this chunk
-        float    sum[VEC];
+// All of a chunk's keys, then all of its rows, are on their way at once: two trips to memory.  Then they pass through the first registers
+// one by one: a loop whose code were there for each of them would come from memory too, which a small call waits for.
+template <bool TINY>
+__global__ __launch_bounds__(EMB_THREADS) void embedding_sum_kernel(int rows, int vocab, int d, int pieces, int pitch, const u64* __restrict__ keys,
+                                                                    const uint16_t* __restrict__ dy, float scale, const uint16_t* add, uint16_t* dw,
+                                                                    float* __restrict__ part, mp_scale_state* st) {
+    const Piece     at(d, pieces);
+    const long long p0 = at.row * EMB_CHUNK, p1 = min((long long)rows, p0 + EMB_CHUNK);
+    bool            bad = false;
+    if (p0 < rows) {
+        unsigned       token[EMB_CHUNK + 1];
+        Words          x[EMB_CHUNK];
+        const unsigned before = p0 > 0 ? token_of(keys[p0 - 1]) : ~0u;
+        token[EMB_CHUNK]      = p1 < rows ? token_of(keys[p1]) : ~0u;
+        u64 key[EMB_CHUNK];
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) sum[k] = 0.f;
-        bool       some  = false;
-        const auto close = [&](bool tail) {
-            if (!some || prev >= (unsigned)vocab) return;
-            if (whole && !tail) {
-                bad |= finish_row<VEC>(sum, scale, dw + (long long)prev * d + at.col, add ? add + (long long)prev * d + at.col : nullptr);
-            } else {
-                float* o = part + (at.chunk * 2 + (whole ? 1 : 0)) * d + at.col;
+        for (int j = 0; j < EMB_CHUNK; ++j) key[j] = p0 + j < p1 ? keys[p0 + j] : ~0ull;
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) o[k] = sum[k];
-            }
-        };
-        constexpr int AHEAD = 8;
-        for (long long p = at.p0; p < at.p1; p += AHEAD) {
-            u64       key[AHEAD];
-            Part<VEC> x[AHEAD];
-#pragma unroll
-            for (int j = 0; j < AHEAD; ++j) key[j] = p + j < at.p1 ? keys[p + j] : ~0ull;
-#pragma unroll
-            for (int j = 0; j < AHEAD; ++j)
-                if (token_of(key[j]) < (unsigned)vocab) x[j].load(dy + (long long)(unsigned)key[j] * d + at.col);
-#pragma unroll
-            for (int j = 0; j < AHEAD; ++j) {
-                if (p + j >= at.p1) break;
-                const unsigned t = token_of(key[j]);
-                if (t != prev) {
-                    close(false);
-                    prev  = t;
-                    whole = true;
-#pragma unroll
-                    for (int k = 0; k < VEC; ++k) sum[k] = 0.f;
-                }
-                some = true;
-                if (t < (unsigned)vocab) {
-#pragma unroll
-                    for (int k = 0; k < VEC; ++k) sum[k] += x[j].x[k];
-                }
-            }
+        for (int j = 0; j < EMB_CHUNK; ++j) {
+            token[j] = token_of(key[j]);
+            // (a token outside the table is the last one; what is loaded for it is not used)
+            x[j] = load_piece<TINY>(dy + (token[j] < (unsigned)vocab ? (long long)(unsigned)key[j] * d : 0) + at.col, at);
         }
-        close(at.p1 < rows && token_of(keys[at.p1]) == prev);
+        Part sum;
+        bool whole = token[0] != before;  // whether the open sum began in this chunk
+        sum.zero();
+#pragma unroll 1
+        for (int j = 0; j < EMB_CHUNK; ++j) {
+            const unsigned t = token[0];
+            if (t >= (unsigned)vocab) break;
+            Part one;
+            one.set(x[0]);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum.x[k] += one.x[k];
+            if (token[1] != t) {
+                if (whole) bad |= finish_row<TINY>(sum, scale, dw + (long long)t * d + at.col, add ? add + (long long)t * d + at.col : nullptr, at);
+                else store_part(part + at.row * 2 * pitch + at.col, sum);
+                sum.zero();
+                whole = true;
+            } else if (j == EMB_CHUNK - 1) {
+                store_part(part + (at.row * 2 + (whole ? 1 : 0)) * pitch + at.col, sum);
+            }
+#pragma unroll
+            for (int i = 0; i < EMB_CHUNK; ++i) token[i] = token[i + 1];
+#pragma unroll
+            for (int i = 0; i + 1 < EMB_CHUNK; ++i) x[i] = x[i + 1];
+        }
     }
     if (st && __any(bad) && (threadIdx.x & 63) == 0) atomicOr(&st->found_inf, 1);
 }
 
-// Sums that cross a border, by the chunk they begin in.
-template <int VEC>
-__global__ __launch_bounds__(EMB_THREADS) void embedding_join_kernel(int rows, int vocab, int d, int lanes, int blocks, const u64* __restrict__ keys,
+// Sums that cross a border, by the chunk they begin in.  A frequent token's partial sums are asked for several at a time, whether or not
+// they are still its own.
+constexpr int JOIN_AHEAD = 16;
+template <bool TINY>
+__global__ __launch_bounds__(EMB_THREADS) void embedding_join_kernel(int rows, int vocab, int d, int pieces, int pitch, const u64* __restrict__ keys,
                                                                      float scale, const uint16_t* add, uint16_t* dw, const float* __restrict__ part,
                                                                      mp_scale_state* st) {
-    const SumAt<VEC> at(rows, d, lanes, blocks);
-    bool             bad = false;
-    if (at.in && at.p1 < rows) {
-        const unsigned t      = token_of(keys[at.p1 - 1]);
-        const bool     begins = token_of(keys[at.p0]) != t || at.p0 == 0 || token_of(keys[at.p0 - 1]) != t;
-        if (t < (unsigned)vocab && begins && token_of(keys[at.p1]) == t) {
-            float        sum[VEC];
-            const float* o = part + (at.chunk * 2 + 1) * d + at.col;
+    const Piece     at(d, pieces);
+    const long long p0 = at.row * EMB_CHUNK, p1 = p0 + EMB_CHUNK;
+    bool            bad = false;
+    if (p1 < rows) {
+        const unsigned t = token_of(keys[p1 - 1]), first = token_of(keys[p0]), behind = token_of(keys[p1]),
+                       before = p0 > 0 ? token_of(keys[p0 - 1]) : ~0u;
+        if (t < (unsigned)vocab && behind == t && (first != t || before != t)) {
+            Part         sum;
+            const float* o = part + (at.row * 2 + 1) * pitch + at.col;
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) sum[k] = o[k];
-            for (long long c = at.chunk + 1;; ++c) {
-                o = part + c * 2 * d + at.col;
+            for (int k = 0; k < 8; ++k) sum.x[k] = o[k];
+            const long long chunks = ((long long)rows + EMB_CHUNK - 1) / EMB_CHUNK;
+            bool            more   = true;
+            for (long long c = at.row + 1; more; c += JOIN_AHEAD) {
+                f32x4    x[JOIN_AHEAD][2];
+                unsigned next[JOIN_AHEAD];  // token behind chunk c + i
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) sum[k] += o[k];
-                const long long next = (c + 1) * EMB_CHUNK;
-                if (next >= rows || token_of(keys[next]) != t) break;
+                for (int i = 0; i < JOIN_AHEAD; ++i) {
+                    const long long j = min(c + i, chunks - 1);
+                    next[i]           = (c + i + 1) * EMB_CHUNK < rows ? token_of(keys[(c + i + 1) * EMB_CHUNK]) : ~0u;
+                    x[i][0]           = *reinterpret_cast<const f32x4_word*>(part + j * 2 * pitch + at.col);
+                    x[i][1]           = *reinterpret_cast<const f32x4_word*>(part + j * 2 * pitch + at.col + 4);
+                }
+#pragma unroll
+                for (int i = 0; i < JOIN_AHEAD; ++i) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) sum.x[k] = more ? sum.x[k] + x[i][k / 4][k % 4] : sum.x[k];
+                    more = more && next[i] == t;
+                }
             }
-            bad = finish_row<VEC>(sum, scale, dw + (long long)t * d + at.col, add ? add + (long long)t * d + at.col : nullptr);
+            bad = finish_row<TINY>(sum, scale, dw + (long long)t * d + at.col, add ? add + (long long)t * d + at.col : nullptr, at);
         }
     }
     if (st && __any(bad) && (threadIdx.x & 63) == 0) atomicOr(&st->found_inf, 1);
@@ -267,19 +384,20 @@ __global__ __launch_bounds__(EMB_THREADS) void embedding_join_kernel(int rows, i
 static size_t keys_bytes(int rows) { return ((size_t)rows * sizeof(u64) + 255) / 256 * 256; }
 static long long chunks_of(int rows) { return ((long long)rows + EMB_CHUNK - 1) / EMB_CHUNK; }
 
-template <int VEC>
+static int pieces_of(int d) { return (int)(((long long)d + 7) / 8); }
+static int pitch_of(int d) { return d < 8 ? 8 : d; }
+
 static int launch_sums(int rows, int vocab, int d, const u64* keys, const mp_half* dy, float scale, const mp_half* add, mp_half* dw, float* part,
                        mp_scale_state* st, hipStream_t hs) {
-    int lanes = 1;
-    while (lanes < 64 && lanes * VEC < d) lanes *= 2;
-    const int       blocks = (d + lanes * VEC - 1) / (lanes * VEC);
-    const long long wgs    = (chunks_of(rows) * blocks * lanes + EMB_THREADS - 1) / EMB_THREADS;
+    const int       pieces = pieces_of(d);
+    const long long wgs    = (chunks_of(rows) * pieces + EMB_THREADS - 1) / EMB_THREADS;
     MP_REQUIRE(wgs < (1ll << 31), "mp_embedding_bwd: too many rows and columns");
-    hipLaunchKernelGGL(embedding_sum_kernel<VEC>, dim3((unsigned)wgs), dim3(EMB_THREADS), 0, hs, rows, vocab, d, lanes, blocks, keys, dy, scale, add, dw,
-                       part, st);
+    const dim3 grid((unsigned)wgs), block(EMB_THREADS);
+    const auto sums = d < 8 ? embedding_sum_kernel<true> : embedding_sum_kernel<false>;
+    const auto join = d < 8 ? embedding_join_kernel<true> : embedding_join_kernel<false>;
+    hipLaunchKernelGGL(sums, grid, block, 0, hs, rows, vocab, d, pieces, pitch_of(d), keys, dy, scale, add, dw, part, st);
     MP_LAUNCH_CHECK("mp_embedding_bwd(sum)");
-    hipLaunchKernelGGL(embedding_join_kernel<VEC>, dim3((unsigned)wgs), dim3(EMB_THREADS), 0, hs, rows, vocab, d, lanes, blocks, keys, scale, add, dw, part,
-                       st);
+    hipLaunchKernelGGL(join, grid, block, 0, hs, rows, vocab, d, pieces, pitch_of(d), keys, scale, add, dw, part, st);
     MP_LAUNCH_CHECK("mp_embedding_bwd(join)");
     return MP_OK;
 }
@@ -298,21 +416,18 @@ extern "C" int mp_embedding_fwd(int rows, int vocab, int d, const int32_t* token
     if (rc) return rc;
     if (rows == 0) return MP_OK;
     MP_REQUIRE(tokens && w && y, "mp_embedding_fwd: NULL argument");
-    const bool      vec    = (d & 7) == 0 && aligned16(w) && aligned16(y);
-    const int       per    = vec ? d / 8 : d;
-    const long long pieces = (long long)rows * per, wgs = (pieces + EMB_THREADS - 1) / EMB_THREADS;
-    const dim3      grid((unsigned)(wgs < (1 << 20) ? wgs : (1 << 20)));
-    if (vec)
-        hipLaunchKernelGGL(embedding_fwd_kernel<8>, grid, dim3(EMB_THREADS), 0, as_stream(stream), pieces, per, vocab, d, tokens, w, scale, y);
-    else
-        hipLaunchKernelGGL(embedding_fwd_kernel<1>, grid, dim3(EMB_THREADS), 0, as_stream(stream), pieces, per, vocab, d, tokens, w, scale, y);
+    const int       pieces = pieces_of(d);
+    const long long wgs    = ((long long)rows * pieces + EMB_THREADS - 1) / EMB_THREADS;
+    MP_REQUIRE(wgs < (1ll << 31), "mp_embedding_fwd: too many rows and columns");
+    hipLaunchKernelGGL(d < 8 ? embedding_fwd_kernel<true> : embedding_fwd_kernel<false>, dim3((unsigned)wgs), dim3(EMB_THREADS), 0, as_stream(stream), rows,
+                       vocab, d, pieces, tokens, w, scale, y);
     MP_LAUNCH_CHECK("mp_embedding_fwd");
     return MP_OK;
 }
 
 extern "C" size_t mp_embedding_bwd_workspace_bytes(int rows, int vocab, int d) {
     if (rows < 0 || vocab <= 0 || d <= 0) return 0;
-    return 2 * keys_bytes(rows) + (size_t)chunks_of(rows) * 2 * d * sizeof(float) + 256;
+    return 2 * keys_bytes(rows) + (size_t)chunks_of(rows) * 2 * pitch_of(d) * sizeof(float) + 256;
 }
 
 extern "C" int mp_embedding_bwd(int rows, int vocab, int d, const int32_t* tokens, const mp_half* dy, float scale, const mp_half* add, mp_half* dw,
@@ -342,13 +457,12 @@ extern "C" int mp_embedding_bwd(int rows, int vocab, int d, const int32_t* token
     MP_LAUNCH_CHECK("mp_embedding_bwd(sort)");
     if (rows == 0) return MP_OK;
     for (long long run = SORT_RUN; run < rows; run *= MERGE_RUNS) {
-        hipLaunchKernelGGL(embedding_merge_kernel, dim3((rows + EMB_THREADS - 1) / EMB_THREADS), dim3(EMB_THREADS), 0, hs, rows, run, keys, more);
+        hipLaunchKernelGGL(embedding_merge_kernel, dim3((rows + MERGE_KEYS - 1) / MERGE_KEYS), dim3(MERGE_THREADS), 0, hs, rows, (int)run, keys,
+                           more);
         MP_LAUNCH_CHECK("mp_embedding_bwd(merge)");
         u64* t = keys;
         keys   = more;
         more   = t;
     }
-    const bool vec = (d & 7) == 0 && aligned16(dy) && aligned16(dw) && (!add || aligned16(add));
-    return vec ? launch_sums<8>(rows, vocab, d, keys, dy, scale, add, dw, part, st, hs)
-               : launch_sums<1>(rows, vocab, d, keys, dy, scale, add, dw, part, st, hs);
+    return launch_sums(rows, vocab, d, keys, dy, scale, add, dw, part, st, hs);
 }
