@@ -70,12 +70,13 @@ class ScaleCfg:
 
 @dataclass(frozen=True)
 class OptCfg:
-    kind: str = "adam"             # "sgd" | "adam"
+    kind: str = "adam"             # "sgd" | "adam" | "adamw"
     lr: float = 1e-4
     beta1: float = 0.9
     beta2: float = 0.999
     eps: float = 1e-8
     weight_decay: float = 0.0
+    state_bits: int = 32           # 8: Adam's moments as 8-bit codes with a scale for every 256 elements
 
 
 @dataclass(frozen=True)
@@ -112,7 +113,11 @@ class MLPWorkload:
 
 @dataclass(frozen=True)
 class TransformerWorkload:
-    """Configs 2 and 3: a stack of post-LayerNorm encoder layers, MSE loss, Adam."""
+    """Configs 2 and 3: a stack of post-LayerNorm encoder layers, MSE loss, Adam.
+
+    Not part of the configs, each by itself or together: `causal` attention; `n_docs` documents of any lengths packed into the
+    tokens (their starts come with the batch) instead of n_seq sequences of one length; a `vocab` whose embedding, times
+    sqrt(d_model), is the first layer's input."""
     index: int = 2
     n_layers: int = 1
     d_model: int = 512
@@ -123,6 +128,9 @@ class TransformerWorkload:
     steps: int = 50
     opt: OptCfg = OptCfg(kind="adam", lr=1e-4)
     scale: ScaleCfg = ScaleCfg(init_scale=2.0 ** 15, growth_interval=10)
+    causal: bool = False
+    n_docs: int = 0
+    vocab: int = 0
 
     @property
     def tokens(self):
@@ -150,17 +158,28 @@ class TransformerWorkload:
     def masters(self) -> List[Dict[str, np.ndarray]]:
         return [self.layer_masters(l) for l in range(self.n_layers)]
 
+    def embedding(self) -> Dict[str, np.ndarray]:
+        """The table, where there is a vocabulary; its rows times sqrt(d_model) have unit variance."""
+        return {"emb": normal(self.index, "emb", (self.vocab, self.d_model), self.d_model ** -0.5)} if self.vocab else {}
+
     def batch(self) -> Dict[str, np.ndarray]:
         i = self.index
-        return {"x": normal(i, "x", (self.tokens, self.d_model)),
-                "target": normal(i, "target", (self.tokens, self.d_model))}
+        out = {"target": normal(i, "target", (self.tokens, self.d_model))}
+        if self.vocab:
+            out["tokens"] = stream(i, "tokens").integers(0, self.vocab, size=(self.tokens,)).astype(np.int32)
+        else:
+            out["x"] = normal(i, "x", (self.tokens, self.d_model))
+        if self.n_docs:
+            cuts = np.sort(stream(i, "doc_start").integers(0, self.tokens + 1, size=(self.n_docs - 1,)))
+            out["doc_start"] = np.concatenate([[0], cuts, [self.tokens]]).astype(np.int32)
+        return out
 
     def n_params(self) -> int:
         d, f = self.d_model, self.d_ff
-        return self.n_layers * (4 * d * d + 2 * d * f + 3 * d + d + f + d + 4 * d)
+        return self.vocab * d + self.n_layers * (4 * d * d + 2 * d * f + 3 * d + d + f + d + 4 * d)
 
     def gemm_flops_per_step(self) -> float:
-        """2*M*N*K over every contraction of forward + backward (dx and dw)."""
+        """2*M*N*K over every contraction of forward + backward (dx and dw); attention as if every token saw its whole sequence."""
         t, d, f = self.tokens, self.d_model, self.d_ff
         proj = 4 * 2.0 * t * d * d
         ffn = 2 * 2.0 * t * d * f

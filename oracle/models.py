@@ -40,11 +40,14 @@ def mlp_fwd_bwd(P: Policy, w, batch, scale, keep=None):
 
 
 # ------------------------------------------------------------- configs 2, 3
-def encoder_layer_fwd(P: Policy, w, pre, x, n_seq, seq_len, n_heads):
+def encoder_layer_fwd(P: Policy, w, pre, x, n_seq, seq_len, n_heads, seen=None):
     """Post-LayerNorm Transformer encoder layer:
-    y1 = LN(x + Wo attention(Wqkv x)),  y2 = LN(y1 + W2 relu(W1 y1))."""
+    y1 = LN(x + Wo attention(Wqkv x)),  y2 = LN(y1 + W2 relu(W1 y1)).  `seen`: the rows' intervals, for attention under a mask."""
     qkv = L.linear_fwd(P, x, w[pre + "wqkv"], w[pre + "bqkv"])
-    ctx, att = L.attention_fwd(P, qkv, n_seq, seq_len, n_heads)
+    if seen is None:
+        ctx, att = L.attention_fwd(P, qkv, n_seq, seq_len, n_heads)
+    else:
+        ctx, att = L.masked_attention_fwd(P, *np.split(qkv, 3, axis=1), *seen, n_heads, n_heads)
     a = L.linear_fwd(P, ctx, w[pre + "wo"], w[pre + "bo"])
     y1, ln1 = L.layernorm_fwd(P, x, a, w[pre + "ln1_g"], w[pre + "ln1_b"])
     f = L.linear_fwd(P, y1, w[pre + "w1"], w[pre + "b1"], relu=True)
@@ -61,16 +64,22 @@ def encoder_layer_bwd(P: Policy, w, pre, dy2, c, grads):
     dy1 = L.add_store(P, dy1_ffn, dz2)
     dz1, grads[pre + "ln1_g"], grads[pre + "ln1_b"] = L.layernorm_bwd(P, dy1, c["ln1"], w[pre + "ln1_g"])
     dctx, grads[pre + "wo"], grads[pre + "bo"] = L.linear_bwd(P, dz1, c["ctx"], w[pre + "wo"])
-    dqkv = L.attention_bwd(P, dctx, c["att"])
+    dqkv = np.concatenate(L.masked_attention_bwd(P, dctx, c["att"]), axis=1) if isinstance(c["att"], dict) else L.attention_bwd(P, dctx, c["att"])
     dx_att, grads[pre + "wqkv"], grads[pre + "bqkv"] = L.linear_bwd(P, dqkv, c["x"], w[pre + "wqkv"])
     return L.add_store(P, dx_att, dz1)
 
 
-def make_transformer_fwd_bwd(n_layers, n_seq, seq_len, n_heads):
+def make_transformer_fwd_bwd(n_layers, n_seq, seq_len, n_heads, causal=False):
+    """With "doc_start" in the batch its documents take the place of the sequences, with "tokens" the rows of `emb` times sqrt(d)
+    that of the input."""
     def fwd_bwd(P: Policy, w, batch, scale, keep=None):
-        h, caches = batch["x"], []
+        seen, tokens, caches = None, batch.get("tokens"), []
+        if causal or "doc_start" in batch:
+            rows = n_seq * seq_len
+            seen = L.attention_ranges(rows, batch.get("doc_start", np.arange(0, rows + 1, seq_len)), causal)
+        h = batch["x"] if tokens is None else L.embedding_fwd(P, tokens, w["emb"], np.sqrt(float(w["emb"].shape[1])))
         for l in range(n_layers):
-            h, c = encoder_layer_fwd(P, w, f"l{l}.", h, n_seq, seq_len, n_heads)
+            h, c = encoder_layer_fwd(P, w, f"l{l}.", h, n_seq, seq_len, n_heads, seen)
             caches.append(c)
         loss, dh = L.mse_scaled(P, h, batch["target"], scale)
         grads = {}
@@ -78,6 +87,8 @@ def make_transformer_fwd_bwd(n_layers, n_seq, seq_len, n_heads):
             keep.update(y=h, dy=dh, caches=caches)
         for l in range(n_layers - 1, -1, -1):
             dh = encoder_layer_bwd(P, w, f"l{l}.", dh, caches[l], grads)
+        if tokens is not None:
+            grads["emb"] = L.embedding_bwd(P, tokens, dh, w["emb"].shape[0], np.sqrt(float(w["emb"].shape[1])))
         if keep is not None:
             keep["dx"] = dh
         return loss, grads

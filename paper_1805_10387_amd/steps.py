@@ -27,22 +27,27 @@ def _round_up(n: int, k: int) -> int:
 
 class ParamStore:
     """fp32 masters, fp16 copies, fp16 gradients and Adam moments of a model, each kind in one
-    contiguous device arena (every tensor starts on a 16-element boundary, gaps stay zero)."""
+    contiguous device arena (every tensor starts on a 16-element boundary, gaps stay zero).  Moments in 8 bits: their codes
+    and scales instead (`m8`, `v8`, `ms`, `vs`), tensors on the boundaries of the scales' blocks."""
 
-    def __init__(self, masters: Dict[str, np.ndarray], adam: bool):
+    def __init__(self, masters: Dict[str, np.ndarray], adam: bool, state_bits: int = 32):
+        if state_bits not in (8, 32) or (state_bits == 8 and not adam):
+            raise ValueError(f"moments in {state_bits} bits: Adam's are kept in 32 or 8")
+        self.state_bits = state_bits
+        moments32, block = adam and state_bits == 32, ML.MP_STATE8_BLOCK if state_bits == 8 else 16
         self.names = list(masters)
         self.shapes = {k: tuple(v.shape) for k, v in masters.items()}
         self.offsets, off = {}, 0
         for k, v in masters.items():
             self.offsets[k] = off
-            off += _round_up(int(v.size), 16)
+            off += _round_up(int(v.size), block)
         self.total = off
         dev = "cuda"
         self.w32_arena = torch.zeros(off, dtype=torch.float32, device=dev)
         self.w16_arena = torch.zeros(off, dtype=torch.float16, device=dev)
         self.g16_arena = torch.zeros(off, dtype=torch.float16, device=dev)
-        self.m_arena = torch.zeros(off, dtype=torch.float32, device=dev) if adam else None
-        self.v_arena = torch.zeros(off, dtype=torch.float32, device=dev) if adam else None
+        self.m_arena = torch.zeros(off, dtype=torch.float32, device=dev) if moments32 else None
+        self.v_arena = torch.zeros(off, dtype=torch.float32, device=dev) if moments32 else None
         host = np.zeros(off, dtype=np.float32)
         for k, v in masters.items():
             host[self.offsets[k]:self.offsets[k] + v.size] = np.asarray(v, dtype=np.float32).reshape(-1)
@@ -51,13 +56,24 @@ class ParamStore:
         self.w32 = {k: self._view(self.w32_arena, k) for k in self.names}
         self.w16 = {k: self._view(self.w16_arena, k) for k in self.names}
         self.g16 = {k: self._view(self.g16_arena, k) for k in self.names}
-        self.m = {k: self._view(self.m_arena, k) for k in self.names} if adam else {}
-        self.v = {k: self._view(self.v_arena, k) for k in self.names} if adam else {}
+        self.m = {k: self._view(self.m_arena, k) for k in self.names} if moments32 else {}
+        self.v = {k: self._view(self.v_arena, k) for k in self.names} if moments32 else {}
         self.n_params = sum(int(np.prod(s)) for s in self.shapes.values())
+        self.n_tensors = len(self.names)
+        if state_bits == 8:
+            zeros = lambda n, kind: torch.zeros(n, dtype=kind, device=dev)  # noqa: E731
+            self.state8 = dict(m8=zeros(off, torch.int8), v8=zeros(off, torch.uint8), ms=zeros(off // block, torch.float32),
+                               vs=zeros(off // block, torch.float32))
+            self.m8, self.v8 = ({k: self._view(self.state8[n], k) for k in self.names} for n in ("m8", "v8"))
+            self.ms, self.vs = ({k: self.state8[n][self.offsets[k] // block:][:(self.w32[k].numel() + block - 1) // block] for k in self.names}
+                                for n in ("ms", "vs"))
+            self.tensor_list = B.tensor_list8([dict(g16=self.g16[k], w32=self.w32[k], w16=self.w16[k], m8=self.m8[k], v8=self.v8[k],
+                                                    ms=self.ms[k], vs=self.vs[k]) for k in self.names])
+            self.flat_list = B.tensor_list8([dict(g16=self.g16_arena, w32=self.w32_arena, w16=self.w16_arena, **self.state8)])
+            return
         entries = [dict(g16=self.g16[k], w32=self.w32[k], w16=self.w16[k], m=self.m.get(k), v=self.v.get(k))
                    for k in self.names]
         self.tensor_list = B.tensor_list(entries)
-        self.n_tensors = len(entries)
         flat = [dict(g16=self.g16_arena, w32=self.w32_arena, w16=self.w16_arena, m=self.m_arena, v=self.v_arena)]
         self.flat_list = B.tensor_list(flat)
 
@@ -68,7 +84,7 @@ class ParamStore:
 
 class _StepBase:
     def __init__(self, masters: Dict[str, np.ndarray], opt, scale_cfg, prechecked: bool = False, flat_update: bool = False):
-        self.P = ParamStore(masters, adam=(opt.kind == "adam"))
+        self.P = ParamStore(masters, adam=opt.kind in ("adam", "adamw"), state_bits=opt.state_bits)
         self.cfg = B.opt_cfg(opt.kind, opt.lr, opt.beta1, opt.beta2, opt.eps, opt.weight_decay)
         self.st = B.scale_state_alloc()
         mode = ML.MP_SCALE_BACKOFF if scale_cfg.mode == "backoff" else ML.MP_SCALE_STATIC
@@ -98,7 +114,8 @@ class _StepBase:
         flags = ML.MP_UPDATE_PRECHECKED if self.prechecked else ML.MP_UPDATE_DEFAULT
         parts, self._parts = self._parts, None
         tensors, n = (self.P.flat_list, 1) if self.flat_update else (self.P.tensor_list, self.P.n_tensors)
-        B.mp_unscale_check_update_end(tensors, n, self.cfg, self.st, self.counters, flags, parts, self.loss)
+        update = B.mp_unscale_check_update8_end if self.P.state_bits == 8 else B.mp_unscale_check_update_end
+        update(tensors, n, self.cfg, self.st, self.counters, flags, parts, self.loss)
 
     def _mse(self, rows, cols, y, target, dy):
         """Loss and seed gradient; within step() the loss itself is finished by the launch that ends the iteration."""
@@ -136,6 +153,10 @@ def _h16(x: np.ndarray) -> torch.Tensor:
     return dst
 
 
+def _i32(x: np.ndarray) -> torch.Tensor:
+    return torch.from_numpy(np.ascontiguousarray(np.asarray(x, dtype=np.int32))).cuda()
+
+
 # ====================================================================================== config 1
 class MLPStep(_StepBase):
     """x -> relu(W1 x + b1) -> W2 h + b2, MSE loss (config 1)."""
@@ -169,18 +190,23 @@ class MLPStep(_StepBase):
 
 # ====================================================================================== configs 2, 3
 class TransformerStep(_StepBase):
-    """Stack of post-LayerNorm encoder layers with an MSE loss on the last output (configs 2, 3)."""
+    """Stack of post-LayerNorm encoder layers with an MSE loss on the last output (configs 2, 3).
+
+    A causal workload or one of packed documents runs attention under a mask, which set_batch prepares for all layers; one with a
+    vocabulary takes tokens and trains their embedding."""
 
     def __init__(self, wl, masters=None, two_streams=False, fused_attention=True, grouped_dw=True, **kw):
         if masters is None:
-            masters = {f"l{i}.{k}": v for i, lay in enumerate(wl.masters()) for k, v in lay.items()}
+            masters = wl.embedding()
+            masters.update({f"l{i}.{k}": v for i, lay in enumerate(wl.masters()) for k, v in lay.items()})
         super().__init__(masters, wl.opt, wl.scale, **kw)
         self.wl = wl
         self.two_streams = two_streams
         dk_ = wl.d_model // wl.n_heads
         # the fused attention kernels cover head size 64 and sequences up to 128; anything else runs the unfused chain of
         # batched products and softmax kernels (two base layers on 61 sentences of 53 tokens: 671 us that way, 613 us fused)
-        self.fused_attention = fused_attention and dk_ == 64 and wl.seq_len <= 128
+        self.masked = wl.causal or wl.n_docs > 0
+        self.fused_attention = fused_attention and dk_ == 64 and wl.seq_len <= 128 and not self.masked
         self.ld_p = (wl.seq_len + 7) // 8 * 8 if self.fused_attention else wl.seq_len    # rows of the kept probabilities
         self.alpha = 1.0 / math.sqrt(dk_)
         # one launch for the four weight-gradient products of a layer (each alone has too few tiles for the chip);
@@ -203,13 +229,15 @@ class TransformerStep(_StepBase):
         self.x0, self.target = e16_dw(d), e16(T, d)
         self.act: List[dict] = []
         for _ in range(wl.n_layers):
-            self.act.append(dict(qkv=e16(T, 3 * d), p=e16(NB, h, S, self.ld_p)[..., :S], ctx=e16_dw(d), a=e16(T, d), y1=e16_dw(d),
+            self.act.append(dict(qkv=e16(T, 3 * d), ctx=e16_dw(d), a=e16(T, d), y1=e16_dw(d),
                                  f=e16_dw(f), g=e16(T, d), y2=e16_dw(d), mean1=e32(T), rstd1=e32(T), mean2=e32(T),
                                  rstd2=e32(T)))
+            # kept for the attention's backward: the probabilities, or under a mask what each row's sum was
+            self.act[-1].update(dict(lse=e32(h, T)) if self.masked else dict(p=e16(NB, h, S, self.ld_p)[..., :S]))
         # backward temporaries, shared by all layers
         self.gbuf = [e16(T, d), e16(T, d)]
         self.tmp = [dict(dz2=e16_dw(d), df=e16_dw(f), dz1=e16_dw(d), dqkv=e16_dw(3 * d)) for _ in range(2)]
-        self.dy1, self.dctx, self.dp = e16(T, d), e16(T, d), e16(NB, h, S, S)
+        self.dy1, self.dctx, self.dp = e16(T, d), e16(T, d), None if self.masked else e16(NB, h, S, S)
         G = B.gemm_desc
         self.d_qkv = G(T, 3 * d, d, epilogue=ML.MP_EPI_BIAS)
         self.d_o = G(T, d, d, epilogue=ML.MP_EPI_BIAS)
@@ -232,8 +260,18 @@ class TransformerStep(_StepBase):
                           all(B.mp_gemm_bwd_both_joint(x, x) for x in (self.d_qkv, self.d_o, self.d_f1, self.d_f2)))
         self.grouped_dw = self.grouped_dw and not self.joint_bwd
         need = [B.mp_gemm_bwd_dw_workspace_bytes(x, True) for x in (self.d_qkv, self.d_o, self.d_f1, self.d_f2)]
-        need += [B.mp_gemm_bwd_dw_workspace_bytes(self.d_s, False), B.mp_gemm_bwd_dw_workspace_bytes(self.d_c, False),
-                 B.mp_layernorm_bwd_workspace_bytes(T, d)]
+        need.append(B.mp_layernorm_bwd_workspace_bytes(T, d))
+        if self.masked:
+            self.d_att = B.attn_desc(T, T, h, h, dk, ld_q=3 * d, ld_k=3 * d, ld_v=3 * d, alpha=alpha)
+            self.mask = torch.empty(B.mp_attention_mask_bytes(T) // 4, dtype=torch.int32, device="cuda")
+            self.n_docs = wl.n_docs or NB
+            self.doc_start = torch.arange(0, T + 1, S, dtype=torch.int32, device="cuda")
+            need.append(B.mp_attention_masked_bwd_workspace_bytes(self.d_att))
+        else:
+            need += [B.mp_gemm_bwd_dw_workspace_bytes(self.d_s, False), B.mp_gemm_bwd_dw_workspace_bytes(self.d_c, False)]
+        if wl.vocab:
+            self.tokens, self.emb_scale = torch.empty(T, dtype=torch.int32, device="cuda"), math.sqrt(d)
+            need.append(B.mp_embedding_bwd_workspace_bytes(T, wl.vocab, d))
         self._alloc_ws(max(need), B.mp_loss_workspace_bytes(T, d))
         self.ws_side = torch.empty_like(self.ws)
         # partial column sums of a layer's two LayerNorm backwards, finished by its grouped launch (which alternate by layer)
@@ -244,17 +282,32 @@ class TransformerStep(_StepBase):
             self.ln_nparts = B.mp_layernorm_bwd_nparts(T, d)
 
     def set_batch(self, batch):
-        self.x0.copy_(_h16(batch["x"]))
+        wl = self.wl
+        if wl.vocab:
+            self.tokens.copy_(_i32(batch["tokens"]))
+        else:
+            self.x0.copy_(_h16(batch["x"]))
+        if wl.n_docs:
+            starts = _i32(batch["doc_start"])
+            if starts.shape != (wl.n_docs + 1,):
+                raise ValueError(f"{tuple(starts.shape)} document starts for {wl.n_docs} documents")
+            self.doc_start = starts
+        if self.masked:
+            B.mp_attention_mask_docs(wl.tokens, self.n_docs, self.doc_start, self.mask, causal=wl.causal)
         self.target.copy_(_h16(batch["target"]))
 
     def forward(self):
         wl, w = self.wl, self.P.w16
         T, d, h, S, NB = wl.tokens, wl.d_model, wl.n_heads, wl.seq_len, wl.n_seq
         x = self.x0
+        if wl.vocab:
+            B.mp_embedding_fwd(T, wl.vocab, d, self.tokens, w["emb"], self.emb_scale, x)
         for l, a in enumerate(self.act):
             p = f"l{l}."
             B.mp_gemm_fwd(self.d_qkv, x, w[p + "wqkv"], w[p + "bqkv"], None, a["qkv"])
-            if self.fused_attention:
+            if self.masked:
+                B.mp_attention_masked_fwd(self.d_att, self.mask, a["qkv"], a["qkv"][:, d:], a["qkv"][:, 2 * d:], None, a["ctx"], a["lse"])
+            elif self.fused_attention:
                 B.mp_attention_fwd_ldp(NB, h, S, d // h, a["qkv"], 3 * d, self.alpha, a["p"], self.ld_p, a["ctx"], d)
             else:
                 B.mp_gemm_fwd(self.d_s, a["qkv"], a["qkv"][:, d:], None, None, a["p"])
@@ -334,7 +387,10 @@ class TransformerStep(_StepBase):
             linear_bwd(self.d_o, dz1, p + "wo", p + "bo", a["ctx"], self.dctx, False)
             self._t("dctx", l, self.dctx)
             # attention: dP = dctx V^T, dV = P^T dctx, dS = softmax', dQ = alpha dS K, dK = alpha dS^T Q
-            if self.fused_attention:
+            if self.masked:
+                B.mp_attention_masked_bwd(self.d_att, self.mask, a["qkv"], a["qkv"][:, d:], a["qkv"][:, 2 * d:], None, a["ctx"], a["lse"],
+                                          self.dctx, dqkv, dqkv[:, d:], dqkv[:, 2 * d:], ws)
+            elif self.fused_attention:
                 B.mp_attention_bwd_ldp(NB, h, S, d // h, a["qkv"], 3 * d, self.alpha, a["p"], self.ld_p, self.dctx, d, dqkv, 3 * d)
             else:
                 B.mp_gemm_bwd_dx(self.d_c, self.dctx, a["qkv"][:, 2 * d:], self.dp)
@@ -366,6 +422,8 @@ class TransformerStep(_StepBase):
         if side is not None:
             main.wait_stream(side)                   # every weight gradient is complete before the update
         self.dx_input = self.gbuf[wl.n_layers % 2]
+        if wl.vocab:
+            B.mp_embedding_bwd(T, wl.vocab, d, self.tokens, self.dx_input, self.emb_scale, g["emb"], st=st, ws=ws)
 
     def forward_backward(self):
         wl = self.wl
