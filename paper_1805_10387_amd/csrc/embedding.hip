@@ -22,13 +22,6 @@ constexpr int MERGE_RUNS  = 32;
 constexpr int EMB_CHUNK   = 8;
 constexpr int FILL_WGS    = 2048;
 
-// What the lanes of this wave wrote to LDS is there for its other lanes.
-__device__ __forceinline__ void wave_order() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // The product rounded to fp32 before it is rounded to fp16: the compiler else makes one instruction of the two in some places,
 // which rounds once (an element in 10^4 differs, and a call with `add` from one without).
 __device__ __forceinline__ float scaled(float x, float scale) {
@@ -126,10 +119,41 @@ __global__ __launch_bounds__(EMB_THREADS) void embedding_fwd_kernel(int rows, in
 }
 
 // ------------------------------------------------------------------------------------------------ sort
+// The value of the lane whose number differs in bit X.
+template <int X>
+__device__ __forceinline__ unsigned other_lane(unsigned v, int lane) {
+    const auto dpp = [](unsigned x, auto ctrl) { return (unsigned)__builtin_amdgcn_update_dpp((int)x, (int)x, decltype(ctrl)::value, 0xF, 0xF, true); };
+    if constexpr (X == 1) return dpp(v, std::integral_constant<int, 0xB1>{});                                            // quad: 1 0 3 2
+    if constexpr (X == 2) return dpp(v, std::integral_constant<int, 0x4E>{});                                            // quad: 2 3 0 1
+    if constexpr (X == 4) return dpp(dpp(v, std::integral_constant<int, 0x141>{}), std::integral_constant<int, 0x1B>{});  // 7 - i, quad: 3 2 1 0
+    if constexpr (X == 8) return dpp(v, std::integral_constant<int, 0x128>{});                                           // row of 16 rotated by 8
+    if constexpr (X == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return lane & 16 ? r[0] : r[1];
+    }
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return lane & 32 ? r[0] : r[1];
+}
+// Bitonic steps of distances J, J/2 .. 1 in registers: a lane has elements 2 lane and 2 lane + 1.
+template <int J>
+__device__ __forceinline__ void sort_steps(unsigned& x, unsigned& y, bool up, int lane) {
+    if constexpr (J == 1) {
+        const unsigned lo = min(x, y), hi = max(x, y);
+        x = up ? lo : hi;
+        y = up ? hi : lo;
+    } else {
+        const unsigned p = other_lane<J / 2>(x, lane), q = other_lane<J / 2>(y, lane);
+        const bool     least = up == ((lane & (J / 2)) == 0);
+        x = least ? min(x, p) : max(x, p);
+        y = least ? min(y, q) : max(y, q);
+        sort_steps<J / 2>(x, y, up, lane);
+    }
+}
+
 // The first `runs` workgroups sort; the others clear dw (or copy add into it), in words and a last half word.
 __global__ __launch_bounds__(1024) void embedding_sort_kernel(int rows, int vocab, int runs, const int* __restrict__ tokens, u64* __restrict__ keys,
                                                               uint16_t* __restrict__ dw, const uint16_t* __restrict__ add, size_t n, mp_scale_state* st) {
-    __shared__ unsigned s[SORT_RUN];
+    __shared__ uint2 s[2][SORT_RUN / 2];
     if ((int)blockIdx.x >= runs) {
         const size_t step = (size_t)(gridDim.x - runs) * 1024, first = (size_t)(blockIdx.x - runs) * 1024 + threadIdx.x;
         if (!add) {
@@ -149,40 +173,44 @@ __global__ __launch_bounds__(1024) void embedding_sort_kernel(int rows, int voca
         }
         return;
     }
-    const int base = blockIdx.x * SORT_RUN;
+    // A thread has two neighbours.  Distances up to 64 lie in a wave and take no LDS; the ten larger ones go through it, from one half
+    // to the other and so with one barrier (2048 keys: 14 us with every step in LDS, 6 this way).
+    const int base = blockIdx.x * SORT_RUN, t = threadIdx.x, lane = t & 63;
+    unsigned  key[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const int i = threadIdx.x + 1024 * j, p = base + i;
-        unsigned  key = 0xFFFFFFFFu;
+        const int i = 2 * t + j, p = base + i;
+        key[j] = 0xFFFFFFFFu;
         if (p < rows) {
-            const int t = tokens[p];
-            key         = ((unsigned)t < (unsigned)vocab ? (unsigned)t : (unsigned)vocab) << SORT_BITS | (unsigned)i;
+            const int v = tokens[p];
+            key[j]      = ((unsigned)v < (unsigned)vocab ? (unsigned)v : (unsigned)vocab) << SORT_BITS | (unsigned)i;
         }
-        s[i] = key;
     }
-    __syncthreads();
-    int most = 2;  // (what lies behind the last key is the largest)
-    while (most < SORT_RUN && most < rows - base) most *= 2;
-    // Bitonic.  A thread's two elements of a step lie in its wave's 128 for distances up to 64: LDS serves a wave in order, so only
-    // larger distances need the workgroup.
-    for (int k = 2; k <= most; k *= 2)
-        for (int j = k / 2; j > 0; j /= 2) {
-            if (j >= 128) __syncthreads();
-            else wave_order();
-            const int      a = 2 * threadIdx.x - (threadIdx.x & (j - 1)), b = a + j;
-            const unsigned x = s[a], y = s[b];
-            if ((x > y) == ((a & k) == 0)) {
-                s[a] = y;
-                s[b] = x;
-            }
-            if (j >= 128) __syncthreads();
-            else wave_order();
+    sort_steps<1>(key[0], key[1], (lane & 1) == 0, lane);
+    sort_steps<2>(key[0], key[1], (lane & 2) == 0, lane);
+    sort_steps<4>(key[0], key[1], (lane & 4) == 0, lane);
+    sort_steps<8>(key[0], key[1], (lane & 8) == 0, lane);
+    sort_steps<16>(key[0], key[1], (lane & 16) == 0, lane);
+    sort_steps<32>(key[0], key[1], (lane & 32) == 0, lane);
+    sort_steps<64>(key[0], key[1], (t & 64) == 0, lane);
+    int b = 0;
+    // (what lies behind the last key is the largest: runs of nothing else need no merging)
+    for (int k = 256; k <= SORT_RUN && k / 2 < rows - base; k *= 2) {
+        const bool up = k == SORT_RUN || (t & (k / 2)) == 0;
+        for (int j = k / 2; j >= 128; j /= 2, b ^= 1) {
+            s[b][t] = make_uint2(key[0], key[1]);
+            __syncthreads();
+            const uint2 o     = s[b][t ^ (j / 2)];
+            const bool  least = up == ((t & (j / 2)) == 0);
+            key[0] = least ? min(key[0], o.x) : max(key[0], o.x);
+            key[1] = least ? min(key[1], o.y) : max(key[1], o.y);
         }
-    __syncthreads();
+        sort_steps<64>(key[0], key[1], up, lane);
+    }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const int i = threadIdx.x + 1024 * j;
-        if (base + i < rows) keys[base + i] = (u64)(s[i] >> SORT_BITS) << 32 | (unsigned)(base + (s[i] & (SORT_RUN - 1)));
+        const int i = base + 2 * t + j;
+        if (i < rows) keys[i] = (u64)(key[j] >> SORT_BITS) << 32 | (unsigned)(base + (int)(key[j] & (SORT_RUN - 1)));
     }
 }
 
