@@ -6,13 +6,14 @@
  * fp32 master weights; Section 3.2: the optimizer wrapper; Section 3.3:
  * regularisation on the fp32 copy):
  *
- *   forward  : mp_gemm_fwd[_ws] (+ mp_layernorm_fwd, mp_attention_fwd | mp_softmax_fwd,
- *              mp_lstm_cell_fwd | mp_lstm_layer_fwd)
+ *   forward  : mp_gemm_fwd[_ws] (+ mp_layernorm_fwd, mp_attention_fwd | mp_attention_masked_fwd | mp_softmax_fwd,
+ *              mp_embedding_fwd, mp_lstm_cell_fwd | mp_lstm_layer_fwd)
  *   loss     : mp_mse_scaled | mp_softmax_xent_scaled[_db] (seed gradient x loss scale)
  *   backward : mp_gemm_bwd_dx[_ws], mp_gemm_bwd_dw | mp_gemm_bwd_dw_grouped (+ mp_layernorm_bwd,
- *              mp_attention_bwd | mp_softmax_bwd, mp_lstm_cell_bwd | mp_lstm_layer_bwd, mp_colsum)
- *   update   : mp_unscale_check_update   (inspect fp16 gradients, unscale, SGD/Adam on
- *                                         fp32 masters, rewrite the fp16 copies - or skip)
+ *              mp_attention_bwd | mp_attention_masked_bwd | mp_softmax_bwd, mp_embedding_bwd,
+ *              mp_lstm_cell_bwd | mp_lstm_layer_bwd, mp_colsum)
+ *   update   : mp_unscale_check_update[8] (inspect fp16 gradients, unscale, SGD/Adam/AdamW on fp32
+ *                                         masters, rewrite the fp16 copies - or skip; 8: moments in 8 bits)
  *              mp_loss_scale_update      (halve / count / grow the loss scale)
  *
  * Conventions (all entry points):
@@ -434,7 +435,7 @@ typedef struct mp_attn_desc {
     int32_t ld_q, ld_k, ld_v, ld_ctx;     /* multiples of 8 below 2^22, as are those of the gradients     */
     int32_t ld_dq, ld_dk, ld_dv, ld_dctx;
     float   alpha;                        /* > 0                                                          */
-    float   cap;                          /* 0: none                                                      */
+    float   cap;                          /* 0: none; else up to 1024, and alpha / cap below 1e30        */
     int32_t reserved;                     /* 0                                                            */
 } mp_attn_desc;
 
@@ -445,7 +446,8 @@ typedef struct mp_attn_desc {
  * above 1, the row's largest is 1).
  * What a row does not see does not reach it, NaN and infinities included; of a value row that holds one, those rows that see it get
  * non-finite results.  All rows of ctx are written.  Any rows_k >= 0 and rows_q >= 0.
- * 16-byte aligned matrices with leading dimensions and a d_head as above; otherwise MP_E_UNSUPPORTED. */
+ * `mask` is one of rows_q rows.  16-byte aligned matrices with leading dimensions, a d_head and a cap as above; otherwise
+ * MP_E_UNSUPPORTED. */
 int mp_attention_masked_fwd(const mp_attn_desc* desc /* host */, const void* mask, const mp_half* q, const mp_half* k,
                             const mp_half* v, const float* slopes, mp_half* ctx, float* lse, mp_stream stream);
 
@@ -464,7 +466,7 @@ int mp_attention_masked_bwd(const mp_attn_desc* desc /* host */, const void* mas
  * Embedding: rows of a table w[vocab, d] by token (the other end of the vocabulary projection).
  * ------------------------------------------------------------------------------------------ */
 /* y[t] = RNE16(scale w[tokens[t]]); a token outside [0, vocab) gives a zero row.  w, y contiguous, at any element.  tokens: device
- * int32 [rows]. */
+ * int32 [rows].  Up to 2^39 elements of y. */
 int mp_embedding_fwd(int rows, int vocab, int d, const int32_t* tokens, const mp_half* w, float scale, mp_half* y,
                      mp_stream stream);
 

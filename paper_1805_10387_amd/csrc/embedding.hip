@@ -30,8 +30,8 @@ __device__ __forceinline__ float scaled(float x, float scale) {
     return x;
 }
 
-// 8 elements of a row that may begin at any element.  A load asks for the four words, or five, that hold them: a word is the least that
-// memory serves at its full rate.
+// 8 elements of a row that may begin at any element.  A load asks for the four words, or five, that hold them: each holds one of the 8 at
+// least, so nothing behind a page is touched.
 typedef u32x4e   u32x4e_any __attribute__((aligned(2)));
 typedef u32x4e   u32x4e_word __attribute__((aligned(4)));
 typedef f32x4    f32x4_word __attribute__((aligned(4)));
@@ -156,21 +156,24 @@ __global__ __launch_bounds__(1024) void embedding_sort_kernel(int rows, int voca
     __shared__ uint2 s[2][SORT_RUN / 2];
     if ((int)blockIdx.x >= runs) {
         const size_t step = (size_t)(gridDim.x - runs) * 1024, first = (size_t)(blockIdx.x - runs) * 1024 + threadIdx.x;
-        if (!add) {
-            const size_t head = min(n, (size_t)((16 - (reinterpret_cast<uintptr_t>(dw) & 15)) & 15) / 2), n8 = (n - head) / 8;
-            u32x4e*      q    = reinterpret_cast<u32x4e*>(dw + head);
-            for (size_t i = first; i < n8; i += step) q[i] = u32x4e{0u, 0u, 0u, 0u};
-            if (first < head) dw[first] = 0;
-            if (first < n - head - n8 * 8) dw[head + n8 * 8 + first] = 0;
-        } else {
-            bool bad = false;
-            for (size_t i = first; i < n; i += step) {
-                const uint16_t x = add[i];
-                bad |= half_nonfinite(x);
-                dw[i] = x;
-            }
-            if (st && __any(bad) && (threadIdx.x & 63) == 0) atomicOr(&st->found_inf, 1);
+        const size_t head = min(n, (size_t)((16 - (reinterpret_cast<uintptr_t>(dw) & 15)) & 15) / 2), n8 = (n - head) / 8;
+        u32x4e*      q    = reinterpret_cast<u32x4e*>(dw + head);
+        bool         bad  = false;
+        const auto   one  = [&](size_t i) {
+            const uint16_t x = add ? add[i] : 0;
+            bad |= half_nonfinite(x);
+            dw[i] = x;
+        };
+        for (size_t i = first; i < n8; i += step) {
+            u32x4e x = {0u, 0u, 0u, 0u};
+            if (add) x = *reinterpret_cast<const u32x4e_any*>(add + head + 8 * i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) bad |= half_nonfinite((uint16_t)x[k]) || half_nonfinite((uint16_t)(x[k] >> 16));
+            q[i] = x;
         }
+        if (first < head) one(first);
+        if (first < n - head - n8 * 8) one(head + n8 * 8 + first);
+        if (add && st && __any(bad) && (threadIdx.x & 63) == 0) atomicOr(&st->found_inf, 1);
         return;
     }
     // A thread has two neighbours.  Distances up to 64 lie in a wave and take no LDS; the ten larger ones go through it, from one half
@@ -444,6 +447,7 @@ extern "C" int mp_embedding_fwd(int rows, int vocab, int d, const int32_t* token
     if (rc) return rc;
     if (rows == 0) return MP_OK;
     MP_REQUIRE(tokens && w && y, "mp_embedding_fwd: NULL argument");
+    MP_REQUIRE(((reinterpret_cast<uintptr_t>(w) | reinterpret_cast<uintptr_t>(y)) & 1) == 0, "mp_embedding_fwd: w or y is not element-aligned");
     const int       pieces = pieces_of(d);
     const long long wgs    = ((long long)rows * pieces + EMB_THREADS - 1) / EMB_THREADS;
     MP_REQUIRE(wgs < (1ll << 31), "mp_embedding_fwd: too many rows and columns");
@@ -463,6 +467,8 @@ extern "C" int mp_embedding_bwd(int rows, int vocab, int d, const int32_t* token
     int rc = embedding_check("mp_embedding_bwd", rows, vocab, d);
     if (rc) return rc;
     MP_REQUIRE(dw && (rows == 0 || (tokens && dy)), "mp_embedding_bwd: NULL argument");
+    MP_REQUIRE(((reinterpret_cast<uintptr_t>(dy) | reinterpret_cast<uintptr_t>(add) | reinterpret_cast<uintptr_t>(dw)) & 1) == 0,
+               "mp_embedding_bwd: dy, add or dw is not element-aligned");
     if (rows > (1 << 24) || vocab >= (1 << (32 - SORT_BITS))) {
         set_error("mp_embedding_bwd: more than 2^24 rows or a vocabulary of 2^21 or more (%d, %d)", rows, vocab);
         return MP_E_UNSUPPORTED;

@@ -729,6 +729,11 @@ static int check_desc(const char* who, const mp_attn_desc* d) {
     MP_REQUIRE(d->n_heads % d->n_kv_heads == 0, "%s: %d heads do not share %d key / value heads evenly", who, d->n_heads, d->n_kv_heads);
     MP_REQUIRE(d->alpha > 0.f && d->alpha < INFINITY && d->cap >= 0.f && d->cap < INFINITY, "%s: alpha must be positive and cap not negative", who);
     MP_REQUIRE(d->reserved == 0, "%s: reserved is not 0", who);
+    // (tanh is good to 2^-22 in absolute terms, which a larger cap would make errors of a score that fp16 shows)
+    if (d->cap > 0.f && (d->cap > 1024.f || !(d->alpha / d->cap < 1e30f))) {
+        set_error("%s: cap %g above 1024 or too small for alpha %g", who, (double)d->cap, (double)d->alpha);
+        return MP_E_UNSUPPORTED;
+    }
     if (d->d_head > 128 || (d->d_head & 7)) {
         set_error("%s: head size %d is not a multiple of 8 up to 128", who, d->d_head);
         return MP_E_UNSUPPORTED;

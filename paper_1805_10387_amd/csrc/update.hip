@@ -399,7 +399,9 @@ __device__ __forceinline__ void update_share(const UpdBatch8& b, const UpdScalar
             m[k]          = s.beta1 * m[k] + s.omb1 * gk;
             const float v = s.beta2 * (r[k] * r[k]) + s.omb2 * (gk * gk);
             r[k]          = sqrtf(v);
-            w[k]          = w[k] - (rate * m[k]) * __builtin_amdgcn_rcpf(r[k] * rbc2 + s.eps);   // (an ulp of the step)
+            const float by = r[k] * rbc2 + s.eps;
+            // (an ulp of the step; the instruction takes subnormals for 0, which only an eps that is one would be felt by)
+            w[k] = w[k] - (by < 0x1p-120f ? rate * m[k] / by : rate * m[k] * __builtin_amdgcn_rcpf(by));
             mtop          = fmaxf(mtop, fabsf(m[k]));
             rtop          = fmaxf(rtop, r[k]);
         }

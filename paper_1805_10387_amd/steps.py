@@ -263,14 +263,14 @@ class TransformerStep(_StepBase):
         need.append(B.mp_layernorm_bwd_workspace_bytes(T, d))
         if self.masked:
             self.d_att = B.attn_desc(T, T, h, h, dk, ld_q=3 * d, ld_k=3 * d, ld_v=3 * d, alpha=alpha)
-            self.mask = torch.empty(B.mp_attention_mask_bytes(T) // 4, dtype=torch.int32, device="cuda")
+            self.mask = torch.zeros(B.mp_attention_mask_bytes(T) // 4, dtype=torch.int32, device="cuda")
             self.n_docs = wl.n_docs or NB
             self.doc_start = torch.arange(0, T + 1, S, dtype=torch.int32, device="cuda")
             need.append(B.mp_attention_masked_bwd_workspace_bytes(self.d_att))
         else:
             need += [B.mp_gemm_bwd_dw_workspace_bytes(self.d_s, False), B.mp_gemm_bwd_dw_workspace_bytes(self.d_c, False)]
         if wl.vocab:
-            self.tokens, self.emb_scale = torch.empty(T, dtype=torch.int32, device="cuda"), math.sqrt(d)
+            self.tokens, self.emb_scale = torch.zeros(T, dtype=torch.int32, device="cuda"), math.sqrt(d)
             need.append(B.mp_embedding_bwd_workspace_bytes(T, wl.vocab, d))
         self._alloc_ws(max(need), B.mp_loss_workspace_bytes(T, d))
         self.ws_side = torch.empty_like(self.ws)

@@ -85,6 +85,33 @@ def test_many_tokens_and_words(rows, vocab):
     check(rows, vocab, 1, "same")
 
 
+@pytest.mark.parametrize("rows", [7, 8, 9, 15, 16, 17, 127, 129, 257, 511, 1025])
+@pytest.mark.parametrize("kind,d,skew", [("same", 9, 1), ("zipf", 17, 0), ("pads", 8, 3)])
+def test_pieces_and_parts(rows, kind, d, skew):
+    check(rows, 13, d, kind, add=True, skew=skew)
+
+
+def test_three_rounds_of_merging():
+    check(2048 * 32 * 32 + 5000, 50000, 3, "zipf")
+
+
+@pytest.mark.parametrize("other", [0, 3])
+def test_the_second_gradient_where_there_is_no_token(other):
+    """It is copied, whatever its alignment beside dw's, and its infinities are reported."""
+    vocab, d = 700, 19
+    second = S16(np.random.default_rng(other).standard_normal((vocab, d)))
+    for bad in (None, 0, vocab * d - 1, 5000):
+        if bad is not None:
+            second.reshape(-1)[bad] = -np.inf
+        st = mp.scale_state_alloc()
+        mp.mp_scale_state_init(st, ML.MP_SCALE_BACKOFF, 1.0, 3)
+        dw, ws = place(np.full((vocab, d), 7.0), 1), torch.empty(mp.mp_embedding_bwd_workspace_bytes(2, vocab, d), dtype=torch.uint8, device="cuda")
+        mp.mp_embedding_bwd(2, vocab, d, i32([-1, vocab]), place(np.ones((2, d)), 0), 1.0, dw, add=place(second, other), st=st, ws=ws)
+        assert np.array_equal(bits(dw), half_bits(second)) and mp.scale_state_read(st).found_inf == int(bad is not None)
+        if bad is not None:
+            second.reshape(-1)[bad] = 1
+
+
 def test_no_rows():
     dw, ws = torch.full((5, 8), 7.0, dtype=torch.float16, device="cuda"), torch.empty(1024, dtype=torch.uint8, device="cuda")
     mp.mp_embedding_bwd(0, 5, 8, None, None, 1.0, dw, ws=ws)

@@ -154,6 +154,11 @@ def test_head_sizes_and_scores(d, cap, bias):
     p.docs(documents(150, d, 40, front=3, back=9), causal=bool(d % 16)).run().check()
 
 
+@pytest.mark.parametrize("cap,spread", [(0.01, 1.0), (0.5, 8.0), (1024.0, 30.0)])
+def test_small_and_large_caps(cap, spread):
+    Problem(150, 2, 1, 64, seed=5, cap=cap, spread=spread).docs([0, 60, 150], causal=True).run().check()
+
+
 @pytest.mark.parametrize("heads,kv", [(1, 1), (5, 5), (6, 2), (8, 1), (16, 4)])
 def test_head_layouts(heads, kv):
     Problem(170, heads, kv, 64, seed=heads).docs([0, 100, 170], causal=True).run().check()

@@ -118,3 +118,13 @@ def test_structs_match_the_header():
     assert C.sizeof(ML.AttnDesc) == 64 and ML.AttnDesc.alpha.offset == 52 and C.sizeof(ML.TensorDesc8) == 64
     hdr = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "mp.h")).read()
     assert f"#define MP_STATE8_BLOCK {ML.MP_STATE8_BLOCK}\n" in hdr
+
+
+def test_embedding_and_cap_at_their_ends():
+    f, b = lib.mp_embedding_fwd, lib.mp_embedding_bwd
+    assert f(4, 5, 8, A, A + 1, 1.0, A, None) == f(4, 5, 8, A, A, 1.0, A + 3, None) == ML.MP_E_INVAL
+    assert b(4, 5, 8, A, A + 1, 1.0, None, A, None, A, 1 << 40, None) == b(4, 5, 8, A, A, 1.0, A + 1, A, None, A, 1 << 40, None) == ML.MP_E_INVAL
+    for kw in (dict(cap=1025.0), dict(cap=1e-38, alpha=1.0), dict(cap=float("inf"))):
+        d = desc(**kw)
+        assert lib.mp_attention_masked_fwd(C.byref(d), A, A, A, A, None, A, A, None) in (ML.MP_E_UNSUPPORTED, ML.MP_E_INVAL)
+        assert lib.mp_attention_masked_bwd_workspace_bytes(C.byref(d)) == 0
