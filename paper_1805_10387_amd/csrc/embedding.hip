@@ -4,7 +4,7 @@
 // per token and writes the whole table's gradient.  Gradient rows of one token are summed in fp32 in the order of their positions:
 //   1. sort    runs of SORT_RUN tokens in LDS (value, then position: one 32-bit key); the other workgroups of the launch clear dw
 //   2. merge   up to MERGE_RUNS runs into one, each key's place by binary searches (not for a single run)
-//   3. sum     EMB_CHUNK sorted positions a group of lanes, however they are spread over tokens: a token's sum that lies inside a
+//   3. sum     a chunk of sorted positions a group of lanes, however they are spread over tokens: a token's sum that lies inside a
 //              chunk is stored, one that crosses a border is left as partial sums
 //   4. join    partial sums, in the order of the chunks
 // so that neither a token that is every second one nor one that comes once costs more than its rows, without an atomic addition.
@@ -19,7 +19,7 @@ constexpr int EMB_THREADS = 256;
 constexpr int SORT_RUN    = 2048;   // 11 bits of position beside 21 bits of token
 constexpr int SORT_BITS   = 11;
 constexpr int MERGE_RUNS  = 32;
-constexpr int EMB_CHUNK   = 8;
+constexpr int EMB_BATCH   = 8;
 constexpr int FILL_WGS    = 2048;
 
 // The product rounded to fp32 before it is rounded to fp16: the compiler else makes one instruction of the two in some places,
@@ -318,52 +318,59 @@ __device__ __forceinline__ void store_part(float* o, const Part& s) {
     *reinterpret_cast<f32x4_word*>(o + 4) = f32x4{s.x[4], s.x[5], s.x[6], s.x[7]};
 }
 
-// All of a chunk's keys, then all of its rows, are on their way at once: two trips to memory.  Then they pass through the first registers
-// one by one: a loop whose code were there for each of them would come from memory too, which a small call waits for.
+// A chunk is some batches of 8 positions.  All rows of a batch are on their way at once, with the keys of the next.  Then they pass through
+// the first registers one by one: a loop whose code were there for each of them would come from memory too, which a small call waits for.
 template <bool TINY>
-__global__ __launch_bounds__(EMB_THREADS) void embedding_sum_kernel(int rows, int vocab, int d, int pieces, int pitch, const u64* __restrict__ keys,
-                                                                    const uint16_t* __restrict__ dy, float scale, const uint16_t* add, uint16_t* dw,
-                                                                    float* __restrict__ part, mp_scale_state* st) {
+__global__ __launch_bounds__(EMB_THREADS) void embedding_sum_kernel(int rows, int vocab, int d, int pieces, int pitch, int chunk,
+                                                                    const u64* __restrict__ keys, const uint16_t* __restrict__ dy, float scale,
+                                                                    const uint16_t* add, uint16_t* dw, float* __restrict__ part, mp_scale_state* st) {
     const Piece     at(d, pieces);
-    const long long p0 = at.row * EMB_CHUNK, p1 = min((long long)rows, p0 + EMB_CHUNK);
+    const long long p0 = at.row * chunk, p1 = min((long long)rows, p0 + chunk);
     bool            bad = false;
     if (p0 < rows) {
-        unsigned       token[EMB_CHUNK + 1];
-        Words          x[EMB_CHUNK];
-        const unsigned before = p0 > 0 ? token_of(keys[p0 - 1]) : ~0u;
-        token[EMB_CHUNK]      = p1 < rows ? token_of(keys[p1]) : ~0u;
-        u64 key[EMB_CHUNK];
+        const unsigned before = p0 > 0 ? token_of(keys[p0 - 1]) : ~0u, behind = p1 < rows ? token_of(keys[p1]) : ~0u;
+        u64            key[EMB_BATCH];
+        const auto     ask = [&](long long p) {
 #pragma unroll
-        for (int j = 0; j < EMB_CHUNK; ++j) key[j] = p0 + j < p1 ? keys[p0 + j] : ~0ull;
-#pragma unroll
-        for (int j = 0; j < EMB_CHUNK; ++j) {
-            token[j] = token_of(key[j]);
-            // (a token outside the table is the last one; what is loaded for it is not used)
-            x[j] = load_piece<TINY>(dy + (token[j] < (unsigned)vocab ? (long long)(unsigned)key[j] * d : 0) + at.col, at);
-        }
+            for (int j = 0; j < EMB_BATCH; ++j) key[j] = p + j < p1 ? keys[p + j] : ~0ull;
+        };
+        ask(p0);
         Part sum;
-        bool whole = token[0] != before;  // whether the open sum began in this chunk
+        bool whole = token_of(key[0]) != before;  // whether the open sum began in this chunk
         sum.zero();
 #pragma unroll 1
-        for (int j = 0; j < EMB_CHUNK; ++j) {
-            const unsigned t = token[0];
-            if (t >= (unsigned)vocab) break;
-            Part one;
-            one.set(x[0]);
+        for (long long p = p0; p < p1; p += EMB_BATCH) {
+            unsigned token[EMB_BATCH + 1];
+            Words    x[EMB_BATCH];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum.x[k] += one.x[k];
-            if (token[1] != t) {
-                if (whole) bad |= finish_row<TINY>(sum, scale, dw + (long long)t * d + at.col, add ? add + (long long)t * d + at.col : nullptr, at);
-                else store_part(part + at.row * 2 * pitch + at.col, sum);
-                sum.zero();
-                whole = true;
-            } else if (j == EMB_CHUNK - 1) {
-                store_part(part + (at.row * 2 + (whole ? 1 : 0)) * pitch + at.col, sum);
+            for (int j = 0; j < EMB_BATCH; ++j) {
+                token[j] = token_of(key[j]);
+                // (a token outside the table is the last one; what is loaded for it is not used)
+                x[j] = load_piece<TINY>(dy + (token[j] < (unsigned)vocab ? (long long)(unsigned)key[j] * d : 0) + at.col, at);
             }
+            ask(p + EMB_BATCH);
+            token[EMB_BATCH] = p + EMB_BATCH < p1 ? token_of(key[0]) : behind;
+#pragma unroll 1
+            for (int j = 0; j < EMB_BATCH; ++j) {
+                const unsigned t = token[0];
+                if (t >= (unsigned)vocab) break;
+                Part one;
+                one.set(x[0]);
 #pragma unroll
-            for (int i = 0; i < EMB_CHUNK; ++i) token[i] = token[i + 1];
+                for (int k = 0; k < 8; ++k) sum.x[k] += one.x[k];
+                if (token[1] != t) {
+                    if (whole) bad |= finish_row<TINY>(sum, scale, dw + (long long)t * d + at.col, add ? add + (long long)t * d + at.col : nullptr, at);
+                    else store_part(part + at.row * 2 * pitch + at.col, sum);
+                    sum.zero();
+                    whole = true;
+                } else if (p + j + 1 == p1) {
+                    store_part(part + (at.row * 2 + (whole ? 1 : 0)) * pitch + at.col, sum);
+                }
 #pragma unroll
-            for (int i = 0; i + 1 < EMB_CHUNK; ++i) x[i] = x[i + 1];
+                for (int i = 0; i < EMB_BATCH; ++i) token[i] = token[i + 1];
+#pragma unroll
+                for (int i = 0; i + 1 < EMB_BATCH; ++i) x[i] = x[i + 1];
+            }
         }
     }
     if (st && __any(bad) && (threadIdx.x & 63) == 0) atomicOr(&st->found_inf, 1);
@@ -373,11 +380,11 @@ __global__ __launch_bounds__(EMB_THREADS) void embedding_sum_kernel(int rows, in
 // they are still its own.
 constexpr int JOIN_AHEAD = 16;
 template <bool TINY>
-__global__ __launch_bounds__(EMB_THREADS) void embedding_join_kernel(int rows, int vocab, int d, int pieces, int pitch, const u64* __restrict__ keys,
+__global__ __launch_bounds__(EMB_THREADS) void embedding_join_kernel(int rows, int vocab, int d, int pieces, int pitch, int chunk, const u64* __restrict__ keys,
                                                                      float scale, const uint16_t* add, uint16_t* dw, const float* __restrict__ part,
                                                                      mp_scale_state* st) {
     const Piece     at(d, pieces);
-    const long long p0 = at.row * EMB_CHUNK, p1 = p0 + EMB_CHUNK;
+    const long long p0 = at.row * chunk, p1 = p0 + chunk;
     bool            bad = false;
     if (p1 < rows) {
         const unsigned t = token_of(keys[p1 - 1]), first = token_of(keys[p0]), behind = token_of(keys[p1]),
@@ -387,7 +394,7 @@ __global__ __launch_bounds__(EMB_THREADS) void embedding_join_kernel(int rows, i
             const float* o = part + (at.row * 2 + 1) * pitch + at.col;
 #pragma unroll
             for (int k = 0; k < 8; ++k) sum.x[k] = o[k];
-            const long long chunks = ((long long)rows + EMB_CHUNK - 1) / EMB_CHUNK;
+            const long long chunks = ((long long)rows + chunk - 1) / chunk;
             bool            more   = true;
             for (long long c = at.row + 1; more; c += JOIN_AHEAD) {
                 f32x4    x[JOIN_AHEAD][2];
@@ -395,7 +402,7 @@ __global__ __launch_bounds__(EMB_THREADS) void embedding_join_kernel(int rows, i
 #pragma unroll
                 for (int i = 0; i < JOIN_AHEAD; ++i) {
                     const long long j = min(c + i, chunks - 1);
-                    next[i]           = (c + i + 1) * EMB_CHUNK < rows ? token_of(keys[(c + i + 1) * EMB_CHUNK]) : ~0u;
+                    next[i]           = (c + i + 1) * chunk < rows ? token_of(keys[(c + i + 1) * chunk]) : ~0u;
                     x[i][0]           = *reinterpret_cast<const f32x4_word*>(part + j * 2 * pitch + at.col);
                     x[i][1]           = *reinterpret_cast<const f32x4_word*>(part + j * 2 * pitch + at.col + 4);
                 }
@@ -413,22 +420,29 @@ __global__ __launch_bounds__(EMB_THREADS) void embedding_join_kernel(int rows, i
 }
 
 static size_t keys_bytes(int rows) { return ((size_t)rows * sizeof(u64) + 255) / 256 * 256; }
-static long long chunks_of(int rows) { return ((long long)rows + EMB_CHUNK - 1) / EMB_CHUNK; }
-
 static int pieces_of(int d) { return (int)(((long long)d + 7) / 8); }
 static int pitch_of(int d) { return d < 8 ? 8 : d; }
+// Sorted positions of a chunk: more of them, up to 64, as long as there are 2^17 threads.  Long chunks leave fewer partial sums; with few
+// threads they leave memory waiting.  Gradients, words by Zipf's law: 65536 rows of 1024 of 50021 words 138 us in chunks of 8, 101 so
+// (of 32); 262144 rows 493 us, 278 so (of 64); 16384 rows of 32768 words 52 us in chunks of 8, 47 so (of 16), 53 with chunks for half the threads.
+static int chunk_of(int rows, int d) {
+    int chunk = EMB_BATCH;
+    while (chunk < 64 && (long long)rows / (2 * chunk) * pieces_of(d) >= (1 << 17)) chunk *= 2;
+    return chunk;
+}
+static long long chunks_of(int rows, int d) { return ((long long)rows + chunk_of(rows, d) - 1) / chunk_of(rows, d); }
 
 static int launch_sums(int rows, int vocab, int d, const u64* keys, const mp_half* dy, float scale, const mp_half* add, mp_half* dw, float* part,
                        mp_scale_state* st, hipStream_t hs) {
     const int       pieces = pieces_of(d);
-    const long long wgs    = (chunks_of(rows) * pieces + EMB_THREADS - 1) / EMB_THREADS;
+    const long long wgs    = (chunks_of(rows, d) * pieces + EMB_THREADS - 1) / EMB_THREADS;
     MP_REQUIRE(wgs < (1ll << 31), "mp_embedding_bwd: too many rows and columns");
     const dim3 grid((unsigned)wgs), block(EMB_THREADS);
     const auto sums = d < 8 ? embedding_sum_kernel<true> : embedding_sum_kernel<false>;
     const auto join = d < 8 ? embedding_join_kernel<true> : embedding_join_kernel<false>;
-    hipLaunchKernelGGL(sums, grid, block, 0, hs, rows, vocab, d, pieces, pitch_of(d), keys, dy, scale, add, dw, part, st);
+    hipLaunchKernelGGL(sums, grid, block, 0, hs, rows, vocab, d, pieces, pitch_of(d), chunk_of(rows, d), keys, dy, scale, add, dw, part, st);
     MP_LAUNCH_CHECK("mp_embedding_bwd(sum)");
-    hipLaunchKernelGGL(join, grid, block, 0, hs, rows, vocab, d, pieces, pitch_of(d), keys, scale, add, dw, part, st);
+    hipLaunchKernelGGL(join, grid, block, 0, hs, rows, vocab, d, pieces, pitch_of(d), chunk_of(rows, d), keys, scale, add, dw, part, st);
     MP_LAUNCH_CHECK("mp_embedding_bwd(join)");
     return MP_OK;
 }
@@ -459,7 +473,7 @@ extern "C" int mp_embedding_fwd(int rows, int vocab, int d, const int32_t* token
 
 extern "C" size_t mp_embedding_bwd_workspace_bytes(int rows, int vocab, int d) {
     if (rows < 0 || vocab <= 0 || d <= 0) return 0;
-    return 2 * keys_bytes(rows) + (size_t)chunks_of(rows) * 2 * pitch_of(d) * sizeof(float) + 256;
+    return 2 * keys_bytes(rows) + (size_t)chunks_of(rows, d) * 2 * pitch_of(d) * sizeof(float) + 256;
 }
 
 extern "C" int mp_embedding_bwd(int rows, int vocab, int d, const int32_t* tokens, const mp_half* dy, float scale, const mp_half* add, mp_half* dw,

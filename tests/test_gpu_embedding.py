@@ -91,6 +91,34 @@ def test_pieces_and_parts(rows, kind, d, skew):
     check(rows, 13, d, kind, add=True, skew=skew)
 
 
+@pytest.mark.parametrize("rows,d", [(20000, 840), (70000, 500), (100003, 672), (140000, 1027)])
+@pytest.mark.parametrize("kind", ["zipf", "pads", "same"])
+def test_long_chunks(rows, d, kind):
+    """Chunks of 16, 32, 64 positions (more rows and columns than the oracle is quick for: the sums in 64 bits on the device)."""
+    vocab, r = 3001, np.random.default_rng(rows)
+    tok = torch.from_numpy(tokens_of(kind, rows, vocab, r).astype(np.int32)).cuda()
+    dy = torch.randn(rows, d, device="cuda", generator=torch.Generator("cuda").manual_seed(rows)).half()
+    dw, ws = empty16(vocab, d), torch.empty(mp.mp_embedding_bwd_workspace_bytes(rows, vocab, d), dtype=torch.uint8, device="cuda")
+    mp.mp_embedding_bwd(rows, vocab, d, tok, dy, 0.5, dw, ws=ws)
+    ok = (tok >= 0) & (tok < vocab)
+    at, x = tok[ok].long(), 0.5 * dy[ok].double()
+    order = torch.argsort(at, stable=True)
+    count = torch.bincount(at, minlength=vocab)
+    end = torch.cumsum(count, 0)
+
+    def sums(v):
+        out = torch.zeros(vocab, *v.shape[1:], dtype=torch.float64, device="cuda")
+        for t in torch.nonzero(count > 50).flatten().tolist():          # (adding these one by one takes a second)
+            out[t] = v[order[end[t] - count[t]:end[t]]].sum(0)
+        few = count[at] <= 50
+        return out.index_add_(0, at[few], v[few])
+    ref, mag, n = sums(x), sums(x.abs()), sums(torch.ones(at.numel(), dtype=torch.float64, device="cuda"))
+    assert torch.all((dw.double() - ref).abs() <= 2.0 ** -11 * ref.abs() + (n[:, None] + 2) * 2.0 ** -24 * mag + 2.0 ** -25)
+    again = torch.empty_like(dw)
+    mp.mp_embedding_bwd(rows, vocab, d, tok, dy, 0.5, again, ws=ws)
+    assert torch.equal(again, dw)
+
+
 def test_three_rounds_of_merging():
     check(2048 * 32 * 32 + 5000, 50000, 3, "zipf")
 
