@@ -7,6 +7,13 @@
 // tile of keys for dk and dv, so that every gradient has one owner and no atomics (7 products instead of the 5 that one pass
 // with atomics would take).
 //
+// Bound: the matrix cores and the vector work of the scores beside them for long rows; for short ones the chain of a workgroup's start
+// (range, first tiles, first product: a kernel whose workgroups have one tile takes 5.5 us).  8 heads of 128 over 2, 12289 causal
+// rows: forward 360 us (0.86 PFLOP/s of the 1.19 that a library product of 8192^3 reaches here), dq 511 us (0.91), dk and dv 810 us
+// (0.76).  16 heads of 64, 8192 rows in 15 documents: 49, 59 and 78 us (0.26 PFLOP/s of what is visible, to which the tiles add 16 %).
+// 32 x 32 tiles of 16 deep are the widest matrix instructions; 128 rows of own, 64 of the other side, and fragments of tiles in LDS
+// (filled by loads that pass the registers by, one tile ahead) keep the operands of two tiles and the results in 256 registers.
+//
 // Masks: query r sees keys [lo, hi).  Whether a tile of pairs is empty, whole or neither follows from four numbers of a 64-row tile
 // (least lo, greatest hi, greatest lo, least hi) that the mask keeps behind the rows' own; only tiles that are neither look at
 // single pairs.
@@ -22,7 +29,7 @@
 
 namespace mp {
 
-constexpr int   MA_THREADS = 256;
+constexpr int   JOIN_THREADS = 256;
 constexpr int   MA_Q       = 128;   // queries of a workgroup, 32 a wave (dk/dv: keys)
 constexpr int   MA_K       = 64;    // keys of a tile (dk/dv: queries)
 constexpr float LOG2E      = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -55,10 +62,17 @@ __global__ __launch_bounds__(64) void mask_kernel(int rows, int rows_k, int n_do
             lo = max(los[r], 0);
             hi = min(his[r], rows_k);
         } else if (n_docs > 0 && r >= start[0] && r < start[n_docs]) {
-            int a = 0, b = n_docs;  // start[a] <= r < start[b]
+            int a = 0, b = n_docs;  // start[a] <= r < start[b]; seven places a trip to memory
             while (b - a > 1) {
-                const int c = (a + b) >> 1;
-                if (start[c] <= r) a = c; else b = c;
+                const int part = (b - a + 7) / 8;
+                int       last = a;
+#pragma unroll
+                for (int i = 1; i < 8; ++i) {
+                    const int c = min(a + part * i, b);
+                    if (start[c] <= r) last = c;
+                }
+                b = min(last + part, b);
+                a = last;
             }
             const int s = max(start[a], 0), e = min(start[b], rows);
             lo = s;
@@ -71,7 +85,7 @@ __global__ __launch_bounds__(64) void mask_kernel(int rows, int rows_k, int n_do
         }
         if (lo >= hi) lo = hi = 0;
     }
-    range[r]        = make_int2(lo, hi);  // (of the last 64 rows all)
+    range[r]        = make_int2(lo, hi);  // (rows up to the next multiple of 64 too)
     const bool some = lo < hi;
     int        a = some ? lo : INT_MAX, b = some ? hi : 0, c = some ? lo : INT_MAX, d = some ? hi : 0;
 #pragma unroll
@@ -503,35 +517,39 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void masked_dq_kernel(AttnArgs a) {
 }
 
 // dk and dv of 128 keys, 32 of them a wave, over the tiles of 64 queries that see any of them, head by head: of all heads that share
-// the keys, or (PART) of a.part_heads of them, whose sums the join kernel adds up.
-template <int D, int MODE>
-__global__ __launch_bounds__(MA_THREADS, D <= 64 ? 2 : 1) void masked_dkv_kernel(AttnArgs a) {
-    constexpr int KK = D / 16, DT = D / 32, ROWB = D <= 64 ? 128 : 256;
+// the keys, or of a.part_heads of them, whose sums the join kernel adds up.  Teams as above, each with every SPLITth tile.
+template <int D, int MODE, int SPLIT>
+__global__ __launch_bounds__(256 * SPLIT, D <= 64 ? 2 : 1) void masked_dkv_kernel(AttnArgs a) {
+    constexpr int      KK = D / 16, DT = D / 32, ROWB = D <= 64 ? 128 : 256;
+    constexpr unsigned SIZE = MA_K * ROWB;
     typedef TileLoad<ROWB, 4> Load;
     typedef LdsTile<ROWB>     Tile;
     struct Stats {
         float lse2[MA_K], delta[MA_K];
         int2  range[2 * MA_K];  // (a wave's load is twice as long)
     };
-    __shared__ __align__(256) char Qs[2][MA_K * ROWB], Gs[2][MA_K * ROWB];
-    __shared__ __align__(16) Stats stats[2];
+    __shared__ __align__(256) char tiles_of[SPLIT][2][2][SIZE];  // queries, gradients of two tiles
+    __shared__ __align__(16) Stats stats_of[SPLIT][2];
 
     const int kv_heads = a.heads / a.group, parts = a.group / a.part_heads, per = kv_heads * parts;
     const int id = blockIdx.x % per, kvh = id / parts, h0 = kvh * a.group + id % parts * a.part_heads, kt = blockIdx.x / per;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hf = lane >> 5;
+    const int lane = threadIdx.x & 63, wave8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = wave8 & 3, team = wave8 >> 2, hf = lane >> 5;
+    Stats* const stats = stats_of[team];
     const int k0 = kt * MA_Q, n0 = k0 + 32 * wave, n = n0 + (lane & 31);
     const int qtiles = a.rows_pad / MA_K;
 
     // the tiles to come, one by one
+    const int          end = h0 + a.part_heads;
     int                h = h0, base = -64, q0 = 0;
     int4               bounds = make_int4(0, 0, 0, 0), t4 = bounds;
     unsigned long long todo = 0;
     const auto         advance = [&]() {
         while (todo == 0) {
+            if (h == end) return false;  // (asked again behind the end: no more either)
             base += 64;
             if (base >= qtiles) {
                 base = 0;
-                if (++h >= h0 + a.part_heads) return false;
+                if (++h == end) return false;
             }
             bounds = base + lane < qtiles ? a.tile[base + lane] : make_int4(INT_MAX, 0, INT_MAX, 0);
             todo   = __ballot(bounds.x < k0 + MA_Q && bounds.y > k0);  // (the same in every wave)
@@ -543,19 +561,36 @@ __global__ __launch_bounds__(MA_THREADS, D <= 64 ? 2 : 1) void masked_dkv_kernel
                        __builtin_amdgcn_readlane(bounds.w, i));
         return true;
     };
+    // a step: one tile for each team
+    struct Step {
+        int  q0, h;
+        int4 t;
+        bool mine, whole;  // whether this team has a tile; whether all keys are seen whole in every team's
+    };
+    const auto take = [&](Step& x) {
+        x.mine = false, x.whole = true;
+        for (int i = 0; i < SPLIT; ++i) {
+            if (!advance()) return i > 0;
+            x.whole = x.whole && t4.z <= k0 && t4.w >= k0 + MA_Q;
+            if (i == team) x.mine = true, x.q0 = q0, x.h = h, x.t = t4;
+        }
+        return true;
+    };
     Load lq, lg;
     lq.init(a.ld_q, a.d, wave, lane);
     lg.init(a.ld_dctx, a.d, wave, lane);
-    const auto issue = [&](int b) {
-        lq.issue(a.q + h * a.d, a.ld_q, q0, a.rows_q, a.d, Qs[b], wave);
-        lg.issue(a.dctx + h * a.d, a.ld_dctx, q0, a.rows_q, a.d, Gs[b], wave);
-        const long long at = (long long)h * a.rows_pad + q0;
+    const auto issue = [&](int b, const Step& x) {
+        if (!x.mine) return;
+        lq.issue(a.q + x.h * a.d, a.ld_q, x.q0, a.rows_q, a.d, tiles_of[team][b][0], wave);
+        lg.issue(a.dctx + x.h * a.d, a.ld_dctx, x.q0, a.rows_q, a.d, tiles_of[team][b][1], wave);
+        const long long at = (long long)x.h * a.rows_pad + x.q0;
         if (wave == 0) load_words(a.lse2 + at, stats[b].lse2, lane);
         if (wave == 1) load_words(a.delta + at, stats[b].delta, lane);
-        if (wave == 2) load_ranges(a.range + q0, stats[b].range, lane);
+        if (wave == 2) load_ranges(a.range + x.q0, stats[b].range, lane);
     };
-    bool more = advance();
-    if (more) issue(0);
+    Step now, next;
+    bool more = take(next);
+    if (more) issue(0, next);
     f16x8 kf[KK], vf[KK];
     row_frags<KK>(kf, n < a.rows_k ? a.k + (long long)n * a.ld_k + kvh * a.d : nullptr, a.d, hf);
     row_frags<KK>(vf, n < a.rows_k ? a.v + (long long)n * a.ld_v + kvh * a.d : nullptr, a.d, hf);
@@ -566,24 +601,26 @@ __global__ __launch_bounds__(MA_THREADS, D <= 64 ? 2 : 1) void masked_dkv_kernel
     settle<KK>(vf);
     const float c = MODE ? 1.f : a.alpha * LOG2E;
 
-    const unsigned     at_q = lds_address(Qs) + Tile::plain(lane), at_g = lds_address(Gs) + Tile::plain(lane);
-    const unsigned     at_tq = lds_address(Qs) + Tile::across(lane), at_tg = lds_address(Gs) + Tile::across(lane);
-    constexpr unsigned SIZE = MA_K * ROWB;
-    bool               ever = false;  // (the other half of the wave has the other queries)
+    const unsigned at_q = lds_address(tiles_of[team][0][0]) + Tile::plain(lane), at_g = at_q + SIZE;
+    const unsigned at_tq = lds_address(tiles_of[team][0][0]) + Tile::across(lane), at_tg = at_tq + SIZE;
+    bool           ever = false;  // (the other half of the wave has the other queries)
     for (int b = 0; more; b ^= 1) {
-        const int  m0 = q0, head = h;
-        const int4 t  = t4;
+        now = next;
         arrive();
-        more = advance();
-        if (more) issue(b ^ 1);
-        if (!(t.z <= k0 && t.w >= k0 + MA_Q)) {
-            Load::clean(Qs[b], nullptr, wave, lane);
-            Load::clean(Gs[b], nullptr, wave, lane);
+        more = take(next);
+        if (more) issue(b ^ 1, next);
+        const int4 t = now.t;
+        if (!now.whole) {
+            if (now.mine && !(t.z <= k0 && t.w >= k0 + MA_Q)) {
+                Load::clean(tiles_of[team][b][0], nullptr, wave, lane);
+                Load::clean(tiles_of[team][b][1], nullptr, wave, lane);
+            }
             lds_barrier();
         }
-        if (t.x >= n0 + 32 || t.y <= n0) continue;
+        if (!now.mine || t.x >= n0 + 32 || t.y <= n0) continue;
+        const int m0 = now.q0, head = now.h;
         const float slope2 = MODE && a.slopes ? a.slopes[head] * LOG2E : 0.f;
-        const unsigned xq = at_q + b * SIZE, xg = at_g + b * SIZE, tq = at_tq + b * SIZE, tg = at_tg + b * SIZE;
+        const unsigned xq = at_q + b * 2 * SIZE, xg = at_g + b * 2 * SIZE, tq = at_tq + b * 2 * SIZE, tg = at_tg + b * 2 * SIZE;
         // which of this lane's 16 queries of each half see its key
         unsigned   seen[2] = {0xFFFFu, 0xFFFFu};
         const bool all     = t.z <= n0 && t.w >= n0 + 32;
@@ -683,6 +720,29 @@ __global__ __launch_bounds__(MA_THREADS, D <= 64 ? 2 : 1) void masked_dkv_kernel
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) dk[dt] = dv[dt] = zero16();
     }
+    if constexpr (SPLIT > 1) {  // the second team's sums to the first, through the tiles' LDS
+        static_assert(sizeof(tiles_of) >= 32 * DT * 256 * sizeof(float), "the sums fit");
+        float* const ex = reinterpret_cast<float*>(tiles_of) + (threadIdx.x & 255);
+        lds_barrier();
+        if (team == 1) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    ex[512 * (16 * dt + r)]       = dk[dt][r];
+                    ex[512 * (16 * dt + r) + 256] = dv[dt][r];
+                }
+        }
+        lds_barrier();
+        if (team == 1) return;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                dk[dt][r] += ex[512 * (16 * dt + r)];
+                dv[dt][r] += ex[512 * (16 * dt + r) + 256];
+            }
+    }
     if (a.part_heads == a.group) {
         const bool in = n < a.rows_k;
         store_rows<DT>(in ? a.dv + (long long)n * a.ld_dv + kvh * a.d : nullptr, dv, 1.f / P_SCALE, a.d, hf);
@@ -703,9 +763,9 @@ __global__ __launch_bounds__(MA_THREADS, D <= 64 ? 2 : 1) void masked_dkv_kernel
 }
 
 // Sums of the parts of a key / value head, in order: 4 columns a thread.
-__global__ __launch_bounds__(MA_THREADS) void masked_join_kernel(AttnArgs a) {
+__global__ __launch_bounds__(JOIN_THREADS) void masked_join_kernel(AttnArgs a) {
     const int       kv_heads = a.heads / a.group, parts = a.group / a.part_heads, per = a.d / 4;
-    const long long i = (long long)blockIdx.x * MA_THREADS + threadIdx.x, row = i / per / kv_heads;
+    const long long i = (long long)blockIdx.x * JOIN_THREADS + threadIdx.x, row = i / per / kv_heads;
     if (row >= a.rows_k) return;
     const int kvh = (int)(i / per % kv_heads), col = (int)(i % per) * 4;
     f32x4     dk = {0.f, 0.f, 0.f, 0.f}, dv = dk;
@@ -780,6 +840,21 @@ static AttnArgs attn_args(const mp_attn_desc* d, const void* mask, const float* 
         MA_CASES(32, kernel, threads, grid, a, __VA_ARGS__); MA_CASES(64, kernel, threads, grid, a, __VA_ARGS__);  \
         MA_CASES(96, kernel, threads, grid, a, __VA_ARGS__); MA_CASES(128, kernel, threads, grid, a, __VA_ARGS__); \
     }
+// the same where only the kernels of head sizes up to 64 exist
+#define MA_LAUNCH_64(kernel, threads, grid, a, ...)                                                                \
+    switch (((a).d + 31) / 32 * 4 + ((a).cap > 0.f ? CAP : 0) + ((a).slopes ? BIAS : 0)) {                          \
+        MA_CASES(32, kernel, threads, grid, a, __VA_ARGS__); MA_CASES(64, kernel, threads, grid, a, __VA_ARGS__);  \
+    }
+
+// Two teams a workgroup where there are fewer workgroups than these.  A compute unit takes two workgroups of one team or one of two, so
+// teams fill the chip with half as many; with more workgroups than that, one team each balances better (it has no join, and long
+// workgroups run beside short ones).  us with two teams / one.  Forward, every key seen, 8192 rows: heads of 128, 256 workgroups
+// 150 / 181, 512 330 / 302, 768 453 / 448, 1024 579 / 552; causal 776 353 / 487; heads of 64, 256 workgroups 100 / 130, 512 166 / 172;
+// 1024 of documents of about 500 rows 52 / 46.  (All calls of a size take one rule, so causal ones decide for 768.)  dq likewise: causal 776
+// workgroups of heads of 128, whole backward 1242 / 1350.  dk and dv, heads up to 64, whole backward, causal: 256 workgroups of one document
+// 118 / 138, of documents of 64 rows 38 / 41, 384 130 / 149, 512 of documents of 512 rows 59 / 54.  Heads above 64 need a wave's
+// full registers there, which leaves no room for a second team.
+constexpr long long ONE_TEAM = 1024, ONE_TEAM_DKV = 512;
 
 }  // namespace mp
 
@@ -829,7 +904,7 @@ extern "C" int mp_attention_masked_fwd(const mp_attn_desc* desc, const void* mas
     AttnArgs a = attn_args(desc, mask, slopes);
     a.q = q, a.k = k, a.v = v, a.out = ctx, a.lse = lse;
     const long long wgs = (long long)((desc->rows_q + MA_Q - 1) / MA_Q) * desc->n_heads;
-    if (wgs >= 1024)
+    if (wgs >= ONE_TEAM)
         MA_LAUNCH(masked_fwd_kernel, 256, wgs, a, as_stream(stream), 1)
     else
         MA_LAUNCH(masked_fwd_kernel, 512, wgs, a, as_stream(stream), 2)
@@ -838,7 +913,9 @@ extern "C" int mp_attention_masked_fwd(const mp_attn_desc* desc, const void* mas
 }
 
 // How many of the heads that share keys a workgroup of dk and dv takes: all of them where that gives every compute unit two workgroups
-// (their sums then stay in registers), else one, with sums in fp32 through memory.
+// (their sums then stay in registers), else one, with sums in fp32 through memory.  8 heads of 128 over 2, one document of 12289 rows
+// (194 workgroups or 776): 2.61 ms with all, 1.98 apart (when it was made; 0.81 with the steps that followed).  Parts of the queries instead, of 12
+// tiles or more, gained 13 % for one long document without shared keys and cost up to 26 % elsewhere: their sums go through memory.
 static int part_heads(const mp_attn_desc* d) {
     const int group = d->n_heads / d->n_kv_heads;
     return (long long)((d->rows_k + MA_Q - 1) / MA_Q) * d->n_kv_heads >= 512 ? group : 1;
@@ -884,18 +961,22 @@ extern "C" int mp_attention_masked_bwd(const mp_attn_desc* desc, const void* mas
     a.part_heads = part_heads(desc);
     if (d.rows_q > 0) {
         const long long wgs = (long long)((d.rows_q + MA_Q - 1) / MA_Q) * d.n_heads;
-        if (wgs >= 1024)
+        if (wgs >= ONE_TEAM)
             MA_LAUNCH(masked_dq_kernel, 256, wgs, a, hs, 1)
         else
             MA_LAUNCH(masked_dq_kernel, 512, wgs, a, hs, 2)
         MP_LAUNCH_CHECK(who);
     }
     if (d.rows_k > 0) {
-        MA_LAUNCH(masked_dkv_kernel, MA_THREADS, (long long)((d.rows_k + MA_Q - 1) / MA_Q) * (d.n_heads / a.part_heads), a, hs);
+        const long long wgs = (long long)((d.rows_k + MA_Q - 1) / MA_Q) * (d.n_heads / a.part_heads);
+        if (d.d_head > 64 || wgs >= ONE_TEAM_DKV)
+            MA_LAUNCH(masked_dkv_kernel, 256, wgs, a, hs, 1)
+        else
+            MA_LAUNCH_64(masked_dkv_kernel, 512, wgs, a, hs, 2)
         MP_LAUNCH_CHECK(who);
         if (a.part_heads < a.group) {
             const long long quads = (long long)d.rows_k * d.n_kv_heads * (d.d_head / 4);
-            hipLaunchKernelGGL(masked_join_kernel, dim3((unsigned)((quads + MA_THREADS - 1) / MA_THREADS)), dim3(MA_THREADS), 0, hs, a);
+            hipLaunchKernelGGL(masked_join_kernel, dim3((unsigned)((quads + JOIN_THREADS - 1) / JOIN_THREADS)), dim3(JOIN_THREADS), 0, hs, a);
             MP_LAUNCH_CHECK(who);
         }
     }

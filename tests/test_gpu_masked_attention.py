@@ -273,6 +273,25 @@ def test_captured_and_replayed_with_other_documents():
             assert torch.equal(v, q.results()[k]), (s, k)
 
 
+@pytest.mark.parametrize("rows,window", [(4224, 70), (4170, 0), (8193, 65)])
+def test_more_than_64_tiles_of_queries(rows, window):
+    """The tiles that see a key are found 64 at a time; their number is odd for some keys."""
+    start = [0, rows] if window else np.concatenate([np.arange(0, rows, 100), [rows]])
+    p = Problem(rows, 1, 1, 8, seed=rows).docs(start, causal=True, window=window).run()
+    q, k, v = (torch.from_numpy(np.asarray(x, np.float64)).cuda() for x in (p.q, p.k, p.v))
+    at = torch.arange(rows, device="cuda")
+    seen = (at[None] >= i32(p.lo)[:, None]) & (at[None] < i32(p.hi)[:, None])
+    prob = torch.softmax((p.alpha * q @ k.T).masked_fill(~seen, -np.inf), 1)
+    do = torch.from_numpy(np.asarray(p.do, np.float64)).cuda()
+    dp = do @ v.T
+    ds = prob * (dp - (prob * dp).sum(1, keepdim=True))
+    # (errors of a key's sums by the oracle's check: half a step of each of p, ds and of ctx in delta, all of the magnitudes' sums)
+    r = p.results()
+    for name, ref, mag in (("dk", p.alpha * ds.T @ q, p.alpha * (ds.abs() + prob * (do.abs() @ (prob @ v).abs().T).diagonal()[:, None]).T @ q.abs()),
+                           ("dv", prob.T @ do, prob.T @ do.abs())):
+        assert torch.all((r[name].double() - ref).abs() <= 2.0 ** -9 * mag + 2.0 ** -11 * ref.abs() + 2.0 ** -20), name
+
+
 def test_offsets_beyond_32_bits():
     """Rows so far apart that elements lie beyond 2^31: the first and last rows of a long matrix against the same rows packed."""
     rows, ld = 40000, 65536                       # 2.6e9 elements
