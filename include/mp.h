@@ -442,8 +442,8 @@ typedef struct mp_attn_desc {
 /*     t = alpha q k^T;   s = cap tanh(t / cap)  (cap > 0), else t;   s -= slopes[h] |r - c|  (slopes given)
  *     p = softmax_fp32 of s over the keys that the row sees;   ctx = RNE16(p v);   lse = log(sum exp(s))
  * slopes: device fp32 [n_heads] or NULL.  lse: device fp32 [n_heads, rows_q], kept for the backward call.  A row that sees nothing
- * has ctx 0 and lse -inf.  Scores stay fp32; the exponentials enter the second product rounded to fp16, unnormalised (none is
- * above 1, the row's largest is 1).
+ * has ctx 0 and lse -inf.  Scores stay fp32; the exponentials enter the second product rounded to fp16, unnormalised (relative to a
+ * maximum that may lag by a factor of 2^8: none is above that, the row's largest not below 1).
  * What a row does not see does not reach it, NaN and infinities included; of a value row that holds one, those rows that see it get
  * non-finite results.  All rows of ctx are written.  Any rows_k >= 0 and rows_q >= 0.
  * `mask` is one of rows_q rows.  16-byte aligned matrices with leading dimensions, a d_head and a cap as above; otherwise

@@ -2,14 +2,15 @@
 //
 // Both are bound by HBM: forward reads a table row per token (or finds it in the caches) and writes a row, backward reads a gradient row
 // per token and writes the whole table's gradient.  Gradient rows of one token are summed in fp32 in the order of their positions:
-//   1. sort    runs of SORT_RUN tokens in LDS (value, then position: one 32-bit key); the other workgroups of the launch clear dw
+//   1. sort    runs of SORT_RUN tokens (value, then position: one 32-bit key); the other workgroups of the launch clear dw
 //   2. merge   up to MERGE_RUNS runs into one, each key's place by binary searches (not for a single run)
 //   3. sum     a chunk of sorted positions a group of lanes, however they are spread over tokens: a token's sum that lies inside a
 //              chunk is stored, one that crosses a border is left as partial sums
 //   4. join    partial sums, in the order of the chunks
 // so that neither a token that is every second one nor one that comes once costs more than its rows, without an atomic addition.
-// us forward / sort / merge / sum / join, the word of rank r about as often as 1 / (r + 3): 61 rows of 192 2.8 / 2.7 / - / 7.7 / 3.5 (launches), 8192 of 1024 and 32768 words 8.4 (4.0 TB/s) /
-// 11.8 (the clearing, 5.7 TB/s) / 6.4 / 12.7 / 6.6, 65521 of 515 and 50021 words 31.9 (3.7 TB/s) / 9.6 / 21.6 / 42.5 / 9.4.
+// us forward / sort / merge / sum / join, the word of rank r about as often as 1 / (r + 3): 61 rows of 192 2.8 / 2.7 / - / 7.7 / 3.5 (launches),
+// 8192 of 1024 and 32768 words 8.4 (4.0 TB/s) / 11.8 (the clearing, 5.7 TB/s) / 6.4 / 12.7 / 6.6, 65521 of 515 and 50021 words
+// 31.9 (3.7 TB/s) / 9.6 / 21.6 / 42.5 / 9.4.
 #include "common.hpp"
 
 namespace mp {

@@ -273,6 +273,15 @@ def test_captured_and_replayed_with_other_documents():
             assert torch.equal(v, q.results()[k]), (s, k)
 
 
+@pytest.mark.parametrize("d,kv,cap,bias", [(32, 512, 0.0, False), (64, 256, 0.0, False), (64, 512, 5.0, True), (40, 256, 0.0, True), (96, 256, 3.0, False),
+                                           (128, 256, 0.0, True)])
+def test_as_many_workgroups_as_one_team_takes(d, kv, cap, bias):
+    """1024 workgroups of queries (2 x 512 heads), 512 and more of keys: one team each, heads that share keys summed in registers."""
+    p = Problem(129, 512, kv, d, seed=d, cap=cap, bias=bias, spread=2.0 if cap else 1.0)
+    p.docs([0, 50, 50, 128], causal=d != 64).run().check()
+    p.docs([2, 129], causal=True, window=40).run().check()
+
+
 @pytest.mark.parametrize("rows,window", [(4224, 70), (4170, 0), (8193, 65)])
 def test_more_than_64_tiles_of_queries(rows, window):
     """The tiles that see a key are found 64 at a time; their number is odd for some keys."""
