@@ -161,3 +161,24 @@ def test_captured_iterations_with_the_end_of_the_iteration():
         assert (s.scale, s.opt_step, s.skipped_steps) == (ost.scale, ost.opt_step, ost.skipped_steps)
         for t, d in zip(host, dev):
             assert all(same(d[k], t[k]) for k in ("m8", "v8", "ms", "vs")), step
+
+
+def test_a_tensor_of_more_than_2_to_31_elements():
+    """Its last blocks get what a tensor of these blocks alone gets."""
+    head, n = 2 ** 31 + 512, 700
+    host = tensors8([n], 4)[0]
+    kinds = dict(g16=torch.float16, w16=torch.float16, w32=torch.float32, m8=torch.int8, v8=torch.uint8, ms=torch.float32, vs=torch.float32)
+    at = lambda k: head // 256 if k in ("ms", "vs") else head  # noqa: E731
+    small = to_device(host)
+    big = {k: torch.zeros(at(k) + small[k].numel(), dtype=t, device="cuda") for k, t in kinds.items()}
+    for k in kinds:
+        big[k][at(k):] = small[k]
+    cfg = mp.opt_cfg("adamw", 1e-3, weight_decay=0.1)
+    for t in (small, big):
+        mp.mp_unscale_check_update8(mp.tensor_list8([t]), 1, cfg, state(2.0 ** 7, 3))
+    for k in kinds:
+        assert torch.equal(big[k][at(k):], small[k]), k
+        assert int(torch.count_nonzero(big[k][:1000])) == 0 and int(torch.count_nonzero(big[k][at(k) - 1000:at(k)])) == 0
+    m = torch.empty(head + n, dtype=torch.float32, device="cuda")
+    mp.mp_state8_decode(head + n, big["m8"], big["ms"], None, None, m, None)
+    assert same(m[head:], O.state8_decode(MIXED, small["m8"].cpu().numpy(), small["ms"].cpu().numpy(), False)) and int(torch.count_nonzero(m[head - 1000:head])) == 0

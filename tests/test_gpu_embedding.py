@@ -123,6 +123,26 @@ def test_three_rounds_of_merging():
     check(2048 * 32 * 32 + 5000, 50000, 3, "zipf")
 
 
+def test_offsets_beyond_32_bits():
+    """A table of 2.2e9 elements: the rows of a few tokens, and zeros everywhere else."""
+    vocab, d = 2000003, 1100
+    w, dw = (torch.zeros(vocab, d, dtype=torch.float16, device="cuda") for _ in range(2))
+    tok = [vocab - 1, 5, 1960000, vocab - 1]
+    r = np.random.default_rng(1)
+    rows, dy, y = S16(r.standard_normal((4, d))), S16(r.standard_normal((4, d))), empty16(4, d)
+    rows[3] = rows[0]
+    w[torch.tensor(tok, device="cuda")] = h16(rows)
+    mp.mp_embedding_fwd(4, vocab, d, i32(tok), w, 2.0, y)
+    assert np.array_equal(bits(y), half_bits(S16(2 * rows)))
+    dw[::1000] = 7
+    mp.mp_embedding_bwd(4, vocab, d, i32(tok), h16(dy), 1.0, dw, ws=ws_bytes(mp.mp_embedding_bwd_workspace_bytes(4, vocab, d)))
+    want = {vocab - 1: S16((dy[0].astype(np.float32) + dy[3]).astype(np.float32)), 5: dy[1], 1960000: dy[2]}
+    for t, x in want.items():
+        assert np.array_equal(bits(dw[t]), half_bits(x)), t
+        dw[t] = 0
+    assert all(int(torch.count_nonzero(dw[i:i + 100000])) == 0 for i in range(0, vocab, 100000))
+
+
 @pytest.mark.parametrize("other", [0, 3])
 def test_the_second_gradient_where_there_is_no_token(other):
     """It is copied, whatever its alignment beside dw's, and its infinities are reported."""

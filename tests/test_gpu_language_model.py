@@ -122,6 +122,20 @@ def test_moments_in_8_bits_in_the_other_steps(make):
         assert np.all(np.abs(x - y) <= 2.0 ** -23 * np.abs(x) + 2.0 ** -20 * ADAMW.lr), n
 
 
+def test_iterations_on_a_stream_of_their_own():
+    wl, other = replace(BASE, causal=True, n_docs=7, vocab=301, opt=ADAMW8), torch.cuda.Stream()
+    a, b = St.TransformerStep(wl), St.TransformerStep(wl)
+    torch.cuda.synchronize()
+    for k in range(3):
+        a.set_batch(batches(wl)(k))
+        a.step()
+        with torch.cuda.stream(other):
+            b.set_batch(batches(wl)(k))
+            b.step()
+    torch.cuda.synchronize()
+    assert torch.equal(a.P.w32_arena, b.P.w32_arena) and float(a.loss) == float(b.loss)
+
+
 def test_document_starts_that_do_not_fit():
     wl = replace(BASE, n_docs=4)
     step = St.TransformerStep(wl)
