@@ -101,7 +101,10 @@ __global__ __launch_bounds__(64) void mask_kernel(int rows, int rows_k, int n_do
 // ------------------------------------------------------------------------------------------------ scores
 // What is done to q k^T: nothing but the scale (to base 2: one factor beside the exponential's), a distance bias, a cap, or both.
 enum { PLAIN = 0, BIAS = 1, CAP = 2 };
-// Base-2 scores in place.  Lanes own one index, registers the other; dist: query less key (or the reverse) at register 0.
+// Scores in place, to base 2 once they are multiplied by unit(): a factor that costs nothing beside the exponential's.  Lanes own one
+// index, registers the other; dist: query less key (or the reverse) at register 0.
+template <int MODE>
+__device__ __forceinline__ float unit(const AttnArgs& a) { return MODE & BIAS ? 1.f : (MODE == CAP ? a.cap : a.alpha) * LOG2E; }
 template <int MODE>
 __device__ __forceinline__ void scores(const AttnArgs& a, f32x16& s, float slope2, int dist) {
     if (MODE == PLAIN) return;
@@ -109,8 +112,9 @@ __device__ __forceinline__ void scores(const AttnArgs& a, f32x16& s, float slope
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
         // tanh(x) = 1 - 2 / (exp(2x) + 1): an absolute error of 1e-7, which is what counts for a score
-        if (MODE & CAP) s[r] = c * fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[r] * k) + 1.f), 1.f);
+        if (MODE & CAP) s[r] = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[r] * k) + 1.f), 1.f);
         else s[r] *= k;
+        if (MODE == (CAP | BIAS)) s[r] *= c;
         if (MODE & BIAS) s[r] = fmaf(-slope2, fabsf(at + (float)(8 * (r >> 2) + (r & 3))), s[r]);
     }
 }
@@ -118,8 +122,7 @@ __device__ __forceinline__ void scores(const AttnArgs& a, f32x16& s, float slope
 template <int MODE>
 __device__ __forceinline__ float fade(const AttnArgs& a, float s, float slope2, float dist) {
     if (!(MODE & CAP)) return 1.f;
-    if (MODE & BIAS) s = fmaf(slope2, fabsf(dist), s);
-    const float t = s * (1.f / (a.cap * LOG2E));
+    const float t = MODE & BIAS ? fmaf(slope2, fabsf(dist), s) * (1.f / (a.cap * LOG2E)) : s;
     return fmaxf(fmaf(-t, t, 1.f), 0.f);
 }
 
@@ -232,7 +235,7 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void masked_fwd_kernel(AttnArgs a) 
     f16x8 qf[KK];
     row_frags<KK>(qf, m < a.rows_q ? a.q + (long long)m * a.ld_q + h * a.d : nullptr, a.d, hf);
     const float slope2 = MODE && a.slopes ? a.slopes[h] * LOG2E : 0.f;
-    const float c      = MODE ? 1.f : a.alpha * LOG2E;  // scores to base 2
+    const float c      = unit<MODE>(a);  // scores to base 2
     f32x16      o[DT];
     float       ref = -INFINITY, sum = 0.f;
 #pragma unroll
@@ -370,7 +373,7 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void masked_dq_kernel(AttnArgs a) {
     row_frags<KK>(qf, m < a.rows_q ? a.q + (long long)m * a.ld_q + h * a.d : nullptr, a.d, hf);
     row_frags<KK>(gf, m < a.rows_q ? a.dctx + (long long)m * a.ld_dctx + h * a.d : nullptr, a.d, hf);
     const float slope2 = MODE && a.slopes ? a.slopes[h] * LOG2E : 0.f;
-    const float c      = MODE ? 1.f : a.alpha * LOG2E;
+    const float c      = unit<MODE>(a);
     float       lse2 = INFINITY, delta = 0.f;
     if (m < a.rows_q) {
         lse2 = a.lse_in[(long long)h * a.rows_q + m] * LOG2E;
@@ -602,7 +605,7 @@ __global__ __launch_bounds__(256 * SPLIT, D <= 64 ? 2 : 1) void masked_dkv_kerne
     for (int dt = 0; dt < DT; ++dt) dk[dt] = dv[dt] = zero16();
     settle<KK>(kf);
     settle<KK>(vf);
-    const float c = MODE ? 1.f : a.alpha * LOG2E;
+    const float c = unit<MODE>(a);
 
     const unsigned at_q = lds_address(tiles_of[team][0][0]) + Tile::plain(lane), at_g = at_q + SIZE;
     const unsigned at_tq = lds_address(tiles_of[team][0][0]) + Tile::across(lane), at_tg = at_tq + SIZE;
