@@ -76,7 +76,7 @@ class OptCfg:
     beta2: float = 0.999
     eps: float = 1e-8
     weight_decay: float = 0.0
-    state_bits: int = 32           # 8: Adam's moments as 8-bit codes with a scale for every 256 elements
+    state_bits: int = 32           # 8: Adam's moments as 8-bit codes with a scale for every 256 elements, rounded without bias
 
 
 @dataclass(frozen=True)

@@ -126,10 +126,43 @@ def state8_encode(P: Policy, m, root):
     return qm.reshape(-1)[:n].astype(np.int8), ms, qv.reshape(-1)[:n].astype(np.uint8), vs
 
 
+def state8_uniforms(ms, vs, step):
+    """Two numbers in (0, 1) for each element of each block, 16 bits and a half: for m's codes and for v's.  They come from the block's
+    new scales (their fp32 bits), the step and the element's place in the block, so that a tensor's place in a list or an arena does not
+    matter.  The multipliers are odd words of the fractions of sqrt 2, 3, 5, 7 and of the golden ratio."""
+    u32 = lambda x: np.asarray(x, np.float32).view(np.uint32)  # noqa: E731
+    word, lane = np.uint32, np.arange(STATE8_BLOCK // 4, dtype=np.uint32)
+    x = (u32(ms) + u32(vs) * word(0x9E3779B9) + word(step * 0xA54FF53B & 0xFFFFFFFF))[:, None] + lane * word(0x3C6EF373)
+    x = (x ^ (x >> word(16))) * word(0x6A09E667)
+    x = (x ^ (x >> word(15))) * word(0xBB67AE85)
+    x = x ^ (x >> word(16))
+    x = x[:, :, None] * np.array([0x6A09E667, 0xBB67AE85, 0x3C6EF373, 0xA54FF53B], np.uint32)
+    x = (x ^ (x >> word(15))).reshape(-1, STATE8_BLOCK)
+    return [(y.astype(np.float32) + np.float32(0.5)) * np.float32(2.0 ** -16) for y in (x & word(0xFFFF), x >> word(16))]
+
+
+def state8_encode_unbiased(P: Policy, m, root, step):
+    """As state8_encode, but a value between two codes takes the upper one as often as it is nearer to what that stands for, so that what
+    the codes stand for is m and v in the mean (v's least code apart, which a v > 0 does not go below)."""
+    A, n = P.scalar, np.asarray(m).size
+    _, ms, _, vs = state8_encode(P, m, root)
+    mb, rb = _blocks(m, P), _blocks(root, P)
+    um, uv = (P.island(u) for u in state8_uniforms(ms, vs, step))
+    fit = lambda s, k: np.where(s > 0, A(k) / np.where(s > 0, s, A(1)), A(0))[:, None]  # noqa: E731
+    z, y = np.abs(mb) * fit(ms, 16129.0), rb * fit(vs, 65025.0)
+    q = np.minimum(np.floor(np.sqrt(z)), A(126))                        # values go with q^2 ...
+    qm = (q + ((z - q * q) - um * (2 * q + 1) > 0)) * np.sign(mb)
+    q = np.minimum(np.floor(np.sqrt(y)), A(254))                        # ... and with q^4
+    qv = q + ((y - q * q) * (y + q * q) - uv * ((2 * q + 1) * (2 * (q * (q + 1)) + 1)) > 0)
+    qv = np.where((rb > 0) & (vs > 0)[:, None], np.maximum(qv, 1), qv)
+    return qm.reshape(-1)[:n].astype(np.int8), ms, qv.reshape(-1)[:n].astype(np.uint8), vs
+
+
 def unscale_check_update8(P: Policy, tensors: List[Dict[str, np.ndarray]], opt, st: ScaleState) -> int:
     """unscale_check_update with moments in 8 bits (keys m8, ms, v8, vs instead of m, v; opt.kind "adam" or "adamw"):
         m = b1 decode(m8) + (1-b1) g,  v = b2 decode(v8) + (1-b2) g^2,
-        w32 -= ((lr / (1-b1^t)) m) / (sqrt(v) (1 / sqrt(1-b2^t)) + eps),  then the moments are encoded."""
+        w32 -= ((lr / (1-b1^t)) m) / (sqrt(v) (1 / sqrt(1-b2^t)) + eps),  then the moments are encoded.
+    opt.state_bits 8, as an iteration is configured with it, rounds the codes without bias, as iterations do; else to nearest."""
     if has_nonfinite(P, [t["g16"] for t in tensors]):
         return 1
     A, t = P.scalar, st.opt_step + 1
@@ -146,7 +179,8 @@ def unscale_check_update8(P: Policy, tensors: List[Dict[str, np.ndarray]], opt, 
         root = np.sqrt(v)
         w = w - (rate * m) / (root * rbc2 + A(opt.eps))
         tn["w32"][...] = w.reshape(tn["w32"].shape)
-        tn["m8"][...], tn["ms"][...], tn["v8"][...], tn["vs"][...] = state8_encode(P, m, root)
+        unbiased = opt.state_bits == 8
+        tn["m8"][...], tn["ms"][...], tn["v8"][...], tn["vs"][...] = state8_encode_unbiased(P, m, root, t) if unbiased else state8_encode(P, m, root)
         tn["w16"][...] = P.store(tn["w32"])
     return 0
 

@@ -13,7 +13,7 @@ MP_SCALE_STATIC, MP_SCALE_BACKOFF = 0, 1
 MP_EPI_NONE, MP_EPI_BIAS, MP_EPI_BIAS_RELU = 0, 1, 2
 MP_OPT_SGD, MP_OPT_ADAM, MP_OPT_ADAMW = 0, 1, 2
 MP_STATE8_BLOCK = 256
-MP_UPDATE_DEFAULT, MP_UPDATE_PRECHECKED = 0, 1
+MP_UPDATE_DEFAULT, MP_UPDATE_PRECHECKED, MP_UPDATE_UNBIASED8 = 0, 1, 4
 
 
 class ScaleState(C.Structure):

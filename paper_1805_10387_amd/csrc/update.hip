@@ -117,8 +117,10 @@ struct UpdBatch {
     int                ntensors;
 };
 
-// The same with moments in 8 bits.
+// The same with moments in 8 bits.  UNBIASED_: codes rounded so that their mean is the value, else to nearest.
+template <bool UNBIASED_>
 struct UpdBatch8 {
+    static constexpr bool UNBIASED = UNBIASED_;
     const uint16_t*    g16[UPD_MAX_TENSORS];
     float*             w32[UPD_MAX_TENSORS];
     uint16_t*          w16[UPD_MAX_TENSORS];
@@ -314,6 +316,16 @@ __device__ __forceinline__ float decode_r(unsigned q, float vs) { return (float)
 __device__ __forceinline__ float encode_m(float m, float fit) { return fminf(rintf(sqrtf(fabsf(m) * fit)), 127.f); }
 __device__ __forceinline__ float encode_r(float r, float fit) { return fminf(rintf(sqrtf(r * fit)), 255.f); }
 
+__device__ __forceinline__ void pack4(const float* m, const float* r, float vs, const float* a, const float* b, unsigned& mq, unsigned& vq) {
+    mq = vq = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        mq |= ((unsigned)(int)copysignf(a[k], m[k]) & 255u) << (8 * k);
+        // (a second moment that is not 0 keeps a code that is not 0)
+        vq |= (unsigned)(r[k] > 0.f && vs > 0.f ? fmaxf(b[k], 1.f) : b[k]) << (8 * k);
+    }
+}
+
 // Codes of a lane's 4 elements, ms and vs their block's scales.  The codes are those of correctly rounded quotients and roots.  The
 // instructions for both are good to an ulp, which with the products' roundings is 8e-5 at a root of 255: only a block in which one lies
 // within 1e-4 of the border between two codes, one in ten, needs more.
@@ -335,19 +347,72 @@ __device__ __forceinline__ void encode4(const float* m, const float* r, float ms
             b[k] = encode_r(r[k], vs > 0.f ? 65025.f / vs : 0.f);
         }
     }
-    mq = vq = 0;
+    pack4(m, r, vs, a, b, mq, vq);
+}
+
+// The same without bias.  To nearest, what changes a moment by less than half a code is lost in every step: with beta2 = 0.999 a second
+// moment moves by a thousandth a step and its codes lie 1.6 hundredths apart, so that it never falls while its block's scale stays.  So
+// a value between two codes takes the upper one as often as it is nearer to what that stands for: m in proportion to q^2, v to q^4.
+// What decides comes from the block's scales, the step and the place in the block, so that results repeat and do not depend on where a
+// tensor lies.  16 bits and a half, for m and for v.
+__device__ __forceinline__ unsigned lane_bits(float ms, float vs, int step, int lane) {  // odd words of the fractions of sqrt 2, 3, 5, 7 and of the golden ratio
+    unsigned x = __builtin_bit_cast(unsigned, ms) + __builtin_bit_cast(unsigned, vs) * 0x9E3779B9u + (unsigned)step * 0xA54FF53Bu + (unsigned)lane * 0x3C6EF373u;
+    x = (x ^ (x >> 16)) * 0x6A09E667u;
+    x = (x ^ (x >> 15)) * 0xBB67AE85u;
+    return x ^ (x >> 16);
+}
+struct Uniforms {
+    float m, r;
+    __device__ __forceinline__ Uniforms(unsigned bits, int k) {
+        unsigned x = bits * (k == 0 ? 0x6A09E667u : k == 1 ? 0xBB67AE85u : k == 2 ? 0x3C6EF373u : 0xA54FF53Bu);
+        x ^= x >> 15;
+        m = fmaf((float)(x & 0xFFFFu), 0x1p-16f, 0x1p-17f);
+        r = fmaf((float)(x >> 16), 0x1p-16f, 0x1p-17f);
+    }
+};
+// z = |m| 127^2 / ms and y = r 255^2 / vs are good to 3.6e-7 of themselves where they come from fast instructions, the root rounded down to
+// one.  near: the code may be another than that of z and y as they would be; at a whole root only where u is next to 0 or 1 too, since
+// else the code is the same from either side.  One block in fifteen is.  (Fused where nothing but the last operation rounds.)
+__device__ __forceinline__ bool next_to_a_whole(float root, float q, float u) { return fabsf(root - q - 0.5f) > 0.4999f && fabsf(u - 0.5f) > 0.4995f; }
+__device__ __forceinline__ float unbiased_m(float z, float root, float u, bool& near) {
+    const float q = fminf(floorf(root), 126.f), over = fmaf(-q, q, z) - u * fmaf(2.f, q, 1.f);
+    near |= fabsf(over) <= 2e-6f * z || next_to_a_whole(root, q, u);
+    return over > 0.f ? q + 1.f : q;
+}
+__device__ __forceinline__ float unbiased_r(float y, float root, float u, bool& near) {
+    const float q    = fminf(floorf(root), 254.f);
+    const float over = fmaf(-q, q, y) * fmaf(q, q, y) - u * (fmaf(2.f, q, 1.f) * fmaf(2.f, fmaf(q, q, q), 1.f));
+    near |= fabsf(over) <= 2e-6f * (y * y) || next_to_a_whole(root, q, u);
+    return over > 0.f ? q + 1.f : q;
+}
+__device__ __forceinline__ void encode4_unbiased(const float* m, const float* r, float ms, float vs, unsigned bits, unsigned& mq, unsigned& vq) {
+    float       a[4], b[4];
+    bool        near = false;
+    const float mfit = ms > 0.f ? 16129.f * __builtin_amdgcn_rcpf(ms) : 0.f, rfit = vs > 0.f ? 65025.f * __builtin_amdgcn_rcpf(vs) : 0.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        mq |= ((unsigned)(int)copysignf(a[k], m[k]) & 255u) << (8 * k);
-        // (a second moment that is not 0 keeps a code that is not 0)
-        vq |= (unsigned)(r[k] > 0.f && vs > 0.f ? fmaxf(b[k], 1.f) : b[k]) << (8 * k);
+        const Uniforms u(bits, k);
+        const float    z = fabsf(m[k]) * mfit, y = r[k] * rfit;
+        a[k] = unbiased_m(z, __builtin_amdgcn_sqrtf(z), u.m, near);
+        b[k] = unbiased_r(y, __builtin_amdgcn_sqrtf(y), u.r, near);
     }
+    if (__any(near)) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const Uniforms u(bits, k);
+            const float    z = fabsf(m[k]) * (ms > 0.f ? 16129.f / ms : 0.f), y = r[k] * (vs > 0.f ? 65025.f / vs : 0.f);
+            a[k] = unbiased_m(z, sqrtf(z), u.m, near);
+            b[k] = unbiased_r(y, sqrtf(y), u.r, near);
+        }
+    }
+    pack4(m, r, vs, a, b, mq, vq);
 }
 
 // As above; a wave's 64 x 4 elements are one block of codes, whose scales are the wave's maxima.  Bound by HBM: 75.6 M parameters in 3 launches
-// 253 us (4.8 TB/s; 326 us while every code took correctly rounded roots, which kept the vector units as busy as memory).
-template <int KIND, int ITERS>
-__device__ __forceinline__ void update_share(const UpdBatch8& b, const UpdScalars& s, const mp_scale_state* st) {
+// 253 us (4.8 TB/s; 326 us while every code took correctly rounded roots, which kept the vector units as busy as memory).  Without the
+// inspection 228 us, 280 with codes rounded without bias: their hashes and thresholds are vector work again.
+template <int KIND, int ITERS, bool UNBIASED>
+__device__ __forceinline__ void update_share(const UpdBatch8<UNBIASED>& b, const UpdScalars& s, const mp_scale_state* st) {
     static_assert(64 * UPD_VEC == MP_STATE8_BLOCK, "a wave takes one block of codes at a time");
     const int                t   = find_tensor(b, blockIdx.x);
     const unsigned long long n   = b.n[t];
@@ -414,7 +479,8 @@ __device__ __forceinline__ void update_share(const UpdBatch8& b, const UpdScalar
             b.vs[t][block] = vs;
         }
         unsigned mq, vq;
-        encode4(m, r, ms, vs, mq, vq);
+        if constexpr (UNBIASED) encode4_unbiased(m, r, ms, vs, lane_bits(ms, vs, step, threadIdx.x & 63), mq, vq);
+        else encode4(m, r, ms, vs, mq, vq);
         if (four) {
             __builtin_nontemporal_store(f32x4v{w[0], w[1], w[2], w[3]}, reinterpret_cast<f32x4v*>(b.w32[t] + i));
             __builtin_nontemporal_store((int)mq, reinterpret_cast<int*>(b.m8[t] + i));
@@ -571,7 +637,8 @@ static void set_moments(UpdBatch& b, int k, const mp_tensor_desc& d) {
     b.m[k] = d.m;
     b.v[k] = d.v;
 }
-static void set_moments(UpdBatch8& b, int k, const mp_tensor_desc8& d) {
+template <bool UNBIASED>
+static void set_moments(UpdBatch8<UNBIASED>& b, int k, const mp_tensor_desc8& d) {
     b.m8[k] = d.m8;
     b.v8[k] = d.v8;
     b.ms[k] = d.ms;
@@ -626,7 +693,8 @@ static int unscale_check_update(const Desc* tensors, int ntensors, const mp_opt_
     MP_REQUIRE(ntensors >= 0 && (ntensors == 0 || tensors != nullptr), "mp_unscale_check_update: bad tensor list");
     MP_REQUIRE(cfg->kind == MP_OPT_ADAM || cfg->kind == MP_OPT_ADAMW || (cfg->kind == MP_OPT_SGD && std::is_same<Desc, mp_tensor_desc>::value),
                "mp_unscale_check_update: bad optimizer kind %d", cfg->kind);
-    MP_REQUIRE((flags & ~MP_UPDATE_PRECHECKED) == 0, "mp_unscale_check_update: unknown flags 0x%x", flags);
+    MP_REQUIRE((flags & ~(MP_UPDATE_PRECHECKED | (std::is_same<Desc, mp_tensor_desc8>::value ? MP_UPDATE_UNBIASED8 : 0))) == 0,
+               "mp_unscale_check_update: unknown flags 0x%x", flags);
     for (int i = 0; i < ntensors; ++i) {
         const Desc& d = tensors[i];
         if (d.n == 0) continue;
@@ -714,7 +782,8 @@ extern "C" size_t mp_update_counters_bytes(void) { return (UPD_END_GROUPS + 1) *
 extern "C" int mp_unscale_check_update8(const mp_tensor_desc8* tensors, int ntensors, const mp_opt_cfg* cfg, mp_scale_state* st, int flags,
                                         mp_stream stream) {
     bool ended = false;
-    return unscale_check_update<UpdBatch8>(tensors, ntensors, cfg, st, flags, UpdEnd{}, &ended, stream);
+    return (flags & MP_UPDATE_UNBIASED8 ? unscale_check_update<UpdBatch8<true>, mp_tensor_desc8> : unscale_check_update<UpdBatch8<false>, mp_tensor_desc8>)(
+        tensors, ntensors, cfg, st, flags, UpdEnd{}, &ended, stream);
 }
 
 template <typename Batch, typename Desc>
@@ -736,7 +805,8 @@ extern "C" int mp_unscale_check_update_end(const mp_tensor_desc* tensors, int nt
 
 extern "C" int mp_unscale_check_update8_end(const mp_tensor_desc8* tensors, int ntensors, const mp_opt_cfg* cfg, mp_scale_state* st, int flags,
                                             const mp_mean_parts* parts, float* loss, int32_t* counters, mp_stream stream) {
-    return unscale_check_update_end<UpdBatch8>(tensors, ntensors, cfg, st, flags, parts, loss, counters, stream);
+    return (flags & MP_UPDATE_UNBIASED8 ? unscale_check_update_end<UpdBatch8<true>, mp_tensor_desc8> : unscale_check_update_end<UpdBatch8<false>, mp_tensor_desc8>)(
+        tensors, ntensors, cfg, st, flags, parts, loss, counters, stream);
 }
 
 extern "C" int mp_state8_decode(size_t n, const int8_t* m8, const float* ms, const uint8_t* v8, const float* vs, float* m, float* v, mp_stream stream) {

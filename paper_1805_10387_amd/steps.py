@@ -114,7 +114,9 @@ class _StepBase:
         flags = ML.MP_UPDATE_PRECHECKED if self.prechecked else ML.MP_UPDATE_DEFAULT
         parts, self._parts = self._parts, None
         tensors, n = (self.P.flat_list, 1) if self.flat_update else (self.P.tensor_list, self.P.n_tensors)
-        update = B.mp_unscale_check_update8_end if self.P.state_bits == 8 else B.mp_unscale_check_update_end
+        update = B.mp_unscale_check_update_end
+        if self.P.state_bits == 8:   # (codes to nearest would hold moments up that fall slowly)
+            update, flags = B.mp_unscale_check_update8_end, flags | ML.MP_UPDATE_UNBIASED8
         update(tensors, n, self.cfg, self.st, self.counters, flags, parts, self.loss)
 
     def _mse(self, rows, cols, y, target, dy):
