@@ -444,8 +444,9 @@ typedef struct mp_attn_desc {
  * slopes: device fp32 [n_heads] or NULL.  lse: device fp32 [n_heads, rows_q], kept for the backward call.  A row that sees nothing
  * has ctx 0 and lse -inf.  Scores stay fp32; the exponentials enter the second product rounded to fp16, unnormalised (relative to a
  * maximum that may lag by a factor of 2^8: none is above that, the row's largest not below 1).
- * What a row does not see does not reach it, NaN and infinities included; of a value row that holds one, those rows that see it get
- * non-finite results.  All rows of ctx are written.  Any rows_k >= 0 and rows_q >= 0.
+ * What a row does not see does not reach it, NaN and infinities included.  A row that sees one has non-finite results: of a query or key
+ * row that holds one (whatever its sign, capped or not) NaN in all of the row's ctx and lse, of a value row in ctx.  All rows of ctx are
+ * written.  Any rows_k >= 0 and rows_q >= 0.
  * `mask` is one of rows_q rows.  16-byte aligned matrices with leading dimensions, a d_head and a cap as above; otherwise
  * MP_E_UNSUPPORTED. */
 int mp_attention_masked_fwd(const mp_attn_desc* desc /* host */, const void* mask, const mp_half* q, const mp_half* k,

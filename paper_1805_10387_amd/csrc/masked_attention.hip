@@ -20,8 +20,10 @@
 //
 // What is hidden must not be felt, though 0 x NaN is NaN: scores of hidden pairs are replaced, not added to; and in tiles that are
 // not whole, non-finite elements of the matrices that a zero probability would multiply are zeroed on their way into LDS.
-// Those that are visible still show: forward by a NaN score in their place, backward because a query that sees one has a non-finite
-// lse or delta, and its lse is made so low that its probabilities are infinite.
+// Those that are visible still show.  Forward, an element of v by a NaN score in its place (or by the product), one of q or k by what
+// it makes of the score: q k^T is finite where both rows are (128 x 65504^2 is far from the end of fp32) and never where one is not, and
+// an infinite score becomes NaN before a cap or an exponential could make something finite of it.  Backward because a query that sees one
+// has a non-finite lse or delta, and its lse is made so low that its probabilities are infinite.
 #include "attn_lds.hpp"
 
 #include <limits.h>
@@ -105,14 +107,15 @@ enum { PLAIN = 0, BIAS = 1, CAP = 2 };
 // index, registers the other; dist: query less key (or the reverse) at register 0.
 template <int MODE>
 __device__ __forceinline__ float unit(const AttnArgs& a) { return MODE & BIAS ? 1.f : (MODE == CAP ? a.cap : a.alpha) * LOG2E; }
-template <int MODE>
+// SHOW: an infinite score of a mode with a cap becomes NaN.
+template <int MODE, bool SHOW = false>
 __device__ __forceinline__ void scores(const AttnArgs& a, f32x16& s, float slope2, int dist) {
     if (MODE == PLAIN) return;
     const float k = MODE & CAP ? a.alpha / a.cap * (2.f * LOG2E) : a.alpha * LOG2E, c = a.cap * LOG2E, at = (float)dist;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
         // tanh(x) = 1 - 2 / (exp(2x) + 1): an absolute error of 1e-7, which is what counts for a score
-        if (MODE & CAP) s[r] = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[r] * k) + 1.f), 1.f);
+        if (MODE & CAP) s[r] = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[r] * k) + 1.f), SHOW ? fmaf(s[r], 0.f, 1.f) : 1.f);
         else s[r] *= k;
         if (MODE == (CAP | BIAS)) s[r] *= c;
         if (MODE & BIAS) s[r] = fmaf(-slope2, fabsf(at + (float)(8 * (r >> 2) + (r & 3))), s[r]);
@@ -266,7 +269,16 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void masked_fwd_kernel(AttnArgs a) 
             for (int kk = 0; kk < KK; ++kk) s[t] = mma(Tile::frag(xk, 32 * t, kk), qf[kk], s[t]);
         }
 #pragma unroll
-        for (int t = 0; t < 2; ++t) scores<MODE>(a, s[t], slope2, kb + 32 * t + 4 * hf - m);
+        for (int t = 0; t < 2; ++t) scores<MODE, true>(a, s[t], slope2, kb + 32 * t + 4 * hf - m);
+        // (without a cap +inf and NaN show by themselves; -inf is the largest word there is of a number)
+        if (whole && !(MODE & CAP)) {
+            unsigned low = 0;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) low = max(low, __builtin_bit_cast(unsigned, (float)s[t][r]));
+            sum = low >= 0xFF800000u ? NAN : sum;
+        }
         if (!whole) {  // (also where this wave's queries see all of it: values were zeroed)
             const int      n0  = kb + 4 * hf - x.lo;
             const unsigned len = x.hi - x.lo;
@@ -275,7 +287,7 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void masked_fwd_kernel(AttnArgs a) 
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int   n = 32 * t + 8 * (r >> 2) + (r & 3);
-                    const float v = s[t][r] + bad[n + 4 * hf];
+                    const float v = s[t][r] + (MODE & CAP ? bad[n + 4 * hf] : fmaf(s[t][r], 0.f, bad[n + 4 * hf]));
                     s[t][r]       = (unsigned)(n0 + n) < len ? v : -INFINITY;
                 }
         }
@@ -519,7 +531,8 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void masked_dq_kernel(AttnArgs a) {
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[dt] = zero16();
     }
-    store_rows<DT>(m < a.rows_q ? a.dq + (long long)m * a.ld_dq + h * a.d : nullptr, o, a.alpha, a.d, hf);
+    // (a query whose scores are all -inf has probabilities of 0 all the same)
+    store_rows<DT>(m < a.rows_q ? a.dq + (long long)m * a.ld_dq + h * a.d : nullptr, o, lse2 < -1e38f ? NAN : a.alpha, a.d, hf);
 }
 
 // dk and dv of 128 keys, 32 of them a wave, over the tiles of 64 queries that see any of them, head by head: of all heads that share
