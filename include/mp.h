@@ -453,7 +453,8 @@ int mp_attention_masked_fwd(const mp_attn_desc* desc /* host */, const void* mas
                             const mp_half* v, const float* slopes, mp_half* ctx, float* lse, mp_stream stream);
 
 /* Gradients of the above, from its inputs and results (delta = sum_d dctx ctx in fp32 from the stored ctx):
- *     dp = dctx v^T,  ds = p (dp - delta) (1 - tanh(t / cap)^2)     (fp32, then rounded to fp16 as an operand)
+ *     dp = dctx v^T,  ds = p (dp - delta) (1 - tanh(t / cap)^2)     (fp32, then rounded to fp16 as an operand: times 2^10, which keeps
+ *                                                                   a ds of 2^-35, or as it is where one nearby is above 64)
  *     dq = RNE16(alpha ds k),  dk = RNE16(alpha ds^T q),  dv = RNE16(p^T dctx),  dk and dv summed over the heads that share them.
  * Every row of dq, dk and dv is written (0 where no pair is left).  The sums' order is fixed: two calls give the same bits.  None of
  * the outputs may overlap an input.  ws: device, 16-byte aligned, mp_attention_masked_bwd_workspace_bytes(desc) bytes (0 for a

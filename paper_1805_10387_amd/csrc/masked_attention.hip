@@ -43,7 +43,7 @@ struct AttnArgs {
     uint16_t *      out, *dq, *dk, *dv;
     float*          lse;                 // forward: out
     const float *   lse_in, *slopes;
-    float *         lse2, *delta;        // backward: [n_heads, rows_pad]
+    float *         lse2, *delta;        // backward: [n_heads, rows_pad]; delta twice, the second over P_SCALE
     float*          part;                // dk and dv of a part of a group's heads: [kv_heads * parts, rows_k, 2, d]
     const int2*     range;
     const int4*     tile;
@@ -205,6 +205,23 @@ __device__ __forceinline__ f16x8  words(const unsigned (&w)[8], int e) { return 
 // A barrier behind which the loads of every wave have arrived.
 __device__ __forceinline__ void arrive() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ void step() { __builtin_amdgcn_sched_barrier(0); }
+template <int DT>
+__device__ __forceinline__ bool finite(const f32x16 (&o)[DT]) {
+    bool is = true;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) is = is && fabsf(o[dt][r]) < INFINITY;
+    return is;
+}
+// Whether it holds for any lane of the workgroup.  Behind it everybody is through with the tiles in LDS.
+__device__ __forceinline__ bool any_of_workgroup(bool it, int* vote) {
+    if (threadIdx.x == 0) *vote = 0;
+    lds_barrier();
+    if (__any(it)) *vote = 1;
+    lds_barrier();
+    return __builtin_amdgcn_readfirstlane(*vote) != 0;
+}
 
 // ------------------------------------------------------------------------------------------------ forward
 constexpr float LAZY = 8.f;  // the maximum that exponentials refer to follows when it is 2^8 behind
@@ -354,8 +371,11 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void masked_fwd_kernel(AttnArgs a) 
 // ------------------------------------------------------------------------------------------------ backward
 // dq of 128 queries, 32 of them a wave; teams as in the forward kernel.  Leaves the rows' statistics for the kernel of dk and dv: lse in base 2
 // (+inf where a row sees nothing: its probabilities are then 0; POISON where it or delta is not a number to go by: a visible score's
-// probability is then infinite, and that of a hidden one, exp(-inf - POISON), still 0) less log2 of P_SCALE, and delta / P_SCALE, so
-// that p comes out times P_SCALE and ds = p (dp / P_SCALE - delta) as it is.
+// probability is then infinite, and that of a hidden one, exp(-inf - POISON), still 0) less log2 of P_SCALE, so that p and with it
+// ds = p (dp - delta) come out times P_SCALE, and delta.
+// ds is an fp16 operand: of 10^4 even probabilities and the gradients of a loss over 10^7 elements it is near 10^-8, where fp16 ends, so
+// it keeps the factor.  A workgroup whose sums overflow that way, with a ds above 64, is done again without it, and then ends where ds
+// itself does.  (Not for rows whose sums are not finite anyway; dk and dv of keys that such rows see are done twice.)
 // delta = sum p dp is formed as sum dctx ctx from the ctx that was stored in fp16, whose rounding moves it by 2^-12 |dctx| |ctx|: gradients are
 // off by 3e-4 of their norm as with an exact one, by 4 to 6e-4 where p (dp - delta) cancels.  Taking sum p dp itself out of ds afterwards
 // would need sum p k, a fourth product with results of its own, and heads of 128 have no registers left here.
@@ -366,6 +386,7 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void masked_dq_kernel(AttnArgs a) {
     typedef TileLoad<ROWB, 4> Load;
     typedef LdsTile<ROWB>     Tile;
     __shared__ __align__(256) char tiles_of[SPLIT][2][2][SIZE];  // keys, values of two tiles
+    __shared__ int vote;
 
     const int tiles = (a.rows_q + MA_Q - 1) / MA_Q;
     const int h = blockIdx.x % a.heads, qt = tiles - 1 - blockIdx.x / a.heads, kvh = h / a.group;
@@ -402,20 +423,22 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void masked_dq_kernel(AttnArgs a) {
     else if (!(fabsf(lse2) < INFINITY && fabsf(delta) < INFINITY))
         lse2 = POISON, delta = 0.f;
     lse2 -= P_LOG2;
-    delta *= 1.f / P_SCALE;
     if (team == 0 && hf == 0 && m < a.rows_pad) {
-        a.lse2[(long long)h * a.rows_pad + m]  = lse2;
-        a.delta[(long long)h * a.rows_pad + m] = delta;
+        a.lse2[(long long)h * a.rows_pad + m]              = lse2;
+        a.delta[(long long)h * a.rows_pad + m]             = delta;
+        a.delta[(long long)(h + a.heads) * a.rows_pad + m] = delta * (1.f / P_SCALE);
     }
     f32x16 o[DT];
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[dt] = zero16();
+    float  kept = 1.f;  // of P_SCALE, that ds has
     settle<KK>(qf);
     settle<KK>(gf);
     asm volatile("" : "+v"(lse2), "+v"(delta));
     const unsigned at_k = lds_address(tiles_of[team][0][0]) + Tile::plain(lane), at_v = lds_address(tiles_of[team][0][1]) + Tile::plain(lane);
     const unsigned at_t = lds_address(tiles_of[team][0][0]) + Tile::across(lane);
 
+again:
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[dt] = zero16();
     int b = 0;
     for (int k0 = x.glo; k0 < x.ghi; k0 += MA_K * SPLIT, b ^= 1) {
         const int kb = k0 + MA_K * team, next = kb + MA_K * SPLIT;
@@ -484,7 +507,7 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void masked_dq_kernel(AttnArgs a) {
                 for (int y = 0; y < 2; ++y) {
                     const int   r = 2 * e + y;
                     const float p = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -lse2));  // (times P_SCALE)
-                    d[y] = p * fmaf(dp[u][r], 1.f / P_SCALE, -delta);
+                    d[y] = p * fmaf(dp[u][r], kept, -delta);
                     if (MODE & CAP) d[y] *= fade<MODE>(a, s[u][r], slope2, (float)(kb + 32 * u + 4 * hf - m + 8 * (r >> 2) + (r & 3)));
                 }
                 ds[u][e] = pack_f16(d[0], d[1]);
@@ -509,6 +532,15 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void masked_dq_kernel(AttnArgs a) {
             if (i >= 2 * PP && i < 2 * PP + GP) weights(1, 8 * (i - 2 * PP) / GP, 8 * (i - 2 * PP + 1) / GP);
         }
     }
+    if (kept == 1.f && any_of_workgroup(fabsf(lse2) < 1e38f && !finite(o), &vote)) {
+        kept = 1.f / P_SCALE;
+        delta *= kept;
+        if (x.glo + MA_K * team < x.ghi) {
+            lk.issue(K, a.ld_k, x.glo + MA_K * team, a.rows_k, a.d, tiles_of[team][0][0], wave);
+            lv.issue(V, a.ld_v, x.glo + MA_K * team, a.rows_k, a.d, tiles_of[team][0][1], wave);
+        }
+        goto again;
+    }
     if constexpr (SPLIT > 1) {  // the second team's sums to the first, through the tiles' LDS
         static_assert(sizeof(tiles_of) >= 16 * DT * 256 * sizeof(float), "the sums fit");
         float* const ex = reinterpret_cast<float*>(tiles_of) + (threadIdx.x & 255);
@@ -532,7 +564,7 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void masked_dq_kernel(AttnArgs a) {
         for (int dt = 0; dt < DT; ++dt) o[dt] = zero16();
     }
     // (a query whose scores are all -inf has probabilities of 0 all the same)
-    store_rows<DT>(m < a.rows_q ? a.dq + (long long)m * a.ld_dq + h * a.d : nullptr, o, lse2 < -1e38f ? NAN : a.alpha, a.d, hf);
+    store_rows<DT>(m < a.rows_q ? a.dq + (long long)m * a.ld_dq + h * a.d : nullptr, o, lse2 < -1e38f ? NAN : a.alpha / (P_SCALE * kept), a.d, hf);
 }
 
 // dk and dv of 128 keys, 32 of them a wave, over the tiles of 64 queries that see any of them, head by head: of all heads that share
@@ -549,6 +581,7 @@ __global__ __launch_bounds__(256 * SPLIT, D <= 64 ? 2 : 1) void masked_dkv_kerne
     };
     __shared__ __align__(256) char tiles_of[SPLIT][2][2][SIZE];  // queries, gradients of two tiles
     __shared__ __align__(16) Stats stats_of[SPLIT][2];
+    __shared__ int vote;
 
     const int kv_heads = a.heads / a.group, parts = a.group / a.part_heads, per = kv_heads * parts;
     const int id = blockIdx.x % per, kvh = id / parts, h0 = kvh * a.group + id % parts * a.part_heads, kt = blockIdx.x / per;
@@ -598,13 +631,15 @@ __global__ __launch_bounds__(256 * SPLIT, D <= 64 ? 2 : 1) void masked_dkv_kerne
     Load lq, lg;
     lq.init(a.ld_q, a.d, wave, lane);
     lg.init(a.ld_dctx, a.d, wave, lane);
+    float        kept = 1.f;  // of P_SCALE, that ds has
+    const float* delta = a.delta;
     const auto issue = [&](int b, const Step& x) {
         if (!x.mine) return;
         lq.issue(a.q + x.h * a.d, a.ld_q, x.q0, a.rows_q, a.d, tiles_of[team][b][0], wave);
         lg.issue(a.dctx + x.h * a.d, a.ld_dctx, x.q0, a.rows_q, a.d, tiles_of[team][b][1], wave);
         const long long at = (long long)x.h * a.rows_pad + x.q0;
         if (wave == 0) load_words(a.lse2 + at, stats[b].lse2, lane);
-        if (wave == 1) load_words(a.delta + at, stats[b].delta, lane);
+        if (wave == 1) load_words(delta + at, stats[b].delta, lane);
         if (wave == 2) load_ranges(a.range + x.q0, stats[b].range, lane);
     };
     Step now, next;
@@ -614,8 +649,6 @@ __global__ __launch_bounds__(256 * SPLIT, D <= 64 ? 2 : 1) void masked_dkv_kerne
     row_frags<KK>(kf, n < a.rows_k ? a.k + (long long)n * a.ld_k + kvh * a.d : nullptr, a.d, hf);
     row_frags<KK>(vf, n < a.rows_k ? a.v + (long long)n * a.ld_v + kvh * a.d : nullptr, a.d, hf);
     f32x16 dk[DT], dv[DT];
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) dk[dt] = dv[dt] = zero16();
     settle<KK>(kf);
     settle<KK>(vf);
     const float c = unit<MODE>(a);
@@ -623,6 +656,9 @@ __global__ __launch_bounds__(256 * SPLIT, D <= 64 ? 2 : 1) void masked_dkv_kerne
     const unsigned at_q = lds_address(tiles_of[team][0][0]) + Tile::plain(lane), at_g = at_q + SIZE;
     const unsigned at_tq = lds_address(tiles_of[team][0][0]) + Tile::across(lane), at_tg = at_tq + SIZE;
     bool           ever = false;  // (the other half of the wave has the other queries)
+again:
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) dk[dt] = dv[dt] = zero16();
     for (int b = 0; more; b ^= 1) {
         now = next;
         arrive();
@@ -708,7 +744,7 @@ __global__ __launch_bounds__(256 * SPLIT, D <= 64 ? 2 : 1) void masked_dkv_kerne
                 for (int x = 0; x < 4; ++x) {
                     const int r = 4 * e + x;
                     p[x]        = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -l4[x]));  // (P_SCALE is in it)
-                    d[x]        = p[x] * fmaf(dp[u][r], 1.f / P_SCALE, -d4[x]);
+                    d[x]        = p[x] * fmaf(dp[u][r], kept, -d4[x]);
                     if (MODE & CAP) d[x] *= fade<MODE>(a, s[u][r], slope2, (float)(m0 + 32 * u + 4 * hf - n + 8 * e + x));
                 }
                 pk[u][2 * e]      = pack_f16(p[0], p[1]);
@@ -735,7 +771,15 @@ __global__ __launch_bounds__(256 * SPLIT, D <= 64 ? 2 : 1) void masked_dkv_kerne
             if (i >= PARTS && i < 3 * PARTS) weights(i / PARTS - 1, i % PARTS);
         }
     }
-    if (!(__ballot(ever) >> (lane & 31) & 0x100000001ull)) {  // (a key that nobody sees may hold anything, and 0 x NaN has reached its sums)
+    const bool seen_once = __ballot(ever) >> (lane & 31) & 0x100000001ull;
+    if (kept == 1.f && any_of_workgroup(seen_once && !finite(dk), &vote)) {
+        kept = 1.f / P_SCALE, delta += (long long)a.heads * a.rows_pad;
+        h = h0, base = -64, todo = 0;
+        more = take(next);
+        if (more) issue(0, next);
+        goto again;
+    }
+    if (!seen_once) {  // (a key that nobody sees may hold anything, and 0 x NaN has reached its sums)
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) dk[dt] = dv[dt] = zero16();
     }
@@ -765,16 +809,17 @@ __global__ __launch_bounds__(256 * SPLIT, D <= 64 ? 2 : 1) void masked_dkv_kerne
     if (a.part_heads == a.group) {
         const bool in = n < a.rows_k;
         store_rows<DT>(in ? a.dv + (long long)n * a.ld_dv + kvh * a.d : nullptr, dv, 1.f / P_SCALE, a.d, hf);
-        store_rows<DT>(in ? a.dk + (long long)n * a.ld_dk + kvh * a.d : nullptr, dk, a.alpha, a.d, hf);
+        store_rows<DT>(in ? a.dk + (long long)n * a.ld_dk + kvh * a.d : nullptr, dk, a.alpha / (P_SCALE * kept), a.d, hf);
     } else if (n < a.rows_k) {
-        float* to = a.part + ((long long)id * a.rows_k + n) * 2 * a.d;
+        float*      to = a.part + ((long long)id * a.rows_k + n) * 2 * a.d;
+        const float k  = 1.f / (P_SCALE * kept);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int col = 32 * dt + 8 * e + 4 * hf;
                 if (col < a.d) {
-                    *reinterpret_cast<f32x4*>(to + col)       = f32x4{dk[dt][4 * e], dk[dt][4 * e + 1], dk[dt][4 * e + 2], dk[dt][4 * e + 3]};
+                    *reinterpret_cast<f32x4*>(to + col)       = f32x4{dk[dt][4 * e] * k, dk[dt][4 * e + 1] * k, dk[dt][4 * e + 2] * k, dk[dt][4 * e + 3] * k};
                     *reinterpret_cast<f32x4*>(to + a.d + col) = f32x4{dv[dt][4 * e], dv[dt][4 * e + 1], dv[dt][4 * e + 2], dv[dt][4 * e + 3]};
                 }
             }
@@ -939,7 +984,7 @@ static int part_heads(const mp_attn_desc* d) {
     const int group = d->n_heads / d->n_kv_heads;
     return (long long)((d->rows_k + MA_Q - 1) / MA_Q) * d->n_kv_heads >= 512 ? group : 1;
 }
-static size_t stats_bytes(const mp_attn_desc* d) { return (size_t)rows64(d->rows_q) * 64 * d->n_heads * 2 * sizeof(float); }
+static size_t stats_bytes(const mp_attn_desc* d) { return (size_t)rows64(d->rows_q) * 64 * d->n_heads * 3 * sizeof(float); }
 static size_t parts_bytes(const mp_attn_desc* d) {
     const int group = d->n_heads / d->n_kv_heads;
     return group == part_heads(d) ? 0 : (size_t)d->n_heads * d->rows_k * 2 * d->d_head * sizeof(float);
@@ -976,7 +1021,7 @@ extern "C" int mp_attention_masked_bwd(const mp_attn_desc* desc, const void* mas
     a.q = q, a.k = k, a.v = v, a.ctx = ctx, a.lse_in = lse, a.dctx = dctx, a.dq = dq, a.dk = dk, a.dv = dv;
     a.lse2  = static_cast<float*>(ws);
     a.delta = a.lse2 + (size_t)a.rows_pad * a.heads;
-    a.part  = a.delta + (size_t)a.rows_pad * a.heads;
+    a.part  = a.delta + (size_t)a.rows_pad * a.heads * 2;
     a.part_heads = part_heads(desc);
     if (d.rows_q > 0) {
         const long long wgs = (long long)((d.rows_q + MA_Q - 1) / MA_Q) * d.n_heads;

@@ -51,3 +51,56 @@ def test_what_is_visible_and_not_finite_is_felt(bad, cap, d, bias, heads, causal
             for name in ("ctx", "dq"):
                 assert torch.equal(clean[name][~see], got[name][~see]), (which, name)
             assert torch.equal(clean["lse"][:, ~see], got["lse"][:, ~see])
+
+
+def small_gradients(rows, heads, kv, d, size, ctx_of=0):
+    """Many keys of almost even weight, queries and gradients that point one way: every ds = p (dp - delta) is near size / rows."""
+    p = Problem(rows, heads, kv, d, seed=3, apart=True)
+    r = np.random.default_rng(4)
+    p.q, p.k, p.v = S16(1 + 0.1 * r.standard_normal(p.q.shape)), S16(0.02 * r.standard_normal(p.k.shape)), S16(r.standard_normal(p.v.shape))
+    p.do = S16(size * (1 + 0.1 * r.standard_normal(p.do.shape)))
+    for dev, host in zip(p.dev + [p.ddo], (p.q, p.k, p.v, p.do)):
+        dev[:, :host.shape[1]] = h16(host)
+    return p
+
+
+@pytest.mark.parametrize("rows,heads,kv,d", [(4096, 2, 2, 64), (4096, 2, 1, 128), (4096, 64, 64, 8)])
+def test_gradients_of_scores_below_the_end_of_fp16(rows, heads, kv, d):
+    """ds near 2^-27, whose sums over 4096 queries fp16 has.  Rounded to fp16 times 2^10, a ds is off by 2^-11 of itself and 2^-35 where
+    that is below fp16's normal range; delta by the rounding of ctx (2^-11 |ctx|) and its own of it; otherwise as the bounds of the
+    masked attention tests, whose scores' error E is below 2^-20 here."""
+    p = small_gradients(rows, heads, kv, d, 2.0 ** -15 / d ** 0.5).docs([0, rows]).run()
+    got = p.results()
+    T = lambda x, n: torch.from_numpy(np.asarray(x, np.float64)).cuda().view(-1, n, d).transpose(0, 1).contiguous()  # noqa: E731
+    q, k, v, do = T(p.q, heads), T(p.k, kv), T(p.v, kv), T(p.do, heads)
+    dk, mag = torch.zeros_like(k), torch.zeros_like(k)
+    for h in range(heads):
+        g = h // (heads // kv)
+        pr = torch.softmax(p.alpha * (q[h] @ k[g].T.contiguous()), 1)
+        ctx = pr @ v[g]
+        ds = pr * (do[h] @ v[g].T.contiguous() - (do[h] * ctx).sum(1, keepdim=True))
+        e = (2.0 ** -11 + 2.0 ** -17) * ds.abs() + 2.0 ** -35 + pr * ((do[h].abs() * (2.0 ** -10 * ctx.abs() + 2.0 ** -24)).sum(1, keepdim=True) + d * 2.0 ** -24 * (do[h].abs() @ v[g].abs().T.contiguous()))
+        dq, bound = p.alpha * ds @ k[g], p.alpha * e @ k[g].abs()
+        cols = slice(h * d, h * d + d)
+        assert torch.all((got["dq"][:, cols].double() - dq).abs() <= bound + 2.0 ** -11 * dq.abs() + 2.0 ** -25)
+        dk[g] += p.alpha * ds.T.contiguous() @ q[h]
+        mag[g] += p.alpha * e.T.contiguous() @ q[h].abs()
+        assert ds.abs().median() < 2.0 ** -25
+    got_dk = got["dk"].double().view(rows, kv, d).transpose(0, 1)
+    assert torch.all((got_dk - dk).abs() <= mag + 2.0 ** -11 * dk.abs() + 2.0 ** -25)
+    assert torch.all(mag + 2.0 ** -25 <= 0.25 * dk.abs().amax((1, 2), keepdim=True))       # (what the bound would let pass)
+
+
+@pytest.mark.parametrize("heads,kv,d", [(2, 1, 64), (2, 2, 128), (4, 1, 128), (512, 256, 40)])
+@pytest.mark.parametrize("cap", [0.0, 3.0])
+def test_gradients_of_scores_above_64(heads, kv, d, cap):
+    """Gradients so large that ds times 2^10 is beyond fp16, though ds is not: in some workgroups (keys and queries of one document) and
+    not in others."""
+    rows = 129 if heads > 4 else 400
+    p = Problem(rows, heads, kv, d, seed=heads, cap=cap, spread=2.0, apart=True)
+    p.do[: rows // 2] *= 256
+    p.ddo[:, :p.do.shape[1]] = h16(p.do)
+    p.docs([0, rows // 2, rows], causal=True).run().check()
+    first = {k: v.clone() for k, v in p.results().items()}
+    p.run()
+    assert all(torch.equal(first[k], v) for k, v in p.results().items())
