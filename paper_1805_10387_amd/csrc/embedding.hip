@@ -153,7 +153,8 @@ __device__ __forceinline__ void sort_steps(unsigned& x, unsigned& y, bool up, in
     }
 }
 
-// The first `runs` workgroups sort; the others clear dw (or copy add into it), in words and a last half word.
+// The first `runs` workgroups sort; the others clear dw (or copy add into it, or only look at an add that is dw), in words and a last
+// half word.
 __global__ __launch_bounds__(1024) void embedding_sort_kernel(int rows, int vocab, int runs, const int* __restrict__ tokens, u64* __restrict__ keys,
                                                               uint16_t* __restrict__ dw, const uint16_t* __restrict__ add, size_t n, mp_scale_state* st) {
     __shared__ uint2 s[2][SORT_RUN / 2];
@@ -165,14 +166,14 @@ __global__ __launch_bounds__(1024) void embedding_sort_kernel(int rows, int voca
         const auto   one  = [&](size_t i) {
             const uint16_t x = add ? add[i] : 0;
             bad |= half_nonfinite(x);
-            dw[i] = x;
+            if (add != dw) dw[i] = x;
         };
         for (size_t i = first; i < n8; i += step) {
             u32x4e x = {0u, 0u, 0u, 0u};
             if (add) x = *reinterpret_cast<const u32x4e_any*>(add + head + 8 * i);
 #pragma unroll
             for (int k = 0; k < 4; ++k) bad |= half_nonfinite((uint16_t)x[k]) || half_nonfinite((uint16_t)(x[k] >> 16));
-            q[i] = x;
+            if (add != dw) q[i] = x;
         }
         if (first < head) one(first);
         if (first < n - head - n8 * 8) one(head + n8 * 8 + first);
@@ -500,7 +501,7 @@ extern "C" int mp_embedding_bwd(int rows, int vocab, int d, const int32_t* token
     float*       part = reinterpret_cast<float*>(static_cast<char*>(ws) + 2 * keys_bytes(rows));
     const int    runs = (rows + SORT_RUN - 1) / SORT_RUN;
     const size_t n    = (size_t)vocab * d;
-    const bool   fill = add != dw;
+    const bool   fill = add != dw || st;  // (in place: rows without a token keep what they have, and it is looked at)
     const size_t want = (n + 8191) / 8192;
     const int    wgs  = runs + (fill ? (int)(want < FILL_WGS ? want : FILL_WGS) : 0);
     if (wgs == 0) return MP_OK;
