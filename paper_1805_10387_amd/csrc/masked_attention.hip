@@ -25,6 +25,7 @@
 // an infinite score becomes NaN before a cap or an exponential could make something finite of it.  Backward because a query that sees one
 // has a non-finite lse or delta, and its lse is made so low that its probabilities are infinite.
 #include "attn_lds.hpp"
+#include "mask_rule.hpp"
 
 #include <limits.h>
 #include <math.h>
@@ -76,14 +77,7 @@ __global__ __launch_bounds__(64) void mask_kernel(int rows, int rows_k, int n_do
                 b = min(last + part, b);
                 a = last;
             }
-            const int s = max(start[a], 0), e = min(start[b], rows);
-            lo = s;
-            hi = causal ? r + 1 : e;
-            if (prefix) hi = max(hi, min(e, s + min(prefix[a], rows)));
-            if (window) {
-                lo = max(lo, r - window + 1);
-                if (window < rows) hi = min(hi, r + window);
-            }
+            seen_in_document(r, max(start[a], 0), min(start[b], rows), causal, prefix != nullptr, prefix ? prefix[a] : 0, window, lo, hi);
         }
         if (lo >= hi) lo = hi = 0;
     }
