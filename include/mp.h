@@ -447,7 +447,7 @@ typedef struct mp_attn_desc {
  * What a row does not see does not reach it, NaN and infinities included.  A row that sees one has non-finite results: of a query or key
  * row that holds one (whatever its sign, capped or not) NaN in all of the row's ctx and lse, of a value row in ctx.  All rows of ctx are
  * written.  Any rows_k >= 0 and rows_q >= 0.
- * `mask` is one of rows_q rows.  16-byte aligned matrices with leading dimensions, a d_head and a cap as above; otherwise
+ * `mask` is one of rows_q rows; of intervals that reach beyond rows_k keys, these are seen.  16-byte aligned matrices with leading dimensions, a d_head and a cap as above; otherwise
  * MP_E_UNSUPPORTED. */
 int mp_attention_masked_fwd(const mp_attn_desc* desc /* host */, const void* mask, const mp_half* q, const mp_half* k,
                             const mp_half* v, const float* slopes, mp_half* ctx, float* lse, mp_stream stream);

@@ -168,9 +168,10 @@ struct QueryRange {
         } else {
             x.z = INT_MAX;  // rows behind the last one: not whole
         }
-        // (where nothing is seen, x.x is the largest number there is, and tiles are counted on from glo)
+        // (where nothing is seen, x.x is the largest number there is, and tiles are counted on from glo; a mask may have been made for more
+        // keys, and a tile that ends behind the last one is not whole)
         glo = __builtin_amdgcn_readfirstlane(min(max(x.x, 0), a.rows_k)), ghi = __builtin_amdgcn_readfirstlane(min(x.y, a.rows_k));
-        glo_max = __builtin_amdgcn_readfirstlane(x.z), ghi_min = __builtin_amdgcn_readfirstlane(x.w);
+        glo_max = __builtin_amdgcn_readfirstlane(x.z), ghi_min = __builtin_amdgcn_readfirstlane(min(x.w, a.rows_k));
     }
     __device__ __forceinline__ bool whole(int kb) const { return glo_max <= kb && ghi_min >= kb + MA_K; }
     __device__ __forceinline__ bool none(int kb) const { return wlo >= kb + MA_K || whi <= kb; }

@@ -104,3 +104,20 @@ def test_gradients_of_scores_above_64(heads, kv, d, cap):
     first = {k: v.clone() for k, v in p.results().items()}
     p.run()
     assert all(torch.equal(first[k], v) for k, v in p.results().items())
+
+
+@pytest.mark.parametrize("d,heads", [(64, 2), (128, 2), (40, 512)])
+@pytest.mark.parametrize("keys", [0, 1, 63, 64, 100, 130, 200, 299])
+def test_a_mask_made_for_more_keys(d, heads, keys):
+    """A mask of rows_q rows serves calls of fewer keys than it was made for: they see what of their intervals is there."""
+    rows = 300
+    p = Problem(rows, heads, heads // 2, d, seed=keys, keys=keys)
+    r = np.random.default_rng(keys)
+    lo = np.minimum(r.integers(0, 40, rows), 20) * (np.arange(rows) % 3 == 0)
+    hi = np.full(rows, 300) - r.integers(0, 30, rows) * (np.arange(rows) >= 128)
+    mp.mp_attention_mask_ranges(rows, 300, i32(lo), i32(hi), p.mask)
+    p.lo, p.hi = lo, np.minimum(hi, keys)
+    p.run().check()
+    p.docs([0, rows]).lo[:] = 0                     # one whole document of 300 rows, whose mask is made from the document
+    p.hi[:] = keys
+    p.run().check()
