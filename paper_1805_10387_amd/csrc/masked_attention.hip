@@ -99,29 +99,30 @@ __global__ __launch_bounds__(64) void mask_kernel(int rows, int rows_k, int n_do
 enum { PLAIN = 0, BIAS = 1, CAP = 2 };
 // Scores in place, to base 2 once they are multiplied by unit(): a factor that costs nothing beside the exponential's.  Lanes own one
 // index, registers the other; dist: query less key (or the reverse) at register 0.
-template <int MODE>
-__device__ __forceinline__ float unit(const AttnArgs& a) { return MODE & BIAS ? 1.f : (MODE == CAP ? a.cap : a.alpha) * LOG2E; }
-// SHOW: an infinite score of a mode with a cap becomes NaN.
-template <int MODE, bool SHOW = false>
+// FWD: a score whose cap made it finite becomes NaN.  Backward leaves tanh where there is a cap, and a bias beside it to exponent().
+template <int MODE, bool FWD>
+__device__ __forceinline__ float unit(const AttnArgs& a) { return MODE == CAP || (MODE & CAP && !FWD) ? a.cap * LOG2E : MODE == PLAIN ? a.alpha * LOG2E : 1.f; }
+template <int MODE, bool FWD>
 __device__ __forceinline__ void scores(const AttnArgs& a, f32x16& s, float slope2, int dist) {
     if (MODE == PLAIN) return;
     const float k = MODE & CAP ? a.alpha / a.cap * (2.f * LOG2E) : a.alpha * LOG2E, c = a.cap * LOG2E, at = (float)dist;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
         // tanh(x) = 1 - 2 / (exp(2x) + 1): an absolute error of 1e-7, which is what counts for a score
-        if (MODE & CAP) s[r] = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[r] * k) + 1.f), SHOW ? fmaf(s[r], 0.f, 1.f) : 1.f);
+        if (MODE & CAP) s[r] = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[r] * k) + 1.f), FWD ? fmaf(s[r], 0.f, 1.f) : 1.f);
         else s[r] *= k;
-        if (MODE == (CAP | BIAS)) s[r] *= c;
-        if (MODE & BIAS) s[r] = fmaf(-slope2, fabsf(at + (float)(8 * (r >> 2) + (r & 3))), s[r]);
+        if (MODE == (CAP | BIAS) && FWD) s[r] *= c;
+        if (MODE == BIAS || (MODE & BIAS && FWD)) s[r] = fmaf(-slope2, fabsf(at + (float)(8 * (r >> 2) + (r & 3))), s[r]);
     }
 }
-// d s / d (alpha q k^T) = 1 - tanh^2, out of the score itself (which is cheaper than a register that keeps tanh); 0 for a hidden one's -inf.
+// Backward: log2 of a probability (times P_SCALE) from what scores() left of register r.
 template <int MODE>
-__device__ __forceinline__ float fade(const AttnArgs& a, float s, float slope2, float dist) {
-    if (!(MODE & CAP)) return 1.f;
-    const float t = MODE & BIAS ? fmaf(slope2, fabsf(dist), s) * (1.f / (a.cap * LOG2E)) : s;
-    return fmaxf(fmaf(-t, t, 1.f), 0.f);
+__device__ __forceinline__ float exponent(float s, float c, float lse2, float slope2, float at, int r) {
+    return fmaf(s, c, MODE == (CAP | BIAS) ? fmaf(-slope2, fabsf(at + (float)(8 * (r >> 2) + (r & 3))), -lse2) : -lse2);
 }
+// d s / d (alpha q k^T) = 1 - tanh^2; 0 for a hidden score's -inf.  (tanh out of a score that holds a bias as well would be off by that
+// one's rounding over the cap.)
+__device__ __forceinline__ float fade(float tanh) { return fmaxf(fmaf(-tanh, tanh, 1.f), 0.f); }
 
 // ------------------------------------------------------------------------------------------------ tiles
 __device__ __forceinline__ f32x16 zero16() { return f32x16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}; }
@@ -250,7 +251,7 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void masked_fwd_kernel(AttnArgs a) 
     f16x8 qf[KK];
     row_frags<KK>(qf, m < a.rows_q ? a.q + (long long)m * a.ld_q + h * a.d : nullptr, a.d, hf);
     const float slope2 = MODE && a.slopes ? a.slopes[h] * LOG2E : 0.f;
-    const float c      = unit<MODE>(a);  // scores to base 2
+    const float c      = unit<MODE, true>(a);  // scores to base 2
     f32x16      o[DT];
     float       ref = -INFINITY, sum = 0.f;
 #pragma unroll
@@ -401,7 +402,7 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void masked_dq_kernel(AttnArgs a) {
     row_frags<KK>(qf, m < a.rows_q ? a.q + (long long)m * a.ld_q + h * a.d : nullptr, a.d, hf);
     row_frags<KK>(gf, m < a.rows_q ? a.dctx + (long long)m * a.ld_dctx + h * a.d : nullptr, a.d, hf);
     const float slope2 = MODE && a.slopes ? a.slopes[h] * LOG2E : 0.f;
-    const float c      = unit<MODE>(a);
+    const float c      = unit<MODE, false>(a);
     float       lse2 = INFINITY, delta = 0.f;
     if (m < a.rows_q) {
         lse2 = a.lse_in[(long long)h * a.rows_q + m] * LOG2E;
@@ -495,21 +496,22 @@ again:
             }
         };
         const auto weights = [&](int u, int first, int last) {  // ds of pairs of keys
+            const float at = (float)(kb + 32 * u + 4 * hf - m);
 #pragma unroll
             for (int e = first; e < last; ++e) {
                 float d[2];
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
                     const int   r = 2 * e + y;
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -lse2));  // (times P_SCALE)
+                    const float p = __builtin_amdgcn_exp2f(exponent<MODE>(s[u][r], c, lse2, slope2, at, r));  // (times P_SCALE)
                     d[y] = p * fmaf(dp[u][r], kept, -delta);
-                    if (MODE & CAP) d[y] *= fade<MODE>(a, s[u][r], slope2, (float)(kb + 32 * u + 4 * hf - m + 8 * (r >> 2) + (r & 3)));
+                    if (MODE & CAP) d[y] *= fade(s[u][r]);
                 }
                 ds[u][e] = pack_f16(d[0], d[1]);
             }
         };
         const auto prepare = [&](int u) {
-            scores<MODE>(a, s[u], slope2, kb + 32 * u + 4 * hf - m);
+            scores<MODE, false>(a, s[u], slope2, kb + 32 * u + 4 * hf - m);
             if (!all) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[u][r] = (unsigned)(n0 + 32 * u + 8 * (r >> 2) + (r & 3)) < len ? s[u][r] : -INFINITY;
@@ -646,7 +648,7 @@ __global__ __launch_bounds__(256 * SPLIT, D <= 64 ? 2 : 1) void masked_dkv_kerne
     f32x16 dk[DT], dv[DT];
     settle<KK>(kf);
     settle<KK>(vf);
-    const float c = unit<MODE>(a);
+    const float c = unit<MODE, false>(a);
 
     const unsigned at_q = lds_address(tiles_of[team][0][0]) + Tile::plain(lane), at_g = at_q + SIZE;
     const unsigned at_tq = lds_address(tiles_of[team][0][0]) + Tile::across(lane), at_tg = at_tq + SIZE;
@@ -730,6 +732,7 @@ again:
             }
         };
         const auto weights = [&](int u, int part) {  // probabilities and ds
+            const float at = (float)(m0 + 32 * u + 4 * hf - n);
 #pragma unroll
             for (int e = 4 * part / PARTS; e < 4 * (part + 1) / PARTS; ++e) {
                 const int   i0 = 32 * u + 8 * e + 4 * hf;
@@ -738,9 +741,9 @@ again:
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     const int r = 4 * e + x;
-                    p[x]        = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -l4[x]));  // (P_SCALE is in it)
+                    p[x]        = __builtin_amdgcn_exp2f(exponent<MODE>(s[u][r], c, l4[x], slope2, at, r));  // (P_SCALE is in it)
                     d[x]        = p[x] * fmaf(dp[u][r], kept, -d4[x]);
-                    if (MODE & CAP) d[x] *= fade<MODE>(a, s[u][r], slope2, (float)(m0 + 32 * u + 4 * hf - n + 8 * e + x));
+                    if (MODE & CAP) d[x] *= fade(s[u][r]);
                 }
                 pk[u][2 * e]      = pack_f16(p[0], p[1]);
                 pk[u][2 * e + 1]  = pack_f16(p[2], p[3]);
@@ -749,7 +752,7 @@ again:
             }
         };
         const auto prepare = [&](int u) {
-            scores<MODE>(a, s[u], slope2, m0 + 32 * u + 4 * hf - n);
+            scores<MODE, false>(a, s[u], slope2, m0 + 32 * u + 4 * hf - n);
             if (!all) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[u][r] = seen[u] >> r & 1 ? s[u][r] : -INFINITY;

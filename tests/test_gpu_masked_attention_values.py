@@ -121,3 +121,16 @@ def test_a_mask_made_for_more_keys(d, heads, keys):
     p.docs([0, rows]).lo[:] = 0                     # one whole document of 300 rows, whose mask is made from the document
     p.hi[:] = keys
     p.run().check()
+
+
+@pytest.mark.parametrize("d,heads,rows", [(64, 2, 130), (128, 2, 130), (40, 512, 130)])
+@pytest.mark.parametrize("cap", [0.02, 1.0])
+def test_capped_scores_under_a_large_bias(d, heads, rows, cap):
+    """Keys some thousands of rows away, whose bias is 10^3 to 10^5 caps: what the cap leaves of a gradient does not come out of their sum."""
+    keys = 6000 if heads == 2 else 1500
+    p = Problem(rows, heads, heads // 2, d, seed=d, keys=keys, cap=cap, bias=heads == 2, spread=cap)
+    if heads > 2:
+        p.slopes = np.float32(0.5 / (1 + np.arange(heads) % 7))
+        p.dslopes = f32(p.slopes)
+    lo = keys - 60 + np.arange(rows) % 50
+    p.ranges(lo, lo + 1 + np.arange(rows) % 8).run().check()
