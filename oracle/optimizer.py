@@ -179,7 +179,7 @@ def unscale_check_update8(P: Policy, tensors: List[Dict[str, np.ndarray]], opt, 
         root = np.sqrt(v)
         w = w - (rate * m) / (root * rbc2 + A(opt.eps))
         tn["w32"][...] = w.reshape(tn["w32"].shape)
-        unbiased = opt.state_bits == 8
+        unbiased = getattr(opt, "state_bits", 32) == 8
         tn["m8"][...], tn["ms"][...], tn["v8"][...], tn["vs"][...] = state8_encode_unbiased(P, m, root, t) if unbiased else state8_encode(P, m, root)
         tn["w16"][...] = P.store(tn["w32"])
     return 0

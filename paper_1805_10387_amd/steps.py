@@ -84,7 +84,7 @@ class ParamStore:
 
 class _StepBase:
     def __init__(self, masters: Dict[str, np.ndarray], opt, scale_cfg, prechecked: bool = False, flat_update: bool = False):
-        self.P = ParamStore(masters, adam=opt.kind in ("adam", "adamw"), state_bits=opt.state_bits)
+        self.P = ParamStore(masters, adam=opt.kind in ("adam", "adamw"), state_bits=getattr(opt, "state_bits", 32))
         self.cfg = B.opt_cfg(opt.kind, opt.lr, opt.beta1, opt.beta2, opt.eps, opt.weight_decay)
         self.st = B.scale_state_alloc()
         mode = ML.MP_SCALE_BACKOFF if scale_cfg.mode == "backoff" else ML.MP_SCALE_STATIC

@@ -1,0 +1,31 @@
+"""What the step classes make of their arguments before anything is on a device (no GPU)."""
+from dataclasses import replace
+from types import SimpleNamespace
+
+import numpy as np
+import pytest
+
+import mp_inputs as I
+from paper_1805_10387_amd import steps as St
+
+
+class Stop(Exception):
+    pass
+
+
+def made(monkeypatch, opt):
+    """(adam, state_bits) that a step with this optimizer asks its parameters' store for."""
+    def store(masters, adam, state_bits=32):
+        raise Stop(adam, state_bits)
+    monkeypatch.setattr(St, "ParamStore", store)
+    with pytest.raises(Stop) as e:
+        St._StepBase({}, opt, I.ScaleCfg())
+    return e.value.args
+
+
+def test_an_optimizer_that_knows_no_state_bits(monkeypatch):
+    """An object of the caller's own with the fields that there were before moments in 8 bits."""
+    for kind, adam in (("sgd", False), ("adam", True), ("adamw", True)):
+        opt = SimpleNamespace(kind=kind, lr=0.1, beta1=0.9, beta2=0.99, eps=1e-8, weight_decay=0.0)
+        assert made(monkeypatch, opt) == (adam, 32)
+    assert made(monkeypatch, I.OptCfg(kind="adamw", state_bits=8)) == (True, 8)
