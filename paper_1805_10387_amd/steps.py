@@ -198,6 +198,9 @@ class TransformerStep(_StepBase):
     vocabulary takes tokens and trains their embedding."""
 
     def __init__(self, wl, masters=None, two_streams=False, fused_attention=True, grouped_dw=True, **kw):
+        self.masked = wl.causal or wl.n_docs > 0
+        if self.masked:
+            self.d_att, att_ws = self._masked_attention(wl)
         if masters is None:
             masters = wl.embedding()
             masters.update({f"l{i}.{k}": v for i, lay in enumerate(wl.masters()) for k, v in lay.items()})
@@ -207,7 +210,6 @@ class TransformerStep(_StepBase):
         dk_ = wl.d_model // wl.n_heads
         # the fused attention kernels cover head size 64 and sequences up to 128; anything else runs the unfused chain of
         # batched products and softmax kernels (two base layers on 61 sentences of 53 tokens: 671 us that way, 613 us fused)
-        self.masked = wl.causal or wl.n_docs > 0
         self.fused_attention = fused_attention and dk_ == 64 and wl.seq_len <= 128 and not self.masked
         self.ld_p = (wl.seq_len + 7) // 8 * 8 if self.fused_attention else wl.seq_len    # rows of the kept probabilities
         self.alpha = 1.0 / math.sqrt(dk_)
@@ -264,11 +266,10 @@ class TransformerStep(_StepBase):
         need = [B.mp_gemm_bwd_dw_workspace_bytes(x, True) for x in (self.d_qkv, self.d_o, self.d_f1, self.d_f2)]
         need.append(B.mp_layernorm_bwd_workspace_bytes(T, d))
         if self.masked:
-            self.d_att = B.attn_desc(T, T, h, h, dk, ld_q=3 * d, ld_k=3 * d, ld_v=3 * d, alpha=alpha)
             self.mask = torch.zeros(B.mp_attention_mask_bytes(T) // 4, dtype=torch.int32, device="cuda")
             self.n_docs = wl.n_docs or NB
             self.doc_start = torch.arange(0, T + 1, S, dtype=torch.int32, device="cuda")
-            need.append(B.mp_attention_masked_bwd_workspace_bytes(self.d_att))
+            need.append(att_ws)
         else:
             need += [B.mp_gemm_bwd_dw_workspace_bytes(self.d_s, False), B.mp_gemm_bwd_dw_workspace_bytes(self.d_c, False)]
         if wl.vocab:
@@ -282,6 +283,16 @@ class TransformerStep(_StepBase):
             n = B.mp_layernorm_bwd_workspace_bytes(T, d) // 4
             self.ln_parts = [[e32(n), e32(n)] for _ in range(2)]
             self.ln_nparts = B.mp_layernorm_bwd_nparts(T, d)
+
+    @staticmethod
+    def _masked_attention(wl):
+        """Description and workspace size of the attention calls; a workload that they refuse is refused here."""
+        dk, ld = wl.d_model // wl.n_heads, 3 * wl.d_model
+        desc = B.attn_desc(wl.tokens, wl.tokens, wl.n_heads, wl.n_heads, dk, ld_q=ld, ld_k=ld, ld_v=ld, alpha=1.0 / math.sqrt(dk))
+        size = B.mp_attention_masked_bwd_workspace_bytes(desc)
+        if size == 0:
+            raise ValueError("a causal or packed workload of this shape: " + ML.load().mp_last_error().decode(errors="replace"))
+        return desc, size
 
     def set_batch(self, batch):
         wl = self.wl

@@ -29,3 +29,18 @@ def test_an_optimizer_that_knows_no_state_bits(monkeypatch):
         opt = SimpleNamespace(kind=kind, lr=0.1, beta1=0.9, beta2=0.99, eps=1e-8, weight_decay=0.0)
         assert made(monkeypatch, opt) == (adam, 32)
     assert made(monkeypatch, I.OptCfg(kind="adamw", state_bits=8)) == (True, 8)
+
+
+@pytest.mark.parametrize("kw,says", [(dict(d_model=160, n_heads=8), "head size 20"), (dict(d_model=288, n_heads=2), "head size 144")])
+@pytest.mark.parametrize("mask", [dict(causal=True), dict(n_docs=3)])
+def test_a_head_size_without_a_kernel_is_refused_when_the_step_is_made(monkeypatch, kw, says, mask):
+    """Not at its first iteration; without a mask the unfused chain takes any head size."""
+    def store(masters, adam, state_bits=32):
+        raise Stop()
+    monkeypatch.setattr(St, "ParamStore", store)
+    wl = replace(I.C2_SMALL, **kw)
+    with pytest.raises(ValueError, match=says):
+        St.TransformerStep(replace(wl, **mask), masters={})
+    for ok in (wl, replace(I.C2_SMALL, **mask)):
+        with pytest.raises(Stop):
+            St.TransformerStep(ok, masters={})
