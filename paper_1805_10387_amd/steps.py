@@ -296,15 +296,14 @@ class TransformerStep(_StepBase):
 
     def set_batch(self, batch):
         wl = self.wl
+        if wl.n_docs and np.shape(batch["doc_start"]) != (wl.n_docs + 1,):   # (before anything of the last batch is replaced)
+            raise ValueError(f"{tuple(np.shape(batch['doc_start']))} document starts for {wl.n_docs} documents")
         if wl.vocab:
             self.tokens.copy_(_i32(batch["tokens"]))
         else:
             self.x0.copy_(_h16(batch["x"]))
         if wl.n_docs:
-            starts = _i32(batch["doc_start"])
-            if starts.shape != (wl.n_docs + 1,):
-                raise ValueError(f"{tuple(starts.shape)} document starts for {wl.n_docs} documents")
-            self.doc_start = starts
+            self.doc_start = _i32(batch["doc_start"])
         if self.masked:
             B.mp_attention_mask_docs(wl.tokens, self.n_docs, self.doc_start, self.mask, causal=wl.causal)
         self.target.copy_(_h16(batch["target"]))

@@ -44,3 +44,12 @@ def test_a_head_size_without_a_kernel_is_refused_when_the_step_is_made(monkeypat
     for ok in (wl, replace(I.C2_SMALL, **mask)):
         with pytest.raises(Stop):
             St.TransformerStep(ok, masters={})
+
+
+def test_a_batch_that_does_not_fit_replaces_nothing():
+    step = St.TransformerStep.__new__(St.TransformerStep)
+    step.wl = replace(I.C2_SMALL, n_docs=4, vocab=11)          # (nothing else is there: whatever set_batch did would fail)
+    batch = step.wl.batch()
+    for starts in (np.array([0, 9], np.int32), np.zeros((5, 1), np.int32), [0, 1, 2, 3]):
+        with pytest.raises(ValueError, match="document starts for 4"):
+            step.set_batch(dict(batch, doc_start=starts))
