@@ -447,8 +447,9 @@ typedef struct mp_attn_desc {
  * What a row does not see does not reach it, NaN and infinities included.  A row that sees one has non-finite results: of a query or key
  * row that holds one (whatever its sign, capped or not) NaN in all of the row's ctx and lse, of a value row in ctx.  All rows of ctx are
  * written.  Any rows_k >= 0 and rows_q >= 0.
- * `mask` is one of rows_q rows; of intervals that reach beyond rows_k keys, these are seen.  16-byte aligned matrices with leading dimensions, a d_head and a cap as above; otherwise
- * MP_E_UNSUPPORTED. */
+ * `mask` is one of rows_q rows; of intervals that reach beyond rows_k keys, these are seen.  n_heads (rows_q + 128) and
+ * n_heads (rows_k + 128) below 2^31, otherwise MP_E_INVAL.  16-byte aligned matrices with leading dimensions, a d_head and a cap as
+ * above; otherwise MP_E_UNSUPPORTED. */
 int mp_attention_masked_fwd(const mp_attn_desc* desc /* host */, const void* mask, const mp_half* q, const mp_half* k,
                             const mp_half* v, const float* slopes, mp_half* ctx, float* lse, mp_stream stream);
 
@@ -468,7 +469,7 @@ int mp_attention_masked_bwd(const mp_attn_desc* desc /* host */, const void* mas
  * Embedding: rows of a table w[vocab, d] by token (the other end of the vocabulary projection).
  * ------------------------------------------------------------------------------------------ */
 /* y[t] = RNE16(scale w[tokens[t]]); a token outside [0, vocab) gives a zero row.  w, y contiguous, at any element.  tokens: device
- * int32 [rows].  Up to 2^39 elements of y. */
+ * int32 [rows].  rows ceil(d / 8) up to 2^32 - 256; otherwise MP_E_INVAL. */
 int mp_embedding_fwd(int rows, int vocab, int d, const int32_t* tokens, const mp_half* w, float scale, mp_half* y,
                      mp_stream stream);
 
@@ -692,7 +693,8 @@ int mp_unscale_check_update8(const mp_tensor_desc8* tensors /* host */, int nten
                              mp_scale_state* st, int flags, mp_stream stream);
 int mp_unscale_check_update8_end(const mp_tensor_desc8* tensors /* host */, int ntensors, const mp_opt_cfg* cfg, mp_scale_state* st,
                                  int flags, const mp_mean_parts* parts, float* loss, int32_t* counters, mp_stream stream);
-/* The values that n codes stand for, in fp32 (either pair of outputs and codes may be NULL).  n counts from a block's first element. */
+/* The values that n codes stand for, in fp32 (either pair of outputs and codes may be NULL).  n counts from a block's first element, up
+ * to 2^34 - 1024 of them. */
 int mp_state8_decode(size_t n, const int8_t* m8, const float* ms, const uint8_t* v8, const float* vs, float* m, float* v,
                      mp_stream stream);
 

@@ -32,6 +32,8 @@ int  hip_fail(hipError_t e, const char* what);
 // be NULL) if a stored value is non-finite.  Defined beside the column-sum kernels (glue.hip).
 int finish_colsum_launch(const float* part, int nparts, int cols, mp_half* db, mp_scale_state* st, hipStream_t hs);
 
+// A dispatch counts its work items in 32 bits.
+static inline bool grid_fits(long long workgroups, int threads) { return workgroups * threads < (1ll << 32); }
 static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 static inline hipStream_t as_stream(mp_stream s) { return reinterpret_cast<hipStream_t>(s); }
 

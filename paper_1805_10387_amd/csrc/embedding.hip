@@ -436,11 +436,12 @@ static int chunk_of(int rows, int d) {
 }
 static long long chunks_of(int rows, int d) { return ((long long)rows + chunk_of(rows, d) - 1) / chunk_of(rows, d); }
 
+static long long sum_wgs(int rows, int d) { return (chunks_of(rows, d) * pieces_of(d) + EMB_THREADS - 1) / EMB_THREADS; }
+
 static int launch_sums(int rows, int vocab, int d, const u64* keys, const mp_half* dy, float scale, const mp_half* add, mp_half* dw, float* part,
                        mp_scale_state* st, hipStream_t hs) {
     const int       pieces = pieces_of(d);
-    const long long wgs    = (chunks_of(rows, d) * pieces + EMB_THREADS - 1) / EMB_THREADS;
-    MP_REQUIRE(wgs < (1ll << 31), "mp_embedding_bwd: too many rows and columns");
+    const long long wgs    = sum_wgs(rows, d);
     const dim3 grid((unsigned)wgs), block(EMB_THREADS);
     const auto sums = d < 8 ? embedding_sum_kernel<true> : embedding_sum_kernel<false>;
     const auto join = d < 8 ? embedding_join_kernel<true> : embedding_join_kernel<false>;
@@ -468,7 +469,7 @@ extern "C" int mp_embedding_fwd(int rows, int vocab, int d, const int32_t* token
     MP_REQUIRE(((reinterpret_cast<uintptr_t>(w) | reinterpret_cast<uintptr_t>(y)) & 1) == 0, "mp_embedding_fwd: w or y is not element-aligned");
     const int       pieces = pieces_of(d);
     const long long wgs    = ((long long)rows * pieces + EMB_THREADS - 1) / EMB_THREADS;
-    MP_REQUIRE(wgs < (1ll << 31), "mp_embedding_fwd: too many rows and columns");
+    MP_REQUIRE(grid_fits(wgs, EMB_THREADS), "mp_embedding_fwd: too many rows and columns");
     hipLaunchKernelGGL(d < 8 ? embedding_fwd_kernel<true> : embedding_fwd_kernel<false>, dim3((unsigned)wgs), dim3(EMB_THREADS), 0, as_stream(stream), rows,
                        vocab, d, pieces, tokens, w, scale, y);
     MP_LAUNCH_CHECK("mp_embedding_fwd");
@@ -491,6 +492,7 @@ extern "C" int mp_embedding_bwd(int rows, int vocab, int d, const int32_t* token
         set_error("mp_embedding_bwd: more than 2^24 rows or a vocabulary of 2^21 or more (%d, %d)", rows, vocab);
         return MP_E_UNSUPPORTED;
     }
+    MP_REQUIRE(grid_fits(sum_wgs(rows, d), EMB_THREADS), "mp_embedding_bwd: too many rows and columns");
     if (!ws || !aligned16(ws) || ws_bytes < mp_embedding_bwd_workspace_bytes(rows, vocab, d)) {
         set_error("mp_embedding_bwd: workspace missing, misaligned or smaller than mp_embedding_bwd_workspace_bytes");
         return MP_E_WORKSPACE;

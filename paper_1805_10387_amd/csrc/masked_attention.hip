@@ -863,7 +863,7 @@ static int check_desc(const char* who, const mp_attn_desc* d) {
     const long long w = (long long)d->n_heads * d->d_head, wk = (long long)d->n_kv_heads * d->d_head;
     MP_REQUIRE(w < (1 << 24), "%s: too many heads", who);
     MP_REQUIRE(d->rows_q <= 0x7FFFFF00 && d->rows_k <= 0x7FFFFF00, "%s: too many rows", who);
-    MP_REQUIRE(((long long)d->rows_q + MA_Q) / MA_Q * d->n_heads < (1ll << 31) && ((long long)d->rows_k + MA_Q) / MA_Q * d->n_heads < (1ll << 31),
+    MP_REQUIRE(grid_fits(((long long)d->rows_q + MA_Q) / MA_Q * d->n_heads, 256) && grid_fits(((long long)d->rows_k + MA_Q) / MA_Q * d->n_heads, 256),
                "%s: too many rows and heads", who);
     MP_REQUIRE(d->ld_q >= w && d->ld_k >= wk && d->ld_v >= wk && d->ld_ctx >= w, "%s: a leading dimension is smaller than its rows", who);
     if (((d->ld_q | d->ld_k | d->ld_v | d->ld_ctx) & 7) || (d->ld_q | d->ld_k | d->ld_v | d->ld_ctx) >= (1 << 22)) {

@@ -810,7 +810,7 @@ extern "C" int mp_unscale_check_update8_end(const mp_tensor_desc8* tensors, int 
 }
 
 extern "C" int mp_state8_decode(size_t n, const int8_t* m8, const float* ms, const uint8_t* v8, const float* vs, float* m, float* v, mp_stream stream) {
-    MP_REQUIRE(n < (1ull << 40), "mp_state8_decode: too large");
+    MP_REQUIRE(n < (1ull << 40) && grid_fits((long long)((n + UPD_PIECE - 1) / UPD_PIECE), UPD_THREADS), "mp_state8_decode: too large");
     MP_REQUIRE((!m || (m8 && ms)) && (!v || (v8 && vs)), "mp_state8_decode: an output without its codes and scales");
     const uintptr_t words = reinterpret_cast<uintptr_t>(m) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(ms) | reinterpret_cast<uintptr_t>(vs);
     MP_REQUIRE((words & 3) == 0, "mp_state8_decode: outputs or scales are not element-aligned");
