@@ -9,10 +9,13 @@
 //
 // Bound: the matrix cores and the vector work of the scores beside them for long rows; for short ones the chain of a workgroup's start
 // (range, first tiles, first product: a kernel whose workgroups have one tile takes 5.5 us).  8 heads of 128 over 2, 12289 causal
-// rows: forward 360 us (0.86 PFLOP/s of the 1.19 that a library product of 8192^3 reaches here), dq 511 us (0.91), dk and dv 810 us
-// (0.76).  16 heads of 64, 8192 rows in 15 documents: 49, 59 and 78 us (0.26 PFLOP/s of what is visible, to which the tiles add 16 %).
+// rows: forward (2 products) 358 to 374 us, backward 1220 to 1265, one call after the other; by the profiler, which holds launches apart,
+// 389 us (0.80 PFLOP/s of the 1.19 that a library product of 8192^3 reaches here), dq (3 products) 496 (0.94), dk and dv (4) 803 (0.77).
+// 16 heads of 64, 8192 rows in 15 documents: 50, 60 and 85 us by the profiler (0.30 PFLOP/s of what is visible, to which the tiles
+// add 16 %).
 // 32 x 32 tiles of 16 deep are the widest matrix instructions; 128 rows of own, 64 of the other side, and fragments of tiles in LDS
-// (filled by loads that pass the registers by, one tile ahead) keep the operands of two tiles and the results in 256 registers.
+// (filled by loads that pass the registers by, one tile ahead) keep the operands of two tiles and the results in 256 registers; dk and dv
+// of heads above 64 take 60 to 170 more, and so have one wave a SIMD.
 //
 // Masks: query r sees keys [lo, hi).  Whether a tile of pairs is empty, whole or neither follows from four numbers of a 64-row tile
 // (least lo, greatest hi, greatest lo, least hi) that the mask keeps behind the rows' own; only tiles that are neither look at

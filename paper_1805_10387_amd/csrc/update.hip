@@ -410,7 +410,7 @@ __device__ __forceinline__ void encode4_unbiased(const float* m, const float* r,
 
 // As above; a wave's 64 x 4 elements are one block of codes, whose scales are the wave's maxima.  Bound by HBM: 75.6 M parameters in 3 launches
 // 253 us (4.8 TB/s; 326 us while every code took correctly rounded roots, which kept the vector units as busy as memory).  Without the
-// inspection 228 us, 280 with codes rounded without bias: their hashes and thresholds are vector work again.
+// inspection 229 us, 272 to 282 with codes rounded without bias: their hashes and thresholds are vector work again.
 template <int KIND, int ITERS, bool UNBIASED>
 __device__ __forceinline__ void update_share(const UpdBatch8<UNBIASED>& b, const UpdScalars& s, const mp_scale_state* st) {
     static_assert(64 * UPD_VEC == MP_STATE8_BLOCK, "a wave takes one block of codes at a time");
