@@ -445,8 +445,8 @@ typedef struct mp_attn_desc {
  * has ctx 0 and lse -inf.  Scores stay fp32; the exponentials enter the second product rounded to fp16, unnormalised (relative to a
  * maximum that may lag by a factor of 2^8: none is above that, the row's largest not below 1).
  * What a row does not see does not reach it, NaN and infinities included.  A row that sees one has non-finite results: of a query or key
- * row that holds one (whatever its sign, capped or not) NaN in all of the row's ctx and lse, of a value row in ctx.  All rows of ctx are
- * written.  Any rows_k >= 0 and rows_q >= 0.
+ * row that holds one (whatever its sign, capped or not) NaN in all of the row's ctx and lse, of a value row in ctx, and then in its dq.
+ * All rows of ctx are written; it may not overlap an input.  Any rows_k >= 0 and rows_q >= 0.
  * `mask` is one of rows_q rows; of intervals that reach beyond rows_k keys, these are seen.  n_heads (rows_q + 128) and
  * n_heads (rows_k + 128) below 2^31, otherwise MP_E_INVAL.  16-byte aligned matrices with leading dimensions, a d_head and a cap as
  * above; otherwise MP_E_UNSUPPORTED. */

@@ -9,7 +9,7 @@ pytestmark = pytest.mark.gpu
 import paper_1805_10387_amd as mp
 from oracle import MIXED
 from gpu_util import *
-from test_gpu_masked_attention import Problem, documents
+from test_gpu_masked_attention import Problem
 
 S16 = MIXED.store
 
@@ -53,7 +53,7 @@ def test_what_is_visible_and_not_finite_is_felt(bad, cap, d, bias, heads, causal
             assert torch.equal(clean["lse"][:, ~see], got["lse"][:, ~see])
 
 
-def small_gradients(rows, heads, kv, d, size, ctx_of=0):
+def small_gradients(rows, heads, kv, d, size):
     """Many keys of almost even weight, queries and gradients that point one way: every ds = p (dp - delta) is near size / rows."""
     p = Problem(rows, heads, kv, d, seed=3, apart=True)
     r = np.random.default_rng(4)
