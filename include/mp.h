@@ -6,11 +6,11 @@
  * fp32 master weights; Section 3.2: the optimizer wrapper; Section 3.3:
  * regularisation on the fp32 copy):
  *
- *   forward  : mp_gemm_fwd[_ws] (+ mp_layernorm_fwd, mp_attention_fwd | mp_attention_masked_fwd | mp_softmax_fwd,
- *              mp_embedding_fwd, mp_lstm_cell_fwd | mp_lstm_layer_fwd)
- *   loss     : mp_mse_scaled | mp_softmax_xent_scaled[_db] (seed gradient x loss scale)
+ *   forward  : mp_gemm_fwd[_ws] (+ mp_layernorm_fwd, mp_qk_norm_rope_fwd, mp_attention_fwd | mp_attention_masked_fwd |
+ *              mp_softmax_fwd, mp_embedding_fwd, mp_lstm_cell_fwd | mp_lstm_layer_fwd, mp_token_logprobs)
+ *   loss     : mp_mse_scaled | mp_softmax_xent_scaled[_db] | mp_distill_scaled | mp_token_logprobs_bwd (seed gradient x loss scale)
  *   backward : mp_gemm_bwd_dx[_ws], mp_gemm_bwd_dw | mp_gemm_bwd_dw_grouped (+ mp_layernorm_bwd,
- *              mp_attention_bwd | mp_attention_masked_bwd | mp_softmax_bwd, mp_embedding_bwd,
+ *              mp_attention_bwd | mp_attention_masked_bwd | mp_softmax_bwd, mp_qk_norm_rope_bwd, mp_embedding_bwd,
  *              mp_lstm_cell_bwd | mp_lstm_layer_bwd, mp_colsum)
  *   update   : mp_unscale_check_update[8] (inspect fp16 gradients, unscale, SGD/Adam/AdamW on fp32
  *                                         masters, rewrite the fp16 copies - or skip; 8: moments in 8 bits)
@@ -341,6 +341,63 @@ int mp_softmax_xent_scaled_parts(int rows, int vocab, const mp_half* logits, int
                                  size_t ws_bytes, mp_mean_parts* parts, mp_stream stream);
 
 /* ------------------------------------------------------------------------------------------
+ * What a model says of given tokens, and learning from a larger one (fp32 islands of Section 3.2; seed gradients of Section 3.1 item 1).
+ * ------------------------------------------------------------------------------------------ */
+#define MP_TOP_MAX   128       /* alternatives of a row, classes of a teacher's list */
+#define MP_VOCAB_MAX (1 << 20) /* classes of these calls */
+
+/* z = inv_temperature float(logits), per row in fp32:
+ *     lse = log sum exp z,   logp = z[target] - lse (0 for a target outside [0, vocab)),   entropy = lse - sum softmax(z) z
+ *     top_ids, top_logp [rows, top]: the `top` classes of the largest logits in descending order, equal ones (0 and -0 are) by the lower
+ *     index, and their z - lse.
+ * logits: device fp16, rows ld apart, at any element.  targets, logp: both or neither.  entropy, lse: each may be NULL.  top: 0 (then
+ * top_ids and top_logp NULL) to MP_TOP_MAX and to vocab.  inv_temperature: 2^-8 to 2^8.  A logit of -inf is a class that cannot be.
+ * Rows with NaN or +inf, or without a finite logit, have NaN (in the last case lse -inf); their top_ids are in order all the same, NaN
+ * first.  vocab up to MP_VOCAB_MAX and top up to MP_TOP_MAX, otherwise MP_E_UNSUPPORTED.
+ *   ws    device, 16-byte aligned, mp_token_logprobs_workspace_bytes(rows, vocab, top) bytes (0: NULL is fine). */
+size_t mp_token_logprobs_workspace_bytes(int rows, int vocab, int top);
+int mp_token_logprobs(int rows, int vocab, int top, const mp_half* logits, int ld, const int32_t* targets, float inv_temperature,
+                      float* logp, float* entropy, float* lse, int32_t* top_ids, float* top_logp, void* ws, size_t ws_bytes,
+                      mp_stream stream);
+
+/* Gradient of sum_r dlogp[r] logp[r] + dentropy[r] entropy[r], times the loss scale, p = exp(z - lse):
+ *     dlogits = RNE16( S inv_temperature ( dlogp (1[j = target] - p) - dentropy p (ln p + entropy) ) )
+ * from the forward call's logits, entropy and lse.  dlogp (with targets) or dentropy (with entropy) may be NULL, not both.  st NULL: S = 1.
+ * A row whose dlogp (or target) and dentropy say 0 is zero, whatever it holds.  dlogits shares ld and may be logits. */
+int mp_token_logprobs_bwd(int rows, int vocab, const mp_half* logits, int ld, const int32_t* targets, float inv_temperature,
+                          const float* entropy, const float* lse, const float* dlogp, const float* dentropy, const mp_scale_state* st,
+                          mp_half* dlogits, mp_stream stream);
+
+/* Distillation: each row has a teacher's list of `top` classes (device int32 teacher_ids[rows, top]; those outside [0, vocab) are no
+ * entries) with their log probabilities (device fp32 teacher_logp[rows, top], as mp_token_logprobs leaves them at the same
+ * inv_temperature).  With z = inv_temperature float(logits), p = softmax(z), A the classes listed:
+ *     tail 0:  q = softmax of the row's teacher_logp,  r = 0         tail 1:  q = exp(teacher_logp),  r = max(0, 1 - sum q)
+ *     L  = sum_A q (ln q - ln p) + r (ln r - ln p_rest),  p_rest = sum of p outside A   (no term in r where nothing outside A can be)
+ *     CE = logsumexp(float(logits)) - float(logits)[target]           (temperature 1; 0 for a target outside [0, vocab))
+ *     loss = mean over rows of (weight L + hard_weight CE)
+ *     dlogits = RNE16( float(S / rows) (weight inv_temperature ((Q + r) p - (j in A ? q : r p / p_rest)) + hard_weight (softmax(logits) -
+ *               1[j = target])) ),  Q = sum q
+ * Entries that name one class count as one with the sum of their q.  A row without entries has L = 0; without a target either, a zero
+ * row of dlogits, whatever it holds.  (The factor temperature^2 that keeps gradients alike is the caller's, in weight.)  targets may be NULL
+ * where hard_weight is 0.  dlogits shares ld and may be logits.
+ *   ws    device, 16-byte aligned, mp_distill_workspace_bytes(desc) bytes (0 for a description that the calls refuse). */
+typedef struct mp_distill_desc {
+    int32_t rows, vocab, ld, top;      /* vocab up to MP_VOCAB_MAX, top 1 .. MP_TOP_MAX */
+    float   inv_temperature;           /* 2^-8 .. 2^8                                    */
+    float   weight, hard_weight;       /* finite                                         */
+    int32_t tail;                      /* 0 | 1                                          */
+    int32_t reserved;                  /* 0                                              */
+} mp_distill_desc;
+size_t mp_distill_workspace_bytes(const mp_distill_desc* desc /* host */);
+int mp_distill_scaled(const mp_distill_desc* desc /* host */, const mp_half* logits, const int32_t* teacher_ids, const float* teacher_logp,
+                      const int32_t* targets, const mp_scale_state* st, float* loss, mp_half* dlogits, void* ws, size_t ws_bytes,
+                      mp_stream stream);
+/* The same without the last step, as mp_mse_scaled_parts. */
+int mp_distill_scaled_parts(const mp_distill_desc* desc /* host */, const mp_half* logits, const int32_t* teacher_ids,
+                            const float* teacher_logp, const int32_t* targets, const mp_scale_state* st, mp_half* dlogits, void* ws,
+                            size_t ws_bytes, mp_mean_parts* parts, mp_stream stream);
+
+/* ------------------------------------------------------------------------------------------
  * Bandwidth-bound layer pieces (fp32 arithmetic between fp16 storage points, Section 3.2).
  * ------------------------------------------------------------------------------------------ */
 /* y = RNE16( LN(x + a) * gamma + beta ) over the last dimension d; a may be NULL.  The sum, mean,
@@ -464,6 +521,45 @@ size_t mp_attention_masked_bwd_workspace_bytes(const mp_attn_desc* desc /* host 
 int mp_attention_masked_bwd(const mp_attn_desc* desc /* host */, const void* mask, const mp_half* q, const mp_half* k,
                             const mp_half* v, const float* slopes, const mp_half* ctx, const float* lse, const mp_half* dctx,
                             mp_half* dq, mp_half* dk, mp_half* dv, void* ws, size_t ws_bytes, mp_stream stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Queries and keys on their way to attention: an RMS norm of each head, and the rotation of its columns by position.
+ * With x one head's d_head columns (Section 3.2: fp32 between fp16 storage points):
+ *     n = x (mean x^2 + eps)^(-1/2) g   (n = x where gq and gk are NULL)
+ *     pair i < rot / 2 of n, (a, b) = columns (i, i + rot / 2), or (2 i, 2 i + 1) with `adjacent`, turns by
+ *     t = positions[axis[i]][row] freqs[i]:   y = RNE16(a cos t - b sin t), RNE16(a sin t + b cos t);   columns from rot on: y = RNE16(n)
+ * t is formed in 64 bits, so that far positions keep their angles.
+ * ------------------------------------------------------------------------------------------ */
+#define MP_ROPE_AXES  4
+#define MP_ROPE_PAIRS 128
+typedef struct mp_rope_desc {
+    int32_t rows;
+    int32_t n_heads, n_kv_heads, d_head;      /* d_head a multiple of 8 up to 256                                     */
+    int32_t rot;                              /* columns of a head that turn: a multiple of 4 up to d_head            */
+    int32_t n_axes;                           /* 1 .. MP_ROPE_AXES: of positions (a text's place; time, height, width) */
+    int32_t adjacent;                         /* 0 | 1                                                                */
+    float   eps;                              /* >= 0                                                                 */
+    int32_t ld_q, ld_k, ld_yq, ld_yk;         /* multiples of 8                                                       */
+    int32_t ld_dyq, ld_dyk, ld_dq, ld_dk;
+    int32_t reserved;                         /* 0                                                                    */
+    uint8_t axis[MP_ROPE_PAIRS];              /* of each pair, below n_axes                                           */
+} mp_rope_desc;
+
+/* q[rows, ld_q], k[rows, ld_k] (columns of one fused projection, say) -> yq, yk.  gq, gk: device fp16 [d_head], shared by the heads, both or
+ * neither.  positions: device int32 [n_axes][rows].  freqs: device double [rot / 2], radians a position.  yq may be q and yk k, with
+ * the same leading dimension; otherwise outputs overlap no input.  16-byte aligned matrices and weights, and sizes as above, otherwise
+ * MP_E_UNSUPPORTED. */
+int mp_qk_norm_rope_fwd(const mp_rope_desc* desc /* host */, const mp_half* q, const mp_half* k, const mp_half* gq, const mp_half* gk,
+                        const int32_t* positions, const double* freqs, mp_half* yq, mp_half* yk, mp_stream stream);
+
+/* dq, dk from dyq, dyk and the forward call's inputs (q and k are read with weights only), and dgq, dgk [d_head] = RNE16 of fp32 sums over rows and
+ * heads, in an order that the shape decides (given with gq and gk, overwritten).  dq may be dyq and dk dyk, with the same leading dimension.
+ *   st    as for mp_gemm_bwd_dw (covers dgq and dgk).
+ *   ws    with weights: device, 16-byte aligned, mp_qk_norm_rope_bwd_workspace_bytes(desc) bytes (0 for a description that is refused). */
+size_t mp_qk_norm_rope_bwd_workspace_bytes(const mp_rope_desc* desc /* host */);
+int mp_qk_norm_rope_bwd(const mp_rope_desc* desc /* host */, const mp_half* q, const mp_half* k, const mp_half* gq, const mp_half* gk,
+                        const int32_t* positions, const double* freqs, const mp_half* dyq, const mp_half* dyk, mp_half* dq, mp_half* dk,
+                        mp_half* dgq, mp_half* dgk, mp_scale_state* st, void* ws, size_t ws_bytes, mp_stream stream);
 
 /* ------------------------------------------------------------------------------------------
  * Embedding: rows of a table w[vocab, d] by token (the other end of the vocabulary projection).

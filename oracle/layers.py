@@ -194,6 +194,39 @@ def masked_attention_bwd(P: Policy, dctx, cache):
     return dq, dk, dv
 
 
+# ---------------------------------------------------------------- norms and rotation of heads
+def _turn(P: Policy, n, rot, angles, adjacent):
+    """Pairs of the first `rot` columns of n[rows, heads, d] turned by angles[rows, rot / 2]; columns (i, i + rot / 2), or (2 i, 2 i + 1)."""
+    i = np.arange(rot // 2)
+    a, b = (2 * i, 2 * i + 1) if adjacent else (i, i + rot // 2)
+    c, s = np.cos(angles).astype(P.acc)[:, None], np.sin(angles).astype(P.acc)[:, None]
+    y = n.copy()
+    y[..., a] = n[..., a] * c - n[..., b] * s
+    y[..., b] = n[..., a] * s + n[..., b] * c
+    return y
+
+
+def norm_rope_fwd(P: Policy, x, heads, g, eps, angles, adjacent=False):
+    """Per head: n = g x / sqrt(mean x^2 + eps) (x itself where g is None), its pairs turned by angles[rows, pairs] (64 bits; of the
+    row's positions times the pairs' frequencies), then stored."""
+    rows = x.shape[0]
+    x = x.reshape(rows, heads, -1)
+    r = None if g is None else P.scalar(1) / np.sqrt((x * x).mean(-1, keepdims=True, dtype=P.acc) + P.scalar(eps))
+    n = x if g is None else x * r * g
+    rot = 2 * angles.shape[1]
+    return P.store(_turn(P, n, rot, angles, adjacent)).reshape(rows, -1), dict(x=x, r=r, g=g, angles=angles, adjacent=adjacent)
+
+
+def norm_rope_bwd(P: Policy, dy, c):
+    """u = dy turned back; dg = store(sum of u x r over rows and heads), v = u g, dx = store(r (v - x r mean(v x r)))."""
+    u = _turn(P, dy.reshape(c["x"].shape), 2 * c["angles"].shape[1], -c["angles"], c["adjacent"])
+    if c["g"] is None:
+        return P.store(u).reshape(dy.shape), None
+    hat, v = c["x"] * c["r"], u * c["g"]
+    dx = c["r"] * (v - hat * (v * hat).mean(-1, keepdims=True, dtype=P.acc))
+    return P.store(dx).reshape(dy.shape), P.store((u * hat).sum((0, 1), dtype=P.acc))
+
+
 # ---------------------------------------------------------------- embedding
 def embedding_fwd(P: Policy, tokens, w, scale):
     """y[t] = store(scale w[tokens[t]]); a token outside the table gives a zero row."""
@@ -242,6 +275,84 @@ def softmax_xent_scaled(P: Policy, logits, targets, scale):
     g = np.where(valid[:, None], g, P.scalar(0))
     coef = P.scalar(float(scale) / rows)
     return loss, P.store(coef * g)
+
+
+def _log_softmax(P: Policy, z):
+    with np.errstate(invalid="ignore", divide="ignore"):
+        top = z.max(-1, keepdims=True)
+        shifted = z - np.where(np.isneginf(top), P.scalar(0), top)
+        log_s = np.log(np.exp(shifted).sum(-1, keepdims=True, dtype=P.acc))
+        lse = np.where(np.isneginf(top), P.scalar(0), top) + log_s
+        return shifted - log_s, lse[:, 0]
+
+
+def token_logprobs(P: Policy, logits, targets, inv_temperature=1.0, top=0):
+    """Log probability of each row's target (0 where there is none), entropy, logsumexp, and the `top` largest logits' classes (ties and
+    0 / -0 by the lower one, NaN above all) with their log probabilities."""
+    rows, vocab = logits.shape
+    lp, lse = _log_softmax(P, P.scalar(inv_temperature) * logits)
+    there = (targets >= 0) & (targets < vocab)
+    logp = np.where(there, lp[np.arange(rows), np.where(there, targets, 0)], P.scalar(0))
+    with np.errstate(invalid="ignore"):
+        p = np.exp(lp)
+        entropy = -np.where(p == 0, P.scalar(0), p * np.where(p == 0, P.scalar(0), lp)).sum(-1, dtype=P.acc)
+    entropy = np.where(np.isneginf(lse), P.scalar(np.nan), entropy)
+    ids = np.argsort(-np.where(np.isnan(logits), np.inf, logits) - np.where(np.isnan(logits), 1, 0), axis=1, kind="stable")
+    if np.isnan(logits).any():           # (NaN ahead of +inf)
+        ids = np.stack([sorted(range(vocab), key=lambda j: (not np.isnan(r[j]), -r[j] if not np.isnan(r[j]) else 0.0, j)) for r in logits])
+    ids = ids[:, :top]
+    return logp, entropy, lse, ids, np.take_along_axis(lp, ids, 1)
+
+
+def token_logprobs_bwd(P: Policy, logits, targets, inv_temperature, dlogp, dentropy, scale):
+    """Gradient of sum dlogp logp + dentropy entropy, times the loss scale."""
+    rows, vocab = logits.shape
+    lp, _ = _log_softmax(P, P.scalar(inv_temperature) * logits)
+    p = np.exp(lp)
+    plp = np.where(p == 0, P.scalar(0), p * np.where(p == 0, P.scalar(0), lp))
+    entropy = -plp.sum(-1, keepdims=True, dtype=P.acc)
+    there = (targets >= 0) & (targets < vocab)
+    g = np.where(there, dlogp, P.scalar(0))[:, None]
+    d = -g * p - dentropy[:, None] * (plp + p * entropy)
+    d[np.arange(rows), np.where(there, targets, 0)] += g[:, 0]
+    return P.store(P.scalar(float(scale) * inv_temperature) * d)
+
+
+def distill_scaled(P: Policy, logits, ids, teacher, scale, inv_temperature=1.0, weight=1.0, hard_weight=0.0, targets=None, tail=False):
+    """Mean over rows of weight L + hard_weight CE and the loss-scaled seed gradient.  L: the teacher's distribution q over the classes its
+    list names (ids; others than 0 .. vocab - 1 are no entries, doubles add up) against p = softmax(inv_temperature logits); `tail`: what
+    exp(teacher) leaves of 1 against p's sum over all other classes, else q renormalised.  CE: of the targets, at temperature 1."""
+    rows, vocab = logits.shape
+    lp, _ = _log_softmax(P, P.scalar(inv_temperature) * logits)
+    p = np.exp(lp)
+    total, grad = P.scalar(0), np.zeros_like(p)
+    lp1, _ = _log_softmax(P, logits)
+    for i in range(rows):
+        at = [(int(j), t) for j, t in zip(ids[i], teacher[i]) if 0 <= j < vocab]
+        if at:
+            names = np.array([j for j, _ in at])
+            t = np.array([t for _, t in at], np.float64)
+            w = np.exp(t) if tail else np.exp(t - (0 if np.isneginf(t.max()) else t.max()))
+            if not tail:
+                w = w / (w.sum() if w.sum() > 0 else 1)
+            q = np.zeros(vocab, np.float64)
+            np.add.at(q, names, w)
+            rest = np.ones(vocab, bool)
+            rest[names] = False
+            left = max(0.0, 1 - w.sum()) if tail and (lp[i][rest] > -np.inf).any() else 0.0
+            n = q > 0
+            total += P.scalar(weight * float((q[n] * (np.log(q[n]) - lp[i][n])).sum()))
+            d = p[i] * P.scalar(w.sum() + left) - q.astype(P.acc)
+            if left > 0:
+                lp_rest, lse_rest = _log_softmax(P, np.where(rest, lp[i], -np.inf)[None])   # (relative to p's own: lse_rest = ln p_rest)
+                total += P.scalar(weight * left * (np.log(left) - float(lse_rest[0])))
+                d = d - P.scalar(left) * np.exp(lp_rest[0])
+            grad[i] += P.scalar(weight * inv_temperature) * d
+        if hard_weight and targets is not None and 0 <= targets[i] < vocab:
+            total -= P.scalar(hard_weight) * lp1[i, targets[i]]
+            grad[i] += P.scalar(hard_weight) * np.exp(lp1[i])
+            grad[i, targets[i]] -= P.scalar(hard_weight)
+    return total / P.scalar(rows), P.store(P.scalar(float(scale) / rows) * grad)
 
 
 # ---------------------------------------------------------------- LSTM

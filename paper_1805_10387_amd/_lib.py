@@ -13,6 +13,7 @@ MP_SCALE_STATIC, MP_SCALE_BACKOFF = 0, 1
 MP_EPI_NONE, MP_EPI_BIAS, MP_EPI_BIAS_RELU = 0, 1, 2
 MP_OPT_SGD, MP_OPT_ADAM, MP_OPT_ADAMW = 0, 1, 2
 MP_STATE8_BLOCK = 256
+MP_TOP_MAX, MP_VOCAB_MAX, MP_ROPE_AXES, MP_ROPE_PAIRS = 128, 1 << 20, 4, 128
 MP_UPDATE_DEFAULT, MP_UPDATE_PRECHECKED, MP_UPDATE_UNBIASED8 = 0, 1, 4
 
 
@@ -69,6 +70,19 @@ class AttnDesc(C.Structure):
                 ("alpha", C.c_float), ("cap", C.c_float), ("reserved", C.c_int32)]
 
 
+class RopeDesc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("d_head", C.c_int32), ("rot", C.c_int32),
+                ("n_axes", C.c_int32), ("adjacent", C.c_int32), ("eps", C.c_float),
+                ("ld_q", C.c_int32), ("ld_k", C.c_int32), ("ld_yq", C.c_int32), ("ld_yk", C.c_int32),
+                ("ld_dyq", C.c_int32), ("ld_dyk", C.c_int32), ("ld_dq", C.c_int32), ("ld_dk", C.c_int32),
+                ("reserved", C.c_int32), ("axis", C.c_uint8 * MP_ROPE_PAIRS)]
+
+
+class DistillDesc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("vocab", C.c_int32), ("ld", C.c_int32), ("top", C.c_int32), ("inv_temperature", C.c_float),
+                ("weight", C.c_float), ("hard_weight", C.c_float), ("tail", C.c_int32), ("reserved", C.c_int32)]
+
+
 class OptCfg(C.Structure):
     _fields_ = [("kind", C.c_int32), ("reserved", C.c_int32), ("lr", C.c_double), ("beta1", C.c_double),
                 ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double)]
@@ -109,6 +123,12 @@ SIGNATURES = {
     "mp_loss_scale_update_mean": (_I, [_P, C.POINTER(MeanParts), _P, _P]),
     "mp_softmax_xent_scaled_db": (_I, [_I, _I, _P, _I, _P, _P, _P, _P, _P, _P, _SZ, _P]),
     "mp_softmax_xent_scaled_db_copy": (_I, [_I, _I, _P, _I, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "mp_token_logprobs_workspace_bytes": (_SZ, [_I, _I, _I]),
+    "mp_token_logprobs": (_I, [_I, _I, _I, _P, _I, _P, _F, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "mp_token_logprobs_bwd": (_I, [_I, _I, _P, _I, _P, _F, _P, _P, _P, _P, _P, _P, _P]),
+    "mp_distill_workspace_bytes": (_SZ, [C.POINTER(DistillDesc)]),
+    "mp_distill_scaled": (_I, [C.POINTER(DistillDesc), _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "mp_distill_scaled_parts": (_I, [C.POINTER(DistillDesc), _P, _P, _P, _P, _P, _P, _P, _SZ, C.POINTER(MeanParts), _P]),
     "mp_layernorm_fwd": (_I, [_I, _I, _P, _P, _P, _P, _F, _P, _P, _P, _P]),
     "mp_layernorm_bwd_workspace_bytes": (_SZ, [_I, _I]),
     "mp_layernorm_bwd": (_I, [_I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
@@ -126,6 +146,9 @@ SIGNATURES = {
     "mp_attention_masked_fwd": (_I, [C.POINTER(AttnDesc), _P, _P, _P, _P, _P, _P, _P, _P]),
     "mp_attention_masked_bwd_workspace_bytes": (_SZ, [C.POINTER(AttnDesc)]),
     "mp_attention_masked_bwd": (_I, [C.POINTER(AttnDesc), _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "mp_qk_norm_rope_fwd": (_I, [C.POINTER(RopeDesc), _P, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "mp_qk_norm_rope_bwd_workspace_bytes": (_SZ, [C.POINTER(RopeDesc)]),
+    "mp_qk_norm_rope_bwd": (_I, [C.POINTER(RopeDesc), _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
     "mp_embedding_fwd": (_I, [_I, _I, _I, _P, _P, _F, _P, _P]),
     "mp_embedding_bwd_workspace_bytes": (_SZ, [_I, _I, _I]),
     "mp_embedding_bwd": (_I, [_I, _I, _I, _P, _P, _F, _P, _P, _P, _P, _SZ, _P]),

@@ -233,6 +233,40 @@ def mp_softmax_xent_scaled_db_copy(rows, vocab, logits, ld, targets, st, loss, d
                                                    _p(db), _p(ws), ws.numel() * ws.element_size(), _stream()))
 
 
+def mp_token_logprobs_workspace_bytes(rows: int, vocab: int, top: int) -> int:
+    return L.load().mp_token_logprobs_workspace_bytes(rows, vocab, top)
+
+
+def mp_token_logprobs(rows, vocab, top, logits, ld, targets, inv_temperature, logp, entropy, lse, top_ids=None, top_logp=None, ws=None):
+    _check(L.load().mp_token_logprobs(rows, vocab, top, _p(logits), ld, _p(targets), inv_temperature, _p(logp), _p(entropy), _p(lse), _p(top_ids),
+                                      _p(top_logp), _p(ws), _nbytes(ws), _stream()))
+
+
+def mp_token_logprobs_bwd(rows, vocab, logits, ld, targets, inv_temperature, entropy, lse, dlogp, dentropy, st, dlogits):
+    _check(L.load().mp_token_logprobs_bwd(rows, vocab, _p(logits), ld, _p(targets), inv_temperature, _p(entropy), _p(lse), _p(dlogp), _p(dentropy),
+                                          _p(st), _p(dlogits), _stream()))
+
+
+def distill_desc(rows, vocab, top, ld=None, inv_temperature=1.0, weight=1.0, hard_weight=0.0, tail=False) -> L.DistillDesc:
+    return L.DistillDesc(rows, vocab, vocab if ld is None else ld, top, inv_temperature, weight, hard_weight, int(tail), 0)
+
+
+def mp_distill_workspace_bytes(desc) -> int:
+    return L.load().mp_distill_workspace_bytes(C.byref(desc))
+
+
+def mp_distill_scaled(desc, logits, teacher_ids, teacher_logp, targets, st, loss, dlogits, ws):
+    _check(L.load().mp_distill_scaled(C.byref(desc), _p(logits), _p(teacher_ids), _p(teacher_logp), _p(targets), _p(st), _p(loss), _p(dlogits),
+                                      _p(ws), _nbytes(ws), _stream()))
+
+
+def mp_distill_scaled_parts(desc, logits, teacher_ids, teacher_logp, targets, st, dlogits, ws) -> L.MeanParts:
+    parts = L.MeanParts()
+    _check(L.load().mp_distill_scaled_parts(C.byref(desc), _p(logits), _p(teacher_ids), _p(teacher_logp), _p(targets), _p(st), _p(dlogits),
+                                            _p(ws), _nbytes(ws), C.byref(parts), _stream()))
+    return parts
+
+
 # ------------------------------------------------------------------ bandwidth-bound pieces
 def mp_layernorm_fwd(rows, d, x, a, gamma, beta, eps, y, mean, rstd):
     _check(L.load().mp_layernorm_fwd(rows, d, _p(x), _p(a), _p(gamma), _p(beta), eps, _p(y), _p(mean), _p(rstd), _stream()))
@@ -317,6 +351,36 @@ def mp_attention_masked_bwd_workspace_bytes(desc) -> int:
 def mp_attention_masked_bwd(desc, mask, q, k, v, slopes, ctx, lse, dctx, dq, dk, dv, ws):
     _check(L.load().mp_attention_masked_bwd(C.byref(desc), _p(mask), _p(q), _p(k), _p(v), _p(slopes), _p(ctx), _p(lse), _p(dctx), _p(dq),
                                             _p(dk), _p(dv), _p(ws), _nbytes(ws), _stream()))
+
+
+def rope_desc(rows, n_heads, n_kv_heads, d_head, rot=None, n_axes=1, axis=None, adjacent=False, eps=1e-6, ld_q=None, ld_k=None, ld_yq=None,
+              ld_yk=None, ld_dyq=None, ld_dyk=None, ld_dq=None, ld_dk=None) -> L.RopeDesc:
+    """Leading dimensions: one matrix after the other where not given; those of gradients are their matrices' where not given.  axis: of
+    each of the rot / 2 pairs, the first one where not given."""
+    first = lambda *v: next(x for x in v if x is not None)  # noqa: E731
+    d = L.RopeDesc(rows, n_heads, n_kv_heads, d_head, first(rot, d_head), n_axes, int(adjacent), eps)
+    d.ld_q, d.ld_k = first(ld_q, n_heads * d_head), first(ld_k, n_kv_heads * d_head)
+    d.ld_yq, d.ld_yk = first(ld_yq, n_heads * d_head), first(ld_yk, n_kv_heads * d_head)
+    d.ld_dyq, d.ld_dyk, d.ld_dq, d.ld_dk = first(ld_dyq, d.ld_yq), first(ld_dyk, d.ld_yk), first(ld_dq, d.ld_q), first(ld_dk, d.ld_k)
+    if axis is not None:
+        if len(axis) != d.rot // 2 or len(axis) > L.MP_ROPE_PAIRS or any(not 0 <= a < 256 for a in axis):
+            raise ValueError(f"axes of {len(axis)} pairs for {d.rot // 2}, or not of 0 to 255")
+        for i, a in enumerate(axis):
+            d.axis[i] = int(a)
+    return d
+
+
+def mp_qk_norm_rope_fwd(desc, q, k, gq, gk, positions, freqs, yq, yk):
+    _check(L.load().mp_qk_norm_rope_fwd(C.byref(desc), _p(q), _p(k), _p(gq), _p(gk), _p(positions), _p(freqs), _p(yq), _p(yk), _stream()))
+
+
+def mp_qk_norm_rope_bwd_workspace_bytes(desc) -> int:
+    return L.load().mp_qk_norm_rope_bwd_workspace_bytes(C.byref(desc))
+
+
+def mp_qk_norm_rope_bwd(desc, q, k, gq, gk, positions, freqs, dyq, dyk, dq, dk, dgq=None, dgk=None, st=None, ws=None):
+    _check(L.load().mp_qk_norm_rope_bwd(C.byref(desc), _p(q), _p(k), _p(gq), _p(gk), _p(positions), _p(freqs), _p(dyq), _p(dyk), _p(dq), _p(dk),
+                                        _p(dgq), _p(dgk), _p(st), _p(ws), _nbytes(ws), _stream()))
 
 
 def mp_embedding_fwd(rows, vocab, d, tokens, w, scale, y):

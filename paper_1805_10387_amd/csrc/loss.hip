@@ -278,6 +278,12 @@ __global__ __launch_bounds__(LOSS_THREADS) void xent_kernel(int vocab, int ld, c
 
 using namespace mp;
 
+int mp::finish_mean_launch(const mp_mean_parts& parts, float* out, hipStream_t hs) {
+    launch_finish_mean(parts, out, hs);
+    MP_LAUNCH_CHECK("mean of partial sums");
+    return MP_OK;
+}
+
 static int loss_blocks(long long units) {
     long long b = (units + LOSS_THREADS * 4 - 1) / (LOSS_THREADS * 4);
     if (b < 1) b = 1;

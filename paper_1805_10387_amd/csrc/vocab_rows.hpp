@@ -1,0 +1,108 @@
+// Rows of fp16 logits in the registers of a workgroup: loads at any alignment, sums of exponentials against a running reference.
+#pragma once
+#include "common.hpp"
+
+namespace mp {
+
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4    u32x4_any __attribute__((aligned(2)));  // stores at any element: the hardware takes them
+
+constexpr float    LOG2E    = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+constexpr unsigned NEG_INF2 = 0xFC00FC00u;  // a pair of -inf
+
+// A stretch of a row, cut into 16-byte pieces of memory (not of the row: rows of an odd length start anywhere, and a load that crosses
+// the pieces takes three times as long).  Piece v holds elements 8 v - head + k, k < 8, of which the first and the last piece
+// may have some outside [0, len).
+struct Stretch {
+    const uint16_t* base;  // 16-byte aligned, `head` elements ahead of the first
+    int             head, len;
+    __device__ __forceinline__ Stretch(const uint16_t* p, int len_) : head((int)((reinterpret_cast<uintptr_t>(p) >> 1) & 7)), len(len_) { base = p - head; }
+    __device__ __forceinline__ int  pieces() const { return (head + len + 7) >> 3; }
+    __device__ __forceinline__ bool whole(int v) const { return 8 * v >= head && 8 * v + 8 <= head + len; }
+    // what is outside reads as -inf
+    __device__ __forceinline__ u32x4 load(int v) const {
+        u32x4 q = {NEG_INF2, NEG_INF2, NEG_INF2, NEG_INF2};
+        if (whole(v)) {
+            q = *reinterpret_cast<const u32x4*>(base + 8u * (unsigned)v);
+        } else if (v < pieces()) {
+            unsigned x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = 8 * v + k >= head && 8 * v + k < head + len ? base[8u * (unsigned)v + k] : 0xFC00u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) q[k] = x[2 * k] | (x[2 * k + 1] << 16);
+        }
+        return q;
+    }
+    // out: where element 0 belongs
+    __device__ __forceinline__ void store(uint16_t* out, int v, const u32x4 q) const {
+        uint16_t* o = out - head + 8u * (unsigned)v;
+        if (whole(v)) {
+            *reinterpret_cast<u32x4_any*>(o) = q;
+        } else if (v < pieces()) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (8 * v + k >= head && 8 * v + k < head + len) o[k] = (uint16_t)((k & 1) ? q[k >> 1] >> 16 : q[k >> 1] & 0xFFFFu);
+        }
+    }
+};
+
+__device__ __forceinline__ f16x2 as_pair(unsigned w) { return __builtin_bit_cast(f16x2, w); }
+// (the builtin maximum first makes every operand quiet, which is an instruction more each)
+__device__ __forceinline__ unsigned pair_max(unsigned a, unsigned b) {
+    unsigned d;
+    asm("v_pk_max_f16 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b));
+    return d;
+}
+template <int N>
+__device__ __forceinline__ float max_of(const u32x4* q) {
+    unsigned m = pair_max(pair_max(q[0][0], q[0][1]), pair_max(q[0][2], q[0][3]));
+#pragma unroll
+    for (int i = 1; i < N; ++i) m = pair_max(m, pair_max(pair_max(q[i][0], q[i][1]), pair_max(q[i][2], q[i][3])));
+    return fmaxf((float)as_pair(m)[0], (float)as_pair(m)[1]);
+}
+
+// Sums over exponentials of base 2, y = c2 x - ref with c2 = log2(e) / temperature:  s = sum 2^y, t = sum 2^y y (for the entropy).
+// ref is the largest c2 x so far as rounded, so that y of the largest is 0 to its last bit; never below the floor, which is below
+// every finite logit, so that a row of -inf makes no NaN of differences.  +inf and NaN make s NaN.
+constexpr float REF_FLOOR = -70000.f;
+template <bool ENTROPY>
+struct Sums {
+    float ref, s, t;
+    __device__ __forceinline__ explicit Sums(float c2) : ref(REF_FLOOR * c2), s(0.f), t(0.f) {}
+    __device__ __forceinline__ void move(float to) {  // to >= ref
+        const float d = ref - to, k = __builtin_amdgcn_exp2f(d);
+        if (ENTROPY) t = k * (t + d * s);
+        s *= k;
+        ref = to;
+    }
+    __device__ __forceinline__ void add(float y) {
+        const float e = __builtin_amdgcn_exp2f(y);
+        s += e;
+        if (ENTROPY) t = fmaf(e, fmaxf(y, -150.f), t);  // (0 x -inf; 2^-150 is 0)
+    }
+    // N pieces whose largest logit is `top`
+    template <int N>
+    __device__ __forceinline__ void add_pieces(const u32x4* q, float c2, float top) {
+        move(fmaxf(ref, top * c2));
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                add(fmaf((float)as_pair(q[i][k])[0], c2, -ref));
+                add(fmaf((float)as_pair(q[i][k])[1], c2, -ref));
+            }
+    }
+    __device__ __forceinline__ void add_sums(float ref2, float s2, float t2) {
+        const float to = fmaxf(ref, ref2), d = ref2 - to, k = __builtin_amdgcn_exp2f(d);
+        move(to);
+        if (ENTROPY) t += k * (t2 + d * s2);
+        s += k * s2;
+    }
+    __device__ __forceinline__ void over_wave() {
+        move(wave_max(ref));
+        s = wave_sum(s);
+        if (ENTROPY) t = wave_sum(t);
+    }
+};
+
+}  // namespace mp
