@@ -11,7 +11,7 @@
 // gradients wait in LDS, and a map from pieces to entries tells each piece which of its elements to replace.  For r the sum over
 // "all others" is formed without A, not as a difference of sums, which would lose it where the student is sure of A.
 //
-// Rows longer than 131064 classes, or too few for the chip, are cut into chunks: one launch for the sums, one for the gradient.
+// Rows longer than 139256 classes, or too few for the chip, are cut into chunks: one launch for the sums, one for the gradient.
 #include <cmath>
 
 #include "vocab_rows.hpp"
@@ -33,81 +33,133 @@ struct DistillArgs {
     float*          chosen;   // chunks: [row][MP_TOP_MAX + 1], the student's logits of the entries
 };
 
+// The entries of a row, in LDS: one wave's work.  The last one is the target's.
 struct EntryLds {
-    int            id[MP_TOP_MAX + 1], next[MP_TOP_MAX + 1];
-    float          q[MP_TOP_MAX];
-    unsigned short value[MP_TOP_MAX + 1];
+    int      id[MP_TOP_MAX + 1];
+    float    t[MP_TOP_MAX], q[MP_TOP_MAX], x[MP_TOP_MAX + 1];  // the teacher's log probability, q, the student's logit
+    unsigned info[MP_TOP_MAX + 1];                             // as in the map; there for those behind the first one of a word
 };
+// A word of the map, 0 where there is no entry: the next entry of the word + 1, the element's place among the word's, flags, its gradient.
+constexpr unsigned MAP_NEXT = 0xFFu, MAP_TARGET = 1u << 12, MAP_THERE = 1u << 13;
+__device__ __forceinline__ int map_place(unsigned w) { return (int)(w >> 8) & 15; }
 struct RowFactors {
     float a, ref, b, ref2;  // gradient outside A: a 2^(c2 x - ref) + b 2^(log2(e) x - ref2)
     int   none;             // a zero row, whatever it holds
 };
 
-// One wave's view of a row's entries: lane l has entries l and l + 64.  SHIFT: 2^SHIFT elements share a word of the map.
+// One wave's view of a row's entries: lane l has entries l and l + 64, lane 0 the target's as well.  SHIFT: 2^SHIFT elements share a word
+// of the map.
 template <int SHIFT>
 struct Entries {
-    int   id[2], target;
-    float t[2], x[2], xt;
-    bool  there[2], listed, twice;  // listed: the target is in A.  twice: some class is named more than once
+    const DistillArgs& a;
+    EntryLds&          l;
+    unsigned*          map;
+    int                first;              // class that the stretch begins with
+    int                target;
+    bool               some, listed, twice;  // entries that there are; the target is in A; some class is named more than once
 
-    __device__ __forceinline__ void load(const DistillArgs& a, long long row) {
-        const int lane = threadIdx.x & 63;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const bool in = lane + 64 * s < a.top;
-            id[s] = in ? a.ids[row * a.top + lane + 64 * s] : -1;
-            t[s]  = in ? a.teacher[row * a.top + lane + 64 * s] : 0.f;
-        }
-        target = a.targets ? a.targets[row] : -1;
+    __device__ __forceinline__ static int lane() { return threadIdx.x & 63; }
+    __device__ __forceinline__ bool       there(int c) const { return c >= 0 && c < a.vocab; }
+    template <typename F>
+    __device__ __forceinline__ void each(F&& f) const {
+#pragma unroll 1
+        for (int e = lane(); e < a.top; e += 64) f(e);
     }
-    // place of a class in the stretch, or -1
-    __device__ __forceinline__ static int place(const DistillArgs& a, const Stretch& z, int first, int c) {
-        return c >= first && c < a.vocab && c - first < z.len ? c - first : -1;
+    // word of the map for class c, or -1: another stretch's, or none
+    __device__ __forceinline__ int word(const Stretch& z, int c) const { return c >= first && c < a.vocab && c - first < z.len ? (c - first + z.head) >> SHIFT : -1; }
+
+    // a row's list on its way, and then in place
+    struct Ahead {
+        int   id[2], target;
+        float t[2];
+    };
+    __device__ __forceinline__ static Ahead fetch(const DistillArgs& a, long long row) {
+        Ahead h;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const long long e = row * a.top + min(lane() + 64 * s, a.top - 1);
+            h.id[s]           = a.ids[e];
+            h.t[s]            = a.teacher[e];
+        }
+        h.target = a.targets ? a.targets[row] : -1;
+        return h;
     }
-    // into the map of the row's pieces, those that lie in the stretch
-    __device__ __forceinline__ void insert(const DistillArgs& a, const Stretch& z, int first, unsigned* map, EntryLds& l) {
-        const int lane = threadIdx.x & 63;
-        bool      eq   = false;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            there[s] = id[s] >= 0 && id[s] < a.vocab;
-            eq |= there[s] && id[s] == target;
-        }
-        listed     = __any(eq);
-        bool again = false;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int e = lane + 64 * s, at = place(a, z, first, id[s]);
-            if (e < a.top) l.id[e] = id[s];
-            if (at >= 0) l.next[e] = (int)atomicExch(&map[(at + z.head) >> SHIFT], (unsigned)e + 1);
-        }
-        __builtin_amdgcn_wave_barrier();
+    __device__ __forceinline__ void settle(const Ahead& h) {
 #pragma unroll
         for (int s = 0; s < 2; ++s)
-            if (place(a, z, first, id[s]) >= 0)
-                for (int o = l.next[lane + 64 * s]; o; o = l.next[o - 1]) again |= l.id[o - 1] == id[s];
-        twice        = a.chunks > 1 || __any(again);  // (the rest of a list may lie in another chunk)
-        const int at = place(a, z, first, target);
-        if (lane == 0 && !listed && at >= 0) {
-            l.id[DI_TARGET]   = target;
-            l.next[DI_TARGET] = (int)atomicExch(&map[(at + z.head) >> SHIFT], (unsigned)DI_TARGET + 1);
-        }
-    }
-    __device__ __forceinline__ void remove(const DistillArgs& a, const Stretch& z, int first, unsigned* map) const {
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int at = place(a, z, first, id[s]);
-            if (at >= 0) map[(at + z.head) >> SHIFT] = 0;
-        }
-        const int at = place(a, z, first, target);
-        if ((threadIdx.x & 63) == 0 && at >= 0) map[(at + z.head) >> SHIFT] = 0;
+            if (lane() + 64 * s < a.top) {
+                l.id[lane() + 64 * s] = h.id[s];
+                l.t[lane() + 64 * s]  = h.t[s];
+            }
+        target = h.target;
+        if (lane() == 0) l.id[DI_TARGET] = target;
     }
     // the student's logits of the entries
-    __device__ __forceinline__ void gather(const DistillArgs& a, long long row) {
+    struct Logits {
+        uint16_t x[2], target;
+    };
+    __device__ __forceinline__ Logits fetch_logits(long long row) const {
         const uint16_t* z = a.logits + row * a.ld;
+        Logits          h;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) x[s] = there[s] ? h2f(z[id[s]]) : -INFINITY;
-        xt = target >= 0 && target < a.vocab ? h2f(z[target]) : 0.f;
+        for (int s = 0; s < 2; ++s) {
+            const int c = l.id[min(lane() + 64 * s, a.top - 1)];
+            h.x[s]      = z[there(c) ? c : 0];
+        }
+        h.target = z[there(target) ? target : 0];
+        return h;
+    }
+    __device__ __forceinline__ void settle_logits(const Logits& h) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            if (lane() + 64 * s < a.top) l.x[lane() + 64 * s] = h2f(h.x[s]);
+        if (lane() == 0) l.x[DI_TARGET] = h2f(h.target);
+    }
+    // into the map of the row's pieces, those that lie in the stretch
+    __device__ __forceinline__ void insert(const Stretch& z) {
+        bool any = false, eq = false;
+        each([&](int e) {
+            any |= there(l.id[e]);
+            eq |= l.id[e] == target;
+        });
+        some   = __any(any);
+        listed = __any(eq) && there(target);
+        const auto enter = [&](int e, unsigned flag) {
+            const int c = l.id[e], w = word(z, c);
+            if (w >= 0) l.info[e] = atomicExch(&map[w], (unsigned)e + 1) | (unsigned)((c - first + z.head) & ((1 << SHIFT) - 1)) << 8 | flag | MAP_THERE;
+        };
+        each([&](int e) { enter(e, 0u); });
+        if (lane() == 0 && !listed) enter(DI_TARGET, MAP_TARGET);
+        __builtin_amdgcn_wave_barrier();
+        bool again = false;
+        each([&](int e) {
+            if (word(z, l.id[e]) >= 0)
+                for (unsigned o = l.info[e] & MAP_NEXT; o; o = l.info[o - 1] & MAP_NEXT) again |= l.id[o - 1] == l.id[e];
+        });
+        twice = a.chunks > 1 || __any(again);  // (the rest of a list may lie in another chunk)
+        // the first one of a word moves into it; indices are below 256 and what moves in is above
+        const auto head = [&](int e) {
+            const int w = word(z, l.id[e]);
+            if (w >= 0 && map[w] == (unsigned)e + 1) map[w] = l.info[e];
+        };
+        each(head);
+        if (lane() == 0 && !listed) head(DI_TARGET);
+    }
+    // the entry's gradient, where its word of the map will find it
+    __device__ __forceinline__ void put(const Stretch& z, int e, float value) const {
+        const int w = word(z, l.id[e]);
+        if (w < 0) return;
+        const unsigned info = l.info[e], full = info | (unsigned)f2h(value) << 16;
+        if (map[w] == info) map[w] = full;
+        else l.info[e] = full;
+    }
+    __device__ __forceinline__ void remove(const Stretch& z) const {
+        const auto out = [&](int e) {
+            const int w = word(z, l.id[e]);
+            if (w >= 0) map[w] = 0;
+        };
+        each(out);
+        if (lane() == 0) out(DI_TARGET);
     }
 };
 
@@ -120,61 +172,65 @@ __device__ __forceinline__ double wave_sum64(double v) {
 // One wave: the row's loss, its factors, and the entries' gradients.  one, two: sums at the temperature and (TWO) at 1, without A if
 // TAIL.
 template <bool TAIL, bool TWO, int SHIFT>
-__device__ __forceinline__ void finish_row(const DistillArgs& a, const Entries<SHIFT>& n, const Sums<false> one, const Sums<false> two, EntryLds& l, RowFactors& out,
+__device__ __forceinline__ void finish_row(const Entries<SHIFT>& n, const Stretch& z, const Sums<false> one, const Sums<false> two, RowFactors& out,
                                            float* row_loss) {
-    const int  lane   = threadIdx.x & 63;
-    const bool some   = __any(n.there[0] || n.there[1]);
-    const bool real   = n.target >= 0 && n.target < a.vocab && a.hard != 0.f;
-    const float scale = (float)((double)a.st->scale / (double)a.rows), wc = some ? a.weight * a.inv_temperature * scale : 0.f, hs = real ? a.hard * scale : 0.f;
-    float      q[2], r = 0.f, sum_q;
+    const DistillArgs& a     = n.a;
+    EntryLds&          l     = n.l;
+    const bool         real  = n.there(n.target);
+    const float        scale = (float)((double)a.st->scale / (double)a.rows), wc = n.some ? a.weight * a.inv_temperature * scale : 0.f, hs = real ? a.hard * scale : 0.f;
+    float              r = 0.f, sum_q;
     if (TAIL) {
-        double w[2];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            w[s] = n.there[s] ? exp((double)n.t[s]) : 0.0;  // (64 bits: 1 minus their sum is often next to nothing)
-            q[s] = (float)w[s];
-        }
-        const double sum = wave_sum64(w[0] + w[1]);
-        sum_q            = (float)sum;
-        if (some && one.s > 0.f && sum < 1.0) r = (float)(1.0 - sum);
+        double sum = 0.0;
+        n.each([&](int e) {
+            const double q = n.there(l.id[e]) ? exp((double)l.t[e]) : 0.0;  // (64 bits: 1 minus their sum is often next to nothing)
+            l.q[e]         = (float)q;
+            sum += q;
+        });
+        sum   = wave_sum64(sum);
+        sum_q = (float)sum;
+        if (n.some && one.s > 0.f && sum < 1.0) r = (float)(1.0 - sum);
     } else {
-        float m = wave_max(fmaxf(n.there[0] ? n.t[0] : -INFINITY, n.there[1] ? n.t[1] : -INFINITY));
-        m       = m == -INFINITY ? 0.f : m;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) q[s] = n.there[s] ? expf(n.t[s] - m) : 0.f;
-        const float sum = wave_sum(q[0] + q[1]), inv = sum == 0.f ? 0.f : 1.f / sum;
-        q[0] *= inv;
-        q[1] *= inv;
+        float m = -INFINITY, sum = 0.f;
+        n.each([&](int e) { m = fmaxf(m, n.there(l.id[e]) ? l.t[e] : -INFINITY); });
+        m = wave_max(m);
+        m = m == -INFINITY ? 0.f : m;
+        n.each([&](int e) {
+            const float q = n.there(l.id[e]) ? expf(l.t[e] - m) : 0.f;
+            l.q[e]        = q;
+            sum += q;
+        });
+        sum             = wave_sum(sum);
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        n.each([&](int e) { l.q[e] *= inv; });
         sum_q = sum * inv;
     }
-    bool first[2] = {n.there[0], n.there[1]};
-    if (n.twice) {  // a class counts once, with the sum of its entries in their order
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-            if (lane + 64 * s < a.top) l.q[lane + 64 * s] = q[s];
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            float sum  = 0.f;
-            bool  seen = false;
-            for (int j = 0; j < a.top; ++j)
-                if (l.id[j] == n.id[s]) {
-                    sum += l.q[j];
-                    seen |= j < lane + 64 * s;
-                }
-            if (n.there[s]) {
-                q[s]     = sum;
-                first[s] = !seen;
+    __builtin_amdgcn_wave_barrier();
+    // q of entry e's class and whether e is its first entry: a class counts once, with the sum of its entries in their order
+    const auto class_of = [&](int e, float& q) {
+        q = l.q[e];
+        if (!n.twice) return true;
+        q          = 0.f;
+        bool first = true;
+        for (int j = 0; j < a.top; ++j)
+            if (l.id[j] == l.id[e]) {
+                q += l.q[j];
+                first &= j >= e;
             }
-        }
-    }
+        return first;
+    };
     Sums<false> all = one, at1 = two;
     if (TAIL) {
-        const float top         = wave_max(fmaxf(n.x[0], n.x[1]));
-        const auto  with_listed = [&](Sums<false>& t, float c2) {
+        float top = -INFINITY;
+        n.each([&](int e) { top = fmaxf(top, n.there(l.id[e]) ? l.x[e] : -INFINITY); });
+        top                    = wave_max(top);
+        const auto with_listed = [&](Sums<false>& t, float c2) {
             t.move(fmaxf(t.ref, top * c2));
-            t.s += wave_sum((first[0] ? __builtin_amdgcn_exp2f(fmaf(n.x[0], c2, -t.ref)) : 0.f) +
-                            (first[1] ? __builtin_amdgcn_exp2f(fmaf(n.x[1], c2, -t.ref)) : 0.f));
+            float sum = 0.f;
+            n.each([&](int e) {
+                float q;
+                if (n.there(l.id[e]) && class_of(e, q)) sum += __builtin_amdgcn_exp2f(fmaf(l.x[e], c2, -t.ref));
+            });
+            t.s += wave_sum(sum);
         };
         with_listed(all, a.c2);
         if (TWO) with_listed(at1, LOG2E);
@@ -186,23 +242,27 @@ __device__ __forceinline__ void finish_row(const DistillArgs& a, const Entries<S
     f.ref  = TAIL ? one.ref : all.ref;
     f.b    = TWO ? hs * inv_1 : 0.f;
     f.ref2 = at1.ref;
-    f.none = !some && !real;
+    f.none = !n.some && !real;
     float kl = 0.f;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        const float y = fmaf(n.x[s], a.c2, -all.ref), p = __builtin_amdgcn_exp2f(y) * inv_s, p1 = TWO ? __builtin_amdgcn_exp2f(fmaf(n.x[s], LOG2E, -at1.ref)) * inv_1 : p;
-        if (n.there[s]) l.value[lane + 64 * s] = f2h(wc * (p * u - q[s]) + (real ? hs * (p1 - (n.id[s] == n.target ? 1.f : 0.f)) : 0.f));
-        if (first[s] && q[s] != 0.f) kl += q[s] * (logf(q[s]) - LN2 * (y - log_s));
-    }
+    n.each([&](int e) {
+        if (!n.there(l.id[e])) return;
+        const float y = fmaf(l.x[e], a.c2, -all.ref), p = __builtin_amdgcn_exp2f(y) * inv_s;
+        const float p1 = TWO ? __builtin_amdgcn_exp2f(fmaf(l.x[e], LOG2E, -at1.ref)) * inv_1 : p;
+        float       q;
+        const bool  first = class_of(e, q);
+        n.put(z, e, wc * (p * u - q) + (real ? hs * (p1 - (l.id[e] == n.target ? 1.f : 0.f)) : 0.f));
+        if (first && q != 0.f) kl += q * (logf(q) - LN2 * (y - log_s));
+    });
     kl = wave_sum(kl);
     if (TAIL && r > 0.f) kl += r * (logf(r) - LN2 * ((one.ref - all.ref) + (log2f(one.s) - log_s)));
-    if (lane == 0) {
-        float loss = some ? a.weight * kl : 0.f;
+    if (n.lane() == 0) {
+        float loss = n.some ? a.weight * kl : 0.f;
         if (real) {
-            loss -= a.hard * (LN2 * (TWO ? fmaf(n.xt, LOG2E, -at1.ref) - log2f(at1.s) : fmaf(n.xt, a.c2, -all.ref) - log_s));
+            const float x = l.x[DI_TARGET];
+            loss -= a.hard * (LN2 * (TWO ? fmaf(x, LOG2E, -at1.ref) - log2f(at1.s) : fmaf(x, a.c2, -all.ref) - log_s));
             if (!n.listed)
-                l.value[DI_TARGET] =
-                    f2h(f.a * __builtin_amdgcn_exp2f(fmaf(n.xt, a.c2, -f.ref)) + (TWO ? f.b * __builtin_amdgcn_exp2f(fmaf(n.xt, LOG2E, -f.ref2)) : 0.f) - hs);
+                n.put(z, DI_TARGET,
+                      f.a * __builtin_amdgcn_exp2f(fmaf(x, a.c2, -f.ref)) + (TWO ? f.b * __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -f.ref2)) : 0.f) - hs);
         }
         if (row_loss) *row_loss = loss;
         out = f;
@@ -219,58 +279,67 @@ __device__ __forceinline__ void set_half(u32x4& q, int k, unsigned h) {
 template <int SHIFT>
 __host__ __device__ constexpr int map_words(int len) { return (len + 7 + (1 << SHIFT) - 1) >> SHIFT; }
 
-// FUSED: whole rows, in turn.  SUMS, GRADIENT: one chunk of one row, sums out or in through a.sums.
-enum { DI_FUSED = 0, DI_SUMS = 1, DI_GRADIENT = 2 };
+// SUMS, GRADIENT: one chunk of one row, sums out or in through a.sums.  FUSED: a whole row.  IN_TURN: whole rows, the next one's pieces
+// loaded as the gradient leaves their registers.
+enum { DI_SUMS, DI_GRADIENT, DI_FUSED, DI_IN_TURN };
 
 template <int THREADS, int VECS, bool TAIL, bool TWO, int MODE, int SHIFT>
 __global__ __launch_bounds__(THREADS) void distill_kernel(const DistillArgs a) {
-    extern __shared__ unsigned map[];  // entry + 1 of each piece, others behind it in EntryLds::next; 0: none
+    extern __shared__ unsigned map[];
     __shared__ EntryLds        l;
     __shared__ RowFactors      factors;
     __shared__ float           red[THREADS / 64][4];
-    constexpr int              NW = THREADS / 64, G = VECS < 4 ? VECS : 4;
+    constexpr int              NW = THREADS / 64, G = VECS % 4 == 0 ? 4 : VECS % 2 == 0 ? 2 : 1;
     const int                  tid = threadIdx.x, wave = tid >> 6;
-    long long                  row   = MODE == DI_FUSED ? blockIdx.x : blockIdx.x / a.chunks;
-    const int                  chunk = MODE == DI_FUSED ? 0 : blockIdx.x - (int)row * a.chunks, first = chunk * a.chunk, len = min(a.chunk, a.vocab - first);
+    long long                  row   = MODE >= DI_FUSED ? blockIdx.x : blockIdx.x / a.chunks;
+    const int                  chunk = MODE >= DI_FUSED ? 0 : blockIdx.x - (int)row * a.chunks, first = chunk * a.chunk, len = min(a.chunk, a.vocab - first);
+    const int                  most  = (len + 14) >> 3;  // pieces, wherever a row starts
+    typedef Entries<SHIFT>     Row;
+    Row                        n{a, l, map, first, -1, false, false, false};
     Stretch                    z(a.logits + row * a.ld + first, len);
-    Entries<SHIFT>             n, ahead;
     u32x4                      raw[VECS];
+    typename Row::Ahead        ahead;
+    if (wave == 0) ahead = Row::fetch(a, row);
 #pragma unroll
     for (int i = 0; i < VECS; ++i) raw[i] = z.load(i * THREADS + tid);
-    if (wave == 0) n.load(a, row);
     for (int v = tid; v < map_words<SHIFT>(a.chunk); v += THREADS) map[v] = 0;
-    const auto replace = [&](u32x4& q, int v, int e, unsigned h) {
-        const int at = l.id[e] - first + z.head;
-        if (SHIFT == 3 || (at >> 3) == v) set_half(q, at & 7, h);
+    // f(place in the piece, word of the map) for the entries of piece v
+    const auto entries_of = [&](int v, auto&& f) {
+        if (v < z.pieces())
+            for (unsigned w = map[v >> (SHIFT - 3)]; w; w = (w & MAP_NEXT) ? l.info[(w & MAP_NEXT) - 1] : 0u)
+                if (SHIFT == 3 || (map_place(w) >> 3) == (v & 1)) f(map_place(w) & 7, w);
     };
     lds_barrier();
     for (;;) {
-        const long long next = row + gridDim.x;
-        int             at   = tid;
+        const long long      next = row + gridDim.x;
+        const bool           more = MODE == DI_IN_TURN && next < a.rows;
+        int                  at   = tid;
+        typename Row::Logits logits;
         asm("" : "+v"(at));  // (places of the pieces are formed where they are used, not kept in registers from row to row)
         if (wave == 0) {
-            n.insert(a, z, first, map, l);
-            if (MODE != DI_GRADIENT) n.gather(a, row);
+            n.settle(ahead);
+            n.insert(z);
+            if (MODE != DI_GRADIENT) logits = n.fetch_logits(row);
         }
-        if (TAIL && MODE != DI_GRADIENT) lds_barrier();
-        Sums<false> one(a.c2), two(LOG2E);
         if (MODE != DI_GRADIENT) {
+            if (TAIL) lds_barrier();
+            Sums<false> one(a.c2), two(LOG2E);
 #pragma unroll
             for (int i = 0; i < VECS; i += G) {
-                u32x4 q[G];
+                if (i * THREADS < most) {
+                    u32x4 q[G];
 #pragma unroll
-                for (int j = 0; j < G; ++j) {
-                    q[j] = raw[i + j];
-                    if (TAIL) {
-                        const int v = (i + j) * THREADS + at;
-                        if (v < z.pieces())
-                            for (unsigned e = map[v >> (SHIFT - 3)]; e; e = l.next[e - 1])
-                                if (e - 1 != DI_TARGET) replace(q[j], v, e - 1, 0xFC00u);
+                    for (int j = 0; j < G; ++j) {
+                        q[j] = raw[i + j];
+                        if (TAIL)
+                            entries_of((i + j) * THREADS + at, [&](int k, unsigned w) {
+                                if (!(w & MAP_TARGET)) set_half(q[j], k, 0xFC00u);
+                            });
                     }
+                    const float m = max_of<G>(q);
+                    one.template add_pieces<G>(q, a.c2, m);
+                    if (TWO) two.template add_pieces<G>(q, LOG2E, m);
                 }
-                const float m = max_of<G>(q);
-                one.template add_pieces<G>(q, a.c2, m);
-                if (TWO) two.template add_pieces<G>(q, LOG2E, m);
             }
             one.over_wave();
             if (TWO) two.over_wave();
@@ -284,73 +353,71 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const DistillArgs a) {
         }
         if (wave == 0) {
             Sums<false> s1(a.c2), s2(LOG2E);
+            float*      chosen = a.chosen + row * (MP_TOP_MAX + 1);
             if (MODE == DI_GRADIENT) {
-                for (int c = 0; c < a.chunks; ++c) {
+                for (int c = tid; c < a.chunks; c += 64) {
                     const f32x4 v = *reinterpret_cast<const f32x4*>(a.sums + (row * a.chunks + c) * 4);
                     s1.add_sums(v[0], v[1], 0.f);
                     if (TWO) s2.add_sums(v[2], v[3], 0.f);
                 }
-                const float* x = a.chosen + row * (MP_TOP_MAX + 1);
-#pragma unroll
-                for (int s = 0; s < 2; ++s) n.x[s] = n.there[s] ? x[(tid & 63) + 64 * s] : -INFINITY;
-                n.xt = n.target >= 0 && n.target < a.vocab ? x[DI_TARGET] : 0.f;
+                n.each([&](int e) { l.x[e] = chosen[e]; });
+                if (tid == 0) l.x[DI_TARGET] = chosen[DI_TARGET];
+                s1.over_wave();
+                if (TWO) s2.over_wave();
             } else {
 #pragma unroll
                 for (int w = 0; w < NW; ++w) {
                     s1.add_sums(red[w][0], red[w][1], 0.f);
                     if (TWO) s2.add_sums(red[w][2], red[w][3], 0.f);
                 }
+                n.settle_logits(logits);
             }
             if (MODE == DI_SUMS) {
                 if (tid == 0) *reinterpret_cast<f32x4*>(a.sums + (row * a.chunks + chunk) * 4) = f32x4{s1.ref, s1.s, s2.ref, s2.s};
-                float* x = a.chosen + row * (MP_TOP_MAX + 1);
                 if (chunk == 0) {
-#pragma unroll
-                    for (int s = 0; s < 2; ++s)
-                        if (n.there[s]) x[(tid & 63) + 64 * s] = n.x[s];
-                    if (tid == 0) x[DI_TARGET] = n.xt;
+                    n.each([&](int e) { chosen[e] = l.x[e]; });
+                    if (tid == 0) chosen[DI_TARGET] = l.x[DI_TARGET];
                 }
             } else {
-                finish_row<TAIL, TWO, SHIFT>(a, n, s1, s2, l, factors, first == 0 ? a.row_loss + row : nullptr);
+                finish_row<TAIL, TWO, SHIFT>(n, z, s1, s2, factors, first == 0 ? a.row_loss + row : nullptr);
             }
+            if (more) ahead = Row::fetch(a, next);
         }
         if (MODE == DI_SUMS) return;
         lds_barrier();
-        const RowFactors f    = factors;
-        const bool       more = MODE == DI_FUSED && next < a.rows;
-        if (wave == 0 && more) ahead.load(a, next);
-        Stretch   zn(a.logits + (more ? next : row) * a.ld + first, len);
-        uint16_t* dz = a.dlogits + row * a.ld + first;
+        const auto  uniform = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); };
+        const float fa = uniform(factors.a), ref = uniform(factors.ref), fb = uniform(factors.b), ref2 = uniform(factors.ref2);
+        const bool  none = __builtin_amdgcn_readfirstlane(factors.none);
+        Stretch     zn(a.logits + (more ? next : row) * a.ld + first, len);
+        uint16_t*   dz = a.dlogits + row * a.ld + first;
+        asm("" : "+v"(at));
 #pragma unroll
         for (int i = 0; i < VECS; ++i) {
-            const int v = i * THREADS + at;
-            u32x4     o = {0, 0, 0, 0};
-            asm("" : "+v"(raw[i]));  // (or the compiler keeps the sums' halves, taken apart, in twice the registers until here)
-            if (!f.none) {
+            if (i * THREADS < most) {
+                const int v = i * THREADS + at;
+                u32x4     o = {0, 0, 0, 0};
+                asm("" : "+v"(raw[i]));  // (or the compiler keeps the sums' halves, taken apart, in twice the registers until here)
+                if (!none) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    float d[2];
+                    for (int k = 0; k < 4; ++k) {
+                        float d[2];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float x = (float)as_pair(raw[i][k])[h];
-                        d[h]          = f.a * __builtin_amdgcn_exp2f(fmaf(x, a.c2, -f.ref));
-                        if (TWO) d[h] = fmaf(f.b, __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -f.ref2)), d[h]);
+                        for (int h = 0; h < 2; ++h) {
+                            const float x = (float)as_pair(raw[i][k])[h];
+                            d[h]          = fa * __builtin_amdgcn_exp2f(fmaf(x, a.c2, -ref));
+                            if (TWO) d[h] = fmaf(fb, __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -ref2)), d[h]);
+                        }
+                        o[k] = (unsigned)f2h(d[0]) | ((unsigned)f2h(d[1]) << 16);
                     }
-                    o[k] = (unsigned)f2h(d[0]) | ((unsigned)f2h(d[1]) << 16);
+                    entries_of(v, [&](int k, unsigned w) { set_half(o, k, w >> 16); });
                 }
-                if (v < z.pieces())
-                    for (unsigned e = map[v >> (SHIFT - 3)]; e; e = l.next[e - 1])
-                        replace(o, v, e - 1, l.value[e - 1]);
+                z.store(dz, v, o);
+                if (more) raw[i] = zn.load(v);
             }
-            z.store(dz, v, o);
-            if (more) raw[i] = zn.load(v);
         }
         if (!more) return;
         lds_barrier();  // everyone is done with the map
-        if (wave == 0) {
-            n.remove(a, z, first, map);
-            n = ahead;
-        }
+        if (wave == 0) n.remove(z);
         row = next;
         z   = zn;
     }
@@ -363,7 +430,7 @@ using namespace mp;
 namespace {
 
 constexpr int DI_FEW = 256 * 8;      // 16-byte pieces of a chunk
-constexpr int DI_MOST = 1024 * 16;   // of a row in registers
+constexpr int DI_MOST = 1024 * 17;   // of a row in registers
 
 struct DistillPlan {
     int chunks, chunk;  // 0 chunks: rows in registers
@@ -447,13 +514,14 @@ extern "C" int mp_distill_scaled_parts(const mp_distill_desc* d, const mp_half* 
         if (rc == MP_OK) rc = launch_distill<256, 8, DI_GRADIENT>(a, d, n, hs);
     } else {
         const int  pieces = (d->vocab + (even ? 7 : 14)) / 8;
-        const auto grid   = [&](int resident) { return d->rows < 256 * resident ? d->rows : 256 * resident; };
-        if (pieces <= 256) rc = launch_distill<256, 1, DI_FUSED>(a, d, grid(8), hs);
-        else if (pieces <= 256 * 4) rc = launch_distill<256, 4, DI_FUSED>(a, d, grid(6), hs);
-        else if (pieces <= 256 * 8) rc = launch_distill<256, 8, DI_FUSED>(a, d, grid(4), hs);
-        else if (pieces <= 256 * 16) rc = launch_distill<256, 16, DI_FUSED>(a, d, grid(4), hs);
-        else if (pieces <= 512 * 16) rc = launch_distill<512, 16, DI_FUSED>(a, d, grid(2), hs);
-        else rc = launch_distill<1024, 16, DI_FUSED>(a, d, grid(1), hs);
+        if (pieces <= 64) rc = launch_distill<64, 1, DI_FUSED>(a, d, d->rows, hs);
+        else if (pieces <= 64 * 2) rc = launch_distill<64, 2, DI_FUSED>(a, d, d->rows, hs);
+        else if (pieces <= 64 * 4) rc = launch_distill<64, 4, DI_FUSED>(a, d, d->rows, hs);
+        else if (pieces <= 256 * 4) rc = launch_distill<256, 4, DI_FUSED>(a, d, d->rows, hs);
+        else if (pieces <= 256 * 8) rc = launch_distill<256, 8, DI_FUSED>(a, d, d->rows, hs);
+        else if (pieces <= 256 * 16) rc = launch_distill<256, 16, DI_FUSED>(a, d, d->rows, hs);
+        else if (pieces <= 512 * 16) rc = launch_distill<512, 16, DI_FUSED>(a, d, d->rows, hs);
+        else rc = launch_distill<1024, 17, DI_IN_TURN>(a, d, d->rows < 256 ? d->rows : 256, hs);
     }
     if (rc == MP_OK) *parts = mp_mean_parts{row_loss, (double)d->rows, d->rows, 0};
     return rc;

@@ -15,9 +15,9 @@
 
 namespace mp {
 
-constexpr int LP_THREADS = 256, LP_WAVES = LP_THREADS / 64;
-constexpr int LP_FOUND   = 512;  // elements gathered; k is at most MP_TOP_MAX
-constexpr int LP_CHUNKS  = 48;   // a row is cut into at most so many
+constexpr int LP_FOUND  = 512;    // elements gathered; k is at most MP_TOP_MAX
+constexpr int LP_CHUNKS = 48;     // a row is cut into at most so many
+constexpr int LP_LOCAL  = 65536;  // elements of a chunk at most
 
 typedef unsigned long long u64;
 
@@ -30,77 +30,104 @@ __device__ __forceinline__ unsigned order_key(unsigned h) {
 __device__ __forceinline__ float key_value(unsigned key) {
     return key == 0xFFFFu ? NAN : h2f((uint16_t)((key & 0x8000u) ? key & 0x7FFFu : ~key & 0xFFFFu));
 }
-// larger is better: the value, then the lower index.  0 is none.
-__device__ __forceinline__ u64 make_entry(unsigned key, int index) { return ((u64)(key + 1) << 32) | (0x7FFFFFFFu - (unsigned)index); }
-__device__ __forceinline__ unsigned entry_key(u64 e) { return (unsigned)(e >> 32) - 1; }
-__device__ __forceinline__ int      entry_index(u64 e) { return (int)(0x7FFFFFFFu - (unsigned)e); }
+// An element of a chunk in one word, larger is better: its key, then the lower index.  0 is none (no key is).
+__device__ __forceinline__ unsigned make_entry(unsigned key, int local) { return (key << 16) | (unsigned)(LP_LOCAL - 1 - local); }
+__device__ __forceinline__ unsigned entry_key(unsigned e) { return e >> 16; }
+__device__ __forceinline__ int      entry_local(unsigned e) { return LP_LOCAL - 1 - (int)(e & (LP_LOCAL - 1)); }
+// ... of a row
+__device__ __forceinline__ u64      far_entry(unsigned key, int index) { return ((u64)key << 32) | (0x7FFFFFFFu - (unsigned)index); }
+__device__ __forceinline__ unsigned far_key(u64 e) { return (unsigned)(e >> 32); }
+__device__ __forceinline__ int      far_index(u64 e) { return (int)(0x7FFFFFFFu - (unsigned)e); }
 
+template <int THREADS>
 struct TopLds {
-    u64 found[LP_FOUND];
-    int count, equal[LP_WAVES];
-    unsigned short lane_key[LP_THREADS];
-    float bound;
+    static constexpr int WAVES = THREADS / 64, HELD = WAVES > 4 ? 64 : 128, KEYS = 256;
+    u32x4          found[LP_FOUND / 4];  // entries, zeros behind them up to a multiple of 16
+    u32x4          piece[WAVES][HELD];   // pieces with an element that reaches the bound
+    unsigned short place[WAVES][HELD];   // and which they are
+    unsigned short best[KEYS];           // keys of the largest elements of the lanes, of two lanes, or of their pieces
+    int            count, equal[WAVES];
+    float          bound;
+    __device__ __forceinline__ unsigned& entry(int i) { return reinterpret_cast<unsigned*>(found)[i]; }
 };
 
 __device__ __forceinline__ unsigned half_of(const u32x4 q, int k) { return (k & 1) ? q[k >> 1] >> 16 : q[k >> 1] & 0xFFFFu; }
 
-// k-th largest of the lanes' maxima as a value, by one wave; -inf where fewer have one
-__device__ __forceinline__ float kth_of_lanes(const unsigned short* lane_key, int k) {
-    unsigned key[LP_WAVES];
+// k-th largest of 64 N keys as a value, by one wave.  (Not above -inf where fewer than k have one.)
+template <int N>
+__device__ __forceinline__ float kth_of(const unsigned short* keys, int k) {
+    unsigned key[N];
 #pragma unroll
-    for (int i = 0; i < LP_WAVES; ++i) key[i] = lane_key[i * 64 + (threadIdx.x & 63)];
+    for (int i = 0; i < N; ++i) key[i] = keys[i * 64 + (threadIdx.x & 63)];
     unsigned best = 0;
 #pragma unroll
     for (int b = 15; b >= 0; --b) {
         const unsigned c = best | (1u << b);
         int            n = 0;
 #pragma unroll
-        for (int i = 0; i < LP_WAVES; ++i) n += __popcll(__ballot(key[i] >= c));
+        for (int i = 0; i < N; ++i) n += __popcll(__ballot(key[i] >= c));
         if (n >= k) best = c;
     }
     return key_value(best);
 }
 
-// The same by value, bit by bit, from memory (the row is in a cache by now): any values, k elements exactly.
-__device__ __forceinline__ int gather_exact(const Stretch z, const int first, const int k, TopLds& t) {
-    const int  tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, rounds = (z.pieces() + LP_THREADS - 1) / LP_THREADS;
-    const auto each = [&](int v, const u32x4 q, auto&& pred) {  // elements of the stretch that are pred, as bits
-        unsigned hit = 0;
+__device__ __forceinline__ int lanes_ahead(u64 mask) {  // set bits of lower lanes
+    return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u));
+}
+
+// The k largest of the chunk by value, bit by bit: any values, k elements exactly.  A lane with one piece keeps it, otherwise they are read
+// again (the row is in a cache by now; four pieces a lane kept take 140 registers, and 4096 x 2000 with 100 alternatives 26 us, not 19).
+template <int THREADS, int VECS>
+__device__ __forceinline__ int gather_exact(const u32x4 (&raw)[VECS], const Stretch& z, const int k, TopLds<THREADS>& t) {
+    constexpr int  WAVES = THREADS / 64;
+    constexpr bool KEPT = WAVES == 1 && VECS == 1;
+    const int      tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, rounds = (z.pieces() + THREADS - 1) / THREADS;
+    // f(key + 1, or 0 outside the stretch; element)
+    const auto each = [&](int v, const u32x4 q, auto&& f) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int e = 8 * v + j - z.head;
-            hit |= (unsigned)(e >= 0 && e < z.len && pred(order_key(half_of(q, j)))) << j;
+            f(e >= 0 && e < z.len ? order_key(half_of(q, j)) + 1 : 0u, e);
         }
-        return hit;
     };
-    const auto total = [&](int n) {  // over the workgroup, for every thread
-        for (int far = 32; far; far >>= 1) n += __shfl_xor(n, far, 64);
+    const auto every_piece = [&](auto&& f) {
+        if (KEPT) {
+            f(tid, raw[0]);
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < rounds; ++i) f(i * THREADS + tid, z.load(i * THREADS + tid));
+        }
+    };
+    const auto count = [&](unsigned from) {  // elements whose key + 1 is at least that
+        int n = 0;
+        every_piece([&](int v, const u32x4 q) { each(v, q, [&](unsigned key, int) { n += KEPT ? __popcll(__ballot(key >= from)) : (int)(key >= from); }); });
+        if (KEPT) return n;
+        n = (int)wave_sum((float)n);
+        if (WAVES == 1) return n;
         lds_barrier();
         if (lane == 0) t.equal[wave] = n;
         lds_barrier();
         int s = 0;
 #pragma unroll
-        for (int w = 0; w < LP_WAVES; ++w) s += t.equal[w];
+        for (int w = 0; w < WAVES; ++w) s += t.equal[w];
         return s;
     };
-    const auto count = [&](auto&& pred) {
-        int n = 0;
-        for (int i = 0; i < rounds; ++i) n += __popc(each(i * LP_THREADS + tid, z.load(i * LP_THREADS + tid), pred));
-        return total(n);
-    };
-    unsigned best = 0;
-    for (int b = 15; b >= 0; --b) {
+    unsigned best = 0;  // a key + 1
+    for (int b = 16; b >= 0; --b) {
         const unsigned c = best | (1u << b);
-        if (count([&](unsigned key) { return key >= c; }) >= k) best = c;
+        if (c <= 0x10000u && count(c) >= k) best = c;
     }
-    int left = k - count([&](unsigned key) { return key > best; });  // of the elements equal to it, in the order of their indices
+    int left = k - count(best + 1);  // of the elements equal to it, in the order of their indices
     if (tid == 0) t.count = 0;
-    for (int i = 0; i < rounds; ++i) {
-        const int      v    = i * LP_THREADS + tid;
-        const u32x4    q    = z.load(v);
-        const unsigned same = each(v, q, [&](unsigned key) { return key == best; });
-        unsigned       hit  = each(v, q, [&](unsigned key) { return key > best; });
-        int            upto = __popc(same);  // inclusive sum over the wave's lanes
+    every_piece([&](int v, const u32x4 q) {
+        unsigned same = 0, hit = 0;
+        int      j    = 0;
+        each(v, q, [&](unsigned key, int) {
+            same |= (unsigned)(key == best) << j;
+            hit |= (unsigned)(key > best) << j;
+            ++j;
+        });
+        int upto = __popc(same);  // inclusive sum over the wave's lanes
         for (int far = 1; far < 64; far <<= 1) {
             const int n = __shfl_up(upto, far, 64);
             if (lane >= far) upto += n;
@@ -110,61 +137,100 @@ __device__ __forceinline__ int gather_exact(const Stretch z, const int first, co
         lds_barrier();
         int ahead = upto - __popc(same), all = 0;
 #pragma unroll
-        for (int w = 0; w < LP_WAVES; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             ahead += w < wave ? t.equal[w] : 0;
             all += t.equal[w];
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if ((same >> j) & 1) hit |= (unsigned)(ahead++ < left) << j;
+        for (int i = 0; i < 8; ++i)
+            if ((same >> i) & 1) hit |= (unsigned)(ahead++ < left) << i;
         left -= min(left, all);
         int at = atomicAdd(&t.count, __popc(hit));
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if ((hit >> j) & 1) t.found[at++] = make_entry(order_key(half_of(q, j)), first + 8 * v + j - z.head);
-    }
+        j      = 0;
+        each(v, q, [&](unsigned key, int e) {
+            if ((hit >> j++) & 1) t.entry(at++) = make_entry(key - 1, e);
+        });
+    });
     lds_barrier();
     return t.count;
 }
 
-// The k largest of the chunk into t.found, any order; returns their number or more.  All threads; ends with a barrier.
-template <int VECS>
-__device__ int gather_top(u32x4 (&raw)[VECS], const Stretch& z, int first, int k, float lane_top, bool plain, TopLds& t) {
-    const int tid = threadIdx.x, wave = tid >> 6;
-    t.lane_key[tid] = (unsigned short)order_key(f2h(lane_top));
+// The k largest of the chunk, and few others, into t.found in any order; returns their number.  All threads; ends with a barrier.
+template <int THREADS, int VECS>
+__device__ __forceinline__ int gather_top(u32x4 (&raw)[VECS], const Stretch& z, int k, float lane_top, bool plain, TopLds<THREADS>& t) {
+    // of one wave the pieces' maxima (its lanes are few beside k), of eight the maxima of two lanes each
+    constexpr int PIECES = THREADS == 64 ? VECS : 1, SHARE = THREADS == 512 ? 2 : 1, KEYS = PIECES * THREADS / SHARE;
+    const int     tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        float top = PIECES > 1 ? max_of<1>(&raw[i]) : lane_top;
+        if (SHARE > 1) top = fmaxf(top, __shfl_xor(top, 1, 64));
+        if (tid % SHARE == 0) t.best[i * THREADS + tid / SHARE] = (unsigned short)order_key(f2h(top));
+    }
     if (tid == 0) t.count = 0;
     lds_barrier();
     if (wave == 0) {
-        const float b = kth_of_lanes(t.lane_key, k);
-        if (tid == 0) t.bound = b;
+        const float b = kth_of<KEYS / 64>(t.best, k);
+        if (lane == 0) t.bound = b;
     }
     lds_barrier();
     const float bound = t.bound;
     if (plain && bound > -INFINITY) {
-        if (lane_top >= bound) {
+        // each wave its pieces, then eight of these at a time, a lane an element
+        constexpr int HELD  = TopLds<THREADS>::HELD;
+        int           held  = 0;
 #pragma unroll
-            for (int i = 0; i < VECS; ++i) {
-                asm("" : "+v"(raw[i]));  // (or the compiler keeps 100 registers of halves from the sums until here)
-                if (max_of<1>(&raw[i]) >= bound) {
-                    unsigned hit = 0;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) hit |= (unsigned)(h2f((uint16_t)half_of(raw[i], j)) >= bound) << j;
-                    const int at = atomicAdd(&t.count, __popc(hit));
-                    int       n  = 0;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if ((hit >> j) & 1) {
-                            if (at + n < LP_FOUND) t.found[at + n] = make_entry(order_key(half_of(raw[i], j)), first + 8 * (i * LP_THREADS + tid) + j - z.head);
-                            ++n;
-                        }
+        for (int i = 0; i < VECS; ++i) {
+            asm("" : "+v"(raw[i]));  // (or the compiler keeps 100 registers of halves from the sums until here)
+            const bool hit  = max_of<1>(&raw[i]) >= bound;
+            const u64  mask = __ballot(hit);
+            if (mask) {
+                const int at = held + lanes_ahead(mask);
+                if (hit && at < HELD) {
+                    t.piece[wave][at] = raw[i];
+                    t.place[wave][at] = (unsigned short)(i * THREADS + tid);
                 }
+                held += __popcll(mask);
             }
         }
+        __builtin_amdgcn_wave_barrier();
+        for (int b = 0; b < min(held, HELD); b += 8) {
+            const int p = b + (lane >> 3), j = lane & 7;
+            unsigned  h = 0xFC00u;
+            if (p < min(held, HELD)) h = reinterpret_cast<const unsigned short*>(&t.piece[wave][p])[j];
+            const bool ok   = h2f((uint16_t)h) >= bound;
+            const u64  mask = __ballot(ok);
+            int        base = 0;
+            if (lane == 0) base = atomicAdd(&t.count, __popcll(mask));
+            const int at = __builtin_amdgcn_readfirstlane(base) + lanes_ahead(mask);
+            if (ok && at < LP_FOUND) t.entry(at) = make_entry(order_key(h), 8 * t.place[wave][p] + j - z.head);
+        }
+        if (held > HELD && lane == 0) atomicAdd(&t.count, LP_FOUND + 1);
         lds_barrier();
         const int n = t.count;
         if (n <= LP_FOUND) return n;
     }
-    return gather_exact(z, first, k, t);
+    return gather_exact<THREADS, VECS>(raw, z, k, t);
+}
+
+// f(place, entry) for the k best of n entries, each placed by the number ahead of it.
+template <int THREADS, typename F>
+__device__ __forceinline__ void place_entries(TopLds<THREADS>& t, int n, int k, F&& f) {
+    const int tid = threadIdx.x, padded = (n + 15) & ~15;
+    if (tid < padded - n) t.entry(n + tid) = 0;
+    lds_barrier();
+    for (int i = tid; i < n; i += THREADS) {
+        const unsigned mine  = t.entry(i);
+        int            place = 0;
+        for (int j = 0; j < padded / 4; j += 4) {
+            u32x4 e[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) e[u] = t.found[j + u];
+#pragma unroll
+            for (int u = 0; u < 16; ++u) place += e[u >> 2][u & 3] > mine;
+        }
+        if (place < k) f(place, mine);
+    }
 }
 
 struct RowArgs {
@@ -192,100 +258,109 @@ struct RowOut {
         if (a.lse) a.lse[row] = s == 0.f ? -INFINITY : LN2 * (ref + log_s);
         if (a.entropy) a.entropy[row] = LN2 * (log_s - t / s);
     }
-    __device__ __forceinline__ void alternative(int place, u64 e) const {
-        a.top_ids[row * a.top + place]  = entry_index(e);
-        a.top_logp[row * a.top + place] = of(key_value(entry_key(e)));
+    __device__ __forceinline__ void alternative(int place, int index, unsigned key) const {
+        a.top_ids[row * a.top + place]  = index;
+        a.top_logp[row * a.top + place] = of(key_value(key));
     }
 };
 
-template <int VECS, bool TOP>
-__global__ __launch_bounds__(LP_THREADS) void token_logprobs_kernel(const RowArgs a) {
-    __shared__ float  red[LP_WAVES][4];
-    const long long   row   = blockIdx.x / a.chunks;
-    const int         chunk = blockIdx.x - (int)row * a.chunks, first = chunk * a.chunk, len = min(a.chunk, a.vocab - first);
-    const Stretch     z(a.logits + row * a.ld + first, len);
-    const int         tid = threadIdx.x;
-    u32x4             raw[VECS];
+template <int THREADS, int VECS, bool TOP>
+__global__ __launch_bounds__(THREADS) void token_logprobs_kernel(const RowArgs a) {
+    constexpr int    WAVES = THREADS / 64;
+    __shared__ float red[WAVES][4];
+    const long long  row   = blockIdx.x / a.chunks;
+    const int        chunk = blockIdx.x - (int)row * a.chunks, first = chunk * a.chunk, len = min(a.chunk, a.vocab - first);
+    const Stretch    z(a.logits + row * a.ld + first, len);
+    const int        tid = threadIdx.x;
+    u32x4            raw[VECS];
 #pragma unroll
-    for (int i = 0; i < VECS; ++i) raw[i] = z.load(i * LP_THREADS + tid);
-    constexpr int G = VECS < 4 ? VECS : 4;
+    for (int i = 0; i < VECS; ++i) raw[i] = z.load(i * THREADS + tid);
+    constexpr int G = VECS < 4 ? VECS : THREADS > 256 ? 2 : 4;
     Sums<true>    sum(a.c2);
     float         lane_top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < VECS; i += G) {
+        if (i * THREADS >= z.pieces()) break;
         const float m = max_of<G>(raw + i);
         sum.add_pieces<G>(raw + i, a.c2, m);
         lane_top = fmaxf(lane_top, m);
     }
     sum.over_wave();
-    if ((tid & 63) == 0) {
-        red[tid >> 6][0] = sum.ref;
-        red[tid >> 6][1] = sum.s;
-        red[tid >> 6][2] = sum.t;
-    }
-    lds_barrier();
-    Sums<true> all(a.c2);
-#pragma unroll
-    for (int w = 0; w < LP_WAVES; ++w) all.add_sums(red[w][0], red[w][1], red[w][2]);
-    const RowOut out{a, row, all.ref, all.s, all.t};
-    if (tid == 0) {
-        if (a.chunks == 1) {
-            out.row_values();
-        } else {
-            *reinterpret_cast<f32x4*>(a.sums + (row * a.chunks + chunk) * 4) = f32x4{all.ref, all.s, all.t, 0.f};
+    if (WAVES > 1) {
+        if ((tid & 63) == 0) {
+            red[tid >> 6][0] = sum.ref;
+            red[tid >> 6][1] = sum.s;
+            red[tid >> 6][2] = sum.t;
         }
+        lds_barrier();
+        sum = Sums<true>(a.c2);
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) sum.add_sums(red[w][0], red[w][1], red[w][2]);
+    }
+    const RowOut out{a, row, sum.ref, sum.s, sum.t};
+    if (tid == 0) {
+        if (a.chunks == 1) out.row_values();
+        else *reinterpret_cast<f32x4*>(a.sums + (row * a.chunks + chunk) * 4) = f32x4{sum.ref, sum.s, sum.t, 0.f};
     }
     if constexpr (TOP) {
-        __shared__ TopLds top;
-        const int         k = min(a.top, len), n = gather_top<VECS>(raw, z, first, k, lane_top, all.s < INFINITY, top);
-        for (int i = tid; i < n; i += LP_THREADS) {
-            const u64 mine  = top.found[i];
-            int       place = 0;
-            for (int j = 0; j < n; ++j) place += top.found[j] > mine;
-            if (place < k) {
-                if (a.chunks == 1) out.alternative(place, mine);
-                else a.lists[(row * a.chunks + chunk) * a.top + place] = mine;
-            }
-        }
+        __shared__ TopLds<THREADS> top;
+        const int                  k = min(a.top, len), n = gather_top<THREADS, VECS>(raw, z, k, lane_top, sum.s < INFINITY, top);
+        u64*                       list = a.lists + (row * a.chunks + chunk) * a.top;
+        place_entries<THREADS>(top, n, k, [&](int place, unsigned e) {
+            const int index = first + entry_local(e);
+            if (a.chunks == 1) out.alternative(place, index, entry_key(e));
+            else list[place] = far_entry(entry_key(e), index);
+        });
         if (a.chunks > 1)
-            for (int i = k + tid; i < a.top; i += LP_THREADS) a.lists[(row * a.chunks + chunk) * a.top + i] = 0;
+            for (int i = k + tid; i < a.top; i += THREADS) list[i] = 0;
     }
 }
 
-// Chunks of a row joined: sums, and of the sorted lists the first `top`, each entry placed by how many are ahead of it in every list.
-__global__ __launch_bounds__(LP_THREADS) void token_logprobs_join_kernel(const RowArgs a) {
-    extern __shared__ u64 lists[];
+// Chunks of a row joined: sums, and of the sorted lists the first `top`.  Every list has at least ceil(top / chunks) entries that reach
+// the least of the lists' entries at that place; those that do are gathered and placed by counting.
+constexpr int JOIN_THREADS = 256;
+__global__ __launch_bounds__(JOIN_THREADS) void token_logprobs_join_kernel(const RowArgs a) {
+    extern __shared__ u64 found[];
+    __shared__ int        count;
     const long long       row = blockIdx.x;
-    const int             n   = a.chunks * a.top;
-    for (int i = threadIdx.x; i < n; i += LP_THREADS) lists[i] = a.lists[row * n + i];
-    Sums<true> all(a.c2);
-    for (int c = 0; c < a.chunks; ++c) {
-        const f32x4 v = *reinterpret_cast<const f32x4*>(a.sums + (row * a.chunks + c) * 4);
-        all.add_sums(v[0], v[1], v[2]);
+    const int             n = a.chunks * a.top, tid = threadIdx.x, lane = tid & 63;
+    const u64*            lists = a.lists + row * n;
+    Sums<true>            all(a.c2);
+    f32x4                 v = {all.ref, 0.f, 0.f, 0.f};
+    u64                   bound = ~0ull;
+    if (lane < a.chunks) {
+        v = *reinterpret_cast<const f32x4*>(a.sums + (row * a.chunks + lane) * 4);
+        if (a.top) bound = lists[lane * a.top + (a.top + a.chunks - 1) / a.chunks - 1];
     }
+    all.add_sums(v[0], v[1], v[2]);
+    all.over_wave();
     const RowOut out{a, row, all.ref, all.s, all.t};
-    if (threadIdx.x == 0) out.row_values();
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += LP_THREADS) {
-        const u64 mine = lists[i];
-        if (mine == 0) continue;
-        int place = 0;
-        for (int c = 0; c < a.chunks && place < a.top; ++c) {
-            int lo = 0, hi = a.top;  // entries of list c ahead of mine
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (lists[c * a.top + mid] > mine) lo = mid + 1;
-                else hi = mid;
-            }
-            place += lo;
-        }
-        if (place < a.top) out.alternative(place, mine);
+    if (tid == 0) out.row_values();
+    if (a.top == 0) return;
+    for (int far = 32; far; far >>= 1) bound = min(bound, (u64)__shfl_xor((unsigned long long)bound, far, 64));
+    if (tid == 0) count = 0;
+    lds_barrier();
+    for (int i = tid; i < n; i += JOIN_THREADS) {
+        const u64 e = lists[i];
+        if (e != 0 && e >= bound) found[atomicAdd(&count, 1)] = e;
+    }
+    lds_barrier();
+    const int m = count;
+    if (tid < ((m + 7) & ~7) - m) found[m + tid] = 0;
+    lds_barrier();
+    for (int i = tid; i < m; i += JOIN_THREADS) {
+        const u64 mine  = found[i];
+        int       place = 0;
+        for (int j = 0; j < m; j += 8)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) place += found[j + u] > mine;
+        if (place < a.top) out.alternative(place, far_index(mine), far_key(mine));
     }
 }
 
 // dx = RNE16(S c (g (1[target] - p) - h p (ln p + entropy))), S c = scale / temperature; bound by HBM (4 bytes an element).
-constexpr int LPB_VECS = 4;
-__global__ __launch_bounds__(LP_THREADS) void token_logprobs_bwd_kernel(const int vocab, const int ld, const int pieces, const uint16_t* logits,
+constexpr int LPB_VECS = 4, LPB_THREADS = 256;
+__global__ __launch_bounds__(LPB_THREADS) void token_logprobs_bwd_kernel(const int vocab, const int ld, const int pieces, const uint16_t* logits,
                                                                         const int32_t* __restrict__ targets, const float c,
                                                                         const float* __restrict__ entropy, const float* __restrict__ lse,
                                                                         const float* __restrict__ dlogp, const float* __restrict__ dentropy,
@@ -295,7 +370,7 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_bwd_kernel(const in
     const Stretch   z(logits + row * ld, vocab);
     u32x4           raw[LPB_VECS];
 #pragma unroll
-    for (int i = 0; i < LPB_VECS; ++i) raw[i] = z.load((piece * LPB_VECS + i) * LP_THREADS + threadIdx.x);
+    for (int i = 0; i < LPB_VECS; ++i) raw[i] = z.load((piece * LPB_VECS + i) * LPB_THREADS + threadIdx.x);
     const int   y  = targets ? targets[row] : -1;
     const float sc = (st ? st->scale : 1.f) * c, g = dlogp && y >= 0 && y < vocab ? sc * dlogp[row] : 0.f, h = dentropy ? sc * dentropy[row] : 0.f;
     const float a = -(g + (dentropy ? h * entropy[row] : 0.f)), l = -lse[row];
@@ -303,7 +378,7 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_bwd_kernel(const in
     const int   vt = g != 0.f ? (y + z.head) >> 3 : -1, kt = (y + z.head) & 7;
 #pragma unroll
     for (int i = 0; i < LPB_VECS; ++i) {
-        const int v = (piece * LPB_VECS + i) * LP_THREADS + threadIdx.x;
+        const int v = (piece * LPB_VECS + i) * LPB_THREADS + threadIdx.x;
         float     d[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
@@ -328,7 +403,7 @@ using namespace mp;
 
 namespace {
 
-constexpr int LP_MOST = 16 * 8 * LP_THREADS;  // elements of a chunk that starts at a piece
+constexpr int LP_MOST = LP_LOCAL;  // elements of a chunk that starts at a piece
 
 struct ChunkPlan {
     int chunks, chunk;
@@ -338,7 +413,7 @@ struct ChunkPlan {
 ChunkPlan chunk_plan(int rows, int vocab, bool even) {
     const int most = even ? LP_MOST : LP_MOST - 8;
     int       n    = (vocab + most - 1) / most;
-    while (n * 2 <= LP_CHUNKS && (long long)rows * n * 2 <= 256 && vocab / (n * 2) >= 2048) n *= 2;
+    while (n > 1 && n * 2 <= LP_CHUNKS && (long long)rows * n * 2 <= 256 && vocab / (n * 2) >= 8192) n *= 2;
     if (n == 1) return {1, vocab};
     const int chunk = ((vocab + n - 1) / n + 7) / 8 * 8;
     return {(vocab + chunk - 1) / chunk, chunk};
@@ -389,25 +464,36 @@ extern "C" int mp_token_logprobs(int rows, int vocab, int top, const mp_half* lo
         set_error("%s: 16-byte aligned workspace of %zu bytes needed, %zu given", what, need, ws_bytes);
         return MP_E_WORKSPACE;
     }
-    MP_REQUIRE(grid_fits((long long)rows * p.chunks, LP_THREADS), "%s: too many rows", what);
+    MP_REQUIRE(grid_fits((long long)rows * p.chunks, 256), "%s: too many rows", what);
     RowArgs a{vocab, ld, top, p.chunks, p.chunk, logits, targets, inv_temperature * LOG2E, logp, entropy, lse, top_logp, top_ids, static_cast<float*>(ws), nullptr};
     if (p.chunks > 1) a.lists = reinterpret_cast<u64*>(static_cast<char*>(ws) + lists_offset(rows, p));
     hipStream_t hs     = as_stream(stream);
-    const dim3  grid((unsigned)(rows * p.chunks)), block(LP_THREADS);
-    const auto  launch = [&](auto vecs) {
-        constexpr int V = decltype(vecs)::value;
-        if (top) hipLaunchKernelGGL((token_logprobs_kernel<V, true>), grid, block, 0, hs, a);
-        else hipLaunchKernelGGL((token_logprobs_kernel<V, false>), grid, block, 0, hs, a);
+    const auto  launch = [&](auto threads, auto vecs) {
+        constexpr int T = decltype(threads)::value, V = decltype(vecs)::value;
+        const dim3    grid((unsigned)(rows * p.chunks));
+        if (top) hipLaunchKernelGGL((token_logprobs_kernel<T, V, true>), grid, dim3(T), 0, hs, a);
+        else hipLaunchKernelGGL((token_logprobs_kernel<T, V, false>), grid, dim3(T), 0, hs, a);
     };
     const int pieces = (p.chunk + (even ? 7 : 14)) / 8;
-    if (pieces <= LP_THREADS) launch(std::integral_constant<int, 1>{});
-    else if (pieces <= 2 * LP_THREADS) launch(std::integral_constant<int, 2>{});
-    else if (pieces <= 4 * LP_THREADS) launch(std::integral_constant<int, 4>{});
-    else if (pieces <= 8 * LP_THREADS) launch(std::integral_constant<int, 8>{});
-    else launch(std::integral_constant<int, 16>{});
+    typedef std::integral_constant<int, 64>   W1;
+    typedef std::integral_constant<int, 256>  W4;
+    typedef std::integral_constant<int, 512>  W8;
+    typedef std::integral_constant<int, 1>    V1;
+    typedef std::integral_constant<int, 2>    V2;
+    typedef std::integral_constant<int, 4>    V4;
+    typedef std::integral_constant<int, 8>    V8;
+    typedef std::integral_constant<int, 16>   V16;
+    if (pieces <= 64) launch(W1{}, V1{});
+    else if (pieces <= 128) launch(W1{}, V2{});
+    else if (pieces <= 256) launch(W1{}, V4{});
+    else if (pieces <= 512) launch(W4{}, V2{});
+    else if (pieces <= 1024) launch(W4{}, V4{});
+    else if (pieces <= 2048) launch(W4{}, V8{});
+    else if (pieces <= 4096) launch(W4{}, V16{});
+    else launch(W8{}, V16{});
     MP_LAUNCH_CHECK("mp_token_logprobs");
     if (p.chunks > 1) {
-        hipLaunchKernelGGL(token_logprobs_join_kernel, dim3(rows), block, (size_t)p.chunks * top * sizeof(u64), hs, a);
+        hipLaunchKernelGGL(token_logprobs_join_kernel, dim3(rows), dim3(JOIN_THREADS), ((size_t)p.chunks * top + 8) * sizeof(u64), hs, a);
         MP_LAUNCH_CHECK("mp_token_logprobs(join)");
     }
     return MP_OK;
@@ -425,9 +511,9 @@ extern "C" int mp_token_logprobs_bwd(int rows, int vocab, const mp_half* logits,
     MP_REQUIRE(!dentropy || entropy, "%s: a gradient of the entropy needs the entropy", what);
     MP_REQUIRE(aligned(logits, 2) && aligned(dlogits, 2) && aligned(st, 4) && aligned(targets, 4) && aligned(entropy, 4) && aligned(lse, 4) && aligned(dlogp, 4) && aligned(dentropy, 4),
                "%s: misaligned pointer", what);
-    const int pieces = ((vocab + 7 + 7) / 8 + LPB_VECS * LP_THREADS - 1) / (LPB_VECS * LP_THREADS);
-    MP_REQUIRE(grid_fits((long long)rows * pieces, LP_THREADS), "%s: too many rows", what);
-    hipLaunchKernelGGL(token_logprobs_bwd_kernel, dim3((unsigned)(rows * pieces)), dim3(LP_THREADS), 0, as_stream(stream), vocab, ld, pieces, logits, targets,
+    const int pieces = ((vocab + 7 + 7) / 8 + LPB_VECS * LPB_THREADS - 1) / (LPB_VECS * LPB_THREADS);
+    MP_REQUIRE(grid_fits((long long)rows * pieces, LPB_THREADS), "%s: too many rows", what);
+    hipLaunchKernelGGL(token_logprobs_bwd_kernel, dim3((unsigned)(rows * pieces)), dim3(LPB_THREADS), 0, as_stream(stream), vocab, ld, pieces, logits, targets,
                        inv_temperature, entropy, lse, dlogp, dentropy, st, dlogits);
     MP_LAUNCH_CHECK("mp_token_logprobs_bwd");
     return MP_OK;
