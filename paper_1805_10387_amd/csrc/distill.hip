@@ -5,13 +5,13 @@
 //     L = sum_A q_u (ln q_u - ln p_u) + r (ln r - ln p_rest),       dL/dz_j = (Q + r) p_j - (j in A ? q_j : r p_j / p_rest)
 //     dx_j = S / rows (weight / temperature dL/dz_j + hard (softmax(x)_j - 1[j = target]))
 //
-// Bound by HBM: 2 bytes a class read, 2 written.  A workgroup holds a row in registers from its sums to its gradient, and takes the
-// next row's pieces into the same registers one by one as the gradient leaves them, so loads and stores run beside each other.
+// Bound by HBM: 2 bytes a class read, 2 written.  A workgroup holds a row in registers from its sums to its gradient; several of them
+// on a compute unit are in different parts of that.
 // Outside A the gradient is one factor a row times the exponential.  The classes of A, at most 128, are one wave's work: their
 // gradients wait in LDS, and a map from pieces to entries tells each piece which of its elements to replace.  For r the sum over
 // "all others" is formed without A, not as a difference of sums, which would lose it where the student is sure of A.
 //
-// Rows longer than 139256 classes, or too few for the chip, are cut into chunks: one launch for the sums, one for the gradient.
+// Rows longer than 135160 classes, or too few for the chip, are cut into chunks: one launch for the sums, one for the gradient.
 #include <cmath>
 
 #include "vocab_rows.hpp"
@@ -38,9 +38,10 @@ struct EntryLds {
     int      id[MP_TOP_MAX + 1];
     float    t[MP_TOP_MAX], q[MP_TOP_MAX], x[MP_TOP_MAX + 1];  // the teacher's log probability, q, the student's logit
     unsigned info[MP_TOP_MAX + 1];                             // as in the map; there for those behind the first one of a word
+    int      again[MP_TOP_MAX];                                // an earlier entry names the class too
 };
 // A word of the map, 0 where there is no entry: the next entry of the word + 1, the element's place among the word's, flags, its gradient.
-constexpr unsigned MAP_NEXT = 0xFFu, MAP_TARGET = 1u << 12, MAP_THERE = 1u << 13;
+constexpr unsigned MAP_NEXT = 0xFFu, MAP_TARGET = 1u << 12, MAP_THERE = 1u << 13, MAP_FIRST = 1u << 14;
 __device__ __forceinline__ int map_place(unsigned w) { return (int)(w >> 8) & 15; }
 struct RowFactors {
     float a, ref, b, ref2;  // gradient outside A: a 2^(c2 x - ref) + b 2^(log2(e) x - ref2)
@@ -68,13 +69,13 @@ struct Entries {
     // word of the map for class c, or -1: another stretch's, or none
     __device__ __forceinline__ int word(const Stretch& z, int c) const { return c >= first && c < a.vocab && c - first < z.len ? (c - first + z.head) >> SHIFT : -1; }
 
-    // a row's list on its way, and then in place
-    struct Ahead {
+    // the row's list on its way, and then in place
+    struct List {
         int   id[2], target;
         float t[2];
     };
-    __device__ __forceinline__ static Ahead fetch(const DistillArgs& a, long long row) {
-        Ahead h;
+    __device__ __forceinline__ List fetch(long long row) const {
+        List h;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const long long e = row * a.top + min(lane() + 64 * s, a.top - 1);
@@ -84,7 +85,7 @@ struct Entries {
         h.target = a.targets ? a.targets[row] : -1;
         return h;
     }
-    __device__ __forceinline__ void settle(const Ahead& h) {
+    __device__ __forceinline__ void settle(const List& h) {
 #pragma unroll
         for (int s = 0; s < 2; ++s)
             if (lane() + 64 * s < a.top) {
@@ -124,6 +125,18 @@ struct Entries {
         });
         some   = __any(any);
         listed = __any(eq) && there(target);
+        bool again = false;
+        if (a.chunks > 1) {  // (entries of one class may all lie in another chunk: the map is a hash table of the whole list first)
+            each([&](int e) {
+                if (there(l.id[e])) l.info[e] = atomicExch(&map[l.id[e] & 255], (unsigned)e + 1);
+            });
+            __builtin_amdgcn_wave_barrier();
+            each([&](int e) {
+                if (there(l.id[e]))
+                    for (unsigned o = l.info[e]; o; o = l.info[o - 1]) again |= l.id[o - 1] == l.id[e];
+            });
+            each([&](int e) { map[l.id[e] & 255] = 0; });
+        }
         const auto enter = [&](int e, unsigned flag) {
             const int c = l.id[e], w = word(z, c);
             if (w >= 0) l.info[e] = atomicExch(&map[w], (unsigned)e + 1) | (unsigned)((c - first + z.head) & ((1 << SHIFT) - 1)) << 8 | flag | MAP_THERE;
@@ -131,16 +144,15 @@ struct Entries {
         each([&](int e) { enter(e, 0u); });
         if (lane() == 0 && !listed) enter(DI_TARGET, MAP_TARGET);
         __builtin_amdgcn_wave_barrier();
-        bool again = false;
         each([&](int e) {
             if (word(z, l.id[e]) >= 0)
                 for (unsigned o = l.info[e] & MAP_NEXT; o; o = l.info[o - 1] & MAP_NEXT) again |= l.id[o - 1] == l.id[e];
         });
-        twice = a.chunks > 1 || __any(again);  // (the rest of a list may lie in another chunk)
+        twice = __any(again);
         // the first one of a word moves into it; indices are below 256 and what moves in is above
         const auto head = [&](int e) {
             const int w = word(z, l.id[e]);
-            if (w >= 0 && map[w] == (unsigned)e + 1) map[w] = l.info[e];
+            if (w >= 0 && map[w] == (unsigned)e + 1) map[w] = l.info[e] |= MAP_FIRST;
         };
         each(head);
         if (lane() == 0 && !listed) head(DI_TARGET);
@@ -149,17 +161,9 @@ struct Entries {
     __device__ __forceinline__ void put(const Stretch& z, int e, float value) const {
         const int w = word(z, l.id[e]);
         if (w < 0) return;
-        const unsigned info = l.info[e], full = info | (unsigned)f2h(value) << 16;
-        if (map[w] == info) map[w] = full;
+        const unsigned full = l.info[e] | (unsigned)f2h(value) << 16;
+        if (full & MAP_FIRST) map[w] = full;
         else l.info[e] = full;
-    }
-    __device__ __forceinline__ void remove(const Stretch& z) const {
-        const auto out = [&](int e) {
-            const int w = word(z, l.id[e]);
-            if (w >= 0) map[w] = 0;
-        };
-        each(out);
-        if (lane() == 0) out(DI_TARGET);
     }
 };
 
@@ -169,105 +173,125 @@ __device__ __forceinline__ double wave_sum64(double v) {
     return v;
 }
 
-// One wave: the row's loss, its factors, and the entries' gradients.  one, two: sums at the temperature and (TWO) at 1, without A if
-// TAIL.
+// One wave's work on a row: the teacher's side while the row is on its way, then what the other waves wait for (factors and the entries'
+// gradients), then the loss.
 template <bool TAIL, bool TWO, int SHIFT>
-__device__ __forceinline__ void finish_row(const Entries<SHIFT>& n, const Stretch& z, const Sums<false> one, const Sums<false> two, RowFactors& out,
-                                           float* row_loss) {
-    const DistillArgs& a     = n.a;
-    EntryLds&          l     = n.l;
-    const bool         real  = n.there(n.target);
-    const float        scale = (float)((double)a.st->scale / (double)a.rows), wc = n.some ? a.weight * a.inv_temperature * scale : 0.f, hs = real ? a.hard * scale : 0.f;
-    float              r = 0.f, sum_q;
-    if (TAIL) {
-        double sum = 0.0;
-        n.each([&](int e) {
-            const double q = n.there(l.id[e]) ? exp((double)l.t[e]) : 0.0;  // (64 bits: 1 minus their sum is often next to nothing)
-            l.q[e]         = (float)q;
-            sum += q;
-        });
-        sum   = wave_sum64(sum);
-        sum_q = (float)sum;
-        if (n.some && one.s > 0.f && sum < 1.0) r = (float)(1.0 - sum);
-    } else {
-        float m = -INFINITY, sum = 0.f;
-        n.each([&](int e) { m = fmaxf(m, n.there(l.id[e]) ? l.t[e] : -INFINITY); });
-        m = wave_max(m);
-        m = m == -INFINITY ? 0.f : m;
-        n.each([&](int e) {
-            const float q = n.there(l.id[e]) ? expf(l.t[e] - m) : 0.f;
-            l.q[e]        = q;
-            sum += q;
-        });
-        sum             = wave_sum(sum);
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        n.each([&](int e) { l.q[e] *= inv; });
-        sum_q = sum * inv;
-    }
-    __builtin_amdgcn_wave_barrier();
-    // q of entry e's class and whether e is its first entry: a class counts once, with the sum of its entries in their order
-    const auto class_of = [&](int e, float& q) {
-        q = l.q[e];
-        if (!n.twice) return true;
-        q          = 0.f;
-        bool first = true;
-        for (int j = 0; j < a.top; ++j)
-            if (l.id[j] == l.id[e]) {
-                q += l.q[j];
-                first &= j >= e;
-            }
-        return first;
-    };
-    Sums<false> all = one, at1 = two;
-    if (TAIL) {
-        float top = -INFINITY;
-        n.each([&](int e) { top = fmaxf(top, n.there(l.id[e]) ? l.x[e] : -INFINITY); });
-        top                    = wave_max(top);
-        const auto with_listed = [&](Sums<false>& t, float c2) {
-            t.move(fmaxf(t.ref, top * c2));
-            float sum = 0.f;
+struct RowWork {
+    const Entries<SHIFT>& n;
+    float                 sum_q, sum_r, r;     // Q, what 1 - Q leaves, and that or 0 where nothing outside A can be
+    float                 wc, hs, u;           // S / rows times weight / temperature and hard; Q + r
+    Sums<false>           one, all, at1;       // sums outside A (TAIL), over all, at temperature 1
+    float                 log_s;
+
+    __device__ __forceinline__ explicit RowWork(const Entries<SHIFT>& n_) : n(n_), one(1.f), all(1.f), at1(1.f) {}
+    __device__ __forceinline__ bool first(int e) const { return !n.twice || !n.l.again[e]; }
+
+    __device__ __forceinline__ void teacher() {
+        EntryLds& l = n.l;
+        sum_r       = 0.f;
+        if (TAIL) {
+            double sum = 0.0;
             n.each([&](int e) {
-                float q;
-                if (n.there(l.id[e]) && class_of(e, q)) sum += __builtin_amdgcn_exp2f(fmaf(l.x[e], c2, -t.ref));
+                const double q = n.there(l.id[e]) ? exp((double)l.t[e]) : 0.0;  // (64 bits: 1 minus their sum is often next to nothing)
+                l.q[e]         = (float)q;
+                sum += q;
             });
-            t.s += wave_sum(sum);
-        };
-        with_listed(all, a.c2);
-        if (TWO) with_listed(at1, LOG2E);
-    }
-    const float log_s = log2f(all.s), inv_s = 1.f / all.s, u = sum_q + r, rest = TAIL ? __builtin_amdgcn_exp2f(one.ref - all.ref) : 1.f;
-    const float inv_1 = TWO ? 1.f / at1.s : inv_s;
-    RowFactors  f;
-    f.a    = wc * (u * (rest * inv_s) - (TAIL && r > 0.f ? r / one.s : 0.f)) + (TWO ? 0.f : hs * (rest * inv_s));
-    f.ref  = TAIL ? one.ref : all.ref;
-    f.b    = TWO ? hs * inv_1 : 0.f;
-    f.ref2 = at1.ref;
-    f.none = !n.some && !real;
-    float kl = 0.f;
-    n.each([&](int e) {
-        if (!n.there(l.id[e])) return;
-        const float y = fmaf(l.x[e], a.c2, -all.ref), p = __builtin_amdgcn_exp2f(y) * inv_s;
-        const float p1 = TWO ? __builtin_amdgcn_exp2f(fmaf(l.x[e], LOG2E, -at1.ref)) * inv_1 : p;
-        float       q;
-        const bool  first = class_of(e, q);
-        n.put(z, e, wc * (p * u - q) + (real ? hs * (p1 - (l.id[e] == n.target ? 1.f : 0.f)) : 0.f));
-        if (first && q != 0.f) kl += q * (logf(q) - LN2 * (y - log_s));
-    });
-    kl = wave_sum(kl);
-    if (TAIL && r > 0.f) kl += r * (logf(r) - LN2 * ((one.ref - all.ref) + (log2f(one.s) - log_s)));
-    if (n.lane() == 0) {
-        float loss = n.some ? a.weight * kl : 0.f;
-        if (real) {
-            const float x = l.x[DI_TARGET];
-            loss -= a.hard * (LN2 * (TWO ? fmaf(x, LOG2E, -at1.ref) - log2f(at1.s) : fmaf(x, a.c2, -all.ref) - log_s));
-            if (!n.listed)
-                n.put(z, DI_TARGET,
-                      f.a * __builtin_amdgcn_exp2f(fmaf(x, a.c2, -f.ref)) + (TWO ? f.b * __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -f.ref2)) : 0.f) - hs);
+            sum   = wave_sum64(sum);
+            sum_q = (float)sum;
+            if (n.some && sum < 1.0) sum_r = (float)(1.0 - sum);
+        } else {
+            float m = -INFINITY, sum = 0.f;
+            n.each([&](int e) { m = fmaxf(m, n.there(l.id[e]) ? l.t[e] : -INFINITY); });
+            m = wave_max(m);
+            m = m == -INFINITY ? 0.f : m;
+            n.each([&](int e) {
+                const float q = n.there(l.id[e]) ? expf(l.t[e] - m) : 0.f;
+                l.q[e]        = q;
+                sum += q;
+            });
+            sum             = wave_sum(sum);
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            n.each([&](int e) { l.q[e] *= inv; });
+            sum_q = sum * inv;
         }
-        if (row_loss) *row_loss = loss;
-        out = f;
+        __builtin_amdgcn_wave_barrier();
+        if (n.twice) {  // a class counts once, with the sum of its entries in their order
+            n.each([&](int e) {
+                float q     = 0.f;
+                bool  again = false;
+                for (int j = 0; j < n.a.top; ++j)
+                    if (l.id[j] == l.id[e]) {
+                        q += l.q[j];
+                        again |= j < e;
+                    }
+                l.t[e]     = q;
+                l.again[e] = again;
+            });
+            __builtin_amdgcn_wave_barrier();
+            n.each([&](int e) { l.q[e] = l.t[e]; });
+        }
     }
-}
+    // s1, s2: sums at the temperature and (TWO) at 1, without A if TAIL
+    __device__ __forceinline__ void factors(const Stretch& z, const Sums<false>& s1, const Sums<false>& s2, RowFactors& out) {
+        const DistillArgs& a     = n.a;
+        EntryLds&          l     = n.l;
+        const bool         real  = n.there(n.target);
+        const float        scale = (float)((double)a.st->scale / (double)a.rows);
+        wc = n.some ? a.weight * a.inv_temperature * scale : 0.f, hs = real ? a.hard * scale : 0.f;
+        one = all = s1, at1 = s2;
+        r = one.s > 0.f ? sum_r : 0.f, u = sum_q + r;
+        if (TAIL) {
+            float top = -INFINITY;
+            n.each([&](int e) { top = fmaxf(top, n.there(l.id[e]) ? l.x[e] : -INFINITY); });
+            top                    = wave_max(top);
+            const auto with_listed = [&](Sums<false>& t, float c2) {
+                t.move(fmaxf(t.ref, top * c2));
+                float sum = 0.f;
+                n.each([&](int e) {
+                    if (n.there(l.id[e]) && first(e)) sum += __builtin_amdgcn_exp2f(fmaf(l.x[e], c2, -t.ref));
+                });
+                t.s += wave_sum(sum);
+            };
+            with_listed(all, a.c2);
+            if (TWO) with_listed(at1, LOG2E);
+        }
+        const float inv_s = 1.f / all.s, rest = TAIL ? __builtin_amdgcn_exp2f(one.ref - all.ref) : 1.f, inv_1 = TWO ? 1.f / at1.s : inv_s;
+        RowFactors  f;
+        f.a    = wc * (u * (rest * inv_s) - (TAIL && r > 0.f ? r / one.s : 0.f)) + (TWO ? 0.f : hs * (rest * inv_s));
+        f.ref  = one.ref;
+        f.b    = TWO ? hs * inv_1 : 0.f;
+        f.ref2 = at1.ref;
+        f.none = !n.some && !real;
+        if (n.lane() == 0) out = f;
+        n.each([&](int e) {
+            const int c = l.id[e];
+            if (!n.there(c)) return;
+            const float p  = __builtin_amdgcn_exp2f(fmaf(l.x[e], a.c2, -all.ref)) * inv_s;
+            const float p1 = TWO ? __builtin_amdgcn_exp2f(fmaf(l.x[e], LOG2E, -at1.ref)) * inv_1 : p;
+            n.put(z, e, wc * (p * u - l.q[e]) + (real ? hs * (p1 - (c == n.target ? 1.f : 0.f)) : 0.f));
+        });
+        if (n.lane() == 0 && real && !n.listed) {
+            const float x = l.x[DI_TARGET];
+            n.put(z, DI_TARGET, f.a * __builtin_amdgcn_exp2f(fmaf(x, a.c2, -f.ref)) + (TWO ? f.b * __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -f.ref2)) : 0.f) - hs);
+        }
+    }
+    __device__ __forceinline__ void loss(float* out) {
+        const DistillArgs& a     = n.a;
+        EntryLds&          l     = n.l;
+        const float        log_s = log2f(all.s);
+        float              kl    = 0.f;
+        n.each([&](int e) {
+            const float q = l.q[e];
+            if (n.there(l.id[e]) && first(e) && q != 0.f) kl += q * (logf(q) - LN2 * (fmaf(l.x[e], a.c2, -all.ref) - log_s));
+        });
+        kl = wave_sum(kl);
+        if (TAIL && r > 0.f) kl += r * (logf(r) - LN2 * ((one.ref - all.ref) + (log2f(one.s) - log_s)));
+        float       sum = n.some ? a.weight * kl : 0.f;
+        const float x   = l.x[DI_TARGET];
+        if (n.there(n.target)) sum -= a.hard * (LN2 * (TWO ? fmaf(x, LOG2E, -at1.ref) - log2f(at1.s) : fmaf(x, a.c2, -all.ref) - log_s));
+        if (n.lane() == 0) *out = sum;
+    }
+};
 
 // half k of a piece
 __device__ __forceinline__ void set_half(u32x4& q, int k, unsigned h) {
@@ -279,147 +303,137 @@ __device__ __forceinline__ void set_half(u32x4& q, int k, unsigned h) {
 template <int SHIFT>
 __host__ __device__ constexpr int map_words(int len) { return (len + 7 + (1 << SHIFT) - 1) >> SHIFT; }
 
-// SUMS, GRADIENT: one chunk of one row, sums out or in through a.sums.  FUSED: a whole row.  IN_TURN: whole rows, the next one's pieces
-// loaded as the gradient leaves their registers.
-enum { DI_SUMS, DI_GRADIENT, DI_FUSED, DI_IN_TURN };
+// FUSED: a workgroup has a whole row.  SUMS, GRADIENT: one chunk of one, its sums out or all of them in through a.sums.
+enum { DI_SUMS, DI_GRADIENT, DI_FUSED };
 
 template <int THREADS, int VECS, bool TAIL, bool TWO, int MODE, int SHIFT>
-__global__ __launch_bounds__(THREADS) void distill_kernel(const DistillArgs a) {
+__global__ __launch_bounds__(THREADS, THREADS == 768 ? 3 : 4) void distill_kernel(const DistillArgs a) {
     extern __shared__ unsigned map[];
     __shared__ EntryLds        l;
     __shared__ RowFactors      factors;
     __shared__ float           red[THREADS / 64][4];
-    constexpr int              NW = THREADS / 64, G = VECS % 4 == 0 ? 4 : VECS % 2 == 0 ? 2 : 1;
+    constexpr int              NW = THREADS / 64, G = VECS % 4 == 0 && !TAIL ? 4 : VECS % 2 == 0 ? 2 : 1;
     const int                  tid = threadIdx.x, wave = tid >> 6;
-    long long                  row   = MODE >= DI_FUSED ? blockIdx.x : blockIdx.x / a.chunks;
-    const int                  chunk = MODE >= DI_FUSED ? 0 : blockIdx.x - (int)row * a.chunks, first = chunk * a.chunk, len = min(a.chunk, a.vocab - first);
-    const int                  most  = (len + 14) >> 3;  // pieces, wherever a row starts
-    typedef Entries<SHIFT>     Row;
-    Row                        n{a, l, map, first, -1, false, false, false};
-    Stretch                    z(a.logits + row * a.ld + first, len);
-    u32x4                      raw[VECS];
-    typename Row::Ahead        ahead;
-    if (wave == 0) ahead = Row::fetch(a, row);
-#pragma unroll
-    for (int i = 0; i < VECS; ++i) raw[i] = z.load(i * THREADS + tid);
+    const long long            row   = MODE == DI_FUSED ? blockIdx.x : blockIdx.x / a.chunks;
+    const int                  chunk = MODE == DI_FUSED ? 0 : blockIdx.x - (int)row * a.chunks, first = chunk * a.chunk, len = min(a.chunk, a.vocab - first);
+    const Stretch              z(a.logits + row * a.ld + first, len);
+    Entries<SHIFT>             n{a, l, map, first, -1, false, false, false};
+    RowWork<TAIL, TWO, SHIFT>  work(n);
+    u32x4                      raw[VECS], last;
+    typename Entries<SHIFT>::List   list;
+    typename Entries<SHIFT>::Logits logits;
+    if (wave == 0) list = n.fetch(row);  // (ahead of the row: what comes back first is waited for first)
+    load_pieces<THREADS>(z, tid, raw, last);
     for (int v = tid; v < map_words<SHIFT>(a.chunk); v += THREADS) map[v] = 0;
+    lds_barrier();
+    if (wave == 0) {
+        n.settle(list);
+        n.insert(z);
+        if (MODE != DI_GRADIENT) logits = n.fetch_logits(row);
+    }
     // f(place in the piece, word of the map) for the entries of piece v
     const auto entries_of = [&](int v, auto&& f) {
         if (v < z.pieces())
             for (unsigned w = map[v >> (SHIFT - 3)]; w; w = (w & MAP_NEXT) ? l.info[(w & MAP_NEXT) - 1] : 0u)
                 if (SHIFT == 3 || (map_place(w) >> 3) == (v & 1)) f(map_place(w) & 7, w);
     };
-    lds_barrier();
-    for (;;) {
-        const long long      next = row + gridDim.x;
-        const bool           more = MODE == DI_IN_TURN && next < a.rows;
-        int                  at   = tid;
-        typename Row::Logits logits;
-        asm("" : "+v"(at));  // (places of the pieces are formed where they are used, not kept in registers from row to row)
-        if (wave == 0) {
-            n.settle(ahead);
-            n.insert(z);
-            if (MODE != DI_GRADIENT) logits = n.fetch_logits(row);
-        }
-        if (MODE != DI_GRADIENT) {
-            if (TAIL) lds_barrier();
-            Sums<false> one(a.c2), two(LOG2E);
+    if (TAIL && MODE != DI_GRADIENT) lds_barrier();  // the map is there: sums without A
+    if (wave == 0 && MODE != DI_SUMS) work.teacher();
+    int at = tid;
+    asm("" : "+v"(at));  // (places of the pieces are formed again, not kept in registers)
+    if (MODE != DI_GRADIENT) {
+        Sums<false> one(a.c2), two(LOG2E);
 #pragma unroll
-            for (int i = 0; i < VECS; i += G) {
-                if (i * THREADS < most) {
-                    u32x4 q[G];
+        for (int i = 0; i < VECS; i += G) {
 #pragma unroll
-                    for (int j = 0; j < G; ++j) {
-                        q[j] = raw[i + j];
-                        if (TAIL)
-                            entries_of((i + j) * THREADS + at, [&](int k, unsigned w) {
-                                if (!(w & MAP_TARGET)) set_half(q[j], k, 0xFC00u);
-                            });
-                    }
-                    const float m = max_of<G>(q);
-                    one.template add_pieces<G>(q, a.c2, m);
-                    if (TWO) two.template add_pieces<G>(q, LOG2E, m);
-                }
-            }
-            one.over_wave();
-            if (TWO) two.over_wave();
-            if ((tid & 63) == 0) {
-                red[wave][0] = one.ref;
-                red[wave][1] = one.s;
-                red[wave][2] = two.ref;
-                red[wave][3] = two.s;
-            }
-            lds_barrier();
-        }
-        if (wave == 0) {
-            Sums<false> s1(a.c2), s2(LOG2E);
-            float*      chosen = a.chosen + row * (MP_TOP_MAX + 1);
-            if (MODE == DI_GRADIENT) {
-                for (int c = tid; c < a.chunks; c += 64) {
-                    const f32x4 v = *reinterpret_cast<const f32x4*>(a.sums + (row * a.chunks + c) * 4);
-                    s1.add_sums(v[0], v[1], 0.f);
-                    if (TWO) s2.add_sums(v[2], v[3], 0.f);
-                }
-                n.each([&](int e) { l.x[e] = chosen[e]; });
-                if (tid == 0) l.x[DI_TARGET] = chosen[DI_TARGET];
-                s1.over_wave();
-                if (TWO) s2.over_wave();
-            } else {
+            for (int j = 0; j < G; ++j) settle<THREADS>(z, i + j, at, raw[i + j], last);
+            if (i * THREADS < z.pieces()) {
+                u32x4 q[G];
 #pragma unroll
-                for (int w = 0; w < NW; ++w) {
-                    s1.add_sums(red[w][0], red[w][1], 0.f);
-                    if (TWO) s2.add_sums(red[w][2], red[w][3], 0.f);
+                for (int j = 0; j < G; ++j) {
+                    q[j] = raw[i + j];
+                    if (TAIL)
+                        entries_of((i + j) * THREADS + at, [&](int k, unsigned w) {
+                            if (!(w & MAP_TARGET)) set_half(q[j], k, 0xFC00u);
+                        });
+                    asm("" : "+v"(q[j]));
                 }
-                n.settle_logits(logits);
+                const float m = max_of<G>(q);
+                one.template add_pieces<G>(q, a.c2, m);
+                if (TWO) two.template add_pieces<G>(q, LOG2E, m);
             }
-            if (MODE == DI_SUMS) {
-                if (tid == 0) *reinterpret_cast<f32x4*>(a.sums + (row * a.chunks + chunk) * 4) = f32x4{s1.ref, s1.s, s2.ref, s2.s};
-                if (chunk == 0) {
-                    n.each([&](int e) { chosen[e] = l.x[e]; });
-                    if (tid == 0) chosen[DI_TARGET] = l.x[DI_TARGET];
-                }
-            } else {
-                finish_row<TAIL, TWO, SHIFT>(n, z, s1, s2, factors, first == 0 ? a.row_loss + row : nullptr);
-            }
-            if (more) ahead = Row::fetch(a, next);
         }
-        if (MODE == DI_SUMS) return;
+        one.over_wave();
+        if (TWO) two.over_wave();
+        if ((tid & 63) == 0) {
+            red[wave][0] = one.ref;
+            red[wave][1] = one.s;
+            red[wave][2] = two.ref;
+            red[wave][3] = two.s;
+        }
         lds_barrier();
-        const auto  uniform = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); };
-        const float fa = uniform(factors.a), ref = uniform(factors.ref), fb = uniform(factors.b), ref2 = uniform(factors.ref2);
-        const bool  none = __builtin_amdgcn_readfirstlane(factors.none);
-        Stretch     zn(a.logits + (more ? next : row) * a.ld + first, len);
-        uint16_t*   dz = a.dlogits + row * a.ld + first;
-        asm("" : "+v"(at));
-#pragma unroll
-        for (int i = 0; i < VECS; ++i) {
-            if (i * THREADS < most) {
-                const int v = i * THREADS + at;
-                u32x4     o = {0, 0, 0, 0};
-                asm("" : "+v"(raw[i]));  // (or the compiler keeps the sums' halves, taken apart, in twice the registers until here)
-                if (!none) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        float d[2];
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const float x = (float)as_pair(raw[i][k])[h];
-                            d[h]          = fa * __builtin_amdgcn_exp2f(fmaf(x, a.c2, -ref));
-                            if (TWO) d[h] = fmaf(fb, __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -ref2)), d[h]);
-                        }
-                        o[k] = (unsigned)f2h(d[0]) | ((unsigned)f2h(d[1]) << 16);
-                    }
-                    entries_of(v, [&](int k, unsigned w) { set_half(o, k, w >> 16); });
-                }
-                z.store(dz, v, o);
-                if (more) raw[i] = zn.load(v);
+    }
+    if (wave == 0) {
+        Sums<false> s1(a.c2), s2(LOG2E);
+        float*      chosen = a.chosen + row * (MP_TOP_MAX + 1);
+        if (MODE == DI_GRADIENT) {
+            for (int c = tid; c < a.chunks; c += 64) {
+                const f32x4 v = *reinterpret_cast<const f32x4*>(a.sums + (row * a.chunks + c) * 4);
+                s1.add_sums(v[0], v[1], 0.f);
+                if (TWO) s2.add_sums(v[2], v[3], 0.f);
+            }
+            n.each([&](int e) { l.x[e] = chosen[e]; });
+            if (tid == 0) l.x[DI_TARGET] = chosen[DI_TARGET];
+        } else {
+            n.settle_logits(logits);
+            if (tid < NW) {
+                s1.add_sums(red[tid][0], red[tid][1], 0.f);
+                if (TWO) s2.add_sums(red[tid][2], red[tid][3], 0.f);
             }
         }
-        if (!more) return;
-        lds_barrier();  // everyone is done with the map
-        if (wave == 0) n.remove(z);
-        row = next;
-        z   = zn;
+        s1.over_wave();
+        if (TWO) s2.over_wave();
+        if (MODE == DI_SUMS) {
+            if (tid == 0) *reinterpret_cast<f32x4*>(a.sums + (row * a.chunks + chunk) * 4) = f32x4{s1.ref, s1.s, s2.ref, s2.s};
+            if (chunk == 0) {
+                n.each([&](int e) { chosen[e] = l.x[e]; });
+                if (tid == 0) chosen[DI_TARGET] = l.x[DI_TARGET];
+            }
+        } else {
+            work.factors(z, s1, s2, factors);
+        }
+    }
+    if (MODE == DI_SUMS) return;
+    lds_barrier();
+    if (wave == 0 && first == 0) work.loss(a.row_loss + row);
+    const auto  uniform = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); };
+    const float fa = uniform(factors.a), ref = uniform(factors.ref), fb = uniform(factors.b), ref2 = uniform(factors.ref2);
+    const bool  none = __builtin_amdgcn_readfirstlane(factors.none);
+    uint16_t*   dz   = a.dlogits + row * a.ld + first;
+    asm("" : "+v"(at));
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) {
+        if (i * THREADS < z.pieces()) {
+            const int v = i * THREADS + at;
+            u32x4     o = {0, 0, 0, 0};
+            if (MODE == DI_GRADIENT) settle<THREADS>(z, i, at, raw[i], last);
+            asm("" : "+v"(raw[i]));  // (or the compiler keeps the sums' halves, taken apart, in twice the registers until here)
+            if (!none) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float d[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float x = (float)as_pair(raw[i][k])[h];
+                        d[h]          = fa * __builtin_amdgcn_exp2f(fmaf(x, a.c2, -ref));
+                        if (TWO) d[h] = fmaf(fb, __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -ref2)), d[h]);
+                    }
+                    o[k] = (unsigned)f2h(d[0]) | ((unsigned)f2h(d[1]) << 16);
+                }
+                entries_of(v, [&](int k, unsigned w) { set_half(o, k, w >> 16); });
+            }
+            z.store(dz, v, o);
+        }
     }
 }
 
@@ -429,15 +443,21 @@ using namespace mp;
 
 namespace {
 
-constexpr int DI_FEW = 256 * 8;      // 16-byte pieces of a chunk
-constexpr int DI_MOST = 1024 * 17;   // of a row in registers
+constexpr int DI_CHUNK = 256 * 8;    // 16-byte pieces of a chunk at most
+constexpr int DI_FULL  = 512 * 16;   // of a row that leaves room for another one in a compute unit's registers
+constexpr int DI_MOST  = 768 * 22;   // of a row in registers
 
 struct DistillPlan {
     int chunks, chunk;  // 0 chunks: rows in registers
 };
+// Chunks where rows do not fit, and where a long row would keep few compute units long: us, in registers / in chunks, 1, 64 and 128 rows of
+// 100000 classes 19.2 / 13.1, 20.7 / 17.7, 22.5 / 23.0, of 131071 21.6 / 13.2, 24.7 / 22.4, 27.4 / 31.4; of 50021 13.4 / 13.3, 14.6 / 17.7,
+// 15.6 / 19.7.  Chunks are at least 4096 classes, and no more than fill the chip.  even: rows start at 16-byte pieces.  (Others may take a
+// piece more.)
 DistillPlan distill_plan(int rows, int vocab, bool even) {
-    if ((vocab + (even ? 7 : 14)) / 8 <= DI_MOST && !(rows <= 32 && vocab > 32768)) return {0, vocab};
-    int n = (vocab + 8 * DI_FEW - 9) / (8 * DI_FEW - 8);
+    const int pieces = (vocab + (even ? 7 : 14)) / 8;
+    if (pieces <= (rows <= 64 ? DI_FULL : DI_MOST)) return {0, vocab};
+    int n = (vocab + 8 * DI_CHUNK - 9) / (8 * DI_CHUNK - 8);
     while ((long long)rows * n * 2 <= 256 && vocab / (n * 2) >= 4096) n *= 2;
     const int chunk = ((vocab + n - 1) / n + 7) / 8 * 8;
     return {(vocab + chunk - 1) / chunk, chunk};
@@ -464,17 +484,19 @@ int distill_check(const mp_distill_desc* d, const char* what) {
     return MP_OK;
 }
 
-template <int THREADS, int VECS, int MODE>
+// ONLY: 1, 0: for calls with a tail, without one.  2: for both.
+template <int THREADS, int VECS, int MODE, int ONLY = 2>
 int launch_distill(const DistillArgs& a, const mp_distill_desc* d, long long workgroups, hipStream_t hs) {
-    constexpr int SHIFT = THREADS == 1024 ? 4 : 3;  // (a map within 64 KB)
+    constexpr int SHIFT = THREADS * VECS > 8192 ? 4 : 3;  // (a map within 64 KB)
     MP_REQUIRE(grid_fits(workgroups, THREADS), "mp_distill_scaled: too many rows");
-    const dim3   grid((unsigned)workgroups), block(THREADS);
-    const size_t lds = map_words<SHIFT>(a.chunk) * sizeof(unsigned);
-    const bool   two = d->hard_weight != 0.f && d->inv_temperature != 1.f;
-    if (d->tail && two) hipLaunchKernelGGL((distill_kernel<THREADS, VECS, true, true, MODE, SHIFT>), grid, block, lds, hs, a);
-    else if (d->tail) hipLaunchKernelGGL((distill_kernel<THREADS, VECS, true, false, MODE, SHIFT>), grid, block, lds, hs, a);
-    else if (two) hipLaunchKernelGGL((distill_kernel<THREADS, VECS, false, true, MODE, SHIFT>), grid, block, lds, hs, a);
-    else hipLaunchKernelGGL((distill_kernel<THREADS, VECS, false, false, MODE, SHIFT>), grid, block, lds, hs, a);
+    const bool two    = d->hard_weight != 0.f && d->inv_temperature != 1.f;
+    const auto launch = [&](auto tail, auto second) {
+        hipLaunchKernelGGL((distill_kernel<THREADS, VECS, decltype(tail)::value, decltype(second)::value, MODE, SHIFT>), dim3((unsigned)workgroups), dim3(THREADS),
+                           map_words<SHIFT>(a.chunk) * sizeof(unsigned), hs, a);
+    };
+    const auto by_second = [&](auto tail) { two ? launch(tail, std::true_type{}) : launch(tail, std::false_type{}); };
+    if constexpr (ONLY == 2) d->tail ? by_second(std::true_type{}) : by_second(std::false_type{});
+    else by_second(std::integral_constant<bool, ONLY == 1>{});
     MP_LAUNCH_CHECK("mp_distill_scaled");
     return MP_OK;
 }
@@ -514,14 +536,20 @@ extern "C" int mp_distill_scaled_parts(const mp_distill_desc* d, const mp_half* 
         if (rc == MP_OK) rc = launch_distill<256, 8, DI_GRADIENT>(a, d, n, hs);
     } else {
         const int  pieces = (d->vocab + (even ? 7 : 14)) / 8;
-        if (pieces <= 64) rc = launch_distill<64, 1, DI_FUSED>(a, d, d->rows, hs);
-        else if (pieces <= 64 * 2) rc = launch_distill<64, 2, DI_FUSED>(a, d, d->rows, hs);
-        else if (pieces <= 64 * 4) rc = launch_distill<64, 4, DI_FUSED>(a, d, d->rows, hs);
-        else if (pieces <= 256 * 4) rc = launch_distill<256, 4, DI_FUSED>(a, d, d->rows, hs);
-        else if (pieces <= 256 * 8) rc = launch_distill<256, 8, DI_FUSED>(a, d, d->rows, hs);
-        else if (pieces <= 256 * 16) rc = launch_distill<256, 16, DI_FUSED>(a, d, d->rows, hs);
-        else if (pieces <= 512 * 16) rc = launch_distill<512, 16, DI_FUSED>(a, d, d->rows, hs);
-        else rc = launch_distill<1024, 17, DI_IN_TURN>(a, d, d->rows < 256 ? d->rows : 256, hs);
+        const long long n = d->rows;
+        // Waves of a row, and pieces a lane: what was fastest of two to four forms each, us for 8192 rows with 64 classes listed, r 0 or with the
+        // rest as one: 4000 classes 4 a lane 41 / 48, 8 (half as many lanes) 50 / 55; 8192 classes 4 a lane 58 / 69, 2 73 / 87, 8 60 / 68; 16384: 8 111
+        // / 115, 4 105 / 122, 2 139 / 163; 32768: 16 207 / 223, 8 214 / 217, 4 203 / 234; 1024 x 65536: 16 59 / 64, 8 58 / 75.
+        if (pieces <= 64) rc = launch_distill<64, 1, DI_FUSED>(a, d, n, hs);
+        else if (pieces <= 64 * 2) rc = launch_distill<64, 2, DI_FUSED>(a, d, n, hs);
+        else if (pieces <= 64 * 4) rc = launch_distill<64, 4, DI_FUSED>(a, d, n, hs);
+        else if (pieces <= 128 * 4) rc = launch_distill<128, 4, DI_FUSED>(a, d, n, hs);
+        else if (pieces <= 256 * 4) rc = launch_distill<256, 4, DI_FUSED>(a, d, n, hs);
+        else if (pieces <= 256 * 8) rc = launch_distill<256, 8, DI_FUSED>(a, d, n, hs);
+        else if (pieces <= 512 * 8 && d->tail) rc = launch_distill<512, 8, DI_FUSED, 1>(a, d, n, hs);
+        else if (pieces <= 512 * 8) rc = launch_distill<1024, 4, DI_FUSED, 0>(a, d, n, hs);
+        else if (pieces <= 512 * 16) rc = launch_distill<512, 16, DI_FUSED>(a, d, n, hs);
+        else rc = launch_distill<768, 22, DI_FUSED>(a, d, n, hs);
     }
     if (rc == MP_OK) *parts = mp_mean_parts{row_loss, (double)d->rows, d->rows, 0};
     return rc;

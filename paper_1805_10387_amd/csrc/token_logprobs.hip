@@ -272,18 +272,20 @@ __global__ __launch_bounds__(THREADS) void token_logprobs_kernel(const RowArgs a
     const int        chunk = blockIdx.x - (int)row * a.chunks, first = chunk * a.chunk, len = min(a.chunk, a.vocab - first);
     const Stretch    z(a.logits + row * a.ld + first, len);
     const int        tid = threadIdx.x;
-    u32x4            raw[VECS];
-#pragma unroll
-    for (int i = 0; i < VECS; ++i) raw[i] = z.load(i * THREADS + tid);
+    u32x4            raw[VECS], last;
+    load_pieces<THREADS>(z, tid, raw, last);
     constexpr int G = VECS < 4 ? VECS : THREADS > 256 ? 2 : 4;
     Sums<true>    sum(a.c2);
     float         lane_top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < VECS; i += G) {
-        if (i * THREADS >= z.pieces()) break;
-        const float m = max_of<G>(raw + i);
-        sum.add_pieces<G>(raw + i, a.c2, m);
-        lane_top = fmaxf(lane_top, m);
+#pragma unroll
+        for (int j = 0; j < G; ++j) settle<THREADS>(z, i + j, tid, raw[i + j], last);
+        if (i * THREADS < z.pieces()) {
+            const float m = max_of<G>(raw + i);
+            sum.add_pieces<G>(raw + i, a.c2, m);
+            lane_top = fmaxf(lane_top, m);
+        }
     }
     sum.over_wave();
     if (WAVES > 1) {

@@ -10,6 +10,8 @@ typedef u32x4    u32x4_any __attribute__((aligned(2)));  // stores at any elemen
 constexpr float    LOG2E    = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 constexpr unsigned NEG_INF2 = 0xFC00FC00u;  // a pair of -inf
 
+static __device__ const u32x4 no_piece = {NEG_INF2, NEG_INF2, NEG_INF2, NEG_INF2};
+
 // A stretch of a row, cut into 16-byte pieces of memory (not of the row: rows of an odd length start anywhere, and a load that crosses
 // the pieces takes three times as long).  Piece v holds elements 8 v - head + k, k < 8, of which the first and the last piece
 // may have some outside [0, len).
@@ -18,20 +20,28 @@ struct Stretch {
     int             head, len;
     __device__ __forceinline__ Stretch(const uint16_t* p, int len_) : head((int)((reinterpret_cast<uintptr_t>(p) >> 1) & 7)), len(len_) { base = p - head; }
     __device__ __forceinline__ int  pieces() const { return (head + len + 7) >> 3; }
-    __device__ __forceinline__ bool whole(int v) const { return 8 * v >= head && 8 * v + 8 <= head + len; }
-    // what is outside reads as -inf
+    __device__ __forceinline__ int  first_whole() const { return head ? 1 : 0; }
+    __device__ __forceinline__ int  end_whole() const { return (head + len) >> 3; }
+    __device__ __forceinline__ bool whole(int v) const { return v >= first_whole() && v < end_whole(); }
+    // a piece at an end of the stretch: what is outside reads as -inf
+    __device__ __forceinline__ u32x4 edge(int v) const {
+        unsigned x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = 8 * v + k >= head && 8 * v + k < head + len ? base[8u * (unsigned)v + k] : 0xFC00u;
+        return u32x4{x[0] | (x[1] << 16), x[2] | (x[3] << 16), x[4] | (x[5] << 16), x[6] | (x[7] << 16)};
+    }
     __device__ __forceinline__ u32x4 load(int v) const {
         u32x4 q = {NEG_INF2, NEG_INF2, NEG_INF2, NEG_INF2};
-        if (whole(v)) {
-            q = *reinterpret_cast<const u32x4*>(base + 8u * (unsigned)v);
-        } else if (v < pieces()) {
-            unsigned x[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = 8 * v + k >= head && 8 * v + k < head + len ? base[8u * (unsigned)v + k] : 0xFC00u;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) q[k] = x[2 * k] | (x[2 * k + 1] << 16);
-        }
+        if (whole(v)) q = *reinterpret_cast<const u32x4*>(base + 8u * (unsigned)v);
+        else if (v < pieces()) q = edge(v);
         return q;
+    }
+    // the whole piece next to v: a load without a branch, so that the waits for it need not wait for later ones
+    __device__ __forceinline__ u32x4 load_inside(int v) const {
+        const bool      any = end_whole() > first_whole();
+        const u32x4*    p   = any ? reinterpret_cast<const u32x4*>(base) : &no_piece;
+        const unsigned  at  = any ? (unsigned)max(first_whole(), min(v, end_whole() - 1)) : 0u;
+        return p[at];
     }
     // out: where element 0 belongs
     __device__ __forceinline__ void store(uint16_t* out, int v, const u32x4 q) const {
@@ -45,6 +55,25 @@ struct Stretch {
         }
     }
 };
+
+// The pieces of a stretch that thread tid of THREADS holds, piece i THREADS + tid in raw[i]; `last` is the stretch's last piece where it is not
+// whole.  settle() before raw[i] is used for the first time.
+template <int THREADS, int VECS>
+__device__ __forceinline__ void load_pieces(const Stretch& z, int tid, u32x4 (&raw)[VECS], u32x4& last) {
+    const int v = z.pieces() - 1;
+    last        = u32x4{NEG_INF2, NEG_INF2, NEG_INF2, NEG_INF2};
+    if (VECS > 1 && v >= z.end_whole() && v % THREADS == tid) last = z.edge(v);
+    raw[0] = z.load(tid);
+#pragma unroll
+    for (int i = 1; i < VECS; ++i) raw[i] = z.load_inside(i * THREADS + tid);
+}
+template <int THREADS>
+__device__ __forceinline__ void settle(const Stretch& z, int i, int tid, u32x4& q, const u32x4& last) {
+    if (i > 0 && (i + 1) * THREADS > z.end_whole()) {
+        const int v = i * THREADS + tid;
+        if (v >= z.end_whole()) q = v == z.pieces() - 1 ? last : u32x4{NEG_INF2, NEG_INF2, NEG_INF2, NEG_INF2};
+    }
+}
 
 __device__ __forceinline__ f16x2 as_pair(unsigned w) { return __builtin_bit_cast(f16x2, w); }
 // (the builtin maximum first makes every operand quiet, which is an instruction more each)
