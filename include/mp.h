@@ -539,7 +539,7 @@ typedef struct mp_rope_desc {
     int32_t n_axes;                           /* 1 .. MP_ROPE_AXES: of positions (a text's place; time, height, width) */
     int32_t adjacent;                         /* 0 | 1                                                                */
     float   eps;                              /* >= 0                                                                 */
-    int32_t ld_q, ld_k, ld_yq, ld_yk;         /* multiples of 8                                                       */
+    int32_t ld_q, ld_k, ld_yq, ld_yk;         /* multiples of 8 below 2^22                                            */
     int32_t ld_dyq, ld_dyk, ld_dq, ld_dk;
     int32_t reserved;                         /* 0                                                                    */
     uint8_t axis[MP_ROPE_PAIRS];              /* of each pair, below n_axes                                           */

@@ -73,6 +73,13 @@ def test_rotation_pointers():
     assert rope_bwd(rope(rows=0), None, None, None, None, None, None, None, None, None, None, None, None, None, 0) == ML.MP_OK
 
 
+@pytest.mark.parametrize("field", ["ld_q", "ld_k", "ld_yq", "ld_yk", "ld_dyq", "ld_dyk", "ld_dq", "ld_dk"])
+def test_rope_offsets_within_a_workgroup_fit_32_bits(field):
+    calls = [rope_fwd] * ("d" not in field[3:]) + [rope_bwd] * ("y" not in field[3:] or "d" in field[3:])
+    for call in calls:
+        assert call(rope(**{field: 1 << 22})) == ML.MP_E_UNSUPPORTED and b"below" in lib.mp_last_error()
+
+
 def test_rotation_of_too_many_rows():
     assert rope_fwd(rope(rows=2 ** 31 - 1)) == ML.MP_E_INVAL and b"too many" in lib.mp_last_error()
 
