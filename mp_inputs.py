@@ -117,7 +117,8 @@ class TransformerWorkload:
 
     Not part of the configs, each by itself or together: `causal` attention; `n_docs` documents of any lengths packed into the
     tokens (their starts come with the batch) instead of n_seq sequences of one length; a `vocab` whose embedding, times
-    sqrt(d_model), is the first layer's input."""
+    sqrt(d_model), is the first layer's input; queries and keys that turn by position on `rope_axes` axes (the positions come with the
+    batch), pair i on axis i mod rope_axes by rope_base^(-2 i / d_head), behind an RMS norm of each head with `qk_norm`."""
     index: int = 2
     n_layers: int = 1
     d_model: int = 512
@@ -131,6 +132,9 @@ class TransformerWorkload:
     causal: bool = False
     n_docs: int = 0
     vocab: int = 0
+    rope_axes: int = 0
+    rope_base: float = 10000.0
+    qk_norm: bool = False
 
     @property
     def tokens(self):
@@ -146,7 +150,7 @@ class TransformerWorkload:
         # q, k, v projections are drawn as three d x d Xavier matrices and
         # stacked: rows [0,d) = q, [d,2d) = k, [2d,3d) = v.
         wqkv = np.concatenate([xavier_uniform(i, p + n, d, d) for n in ("wq", "wk", "wv")], axis=0)
-        return {
+        out = {
             "wqkv": wqkv, "bqkv": zeros((3 * d,)),
             "wo": xavier_uniform(i, p + "wo", d, d), "bo": zeros((d,)),
             "ln1_g": ones((d,)), "ln1_b": zeros((d,)),
@@ -154,6 +158,9 @@ class TransformerWorkload:
             "w2": xavier_uniform(i, p + "w2", d, f), "b2": zeros((d,)),
             "ln2_g": ones((d,)), "ln2_b": zeros((d,)),
         }
+        if self.qk_norm:
+            out.update(qn_g=ones((self.d_head,)), kn_g=ones((self.d_head,)))
+        return out
 
     def masters(self) -> List[Dict[str, np.ndarray]]:
         return [self.layer_masters(l) for l in range(self.n_layers)]
@@ -172,11 +179,24 @@ class TransformerWorkload:
         if self.n_docs:
             cuts = np.sort(stream(i, "doc_start").integers(0, self.tokens + 1, size=(self.n_docs - 1,)))
             out["doc_start"] = np.concatenate([[0], cuts, [self.tokens]]).astype(np.int32)
+        if self.rope_axes:
+            out["positions"] = self.positions(out.get("doc_start", np.arange(0, self.tokens + 1, self.seq_len)))
         return out
+
+    def positions(self, doc_start) -> np.ndarray:
+        """Of each token on each axis [rope_axes, tokens]: its place in its document, taken as a grid with equal sides, the last axis
+        the fastest and the first as long as it has to be."""
+        n = np.arange(self.tokens) - np.asarray(doc_start)[np.searchsorted(doc_start, np.arange(self.tokens), side="right") - 1]
+        side, out = max(2, round(self.seq_len ** (1 / self.rope_axes))), []
+        for _ in range(self.rope_axes - 1):
+            out.insert(0, n % side)
+            n = n // side
+        return np.stack([n] + out).astype(np.int32)
 
     def n_params(self) -> int:
         d, f = self.d_model, self.d_ff
-        return self.vocab * d + self.n_layers * (4 * d * d + 2 * d * f + 3 * d + d + f + d + 4 * d)
+        norms = 2 * self.d_head if self.qk_norm else 0
+        return self.vocab * d + self.n_layers * (4 * d * d + 2 * d * f + 3 * d + d + f + d + 4 * d + norms)
 
     def gemm_flops_per_step(self) -> float:
         """2*M*N*K over every contraction of forward + backward (dx and dw); attention as if every token saw its whole sequence."""
@@ -189,7 +209,11 @@ class TransformerWorkload:
 
 @dataclass(frozen=True)
 class XentWorkload:
-    """Config 4: output projection to the vocabulary + softmax cross-entropy."""
+    """Config 4: output projection to the vocabulary + softmax cross-entropy.
+
+    Not part of the config: a teacher's list of `teacher_top` classes a token with their log probabilities, at `temperature`, which come
+    with the batch.  The loss is then soft_weight times the distance from the teacher, `tail`: what the list leaves of 1 included, plus
+    hard_weight times the cross-entropy."""
     index: int = 4
     tokens: int = 8192
     d_model: int = 1024
@@ -199,6 +223,11 @@ class XentWorkload:
     blowup_factor: float = 1e4
     opt: OptCfg = OptCfg(kind="adam", lr=1e-4)
     scale: ScaleCfg = ScaleCfg(init_scale=2.0 ** 15, growth_interval=4)
+    teacher_top: int = 0
+    temperature: float = 1.0
+    soft_weight: float = 1.0
+    hard_weight: float = 0.0
+    tail: bool = False
 
     def masters(self) -> Dict[str, np.ndarray]:
         return {"w": xavier_uniform(self.index, "w_vocab", self.vocab, self.d_model),
@@ -206,8 +235,13 @@ class XentWorkload:
 
     def batch(self) -> Dict[str, np.ndarray]:
         g = stream(self.index, "targets")
-        return {"h": normal(self.index, "h", (self.tokens, self.d_model)),
-                "targets": g.integers(0, self.vocab, size=(self.tokens,), dtype=np.int64).astype(np.int32)}
+        out = {"h": normal(self.index, "h", (self.tokens, self.d_model)),
+               "targets": g.integers(0, self.vocab, size=(self.tokens,), dtype=np.int64).astype(np.int32)}
+        if self.teacher_top:
+            g = stream(self.index, "teacher")
+            out["teacher_ids"] = np.stack([g.choice(self.vocab, self.teacher_top, replace=False) for _ in range(self.tokens)]).astype(np.int32)
+            out["teacher_logp"] = np.log(g.dirichlet(np.ones(self.teacher_top + 1), self.tokens)[:, :-1]).astype(np.float32)
+        return out
 
 
 @dataclass(frozen=True)

@@ -40,20 +40,25 @@ def mlp_fwd_bwd(P: Policy, w, batch, scale, keep=None):
 
 
 # ------------------------------------------------------------- configs 2, 3
-def encoder_layer_fwd(P: Policy, w, pre, x, n_seq, seq_len, n_heads, seen=None):
+def encoder_layer_fwd(P: Policy, w, pre, x, n_seq, seq_len, n_heads, seen=None, angles=None):
     """Post-LayerNorm Transformer encoder layer:
-    y1 = LN(x + Wo attention(Wqkv x)),  y2 = LN(y1 + W2 relu(W1 y1)).  `seen`: the rows' intervals, for attention under a mask."""
-    qkv = L.linear_fwd(P, x, w[pre + "wqkv"], w[pre + "bqkv"])
+    y1 = LN(x + Wo attention(Wqkv x)),  y2 = LN(y1 + W2 relu(W1 y1)).  `seen`: the rows' intervals, for attention under a mask; `angles`
+    [rows, pairs]: its queries and keys turn by them, behind a norm where there are weights for it."""
+    qkv, turned = L.linear_fwd(P, x, w[pre + "wqkv"], w[pre + "bqkv"]), None
     if seen is None:
         ctx, att = L.attention_fwd(P, qkv, n_seq, seq_len, n_heads)
     else:
-        ctx, att = L.masked_attention_fwd(P, *np.split(qkv, 3, axis=1), *seen, n_heads, n_heads)
+        q, k, v = np.split(qkv, 3, axis=1)
+        if angles is not None:
+            (q, tq), (k, tk) = (L.norm_rope_fwd(P, t, n_heads, w.get(pre + g), L.LN_EPS, angles) for t, g in ((q, "qn_g"), (k, "kn_g")))
+            turned = tq, tk
+        ctx, att = L.masked_attention_fwd(P, q, k, v, *seen, n_heads, n_heads)
     a = L.linear_fwd(P, ctx, w[pre + "wo"], w[pre + "bo"])
     y1, ln1 = L.layernorm_fwd(P, x, a, w[pre + "ln1_g"], w[pre + "ln1_b"])
     f = L.linear_fwd(P, y1, w[pre + "w1"], w[pre + "b1"], relu=True)
     g = L.linear_fwd(P, f, w[pre + "w2"], w[pre + "b2"])
     y2, ln2 = L.layernorm_fwd(P, y1, g, w[pre + "ln2_g"], w[pre + "ln2_b"])
-    return y2, dict(x=x, qkv=qkv, ctx=ctx, att=att, a=a, y1=y1, ln1=ln1, f=f, g=g, ln2=ln2)
+    return y2, dict(x=x, qkv=qkv, turned=turned, ctx=ctx, att=att, a=a, y1=y1, ln1=ln1, f=f, g=g, ln2=ln2)
 
 
 def encoder_layer_bwd(P: Policy, w, pre, dy2, c, grads):
@@ -64,22 +69,34 @@ def encoder_layer_bwd(P: Policy, w, pre, dy2, c, grads):
     dy1 = L.add_store(P, dy1_ffn, dz2)
     dz1, grads[pre + "ln1_g"], grads[pre + "ln1_b"] = L.layernorm_bwd(P, dy1, c["ln1"], w[pre + "ln1_g"])
     dctx, grads[pre + "wo"], grads[pre + "bo"] = L.linear_bwd(P, dz1, c["ctx"], w[pre + "wo"])
-    dqkv = np.concatenate(L.masked_attention_bwd(P, dctx, c["att"]), axis=1) if isinstance(c["att"], dict) else L.attention_bwd(P, dctx, c["att"])
+    if isinstance(c["att"], dict):
+        dq, dk, dv = L.masked_attention_bwd(P, dctx, c["att"])
+        if c["turned"] is not None:
+            (dq, dgq), (dk, dgk) = (L.norm_rope_bwd(P, dt, ct) for dt, ct in zip((dq, dk), c["turned"]))
+            if dgq is not None:
+                grads[pre + "qn_g"], grads[pre + "kn_g"] = dgq, dgk
+        dqkv = np.concatenate([dq, dk, dv], axis=1)
+    else:
+        dqkv = L.attention_bwd(P, dctx, c["att"])
     dx_att, grads[pre + "wqkv"], grads[pre + "bqkv"] = L.linear_bwd(P, dqkv, c["x"], w[pre + "wqkv"])
     return L.add_store(P, dx_att, dz1)
 
 
-def make_transformer_fwd_bwd(n_layers, n_seq, seq_len, n_heads, causal=False):
+def make_transformer_fwd_bwd(n_layers, n_seq, seq_len, n_heads, causal=False, rope_base=10000.0):
     """With "doc_start" in the batch its documents take the place of the sequences, with "tokens" the rows of `emb` times sqrt(d)
-    that of the input."""
+    that of the input; with "positions" [axes, rows] queries and keys turn, pair i on axis i mod axes by rope_base^(-2 i / d_head)."""
     def fwd_bwd(P: Policy, w, batch, scale, keep=None):
-        seen, tokens, caches = None, batch.get("tokens"), []
-        if causal or "doc_start" in batch:
+        seen, tokens, angles, caches = None, batch.get("tokens"), None, []
+        if "positions" in batch:
+            pairs = w["l0.wo"].shape[0] // n_heads // 2
+            axes = np.arange(pairs) % len(batch["positions"])
+            angles = batch["positions"].astype(np.float64)[axes].T * float(rope_base) ** (-np.arange(pairs) / pairs)
+        if causal or "doc_start" in batch or angles is not None:
             rows = n_seq * seq_len
             seen = L.attention_ranges(rows, batch.get("doc_start", np.arange(0, rows + 1, seq_len)), causal)
         h = batch["x"] if tokens is None else L.embedding_fwd(P, tokens, w["emb"], np.sqrt(float(w["emb"].shape[1])))
         for l in range(n_layers):
-            h, c = encoder_layer_fwd(P, w, f"l{l}.", h, n_seq, seq_len, n_heads, seen)
+            h, c = encoder_layer_fwd(P, w, f"l{l}.", h, n_seq, seq_len, n_heads, seen, angles)
             caches.append(c)
         loss, dh = L.mse_scaled(P, h, batch["target"], scale)
         grads = {}
@@ -104,6 +121,19 @@ def xent_head_fwd_bwd(P: Policy, w, batch, scale, keep=None):
     if keep is not None:
         keep.update(logits=logits, dlogits=dlogits, dh=dh)
     return loss, {"w": dw, "b": db}
+
+
+def make_distill_head_fwd_bwd(temperature=1.0, soft_weight=1.0, hard_weight=0.0, tail=False):
+    """The head of config 4 under a teacher's lists, "teacher_ids" and "teacher_logp" of the batch."""
+    def fwd_bwd(P: Policy, w, batch, scale, keep=None):
+        logits = L.linear_fwd(P, batch["h"], w["w"], w["b"])
+        loss, dlogits = L.distill_scaled(P, logits, batch["teacher_ids"], batch["teacher_logp"], scale, 1.0 / temperature, soft_weight,
+                                         hard_weight, batch["targets"], tail)
+        dh, dw, db = L.linear_bwd(P, dlogits, batch["h"], w["w"])
+        if keep is not None:
+            keep.update(logits=logits, dlogits=dlogits, dh=dh)
+        return loss, {"w": dw, "b": db}
+    return fwd_bwd
 
 
 # ------------------------------------------------------------------ config 5
@@ -159,6 +189,6 @@ class Trainer:
 
 
 def island_batch(P: Policy, batch: Dict[str, np.ndarray]) -> Dict[str, np.ndarray]:
-    """Inputs and regression targets enter the model as stored (fp16) tensors;
-    integer class targets pass through."""
-    return {k: (v if np.issubdtype(np.asarray(v).dtype, np.integer) else P.store(v)) for k, v in batch.items()}
+    """Inputs and regression targets enter the model as stored (fp16) tensors; integer class targets and a teacher's log
+    probabilities (fp32 as they are) pass through."""
+    return {k: (v if k == "teacher_logp" or np.issubdtype(np.asarray(v).dtype, np.integer) else P.store(v)) for k, v in batch.items()}

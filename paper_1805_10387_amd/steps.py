@@ -194,13 +194,18 @@ class MLPStep(_StepBase):
 class TransformerStep(_StepBase):
     """Stack of post-LayerNorm encoder layers with an MSE loss on the last output (configs 2, 3).
 
-    A causal workload or one of packed documents runs attention under a mask, which set_batch prepares for all layers; one with a
-    vocabulary takes tokens and trains their embedding."""
+    A causal workload, one of packed documents or one whose queries and keys turn by position runs attention under a mask, which
+    set_batch prepares for all layers; one with a vocabulary takes tokens and trains their embedding."""
 
     def __init__(self, wl, masters=None, two_streams=False, fused_attention=True, grouped_dw=True, **kw):
-        self.masked = wl.causal or wl.n_docs > 0
+        self.rope_axes, self.qk_norm = getattr(wl, "rope_axes", 0), getattr(wl, "qk_norm", False)
+        if self.qk_norm and not self.rope_axes:
+            raise ValueError("norms of queries and keys come with their rotation: rope_axes is 0")
+        self.masked = wl.causal or wl.n_docs > 0 or self.rope_axes > 0
         if self.masked:
             self.d_att, att_ws = self._masked_attention(wl)
+        if self.rope_axes:
+            self.d_rope, rope_ws = self._rotation(wl)
         if masters is None:
             masters = wl.embedding()
             masters.update({f"l{i}.{k}": v for i, lay in enumerate(wl.masters()) for k, v in lay.items()})
@@ -238,6 +243,8 @@ class TransformerStep(_StepBase):
                                  rstd2=e32(T)))
             # kept for the attention's backward: the probabilities, or under a mask what each row's sum was
             self.act[-1].update(dict(lse=e32(h, T)) if self.masked else dict(p=e16(NB, h, S, self.ld_p)[..., :S]))
+            if self.rope_axes:
+                self.act[-1]["qk"] = e16(T, 2 * d)      # queries and keys as attention sees them; qkv keeps the ones before
         # backward temporaries, shared by all layers
         self.gbuf = [e16(T, d), e16(T, d)]
         self.tmp = [dict(dz2=e16_dw(d), df=e16_dw(f), dz1=e16_dw(d), dqkv=e16_dw(3 * d)) for _ in range(2)]
@@ -270,7 +277,11 @@ class TransformerStep(_StepBase):
             self.n_docs = wl.n_docs or NB
             self.doc_start = torch.arange(0, T + 1, S, dtype=torch.int32, device="cuda")
             need.append(att_ws)
-        else:
+        if self.rope_axes:
+            self.positions = torch.zeros(self.rope_axes, T, dtype=torch.int32, device="cuda")
+            self.freqs = torch.from_numpy(float(wl.rope_base) ** (-np.arange(dk // 2) / (dk // 2))).cuda()
+            need.append(rope_ws)
+        if not self.masked:
             need += [B.mp_gemm_bwd_dw_workspace_bytes(self.d_s, False), B.mp_gemm_bwd_dw_workspace_bytes(self.d_c, False)]
         if wl.vocab:
             self.tokens, self.emb_scale = torch.zeros(T, dtype=torch.int32, device="cuda"), math.sqrt(d)
@@ -288,14 +299,30 @@ class TransformerStep(_StepBase):
     def _masked_attention(wl):
         """Description and workspace size of the attention calls; a workload that they refuse is refused here."""
         dk, ld = wl.d_model // wl.n_heads, 3 * wl.d_model
-        desc = B.attn_desc(wl.tokens, wl.tokens, wl.n_heads, wl.n_heads, dk, ld_q=ld, ld_k=ld, ld_v=ld, alpha=1.0 / math.sqrt(dk))
+        ld_qk = 2 * wl.d_model if getattr(wl, "rope_axes", 0) else ld
+        desc = B.attn_desc(wl.tokens, wl.tokens, wl.n_heads, wl.n_heads, dk, ld_q=ld_qk, ld_k=ld_qk, ld_v=ld, ld_dq=ld, ld_dk=ld,
+                           alpha=1.0 / math.sqrt(dk))
         size = B.mp_attention_masked_bwd_workspace_bytes(desc)
         if size == 0:
             raise ValueError("a causal or packed workload of this shape: " + ML.load().mp_last_error().decode(errors="replace"))
         return desc, size
 
+    @staticmethod
+    def _rotation(wl):
+        """Description and workspace size of the calls that turn queries and keys: out of qkv into qk, and the gradients in their place."""
+        dk, ld = wl.d_model // wl.n_heads, 3 * wl.d_model
+        desc = B.rope_desc(wl.tokens, wl.n_heads, wl.n_heads, dk, n_axes=wl.rope_axes, axis=[i % wl.rope_axes for i in range(dk // 2)],
+                           eps=LN_EPS, ld_q=ld, ld_k=ld, ld_yq=2 * wl.d_model, ld_yk=2 * wl.d_model, ld_dyq=ld, ld_dyk=ld)
+        size = B.mp_qk_norm_rope_bwd_workspace_bytes(desc)
+        if size == 0:
+            raise ValueError("a rotation of this shape: " + ML.load().mp_last_error().decode(errors="replace"))
+        return desc, size
+
     def set_batch(self, batch):
         wl = self.wl
+        axes = getattr(wl, "rope_axes", 0)
+        if axes and np.shape(batch["positions"]) != (axes, wl.tokens):
+            raise ValueError(f"positions of shape {tuple(np.shape(batch['positions']))} for {axes} axes of {wl.tokens} tokens")
         if wl.n_docs and np.shape(batch["doc_start"]) != (wl.n_docs + 1,):   # (before anything of the last batch is replaced)
             raise ValueError(f"{tuple(np.shape(batch['doc_start']))} document starts for {wl.n_docs} documents")
         if wl.vocab:
@@ -304,6 +331,8 @@ class TransformerStep(_StepBase):
             self.x0.copy_(_h16(batch["x"]))
         if wl.n_docs:
             self.doc_start = _i32(batch["doc_start"])
+        if axes:
+            self.positions.copy_(_i32(batch["positions"]))
         if self.masked:
             B.mp_attention_mask_docs(wl.tokens, self.n_docs, self.doc_start, self.mask, causal=wl.causal)
         self.target.copy_(_h16(batch["target"]))
@@ -318,7 +347,13 @@ class TransformerStep(_StepBase):
             p = f"l{l}."
             B.mp_gemm_fwd(self.d_qkv, x, w[p + "wqkv"], w[p + "bqkv"], None, a["qkv"])
             if self.masked:
-                B.mp_attention_masked_fwd(self.d_att, self.mask, a["qkv"], a["qkv"][:, d:], a["qkv"][:, 2 * d:], None, a["ctx"], a["lse"])
+                q, k = a["qkv"], a["qkv"][:, d:]
+                if self.rope_axes:
+                    q, k = a["qk"], a["qk"][:, d:]
+                    B.mp_qk_norm_rope_fwd(self.d_rope, a["qkv"], a["qkv"][:, d:], w.get(p + "qn_g"), w.get(p + "kn_g"), self.positions,
+                                          self.freqs, q, k)
+                    self._t("qk", l, q)
+                B.mp_attention_masked_fwd(self.d_att, self.mask, q, k, a["qkv"][:, 2 * d:], None, a["ctx"], a["lse"])
             elif self.fused_attention:
                 B.mp_attention_fwd_ldp(NB, h, S, d // h, a["qkv"], 3 * d, self.alpha, a["p"], self.ld_p, a["ctx"], d)
             else:
@@ -400,8 +435,13 @@ class TransformerStep(_StepBase):
             self._t("dctx", l, self.dctx)
             # attention: dP = dctx V^T, dV = P^T dctx, dS = softmax', dQ = alpha dS K, dK = alpha dS^T Q
             if self.masked:
-                B.mp_attention_masked_bwd(self.d_att, self.mask, a["qkv"], a["qkv"][:, d:], a["qkv"][:, 2 * d:], None, a["ctx"], a["lse"],
+                q, k = (a["qk"], a["qk"][:, d:]) if self.rope_axes else (a["qkv"], a["qkv"][:, d:])
+                B.mp_attention_masked_bwd(self.d_att, self.mask, q, k, a["qkv"][:, 2 * d:], None, a["ctx"], a["lse"],
                                           self.dctx, dqkv, dqkv[:, d:], dqkv[:, 2 * d:], ws)
+                if self.rope_axes:
+                    self._t("dqk", l, dqkv)
+                    B.mp_qk_norm_rope_bwd(self.d_rope, a["qkv"], a["qkv"][:, d:], w.get(p + "qn_g"), w.get(p + "kn_g"), self.positions,
+                                          self.freqs, dqkv, dqkv[:, d:], dqkv, dqkv[:, d:], g.get(p + "qn_g"), g.get(p + "kn_g"), st, ws)
             elif self.fused_attention:
                 B.mp_attention_bwd_ldp(NB, h, S, d // h, a["qkv"], 3 * d, self.alpha, a["p"], self.ld_p, self.dctx, d, dqkv, 3 * d)
             else:
@@ -447,7 +487,10 @@ class TransformerStep(_StepBase):
 # ====================================================================================== config 4
 class XentStep(_StepBase):
     """Hidden states -> vocabulary logits -> softmax cross-entropy (config 4).  After forward_backward() `logits` [T, V],
-    contiguous, holds their gradient."""
+    contiguous, holds their gradient.
+
+    A workload with `teacher_top` learns from the teacher's lists of its batch (arrays, or device tensors as score() of another step
+    gives them) instead; `logits` is then a view of rows ld_v apart."""
 
     def __init__(self, wl, masters=None, **kw):
         super().__init__(masters or wl.masters(), wl.opt, wl.scale, **kw)
@@ -460,14 +503,33 @@ class XentStep(_StepBase):
         # (1021 x 12001: an iteration with products on rows of 12001 156 us, so 149)
         self.ld_v = _round_up(V, 8)
         self.rows16 = torch.empty(T, self.ld_v, dtype=torch.float16, device="cuda")
-        self.logits = self.rows16 if V == self.ld_v else torch.empty(T, V, dtype=torch.float16, device="cuda")
+        self.top = getattr(wl, "teacher_top", 0)
+        if self.top:
+            self.logits = self.rows16[:, :V]
+            self.d_teacher = B.distill_desc(T, V, self.top, self.ld_v, 1.0 / wl.temperature, wl.soft_weight, wl.hard_weight, wl.tail)
+            loss_bytes = B.mp_distill_workspace_bytes(self.d_teacher)
+            if loss_bytes == 0:
+                raise ValueError("a teacher of this kind: " + ML.load().mp_last_error().decode(errors="replace"))
+            self.teacher_ids = torch.empty(T, self.top, dtype=torch.int32, device="cuda")
+            self.teacher_logp = torch.empty(T, self.top, dtype=torch.float32, device="cuda")
+        else:
+            self.logits = self.rows16 if V == self.ld_v else torch.empty(T, V, dtype=torch.float16, device="cuda")
         self.dh = torch.empty(T, d, dtype=torch.float16, device="cuda")
         self.desc = B.gemm_desc(T, V, d, ldy=self.ld_v, epilogue=ML.MP_EPI_BIAS)
-        self.db_with_loss = 16384 < V <= 32768
+        self.db_with_loss = 16384 < V <= 32768 and not self.top
         self._alloc_ws(max(B.mp_gemm_bwd_dw_workspace_bytes(self.desc, not self.db_with_loss), B.mp_gemm_split_workspace_bytes(self.desc)),
+                       loss_bytes if self.top else
                        B.mp_softmax_xent_db_workspace_bytes(T, V) if self.db_with_loss else B.mp_loss_workspace_bytes(T, V))
 
     def set_batch(self, batch):
+        wl = self.wl
+        if getattr(wl, "teacher_top", 0):
+            lists = batch["teacher_ids"], batch["teacher_logp"]
+            for x in lists:
+                if tuple(x.shape) != (wl.tokens, wl.teacher_top):
+                    raise ValueError(f"a teacher's lists of shape {tuple(x.shape)} for {wl.tokens} tokens of {wl.teacher_top}")
+            for mine, x in zip((self.teacher_ids, self.teacher_logp), lists):
+                mine.copy_(torch.as_tensor(x))
         self.h.copy_(_h16(batch["h"]))
         self.targets.copy_(torch.from_numpy(np.asarray(batch["targets"], dtype=np.int32)).cuda())
 
@@ -475,6 +537,15 @@ class XentStep(_StepBase):
         wl, w, g = self.wl, self.P.w16, self.P.g16
         T, V = wl.tokens, wl.vocab
         B.mp_gemm_fwd(self.desc, self.h, w["w"], w["b"], None, self.rows16)
+        if self.top:
+            args = self.d_teacher, self.rows16, self.teacher_ids, self.teacher_logp, self.targets, self.st
+            self._parts = None
+            if self._later:
+                self._parts = B.mp_distill_scaled_parts(*args, self.rows16, self.loss_part)
+            else:
+                B.mp_distill_scaled(*args, self.loss, self.rows16, self.loss_part)
+            B.mp_gemm_bwd_both(self.desc, self.rows16, w["w"], self.dh, self.desc, self.h, g["w"], g["b"], self.st_grad, self.ws)
+            return
         copy = None if V == self.ld_v else self.logits
         # the bias gradient (column sums of dlogits) comes out of the pass that writes dlogits where that pass can, else out of
         # the weight gradient
@@ -488,6 +559,22 @@ class XentStep(_StepBase):
             B.mp_softmax_xent_scaled_copy(T, V, self.rows16, self.ld_v, self.targets, self.st, self.loss, self.rows16, copy, self.loss_part)
         B.mp_gemm_bwd_both(self.desc, self.rows16, w["w"], self.dh, self.desc, self.h, g["w"], None if self.db_with_loss else g["b"],
                            self.st_grad, self.ws)
+
+    def score(self, top: int = 0, temperature: float = 1.0) -> Dict[str, torch.Tensor]:
+        """Of the batch's tokens at a temperature: "logp" of their targets, "entropy" and "lse" [T], and with `top` the most probable
+        classes "ids" with their "top_logp" [T, top] (which a student's batch takes as teacher_ids and teacher_logp).  Changes no
+        parameter; the tensors are the caller's, `rows16` holds the logits."""
+        wl, w = self.wl, self.P.w16
+        T, V = wl.tokens, wl.vocab
+        e32 = lambda *s: torch.empty(s, dtype=torch.float32, device="cuda")  # noqa: E731
+        out = dict(logp=e32(T), entropy=e32(T), lse=e32(T))
+        if top:
+            out.update(ids=torch.empty(T, top, dtype=torch.int32, device="cuda"), top_logp=e32(T, top))
+        ws = torch.empty(B.mp_token_logprobs_workspace_bytes(T, V, top), dtype=torch.uint8, device="cuda")
+        B.mp_gemm_fwd(self.desc, self.h, w["w"], w["b"], None, self.rows16)
+        B.mp_token_logprobs(T, V, top, self.rows16, self.ld_v, self.targets, 1.0 / temperature, out["logp"], out["entropy"], out["lse"],
+                            out.get("ids"), out.get("top_logp"), ws)
+        return out
 
 
 # ====================================================================================== config 5
