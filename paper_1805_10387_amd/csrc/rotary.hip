@@ -4,7 +4,8 @@
 // (a cos t - b sin t, a sin t + b cos t).  Backward with u = the gradient turned back by -t: dg = sum u x^, v = u g,
 // dx = r (v - x^ mean(v x^)); r is formed again from x, so forward keeps nothing.
 //
-// Bound by HBM: forward moves 4 bytes, backward 6 bytes an element.  The angle depends on token and pair only, so a workgroup takes
+// Bound by HBM: forward moves 4 bytes, backward 6 bytes an element (16384 tokens of 16 + 4 heads of 128: 36 us, 4.6 TB/s, and 60 us, 4.2 TB/s;
+// without norms 36 us backward).  The angle depends on token and pair only, so a workgroup takes
 // some tokens, forms their cosines and sines once into LDS, and all heads of these tokens read them there.
 // A lane owns "units" of 2 W columns: W and their partners where halves are paired, 2 W neighbours where neighbours are; a head
 // is then d / (2 W) lanes, filled up to a power of two, whose sums go through lane permutations.

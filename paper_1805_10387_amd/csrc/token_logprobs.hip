@@ -2,8 +2,9 @@
 //
 // z = x / temperature, lse = log sum exp z, logp = z[target] - lse, entropy = lse - sum p z.  One pass: a workgroup holds a row (or a
 // chunk of one) in registers, sums against a running reference (vocab_rows.hpp), and picks the alternatives out of the
-// registers.  Bound by HBM with many rows, by the chain of trips to memory and barriers with few, where rows are cut into more chunks
-// and a second launch joins these.
+// registers.  Bound by HBM with many rows of many classes (8192 x 32768: 97 us, 5.5 TB/s; with 64 alternatives 114 us), by the search for
+// the alternatives with short rows (8192 x 2000 with 20: 17 us, 9.5 without), by the chain of trips to memory and barriers with few
+// (1 x 32768 with 20: 7.4 us).
 //
 // The top `k` of a chunk: the k-th largest of the lanes' own maxima is a bound that at least k elements reach, and with values that are
 // spread over the lanes hardly more.  These are gathered in LDS, and each finds its place by counting those ahead of it, ties by
@@ -41,7 +42,7 @@ __device__ __forceinline__ int      far_index(u64 e) { return (int)(0x7FFFFFFFu 
 
 template <int THREADS>
 struct TopLds {
-    static constexpr int WAVES = THREADS / 64, HELD = WAVES > 4 ? 64 : 128, KEYS = 256;
+    static constexpr int WAVES = THREADS / 64, HELD = WAVES > 4 ? 64 : WAVES > 1 ? 128 : 160, KEYS = 256;
     u32x4          found[LP_FOUND / 4];  // entries, zeros behind them up to a multiple of 16
     u32x4          piece[WAVES][HELD];   // pieces with an element that reaches the bound
     unsigned short place[WAVES][HELD];   // and which they are
@@ -158,22 +159,36 @@ __device__ __forceinline__ int gather_exact(const u32x4 (&raw)[VECS], const Stre
 // The k largest of the chunk, and few others, into t.found in any order; returns their number.  All threads; ends with a barrier.
 template <int THREADS, int VECS>
 __device__ __forceinline__ int gather_top(u32x4 (&raw)[VECS], const Stretch& z, int k, float lane_top, bool plain, TopLds<THREADS>& t) {
-    // of one wave the pieces' maxima (its lanes are few beside k), of eight the maxima of two lanes each
-    constexpr int PIECES = THREADS == 64 ? VECS : 1, SHARE = THREADS == 512 ? 2 : 1, KEYS = PIECES * THREADS / SHARE;
-    const int     tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // KEYS: of one wave the maxima of pieces, or of halves of them where they would be fewer than twice k (8192 x 1000, 20 and 100
+    // alternatives: pieces 12.3 and 39.6 us, halves 14.4 and 27.7), of two those of half a lane's pieces, of eight of two lanes' each
+    const int  tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const auto find_bound = [&](auto keys, auto&& key_top) {
+        constexpr int KEYS = decltype(keys)::value, SHARE = KEYS < THREADS ? THREADS / KEYS : 1;
+        static_assert(KEYS <= TopLds<THREADS>::KEYS, "");
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-        float top = PIECES > 1 ? max_of<1>(&raw[i]) : lane_top;
-        if (SHARE > 1) top = fmaxf(top, __shfl_xor(top, 1, 64));
-        if (tid % SHARE == 0) t.best[i * THREADS + tid / SHARE] = (unsigned short)order_key(f2h(top));
+        for (int i = 0; i < KEYS * SHARE / THREADS; ++i) {
+            float top = key_top(i);
+            if (SHARE > 1) top = fmaxf(top, __shfl_xor(top, 1, 64));
+            if (tid % SHARE == 0) t.best[(i * THREADS + tid) / SHARE] = (unsigned short)order_key(f2h(top));
+        }
+        if (tid == 0) t.count = 0;
+        lds_barrier();
+        if (wave == 0) {
+            const float b = kth_of<KEYS / 64>(t.best, k);
+            if (lane == 0) t.bound = b;
+        }
+        lds_barrier();
+    };
+    if constexpr (THREADS == 64 && VECS <= 2) {
+        if (k <= 32 * VECS) find_bound(std::integral_constant<int, 64 * VECS>{}, [&](int i) { return max_of<1>(&raw[i]); });
+        else find_bound(std::integral_constant<int, 128 * VECS>{}, [&](int i) { return max_of_half(raw[i >> 1], i & 1); });
+    } else if constexpr (THREADS == 64) {
+        find_bound(std::integral_constant<int, 64 * VECS>{}, [&](int i) { return max_of<1>(&raw[i]); });
+    } else if constexpr (THREADS == 128) {
+        find_bound(std::integral_constant<int, 256>{}, [&](int i) { return max_of<VECS / 2>(&raw[i * (VECS / 2)]); });
+    } else {
+        find_bound(std::integral_constant<int, 256>{}, [&](int) { return lane_top; });
     }
-    if (tid == 0) t.count = 0;
-    lds_barrier();
-    if (wave == 0) {
-        const float b = kth_of<KEYS / 64>(t.best, k);
-        if (lane == 0) t.bound = b;
-    }
-    lds_barrier();
     const float bound = t.bound;
     if (plain && bound > -INFINITY) {
         // each wave its pieces, then eight of these at a time, a lane an element
@@ -360,7 +375,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void token_logprobs_join_kernel(const
     }
 }
 
-// dx = RNE16(S c (g (1[target] - p) - h p (ln p + entropy))), S c = scale / temperature; bound by HBM (4 bytes an element).
+// dx = RNE16(S c (g (1[target] - p) - h p (ln p + entropy))), S c = scale / temperature; bound by HBM (4 bytes an element; 8192 x 32768 205 us,
+// 5.2 TB/s).
 constexpr int LPB_VECS = 4, LPB_THREADS = 256;
 __global__ __launch_bounds__(LPB_THREADS) void token_logprobs_bwd_kernel(const int vocab, const int ld, const int pieces, const uint16_t* logits,
                                                                         const int32_t* __restrict__ targets, const float c,
@@ -410,7 +426,10 @@ constexpr int LP_MOST = LP_LOCAL;  // elements of a chunk that starts at a piece
 struct ChunkPlan {
     int chunks, chunk;
 };
-// One chunk a row where that fills the chip; else as many as do, of 2048 elements or more.
+// One chunk a row up to 65536 classes: the second launch, which joins several, costs what shorter ones save (20 alternatives, us of 1, 2, 4, 8
+// and 16 chunks: 1 x 65536 10.6, 11.9, 10.4, 9.8, 10.3; 1 x 32768 8.9, 10.3, 9.8, 9.3, 10.7; 16 x 50021 10.8, 13.2, 11.9, 11.2, 11.4).  Longer
+// rows are cut anyhow, and where they are few to the end that these are no more workgroups than compute units (2, 4, 8 and 16 chunks, 8
+// alternatives: 1 x 131071 10.5, 10.4, 10.3, 10.0; 64 x 131071 14.1, 14.4, 14.1, 15.2; 200 x 131071 26.5, 28.8, 26.9, 28.7).
 // even: rows start at 16-byte pieces.  (Others may take a piece more.)
 ChunkPlan chunk_plan(int rows, int vocab, bool even) {
     const int most = even ? LP_MOST : LP_MOST - 8;
@@ -466,7 +485,7 @@ extern "C" int mp_token_logprobs(int rows, int vocab, int top, const mp_half* lo
         set_error("%s: 16-byte aligned workspace of %zu bytes needed, %zu given", what, need, ws_bytes);
         return MP_E_WORKSPACE;
     }
-    MP_REQUIRE(grid_fits((long long)rows * p.chunks, 256), "%s: too many rows", what);
+    MP_REQUIRE(grid_fits((long long)rows * p.chunks, 512), "%s: too many rows", what);
     RowArgs a{vocab, ld, top, p.chunks, p.chunk, logits, targets, inv_temperature * LOG2E, logp, entropy, lse, top_logp, top_ids, static_cast<float*>(ws), nullptr};
     if (p.chunks > 1) a.lists = reinterpret_cast<u64*>(static_cast<char*>(ws) + lists_offset(rows, p));
     hipStream_t hs     = as_stream(stream);
@@ -478,6 +497,7 @@ extern "C" int mp_token_logprobs(int rows, int vocab, int top, const mp_half* lo
     };
     const int pieces = (p.chunk + (even ? 7 : 14)) / 8;
     typedef std::integral_constant<int, 64>   W1;
+    typedef std::integral_constant<int, 128>  W2;
     typedef std::integral_constant<int, 256>  W4;
     typedef std::integral_constant<int, 512>  W8;
     typedef std::integral_constant<int, 1>    V1;
@@ -485,9 +505,14 @@ extern "C" int mp_token_logprobs(int rows, int vocab, int top, const mp_half* lo
     typedef std::integral_constant<int, 4>    V4;
     typedef std::integral_constant<int, 8>    V8;
     typedef std::integral_constant<int, 16>   V16;
+    // Waves of a row and pieces a lane, us with 8 alternatives, many rows and one: 8192 and 1 x 2000 64 x 4 15.6 and 5.7, 128 x 2 17.0 and 5.2,
+    // 256 x 1 25.1 and 5.4; x 4000 64 x 8 25.3 and 7.8, 128 x 4 24.3 and 6.0, 256 x 2 29.1 and 5.6 (1024 x 4000 7.2 and 7.7, 512 x 4000 7.2 and 6.5
+    // with the last two); x 8192 128 x 8 32.9 and 6.6, 256 x 4 36.4 and 5.9; x 16384 256 x 8 55.2 and 6.7, 512 x 4 74.7 and 6.7; x 32768
+    // 256 x 16 115 and 8.7, 512 x 8 145 and 8.1.
     if (pieces <= 64) launch(W1{}, V1{});
     else if (pieces <= 128) launch(W1{}, V2{});
     else if (pieces <= 256) launch(W1{}, V4{});
+    else if (pieces <= 512 && rows >= 1024) launch(W2{}, V4{});
     else if (pieces <= 512) launch(W4{}, V2{});
     else if (pieces <= 1024) launch(W4{}, V4{});
     else if (pieces <= 2048) launch(W4{}, V8{});

@@ -90,6 +90,11 @@ __device__ __forceinline__ float max_of(const u32x4* q) {
     return fmaxf((float)as_pair(m)[0], (float)as_pair(m)[1]);
 }
 
+__device__ __forceinline__ float max_of_half(const u32x4 q, int h) {
+    const unsigned m = pair_max(q[2 * h], q[2 * h + 1]);
+    return fmaxf((float)as_pair(m)[0], (float)as_pair(m)[1]);
+}
+
 // Sums over exponentials of base 2, y = c2 x - ref with c2 = log2(e) / temperature:  s = sum 2^y, t = sum 2^y y (for the entropy).
 // ref is the largest c2 x so far as rounded, so that y of the largest is 0 to its last bit; never below the floor, which is below
 // every finite logit, so that a row of -inf makes no NaN of differences.  +inf and NaN make s NaN.

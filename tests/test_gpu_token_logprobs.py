@@ -92,6 +92,20 @@ def test_values(kind, shape):
     check(rows_of(kind, rows, vocab), targets, top)
 
 
+@pytest.mark.parametrize("kind", ["plain", "ties", "banned", "ascending", "one lane"])
+@pytest.mark.parametrize("top", [31, 32, 33, 63, 65, 100, 127, 128])
+@pytest.mark.parametrize("vocab", [128, 510, 700, 1021, 1777])
+def test_long_lists_of_short_rows(kind, top, vocab):
+    """Between the ways that the bound is found in, and lists as long as the pieces are many."""
+    check(rows_of(kind, 3, vocab), [0, vocab // 2, vocab - 1], top)
+
+
+@pytest.mark.parametrize("rows", [1023, 1024])
+@pytest.mark.parametrize("vocab,ld,top", [(2049, 2049, 128), (4090, 4097, 20), (4096, 4096, 100), (3001, 3001, 0)])
+def test_many_rows(rows, vocab, ld, top):
+    check(rows_of("plain", rows, vocab), np.arange(rows) % vocab, top, ld=ld, offset=3 if ld > vocab else 0)
+
+
 @pytest.mark.parametrize("offset", range(8))
 @pytest.mark.parametrize("vocab,ld", [(1001, 1001), (4096, 4101), (40, 57), (33000, 33003)])
 def test_any_alignment(offset, vocab, ld):
