@@ -6,9 +6,9 @@
 //     dx_j = S / rows (weight / temperature dL/dz_j + hard (softmax(x)_j - 1[j = target]))
 //
 // Bound by HBM: 2 bytes a class read, 2 written.  A workgroup holds a row in registers from its sums to its gradient; several of them
-// on a compute unit are in different parts of that (8192 x 32768 with 64 listed: 204 us, 5.3 TB/s).  Of rows beyond 65536 classes a unit's
-// registers hold one, and nothing is on its way while it is worked on (1021 x 131071 with 100 listed and the rest: 163 us, 3.3 TB/s; in
-// chunks, read twice, 211 us).
+// on a compute unit are in different parts of that (8192 x 32768 with 64 listed: 206 us, 5.2 TB/s).  Of rows beyond 65536 classes a unit's
+// registers hold one, and nothing is on its way while it is worked on (1021 x 131071 with 100 listed: 145 us, 3.7 TB/s, with the rest 166, with
+// hard labels at another temperature, which doubles the exponentials, 163; in chunks, read twice, 194 and 211).
 // Outside A the gradient is one factor a row times the exponential.  The classes of A, at most 128, are one wave's work: their
 // gradients wait in LDS, and a map from pieces to entries tells each piece which of its elements to replace.  For r the sum over
 // "all others" is formed without A, not as a difference of sums, which would lose it where the student is sure of A.
