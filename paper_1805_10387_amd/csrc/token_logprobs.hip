@@ -2,13 +2,13 @@
 //
 // z = x / temperature, lse = log sum exp z, logp = z[target] - lse, entropy = lse - sum p z.  One pass: a workgroup holds a row (or a
 // chunk of one) in registers, sums against a running reference (vocab_rows.hpp), and picks the alternatives out of the
-// registers.  Bound by HBM with many rows of many classes (8192 x 32768: 97 us, 5.5 TB/s; with 64 alternatives 114 us), by the search for
-// the alternatives with short rows (8192 x 2000 with 20: 17 us, 9.5 without), by the chain of trips to memory and barriers with few
-// (1 x 32768 with 20: 7.4 us).
+// registers.  Bound by HBM with many rows of many classes (8192 x 32768: 97 us, 5.5 TB/s; with 64 alternatives 111 us), by the search for
+// the alternatives with short rows (8192 x 2000 with 20: 15.7 us, 9.3 without), by the chain of trips to memory and barriers with few
+// (1 x 32768 with 20: 6.5 us).
 //
-// The top `k` of a chunk: the k-th largest of the lanes' own maxima is a bound that at least k elements reach, and with values that are
-// spread over the lanes hardly more.  These are gathered in LDS, and each finds its place by counting those ahead of it, ties by
-// index.  Where the bound says nothing (fewer lanes with finite values than k, NaN) or too many reach it (ties), the k-th largest value
+// The top `k` of a chunk: the k-th largest of the lanes' own maxima (or the least of what each wave finds for its share of k) is a bound that at
+// least k elements reach, and with values that are spread over the lanes hardly more.  These are gathered in LDS, and each finds its place by
+// counting those ahead of it, ties by index.  Where the bound says nothing (fewer lanes with finite values than k, NaN) or too many reach it (ties), the k-th largest value
 // is found bit by bit instead, all 16 of them, and of its ties those with the lowest indices are taken.
 #include <cmath>
 
@@ -17,7 +17,6 @@
 namespace mp {
 
 constexpr int LP_FOUND  = 512;    // elements gathered; k is at most MP_TOP_MAX
-constexpr int LP_CHUNKS = 48;     // a row is cut into at most so many
 constexpr int LP_LOCAL  = 65536;  // elements of a chunk at most
 
 typedef unsigned long long u64;
@@ -42,24 +41,21 @@ __device__ __forceinline__ int      far_index(u64 e) { return (int)(0x7FFFFFFFu 
 
 template <int THREADS>
 struct TopLds {
-    static constexpr int WAVES = THREADS / 64, HELD = WAVES > 4 ? 64 : WAVES > 1 ? 128 : 160, KEYS = 256;
+    static constexpr int WAVES = THREADS / 64, HELD = WAVES > 4 ? 64 : WAVES > 1 ? 128 : 160;
     u32x4          found[LP_FOUND / 4];  // entries, zeros behind them up to a multiple of 16
     u32x4          piece[WAVES][HELD];   // pieces with an element that reaches the bound
     unsigned short place[WAVES][HELD];   // and which they are
-    unsigned short best[KEYS];           // keys of the largest elements of the lanes, of two lanes, or of their pieces
-    int            count, equal[WAVES];
+    unsigned short best[256];            // bound_of_all()
     float          bound;
+    int            count, equal[WAVES];
     __device__ __forceinline__ unsigned& entry(int i) { return reinterpret_cast<unsigned*>(found)[i]; }
 };
 
 __device__ __forceinline__ unsigned half_of(const u32x4 q, int k) { return (k & 1) ? q[k >> 1] >> 16 : q[k >> 1] & 0xFFFFu; }
 
-// k-th largest of 64 N keys as a value, by one wave.  (Not above -inf where fewer than k have one.)
+// k-th largest of the wave's 64 N keys as a value.  (Not above -inf where fewer than k have one.)
 template <int N>
-__device__ __forceinline__ float kth_of(const unsigned short* keys, int k) {
-    unsigned key[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) key[i] = keys[i * 64 + (threadIdx.x & 63)];
+__device__ __forceinline__ float kth_of(const unsigned (&key)[N], int k) {
     unsigned best = 0;
 #pragma unroll
     for (int b = 15; b >= 0; --b) {
@@ -156,40 +152,75 @@ __device__ __forceinline__ int gather_exact(const u32x4 (&raw)[VECS], const Stre
     return t.count;
 }
 
-// The k largest of the chunk, and few others, into t.found in any order; returns their number.  All threads; ends with a barrier.
-template <int THREADS, int VECS>
-__device__ __forceinline__ int gather_top(u32x4 (&raw)[VECS], const Stretch& z, int k, float lane_top, bool plain, TopLds<THREADS>& t) {
-    // KEYS: of one wave the maxima of pieces, or of halves of them where they would be fewer than twice k (8192 x 1000, 20 and 100
-    // alternatives: pieces 12.3 and 39.6 us, halves 14.4 and 27.7), of two those of half a lane's pieces, of eight of two lanes' each
-    const int  tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const auto find_bound = [&](auto keys, auto&& key_top) {
-        constexpr int KEYS = decltype(keys)::value, SHARE = KEYS < THREADS ? THREADS / KEYS : 1;
-        static_assert(KEYS <= TopLds<THREADS>::KEYS, "");
+// Keys of the largest elements of a lane's pieces, each N-th of these together.
+template <int N, int VECS>
+__device__ __forceinline__ void lane_keys(const u32x4 (&raw)[VECS], unsigned (&key)[N]) {
 #pragma unroll
-        for (int i = 0; i < KEYS * SHARE / THREADS; ++i) {
-            float top = key_top(i);
-            if (SHARE > 1) top = fmaxf(top, __shfl_xor(top, 1, 64));
-            if (tid % SHARE == 0) t.best[(i * THREADS + tid) / SHARE] = (unsigned short)order_key(f2h(top));
-        }
-        if (tid == 0) t.count = 0;
-        lds_barrier();
-        if (wave == 0) {
-            const float b = kth_of<KEYS / 64>(t.best, k);
-            if (lane == 0) t.bound = b;
-        }
-        lds_barrier();
-    };
-    if constexpr (THREADS == 64 && VECS <= 2) {
-        if (k <= 32 * VECS) find_bound(std::integral_constant<int, 64 * VECS>{}, [&](int i) { return max_of<1>(&raw[i]); });
-        else find_bound(std::integral_constant<int, 128 * VECS>{}, [&](int i) { return max_of_half(raw[i >> 1], i & 1); });
-    } else if constexpr (THREADS == 64) {
-        find_bound(std::integral_constant<int, 64 * VECS>{}, [&](int i) { return max_of<1>(&raw[i]); });
-    } else if constexpr (THREADS == 128) {
-        find_bound(std::integral_constant<int, 256>{}, [&](int i) { return max_of<VECS / 2>(&raw[i * (VECS / 2)]); });
-    } else {
-        find_bound(std::integral_constant<int, 256>{}, [&](int) { return lane_top; });
+    for (int i = 0; i < N; ++i) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = i; j < VECS; j += N) top = fmaxf(top, max_of<1>(&raw[j]));
+        key[i] = order_key(f2h(top));
     }
-    const float bound = t.bound;
+}
+// A value that at least k of the wave's elements reach, and not many more: the k-th largest of the lanes' maxima.  A wave by itself, whose
+// lanes are few beside k, takes those of pieces, or of halves of them where they would be fewer than twice k (8192 x 1000, 20 and 100
+// alternatives: pieces 12.3 and 39.6 us, halves 14.4 and 27.7).
+template <int THREADS, int VECS>
+__device__ __forceinline__ float wave_bound(const u32x4 (&raw)[VECS], float lane_top, int k) {
+    if constexpr (THREADS == 64) {
+        if (VECS <= 2 && k > 32 * VECS) {
+            unsigned halves[2 * VECS];
+#pragma unroll
+            for (int i = 0; i < 2 * VECS; ++i) halves[i] = order_key(f2h(max_of_half(raw[i >> 1], i & 1)));
+            return kth_of<2 * VECS>(halves, k);
+        }
+        unsigned pieces[VECS];
+        lane_keys<VECS>(raw, pieces);
+        return kth_of<VECS>(pieces, k);
+    } else if constexpr (THREADS == 128) {
+        unsigned two[2];
+        lane_keys<2>(raw, two);
+        return kth_of<2>(two, k);
+    } else {
+        const unsigned one[1] = {order_key(f2h(lane_top))};
+        return kth_of<1>(one, k);
+    }
+}
+// The same of all waves' elements, 256 keys of a lane, of two lanes or of half a lane's pieces: keys_in() before a barrier, bound_of_all()
+// behind it.  Ends with a barrier.
+template <int THREADS, int VECS>
+__device__ __forceinline__ void keys_in(const u32x4 (&raw)[VECS], float lane_top, TopLds<THREADS>& t) {
+    const int tid = threadIdx.x;
+    if constexpr (THREADS == 128) {
+        unsigned two[2];
+        lane_keys<2>(raw, two);
+        t.best[tid]           = (unsigned short)two[0];
+        t.best[THREADS + tid] = (unsigned short)two[1];
+    } else {
+        constexpr int SHARE = THREADS / 256;
+        const float   top   = SHARE == 2 ? fmaxf(lane_top, __shfl_xor(lane_top, 1, 64)) : lane_top;
+        if (tid % SHARE == 0) t.best[tid / SHARE] = (unsigned short)order_key(f2h(top));
+    }
+}
+template <int THREADS>
+__device__ __forceinline__ float bound_of_all(int k, TopLds<THREADS>& t) {
+    if (threadIdx.x < 64) {
+        unsigned key[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) key[i] = t.best[i * 64 + threadIdx.x];
+        const float b = kth_of<4>(key, k);
+        if (threadIdx.x == 0) t.bound = b;
+    }
+    lds_barrier();
+    return t.bound;
+}
+
+// The k largest of the chunk, and few others, into t.found in any order; returns their number.  All threads, t.count 0; ends with a barrier.
+// bound: a value that at least k elements reach.
+template <int THREADS, int VECS>
+__device__ __forceinline__ int gather_top(u32x4 (&raw)[VECS], const Stretch& z, int k, float bound, bool plain, TopLds<THREADS>& t) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x;
     if (plain && bound > -INFINITY) {
         // each wave its pieces, then eight of these at a time, a lane an element
         constexpr int HELD  = TopLds<THREADS>::HELD;
@@ -283,6 +314,7 @@ template <int THREADS, int VECS, bool TOP>
 __global__ __launch_bounds__(THREADS) void token_logprobs_kernel(const RowArgs a) {
     constexpr int    WAVES = THREADS / 64;
     __shared__ float red[WAVES][4];
+    __shared__ std::conditional_t<TOP, TopLds<THREADS>, int> top;
     const long long  row   = blockIdx.x / a.chunks;
     const int        chunk = blockIdx.x - (int)row * a.chunks, first = chunk * a.chunk, len = min(a.chunk, a.vocab - first);
     const Stretch    z(a.logits + row * a.ld + first, len);
@@ -302,27 +334,48 @@ __global__ __launch_bounds__(THREADS) void token_logprobs_kernel(const RowArgs a
             lane_top = fmaxf(lane_top, m);
         }
     }
+    // The waves find their bounds side by side ahead of the barrier, each for its share of k, and take the least; where the shares are long, which
+    // makes that one loose, one wave finds it from all lanes behind it (8192 x 8192, 20, 64 and 128 alternatives: shares 34.9, 44.1 and 61.4 us,
+    // one wave 35.5, 41.9 and 56.7; 1 x 32768, 20: 7.9 and 8.5).
+    constexpr int SHARE = THREADS == 128 ? 16 : 6;  // of lanes with two keys, one
+    const int     k = min(a.top, len);
+    const bool    shares = WAVES == 1 || k <= SHARE * WAVES;
+    float         bound  = -INFINITY;
+    if constexpr (TOP) {
+        if (tid == 0) top.count = 0;
+        if (shares) bound = wave_bound<THREADS, VECS>(raw, lane_top, (k + WAVES - 1) / WAVES);
+        else if constexpr (WAVES > 1) keys_in<THREADS, VECS>(raw, lane_top, top);
+    }
     sum.over_wave();
     if (WAVES > 1) {
         if ((tid & 63) == 0) {
             red[tid >> 6][0] = sum.ref;
             red[tid >> 6][1] = sum.s;
             red[tid >> 6][2] = sum.t;
+            red[tid >> 6][3] = bound;
         }
         lds_barrier();
         sum = Sums<true>(a.c2);
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) sum.add_sums(red[w][0], red[w][1], red[w][2]);
+#pragma unroll 4
+        for (int w = 0; w < WAVES; ++w) {
+            sum.add_sums(red[w][0], red[w][1], red[w][2]);
+            bound = fminf(bound, red[w][3]);
+        }
+        asm("" : "+v"(sum.ref), "+v"(sum.s), "+v"(sum.t));  // (or what they are made of stays in registers to the end)
     }
     const RowOut out{a, row, sum.ref, sum.s, sum.t};
-    if (tid == 0) {
-        if (a.chunks == 1) out.row_values();
-        else *reinterpret_cast<f32x4*>(a.sums + (row * a.chunks + chunk) * 4) = f32x4{sum.ref, sum.s, sum.t, 0.f};
-    }
     if constexpr (TOP) {
-        __shared__ TopLds<THREADS> top;
-        const int                  k = min(a.top, len), n = gather_top<THREADS, VECS>(raw, z, k, lane_top, sum.s < INFINITY, top);
-        u64*                       list = a.lists + (row * a.chunks + chunk) * a.top;
+        if constexpr (WAVES > 1) {
+            if (shares && bound == -INFINITY) {  // (a wave has too few finite elements: are there enough in all lanes?)
+                keys_in<THREADS, VECS>(raw, lane_top, top);
+                lds_barrier();
+                bound = bound_of_all(k, top);
+            } else if (!shares) {
+                bound = bound_of_all(k, top);
+            }
+        }
+        const int  n    = gather_top<THREADS, VECS>(raw, z, k, bound, sum.s < INFINITY, top);
+        u64* const list = a.lists + (row * a.chunks + chunk) * a.top;
         place_entries<THREADS>(top, n, k, [&](int place, unsigned e) {
             const int index = first + entry_local(e);
             if (a.chunks == 1) out.alternative(place, index, entry_key(e));
@@ -330,6 +383,10 @@ __global__ __launch_bounds__(THREADS) void token_logprobs_kernel(const RowArgs a
         });
         if (a.chunks > 1)
             for (int i = k + tid; i < a.top; i += THREADS) list[i] = 0;
+    }
+    if (tid == THREADS - 64) {  // (a wave that has few of the places to find, or none)
+        if (a.chunks == 1) out.row_values();
+        else *reinterpret_cast<f32x4*>(a.sums + (row * a.chunks + chunk) * 4) = f32x4{sum.ref, sum.s, sum.t, 0.f};
     }
 }
 
@@ -426,15 +483,13 @@ constexpr int LP_MOST = LP_LOCAL;  // elements of a chunk that starts at a piece
 struct ChunkPlan {
     int chunks, chunk;
 };
-// One chunk a row up to 65536 classes: the second launch, which joins several, costs what shorter ones save (20 alternatives, us of 1, 2, 4, 8
-// and 16 chunks: 1 x 65536 10.6, 11.9, 10.4, 9.8, 10.3; 1 x 32768 8.9, 10.3, 9.8, 9.3, 10.7; 16 x 50021 10.8, 13.2, 11.9, 11.2, 11.4).  Longer
-// rows are cut anyhow, and where they are few to the end that these are no more workgroups than compute units (2, 4, 8 and 16 chunks, 8
-// alternatives: 1 x 131071 10.5, 10.4, 10.3, 10.0; 64 x 131071 14.1, 14.4, 14.1, 15.2; 200 x 131071 26.5, 28.8, 26.9, 28.7).
+// As few chunks as hold a row: the second launch, which joins them, and the trips of more workgroups cost what shorter chunks save (20 alternatives,
+// us of 1, 2, 4, 8 and 16 chunks: 1 x 32768 8.0, 10.3, 9.4, 9.2, 10.6; 1 x 65536 10.2, 11.8, 10.4, 9.4, 9.9; 16 x 50021 10.8, 13.2, 11.3, 10.8, 11.1;
+// 8 alternatives, 2, 4, 8 and 16 chunks: 1 x 131071 9.9, 9.9, 9.9, 9.7; 64 x 131071 14.3, 14.8, 14.0, 15.2; 200 x 131071 27.0, 28.3, 26.7, 28.8).
 // even: rows start at 16-byte pieces.  (Others may take a piece more.)
 ChunkPlan chunk_plan(int rows, int vocab, bool even) {
     const int most = even ? LP_MOST : LP_MOST - 8;
-    int       n    = (vocab + most - 1) / most;
-    while (n > 1 && n * 2 <= LP_CHUNKS && (long long)rows * n * 2 <= 256 && vocab / (n * 2) >= 8192) n *= 2;
+    const int n    = (vocab + most - 1) / most;
     if (n == 1) return {1, vocab};
     const int chunk = ((vocab + n - 1) / n + 7) / 8 * 8;
     return {(vocab + chunk - 1) / chunk, chunk};
@@ -505,10 +560,9 @@ extern "C" int mp_token_logprobs(int rows, int vocab, int top, const mp_half* lo
     typedef std::integral_constant<int, 4>    V4;
     typedef std::integral_constant<int, 8>    V8;
     typedef std::integral_constant<int, 16>   V16;
-    // Waves of a row and pieces a lane, us with 8 alternatives, many rows and one: 8192 and 1 x 2000 64 x 4 15.6 and 5.7, 128 x 2 17.0 and 5.2,
-    // 256 x 1 25.1 and 5.4; x 4000 64 x 8 25.3 and 7.8, 128 x 4 24.3 and 6.0, 256 x 2 29.1 and 5.6 (1024 x 4000 7.2 and 7.7, 512 x 4000 7.2 and 6.5
-    // with the last two); x 8192 128 x 8 32.9 and 6.6, 256 x 4 36.4 and 5.9; x 16384 256 x 8 55.2 and 6.7, 512 x 4 74.7 and 6.7; x 32768
-    // 256 x 16 115 and 8.7, 512 x 8 145 and 8.1.
+    // Waves of a row and pieces a lane, us with 8 alternatives, 8192 rows and 1: of 2000 64 x 4 14.9 and 5.7, 128 x 2 18.2 and 5.2; of 4000 128 x 4 22.8
+    // and 5.3 (1024 rows 6.8, 512 6.7), 256 x 2 28.5 and 5.0 (7.3, 5.9); of 8192 128 x 8 32.3 and 6.0, 256 x 4 35.4 and 5.4; of 16384 256 x 8 51.7 and 6.1,
+    // 512 x 4 74.7 and 6.2; of 32768 256 x 16 101 and 7.9, 512 x 8 118 and 7.3 (128 rows alike, 256 rows 9.2 and 9.4).
     if (pieces <= 64) launch(W1{}, V1{});
     else if (pieces <= 128) launch(W1{}, V2{});
     else if (pieces <= 256) launch(W1{}, V4{});
@@ -516,6 +570,7 @@ extern "C" int mp_token_logprobs(int rows, int vocab, int top, const mp_half* lo
     else if (pieces <= 512) launch(W4{}, V2{});
     else if (pieces <= 1024) launch(W4{}, V4{});
     else if (pieces <= 2048) launch(W4{}, V8{});
+    else if (pieces <= 4096 && rows <= 64) launch(W8{}, V8{});
     else if (pieces <= 4096) launch(W4{}, V16{});
     else launch(W8{}, V16{});
     MP_LAUNCH_CHECK("mp_token_logprobs");

@@ -100,6 +100,18 @@ def test_long_lists_of_short_rows(kind, top, vocab):
     check(rows_of(kind, 3, vocab), [0, vocab // 2, vocab - 1], top)
 
 
+@pytest.mark.parametrize("top", [1, 20, 24, 25, 32, 33, 48, 49, 64, 65, 128])
+@pytest.mark.parametrize("vocab", [2500, 6000, 20000, 50021, 70001])
+@pytest.mark.parametrize("there", [130, 512, 900])
+def test_few_classes_that_can_be(there, vocab, top):
+    """The finite ones side by side, so with some of the waves only: as many as the list, or fewer for some waves; rows many and few."""
+    for rows in (2, 1030 if vocab < 4096 else 3):
+        x = np.full((rows, vocab), -np.inf)
+        first = min(1024, vocab - there)
+        x[:, first:first + there] = rows_of("plain", rows, there)
+        check(x, np.arange(rows) % vocab, top)
+
+
 @pytest.mark.parametrize("rows", [1023, 1024])
 @pytest.mark.parametrize("vocab,ld,top", [(2049, 2049, 128), (4090, 4097, 20), (4096, 4096, 100), (3001, 3001, 0)])
 def test_many_rows(rows, vocab, ld, top):
