@@ -5,7 +5,7 @@
 // dx = r (v - x^ mean(v x^)); r is formed again from x, so forward keeps nothing.
 //
 // Bound by HBM: forward moves 4 bytes, backward 6 bytes an element (16384 tokens of 16 + 4 heads of 128: 36 us, 4.6 TB/s, and 60 us, 4.2 TB/s;
-// without norms 36 us backward).  The angle depends on token and pair only, so a workgroup takes
+// without norms 36 us each way).  The angle depends on token and pair only, so a workgroup takes
 // some tokens, forms their cosines and sines once into LDS, and all heads of these tokens read them there.
 // A lane owns "units" of 2 W columns: W and their partners where halves are paired, 2 W neighbours where neighbours are; a head
 // is then d / (2 W) lanes, filled up to a power of two, whose sums go through lane permutations.
@@ -264,8 +264,8 @@ __global__ __launch_bounds__(RO_THREADS) void rope_fwd_kernel(const RopeArgs a) 
 // Queries, then keys: the sums for their weights are all that a lane keeps from item to item.  A workgroup has one block of tokens, several
 // only where there are more than some thousands of these, so that the weights' gradients are few partial rows: [workgroup][queries, keys][d].
 // The only workgroup writes the gradients themselves.  Three waves a SIMD for W 8 with norms: their values, sums and addresses take some 150
-// registers, and held to the 128 that four waves leave they spill (38.0 against 31.2 us for 8192 tokens of 16 + 16 heads of 64, 40.9 against
-// 31.9 us for 12289 of 8 + 2 of 128); the narrower ones fit (26.0 against 31.1 us for 4096 of 16 + 16 of 80, 40 of them turned, W 4).
+// registers, and held to the 128 that four waves leave they spill (36.8 against 31.0 us for 8192 tokens of 16 + 16 heads of 64, 38.0 against 28.4
+// for 12289 of 8 + 2 of 128); narrower ones fit.
 template <int W, bool ADJ, bool NORM, int LANES>
 __global__ __launch_bounds__(RO_THREADS, W == 8 && NORM ? 3 : 4) void rope_bwd_kernel(const RopeArgs a) {
     extern __shared__ float lds[];
@@ -432,19 +432,38 @@ int rope_pair_log(const mp_rope_desc* d) {
     while (1 << n < d->rot / 2) ++n;
     return n;
 }
-// Tokens a workgroup takes at once: a thousand workgroups, which the chip holds together, up to 16 tokens, which a thread's RO_POS positions
-// cover.  More workgroups of fewer tokens gain nothing forward, and backward each leaves a row of sums (12289 tokens of 8 + 2 heads of 128
-// backward: 13 tokens 31.9 us, 8 in two rounds of 1024 workgroups 37).
+// the widest pieces that neither the turned columns nor the others cut
+int rope_width(const mp_rope_desc* d) {
+    if (d->d_head % 16 == 0 && d->rot % 16 == 0) return 8;
+    return d->rot % 8 == 0 ? 4 : 2;
+}
+// Tokens a workgroup takes at once, up to 16, which a thread's RO_POS positions cover.  A thousand workgroups, which the chip holds together (16 + 16
+// heads of 64 forward, 1, 2, 4, 8 and 16 tokens: 1000 tokens 4.5, 4.4, 4.5, 5.4, 7.6 us; 4096 11.6, 10.1, 8.9, 9.5, 10.9).
+int rope_most_tokens(const mp_rope_desc* d) {
+    const int most = RO_POS * RO_THREADS >> rope_pair_log(d);
+    return most < 16 ? most : 16;
+}
 int rope_tokens(const mp_rope_desc* d) {
-    const int most = RO_POS * RO_THREADS >> rope_pair_log(d) < 16 ? RO_POS * RO_THREADS >> rope_pair_log(d) : 16;
-    const int t    = d->rows / 1024 + (d->rows % 1024 != 0);
+    const int most = rope_most_tokens(d), t = d->rows / 1024 + (d->rows % 1024 != 0);
     return t < 1 ? 1 : t < most ? t : most;
 }
-int rope_bwd_blocks(const mp_rope_desc* d) {
-    const int t = rope_tokens(d), n = d->rows / t + (d->rows % t != 0);
+// Backward with norms, in pieces of 8: 256 workgroups, as each adds its weights' sums up over its lanes and leaves a row of them (16 + 16 heads of 64,
+// 1, 2, 4, 8 and 16 tokens: 1000 tokens 17.0, 12.4, 11.0, 11.6, 14.0 us; 2048 23.6, 18.0, 13.1, 13.0, 14.7; 8192 73, 51, 35.5, 33.0, 30.5); up to 8 tokens
+// one, which leaves none (4 tokens: 8.3 us in four, 6.2 in one).  Narrower pieces have more passes a token (16 + 16 of 80, 40 turned: 4096 tokens 38.4,
+// 28.4, 26.0, 28.3, 36.0).
+int rope_bwd_tokens(const mp_rope_desc* d, bool norm) {
+    if (!norm || rope_width(d) < 8) return rope_tokens(d);
+    const int most = rope_most_tokens(d);
+    if (d->rows <= 8 && d->rows <= most) return d->rows < 1 ? 1 : d->rows;
+    int t = 1;
+    while (t < most && t < d->rows / 256.0) t *= 2;
+    return t;
+}
+int rope_bwd_blocks(const mp_rope_desc* d, bool norm) {
+    const int t = rope_bwd_tokens(d, norm), n = d->rows / t + (d->rows % t != 0);
     return n < 1024 ? n : 1024;
 }
-size_t rope_bwd_bytes(const mp_rope_desc* d) { return (size_t)rope_bwd_blocks(d) * 2 * d->d_head * sizeof(float); }
+size_t rope_bwd_bytes(const mp_rope_desc* d) { return (size_t)rope_bwd_blocks(d, true) * 2 * d->d_head * sizeof(float); }
 
 int rope_check(const mp_rope_desc* d, const char* what) {
     MP_REQUIRE(d, "%s: NULL argument", what);
@@ -473,7 +492,7 @@ int rope_matrix(const char* what, const char* name, const void* p, int ld, long 
     return MP_OK;
 }
 
-RopeArgs rope_args(const mp_rope_desc* d, int w, const int32_t* positions, const double* freqs) {
+RopeArgs rope_args(const mp_rope_desc* d, int w, int tokens, const int32_t* positions, const double* freqs) {
     RopeArgs a{};
     a.rows  = d->rows;
     a.d     = d->d_head;
@@ -481,19 +500,13 @@ RopeArgs rope_args(const mp_rope_desc* d, int w, const int32_t* positions, const
     a.units = d->d_head / (2 * w);
     a.lanes = 1;
     while (a.lanes < a.units) a.lanes *= 2;
-    a.tokens    = rope_tokens(d);
+    a.tokens    = tokens;
     a.pair_log  = rope_pair_log(d);
     a.eps       = d->eps;
     a.positions = positions;
     a.freqs     = freqs;
     for (int i = 0; i < d->rot / 2; ++i) a.axis[i / 16] |= (unsigned)d->axis[i] << 2 * (i % 16);
     return a;
-}
-
-// the widest pieces that neither the turned columns nor the others cut
-int rope_width(const mp_rope_desc* d) {
-    if (d->d_head % 16 == 0 && d->rot % 16 == 0) return 8;
-    return d->rot % 8 == 0 ? 4 : 2;
 }
 
 template <typename F>
@@ -528,7 +541,7 @@ extern "C" int mp_qk_norm_rope_fwd(const mp_rope_desc* d, const mp_half* q, cons
         return MP_E_UNSUPPORTED;
     }
     const int w = rope_width(d);
-    RopeArgs  a = rope_args(d, w, positions, freqs);
+    RopeArgs  a = rope_args(d, w, rope_tokens(d), positions, freqs);
     a.part[0]   = {d->n_heads, d->ld_q, d->ld_yq, 0, q, gq, nullptr, yq, nullptr, nullptr};
     a.part[1]   = {d->n_kv_heads, d->ld_k, d->ld_yk, 0, k, gk, nullptr, yk, nullptr, nullptr};
     const dim3   grid((unsigned)(((long long)d->rows + a.tokens - 1) / a.tokens));
@@ -569,14 +582,14 @@ extern "C" int mp_qk_norm_rope_bwd(const mp_rope_desc* d, const mp_half* q, cons
             return MP_E_UNSUPPORTED;
         }
     }
-    const int nb = rope_bwd_blocks(d);
+    const int nb = rope_bwd_blocks(d, norm);
     if (norm && (!ws || !aligned16(ws) || ws_bytes < rope_bwd_bytes(d))) {
         set_error("%s: 16-byte aligned workspace of %zu bytes needed, %zu given", what, rope_bwd_bytes(d), ws_bytes);
         return MP_E_WORKSPACE;
     }
     if (some) {
         const int w = rope_width(d);
-        RopeArgs  a = rope_args(d, w, positions, freqs);
+        RopeArgs  a = rope_args(d, w, rope_bwd_tokens(d, norm), positions, freqs);
         a.part[0]   = {d->n_heads, d->ld_q, d->ld_dyq, d->ld_dq, q, gq, dyq, nullptr, dq, dgq};
         a.part[1]   = {d->n_kv_heads, d->ld_k, d->ld_dyk, d->ld_dk, k, gk, dyk, nullptr, dk, dgk};
         a.sums      = static_cast<float*>(ws);
