@@ -354,7 +354,7 @@ int mp_softmax_xent_scaled_parts(int rows, int vocab, const mp_half* logits, int
  * top_ids and top_logp NULL) to MP_TOP_MAX and to vocab.  inv_temperature: 2^-8 to 2^8.  A logit of -inf is a class that cannot be.
  * Rows with NaN or +inf, or without a finite logit, have NaN (in the last case lse -inf); their top_ids are in order all the same, NaN
  * first.  vocab up to MP_VOCAB_MAX and top up to MP_TOP_MAX, otherwise MP_E_UNSUPPORTED.
- *   ws    device, 16-byte aligned, mp_token_logprobs_workspace_bytes(rows, vocab, top) bytes (0: NULL is fine). */
+ *   ws    device, 16-byte aligned, mp_token_logprobs_workspace_bytes(rows, vocab, top) bytes (0: NULL is fine), of these rows or of more. */
 size_t mp_token_logprobs_workspace_bytes(int rows, int vocab, int top);
 int mp_token_logprobs(int rows, int vocab, int top, const mp_half* logits, int ld, const int32_t* targets, float inv_temperature,
                       float* logp, float* entropy, float* lse, int32_t* top_ids, float* top_logp, void* ws, size_t ws_bytes,
@@ -380,7 +380,7 @@ int mp_token_logprobs_bwd(int rows, int vocab, const mp_half* logits, int ld, co
  * Entries that name one class count as one with the sum of their q.  A row without entries has L = 0; without a target either, a zero
  * row of dlogits, whatever it holds.  (The factor temperature^2 that keeps gradients alike is the caller's, in weight.)  targets may be NULL
  * where hard_weight is 0.  dlogits shares ld and may be logits.
- *   ws    device, 16-byte aligned, mp_distill_workspace_bytes(desc) bytes (0 for a description that the calls refuse). */
+ *   ws    device, 16-byte aligned, mp_distill_workspace_bytes(desc) bytes (0 for a description that the calls refuse), of these rows or of more. */
 typedef struct mp_distill_desc {
     int32_t rows, vocab, ld, top;      /* vocab up to MP_VOCAB_MAX, top 1 .. MP_TOP_MAX */
     float   inv_temperature;           /* 2^-8 .. 2^8                                    */
@@ -555,7 +555,8 @@ int mp_qk_norm_rope_fwd(const mp_rope_desc* desc /* host */, const mp_half* q, c
 /* dq, dk from dyq, dyk and the forward call's inputs (q and k are read with weights only), and dgq, dgk [d_head] = RNE16 of fp32 sums over rows and
  * heads, in an order that the shape decides (given with gq and gk, overwritten).  dq may be dyq and dk dyk, with the same leading dimension.
  *   st    as for mp_gemm_bwd_dw (covers dgq and dgk).
- *   ws    with weights: device, 16-byte aligned, mp_qk_norm_rope_bwd_workspace_bytes(desc) bytes (0 for a description that is refused). */
+ *   ws    with weights: device, 16-byte aligned, mp_qk_norm_rope_bwd_workspace_bytes(desc) bytes (0 for a description that is refused), of these rows
+ *         or of more. */
 size_t mp_qk_norm_rope_bwd_workspace_bytes(const mp_rope_desc* desc /* host */);
 int mp_qk_norm_rope_bwd(const mp_rope_desc* desc /* host */, const mp_half* q, const mp_half* k, const mp_half* gq, const mp_half* gk,
                         const int32_t* positions, const double* freqs, const mp_half* dyq, const mp_half* dyk, mp_half* dq, mp_half* dk,

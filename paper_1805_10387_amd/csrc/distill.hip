@@ -449,6 +449,7 @@ constexpr int DI_CHUNK = 256 * 8;    // 16-byte pieces of a chunk at most
 constexpr int DI_FULL  = 512 * 16;   // of a row that leaves room for another one in a compute unit's registers
 constexpr int DI_MOST  = 768 * 22;   // of a row in registers
 
+int least_chunks(int vocab) { return (vocab + 8 * DI_CHUNK - 9) / (8 * DI_CHUNK - 8); }
 struct DistillPlan {
     int chunks, chunk;  // 0 chunks: rows in registers
 };
@@ -459,7 +460,7 @@ struct DistillPlan {
 DistillPlan distill_plan(int rows, int vocab, bool even) {
     const int pieces = (vocab + (even ? 7 : 14)) / 8;
     if (pieces <= (rows <= 64 ? DI_FULL : DI_MOST)) return {0, vocab};
-    int n = (vocab + 8 * DI_CHUNK - 9) / (8 * DI_CHUNK - 8);
+    int n = least_chunks(vocab);
     while ((long long)rows * n * 2 <= 256 && vocab / (n * 2) >= 4096) n *= 2;
     const int chunk = ((vocab + n - 1) / n + 7) / 8 * 8;
     return {(vocab + chunk - 1) / chunk, chunk};
@@ -468,9 +469,15 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 size_t distill_bytes(int rows, const DistillPlan& p) {
     return round256((size_t)rows * sizeof(float)) + (p.chunks ? (size_t)rows * (p.chunks * 16 + (MP_TOP_MAX + 1) * sizeof(float)) : 0);
 }
+// for as many rows or fewer, of which some are cut where more are not, or into more chunks, and at any alignment
 size_t distill_most_bytes(int rows, int vocab) {
-    const size_t even = distill_bytes(rows, distill_plan(rows, vocab, true)), any = distill_bytes(rows, distill_plan(rows, vocab, false));
-    return even > any ? even : any;
+    const int pieces = (vocab + 14) / 8;
+    size_t    n      = round256((size_t)rows * sizeof(float));
+    if (pieces > DI_FULL) {
+        const size_t cut = pieces > DI_MOST || rows < 64 ? rows : 64, chunks = cut * least_chunks(vocab);
+        n += (chunks > 256 ? chunks : 256) * 16 + cut * (MP_TOP_MAX + 1) * sizeof(float);
+    }
+    return n;
 }
 
 int distill_check(const mp_distill_desc* d, const char* what) {

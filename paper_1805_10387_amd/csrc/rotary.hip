@@ -463,6 +463,8 @@ int rope_bwd_blocks(const mp_rope_desc* d, bool norm) {
     const int t = rope_bwd_tokens(d, norm), n = d->rows / t + (d->rows % t != 0);
     return n < 1024 ? n : 1024;
 }
+// (for the same heads and as many rows or fewer, of which some have more workgroups)
+size_t rope_most_bytes(const mp_rope_desc* d) { return (size_t)(d->rows < 1024 ? d->rows : 1024) * 2 * d->d_head * sizeof(float); }
 size_t rope_bwd_bytes(const mp_rope_desc* d) { return (size_t)rope_bwd_blocks(d, true) * 2 * d->d_head * sizeof(float); }
 
 int rope_check(const mp_rope_desc* d, const char* what) {
@@ -555,7 +557,7 @@ extern "C" int mp_qk_norm_rope_fwd(const mp_rope_desc* d, const mp_half* q, cons
 }
 
 extern "C" size_t mp_qk_norm_rope_bwd_workspace_bytes(const mp_rope_desc* d) {
-    return rope_check(d, "mp_qk_norm_rope_bwd") == MP_OK ? rope_bwd_bytes(d) + 16 : 0;
+    return rope_check(d, "mp_qk_norm_rope_bwd") == MP_OK ? rope_most_bytes(d) + 16 : 0;
 }
 
 extern "C" int mp_qk_norm_rope_bwd(const mp_rope_desc* d, const mp_half* q, const mp_half* k, const mp_half* gq, const mp_half* gk,

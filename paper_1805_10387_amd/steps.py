@@ -350,8 +350,8 @@ class TransformerStep(_StepBase):
                 q, k = a["qkv"], a["qkv"][:, d:]
                 if self.rope_axes:
                     q, k = a["qk"], a["qk"][:, d:]
-                    B.mp_qk_norm_rope_fwd(self.d_rope, a["qkv"], a["qkv"][:, d:], w.get(p + "qn_g"), w.get(p + "kn_g"), self.positions,
-                                          self.freqs, q, k)
+                    gains = (w[p + "qn_g"], w[p + "kn_g"]) if self.qk_norm else (None, None)
+                    B.mp_qk_norm_rope_fwd(self.d_rope, a["qkv"], a["qkv"][:, d:], *gains, self.positions, self.freqs, q, k)
                     self._t("qk", l, q)
                 B.mp_attention_masked_fwd(self.d_att, self.mask, q, k, a["qkv"][:, 2 * d:], None, a["ctx"], a["lse"])
             elif self.fused_attention:
@@ -440,8 +440,9 @@ class TransformerStep(_StepBase):
                                           self.dctx, dqkv, dqkv[:, d:], dqkv[:, 2 * d:], ws)
                 if self.rope_axes:
                     self._t("dqk", l, dqkv)
-                    B.mp_qk_norm_rope_bwd(self.d_rope, a["qkv"], a["qkv"][:, d:], w.get(p + "qn_g"), w.get(p + "kn_g"), self.positions,
-                                          self.freqs, dqkv, dqkv[:, d:], dqkv, dqkv[:, d:], g.get(p + "qn_g"), g.get(p + "kn_g"), st, ws)
+                    gains, dgains = ((t[p + "qn_g"], t[p + "kn_g"]) if self.qk_norm else (None, None) for t in (w, g))
+                    B.mp_qk_norm_rope_bwd(self.d_rope, a["qkv"], a["qkv"][:, d:], *gains, self.positions, self.freqs, dqkv, dqkv[:, d:],
+                                          dqkv, dqkv[:, d:], *dgains, st, ws)
             elif self.fused_attention:
                 B.mp_attention_bwd_ldp(NB, h, S, d // h, a["qkv"], 3 * d, self.alpha, a["p"], self.ld_p, self.dctx, d, dqkv, 3 * d)
             else:

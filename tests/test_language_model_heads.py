@@ -103,3 +103,20 @@ def test_positions_that_do_not_fit_replace_nothing():
     for bad in (batch["positions"][:1], batch["positions"][:, 1:], batch["positions"].T, np.zeros(step.wl.tokens, np.int32)):
         with pytest.raises(ValueError, match="2 axes of 200 tokens"):
             step.set_batch(dict(batch, positions=bad))
+
+
+def test_norms_without_their_weights_are_not_left_out():
+    """Masters of the caller's own that do not have them: the forward pass says so."""
+    step = St.TransformerStep.__new__(St.TransformerStep)
+    step.wl, step.rope_axes, step.qk_norm, step.masked = replace(I.C2_SMALL, rope_axes=1, qk_norm=True), 1, True, True
+    step.P = SimpleNamespace(w16={"l0.wqkv": None, "l0.bqkv": None})
+    step.x0, step.act, step.trace = None, [dict(qkv=np.zeros((1, 1)), qk=np.zeros((1, 1)))], None
+    step.d_qkv = step.d_rope = step.positions = step.freqs = None
+    calls = []
+    kept, St.B.mp_gemm_fwd = St.B.mp_gemm_fwd, lambda *a: calls.append(a)
+    try:
+        with pytest.raises(KeyError, match="l0.qn_g"):
+            step.forward()
+    finally:
+        St.B.mp_gemm_fwd = kept
+    assert len(calls) == 1

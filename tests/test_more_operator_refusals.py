@@ -1,5 +1,6 @@
 """Refusals of head norms with rotation, token log probabilities and distillation: found on the host, before anything is enqueued (no GPU)."""
 import ctypes as C
+import re
 
 import pytest
 
@@ -154,3 +155,33 @@ def test_structs_and_limits_match_the_header():
     for name in ("MP_ROPE_AXES", "MP_ROPE_PAIRS", "MP_TOP_MAX"):
         assert hdr.split(f"#define {name} ")[1].split()[0] == str(getattr(ML, name)), name
     assert "#define MP_VOCAB_MAX (1 << 20)" in hdr and ML.MP_VOCAB_MAX == 1 << 20
+
+
+def needed(call):
+    assert call() == ML.MP_E_WORKSPACE
+    return int(re.search(rb"of (\d+) bytes", lib.mp_last_error()).group(1))
+
+
+ROWS = [1, 2, 3, 7, 8, 9, 61, 64, 65, 127, 128, 129, 255, 256, 257, 300, 512, 513, 1000, 1024, 1025, 4095, 4096, 4097, 8192, 12289, 16384, 16385, 70000]
+
+
+@pytest.mark.parametrize("d_head,rot", [(64, 64), (128, 64), (80, 40), (256, 256), (24, 4)])
+def test_rotation_workspaces_serve_fewer_rows(d_head, rot):
+    sizes = [lib.mp_qk_norm_rope_bwd_workspace_bytes(C.byref(mp.rope_desc(r, 4, 2, d_head, rot=rot))) for r in ROWS]
+    assert sizes == sorted(sizes)
+    for r, size in zip(ROWS, sizes):
+        assert needed(lambda: rope_bwd(mp.rope_desc(r, 4, 2, d_head, rot=rot), ws=None)) <= size
+
+
+@pytest.mark.parametrize("vocab", [1000, 65529, 65530, 65536, 65537, 100000, 131071, 135161, 200001, 1 << 20])
+def test_vocabulary_workspaces_serve_fewer_rows(vocab):
+    sizes, lp_sizes = [], []
+    for r in ROWS:
+        sizes.append(lib.mp_distill_workspace_bytes(C.byref(mp.distill_desc(r, vocab, 100))))
+        lp_sizes.append(lib.mp_token_logprobs_workspace_bytes(r, vocab, 100))
+        for ld, x in ((vocab, A), (vocab, A + 2), ((vocab + 7) // 8 * 8, A), (vocab + 1, A)):
+            assert needed(lambda: distill(mp.distill_desc(r, vocab, 100, ld=ld), x=x, ws=None)) <= sizes[-1]
+            if lp_sizes[-1]:
+                call = lambda: lp(r, vocab, 100, x=x, ld=ld, ws=None)  # noqa: E731
+                assert call() == ML.MP_E_INVAL or needed(call) <= lp_sizes[-1]
+    assert sizes == sorted(sizes) and lp_sizes == sorted(lp_sizes)
