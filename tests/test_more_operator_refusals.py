@@ -181,7 +181,6 @@ def test_vocabulary_workspaces_serve_fewer_rows(vocab):
         lp_sizes.append(lib.mp_token_logprobs_workspace_bytes(r, vocab, 100))
         for ld, x in ((vocab, A), (vocab, A + 2), ((vocab + 7) // 8 * 8, A), (vocab + 1, A)):
             assert needed(lambda: distill(mp.distill_desc(r, vocab, 100, ld=ld), x=x, ws=None)) <= sizes[-1]
-            if lp_sizes[-1]:
-                call = lambda: lp(r, vocab, 100, x=x, ld=ld, ws=None)  # noqa: E731
-                assert call() == ML.MP_E_INVAL or needed(call) <= lp_sizes[-1]
+            if vocab > 65536:            # (up to there a call may need none)
+                assert needed(lambda: lp(r, vocab, 100, x=x, ld=ld, ws=None)) <= lp_sizes[-1]
     assert sizes == sorted(sizes) and lp_sizes == sorted(lp_sizes)
