@@ -120,6 +120,15 @@ def test_values_and_gradients(shape, norm, adjacent):
     check(p, p.forward(), p.backward())
 
 
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("rows", [2, 7, 8, 9, 255, 257, 513, 1000, 1025, 4097, 16384, 16385, 20011, 33000])
+@pytest.mark.parametrize("heads", [dict(heads=2, kv=1, d=64), dict(heads=1, kv=1, d=40), dict(heads=1, kv=1, d=256)], ids=lambda s: f"d{s['d']}")
+def test_blocks_of_tokens(norm, rows, heads):
+    """Workgroups of 1 to 16 tokens, the last one of fewer; several blocks a workgroup beyond 16384 tokens (8192 of heads of 256)."""
+    p = Problem(5, rows=rows, norm=norm, **heads)
+    check(p, p.forward(), p.backward())
+
+
 @pytest.mark.parametrize("axis", [[0, 1] * 16, [0] * 8 + [1] * 12 + [2] * 12, [3, 0, 2, 1] * 8])
 @pytest.mark.parametrize("adjacent", [False, True])
 def test_several_axes(axis, adjacent):
