@@ -7,8 +7,8 @@
 //
 // Bound by HBM: 2 bytes a class read, 2 written.  A workgroup holds a row in registers from its sums to its gradient; several of them
 // on a compute unit are in different parts of that (8192 x 32768 with 64 listed: 206 us, 5.2 TB/s).  Of rows beyond 65536 classes a unit's
-// registers hold one, and nothing is on its way while it is worked on (1021 x 131071 with 100 listed: 145 us, 3.7 TB/s, with the rest 166, with
-// hard labels at another temperature, which doubles the exponentials, 163; in chunks, read twice, 194 and 211).
+// registers hold one, and nothing is on its way while it is worked on (1021 x 131071 with 100 listed: 147 us, 3.6 TB/s, with the rest 166; in
+// chunks, read twice, 194 and 208).
 // Outside A the gradient is one factor a row times the exponential.  The classes of A, at most 128, are one wave's work: their
 // gradients wait in LDS, and a map from pieces to entries tells each piece which of its elements to replace.  For r the sum over
 // "all others" is formed without A, not as a difference of sums, which would lose it where the student is sure of A.
@@ -45,8 +45,11 @@ struct EntryLds {
 // A word of the map, 0 where there is no entry: the next entry of the word + 1, the element's place among the word's, flags, its gradient.
 constexpr unsigned MAP_NEXT = 0xFFu, MAP_TARGET = 1u << 12, MAP_THERE = 1u << 13, MAP_FIRST = 1u << 14;
 __device__ __forceinline__ int map_place(unsigned w) { return (int)(w >> 8) & 15; }
+// Hard labels: TWO_NONE without these or at temperature 1; TWO_ANY: exponentials of their own; TWO_SQUARES, at temperature 2: squares of the
+// others (1021 x 131071 with 100 listed: without hard labels 147 us, with squares 153, with exponentials 171; 8192 x 32768 with 64 206, 221 and 248).
+enum { TWO_NONE, TWO_ANY, TWO_SQUARES };
 struct RowFactors {
-    float a, ref, b, ref2;  // gradient outside A: a 2^(c2 x - ref) + b 2^(log2(e) x - ref2)
+    float a, ref, b, ref2;  // gradient outside A: a 2^(c2 x - ref) + b 2^(log2(e) x - ref2); TWO_SQUARES: e = 2^(c2 x - ref), e (a + b e)
     int   none;             // a zero row, whatever it holds
 };
 
@@ -177,7 +180,7 @@ __device__ __forceinline__ double wave_sum64(double v) {
 
 // One wave's work on a row: the teacher's side while the row is on its way, then what the other waves wait for (factors and the entries'
 // gradients), then the loss.
-template <bool TAIL, bool TWO, int SHIFT>
+template <bool TAIL, int TWO, int SHIFT>
 struct RowWork {
     const Entries<SHIFT>& n;
     float                 sum_q, sum_r, r;     // Q, what 1 - Q leaves, and that or 0 where nothing outside A can be
@@ -264,7 +267,10 @@ struct RowWork {
         f.b    = TWO ? hs * inv_1 : 0.f;
         f.ref2 = at1.ref;
         f.none = !n.some && !real;
-        if (n.lane() == 0) out = f;
+        if (n.lane() == 0) {
+            out = f;
+            if (TWO == TWO_SQUARES) out.b = f.b * __builtin_amdgcn_exp2f(2.f * f.ref - f.ref2);  // (the other's reference may be a listed logit)
+        }
         n.each([&](int e) {
             const int c = l.id[e];
             if (!n.there(c)) return;
@@ -308,7 +314,7 @@ __host__ __device__ constexpr int map_words(int len) { return (len + 7 + (1 << S
 // FUSED: a workgroup has a whole row.  SUMS, GRADIENT: one chunk of one, its sums out or all of them in through a.sums.
 enum { DI_SUMS, DI_GRADIENT, DI_FUSED };
 
-template <int THREADS, int VECS, bool TAIL, bool TWO, int MODE, int SHIFT>
+template <int THREADS, int VECS, bool TAIL, int TWO, int MODE, int SHIFT>
 __global__ __launch_bounds__(THREADS, THREADS == 768 ? 3 : 4) void distill_kernel(const DistillArgs a) {
     extern __shared__ unsigned map[];
     __shared__ EntryLds        l;
@@ -361,8 +367,12 @@ __global__ __launch_bounds__(THREADS, THREADS == 768 ? 3 : 4) void distill_kerne
                     asm("" : "+v"(q[j]));
                 }
                 const float m = max_of<G>(q);
-                one.template add_pieces<G>(q, a.c2, m);
-                if (TWO) two.template add_pieces<G>(q, LOG2E, m);
+                if (TWO == TWO_SQUARES) {
+                    add_pieces_and_squares<G>(one, two, q, a.c2, m);
+                } else {
+                    one.template add_pieces<G>(q, a.c2, m);
+                    if (TWO) two.template add_pieces<G>(q, LOG2E, m);
+                }
             }
         }
         one.over_wave();
@@ -427,8 +437,9 @@ __global__ __launch_bounds__(THREADS, THREADS == 768 ? 3 : 4) void distill_kerne
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const float x = (float)as_pair(raw[i][k])[h];
-                        d[h]          = fa * __builtin_amdgcn_exp2f(fmaf(x, a.c2, -ref));
-                        if (TWO) d[h] = fmaf(fb, __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -ref2)), d[h]);
+                        const float e = __builtin_amdgcn_exp2f(fmaf(x, a.c2, -ref));
+                        d[h]          = TWO == TWO_SQUARES ? e * fmaf(fb, e, fa) : fa * e;
+                        if (TWO == TWO_ANY) d[h] = fmaf(fb, __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -ref2)), d[h]);
                     }
                     o[k] = (unsigned)f2h(d[0]) | ((unsigned)f2h(d[1]) << 16);
                 }
@@ -498,12 +509,16 @@ template <int THREADS, int VECS, int MODE, int ONLY = 2>
 int launch_distill(const DistillArgs& a, const mp_distill_desc* d, long long workgroups, hipStream_t hs) {
     constexpr int SHIFT = THREADS * VECS > 8192 ? 4 : 3;  // (a map within 64 KB)
     MP_REQUIRE(grid_fits(workgroups, THREADS), "mp_distill_scaled: too many rows");
-    const bool two    = d->hard_weight != 0.f && d->inv_temperature != 1.f;
+    const int two = d->hard_weight == 0.f || d->inv_temperature == 1.f ? TWO_NONE : d->inv_temperature == 0.5f ? TWO_SQUARES : TWO_ANY;
     const auto launch = [&](auto tail, auto second) {
         hipLaunchKernelGGL((distill_kernel<THREADS, VECS, decltype(tail)::value, decltype(second)::value, MODE, SHIFT>), dim3((unsigned)workgroups), dim3(THREADS),
                            map_words<SHIFT>(a.chunk) * sizeof(unsigned), hs, a);
     };
-    const auto by_second = [&](auto tail) { two ? launch(tail, std::true_type{}) : launch(tail, std::false_type{}); };
+    const auto by_second = [&](auto tail) {
+        if (two == TWO_NONE) launch(tail, std::integral_constant<int, TWO_NONE>{});
+        else if (two == TWO_SQUARES) launch(tail, std::integral_constant<int, TWO_SQUARES>{});
+        else launch(tail, std::integral_constant<int, TWO_ANY>{});
+    };
     if constexpr (ONLY == 2) d->tail ? by_second(std::true_type{}) : by_second(std::false_type{});
     else by_second(std::integral_constant<bool, ONLY == 1>{});
     MP_LAUNCH_CHECK("mp_distill_scaled");

@@ -139,4 +139,22 @@ struct Sums {
     }
 };
 
+// As add_pieces of one, and of two with twice its c2: exponentials that are the squares of the others.
+template <int N>
+__device__ __forceinline__ void add_pieces_and_squares(Sums<false>& one, Sums<false>& two, const u32x4* q, float c2, float top) {
+    const float to = fmaxf(one.ref, top * c2), k = __builtin_amdgcn_exp2f(one.ref - to);
+    one.s *= k;
+    two.s *= k * k;
+    one.ref = to;
+    two.ref = 2.f * to;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float e = __builtin_amdgcn_exp2f(fmaf((float)as_pair(q[i][j >> 1])[j & 1], c2, -to));
+            one.s += e;
+            two.s = fmaf(e, e, two.s);
+        }
+}
+
 }  // namespace mp

@@ -67,8 +67,9 @@ def check(x, ids, teacher, targets, c=1.0, w=1.0, hard=0.0, tail=False, scale=2.
         rest = np.ones(vocab, bool)
         rest[ids[i][ok]] = False
         left = max(0.0, 1 - q.sum()) if tail and rest.any() else 0.0
-        size[i] += w * c * (p[i] * (q.sum() + left) + (left * p[i] * rest / max(p[i][rest].sum(), 1e-300) if left else 0))
-        np.add.at(size[i], ids[i][ok], w * c * q)
+        # (what is added up, each term by its size: a weight below 0 makes no term smaller, so |w|)
+        size[i] += abs(w) * c * (p[i] * (q.sum() + left) + (left * p[i] * rest / max(p[i][rest].sum(), 1e-300) if left else 0))
+        np.add.at(size[i], ids[i][ok], abs(w) * c * q)
     if hard:
         for i, t in enumerate(targets):
             if 0 <= t < vocab:
@@ -78,7 +79,8 @@ def check(x, ids, teacher, targets, c=1.0, w=1.0, hard=0.0, tail=False, scale=2.
     err = np.abs(np32(d).astype(np.float64) - want) - tol
     assert err.max() <= 0, (err.max(), np.unravel_index(err.argmax(), err.shape))
     each = (abs(w) + abs(hard)) * unit[:, 0] * (2 + 2 * z + np.log(vocab) + np.abs(np.where(np.isfinite(t64), t64, 0)).max(1))
-    assert abs(loss.item() - float(want_loss)) <= each.mean() + 2.0 ** -20 * abs(float(want_loss)), (loss.item(), want_loss)
+    # (inf where a target is a class that cannot be, on both sides)
+    assert loss.item() == float(want_loss) or abs(loss.item() - float(want_loss)) <= each.mean() + 2.0 ** -20 * abs(float(want_loss)), (loss.item(), want_loss)
     return loss, d, buf
 
 
@@ -187,6 +189,34 @@ def test_non_finite_rows(vocab):
     assert np.isnan(loss.item())
     loss, _, _ = call(x[6:], ids[6:], teacher[6:], targets[6:])
     assert loss.item() == np.inf
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("shape", SHAPES + [(70, 131071, 100), (400, 20000, 64)], ids=str)
+def test_hard_labels_at_temperature_2(shape, tail):
+    """Where one exponential serves both: all vocabularies, a student who is sure of listed and of other classes, far logits, -inf."""
+    x, ids, teacher, targets = problem(11, *shape)
+    check(x, ids, teacher, targets, 0.5, 4.0, 0.5, tail)
+    sure = np.clip(x, -4, 4)
+    sure[0, ids[0, 0]] = 40                                               # its other classes' p at temperature 1 are below 2^-50
+    sure[-1, targets[-1]] = 3000
+    check(sure, ids, teacher, targets, 0.5, -1.0, 0.5, tail)
+    if shape[1] > 100 and shape[2] < shape[1] // 2:
+        x = (x * 2000).astype(np.float16)
+        x[0, ::3] = -np.inf
+        x[0, ids[0]] = 1.0
+        check(x, ids, teacher, targets, 0.5, 4.0, 0.5, tail)
+
+
+@pytest.mark.parametrize("vocab", [200, 140000])
+def test_non_finite_rows_at_temperature_2(vocab):
+    x, ids, teacher, targets = problem(12, 5, vocab, 4)
+    x[0, 100], x[1, 7], x[2] = np.nan, np.inf, -np.inf
+    ids[3], targets[3], x[3, 3] = -1, -1, np.nan
+    for tail in (False, True):
+        loss, d, _ = call(x, ids, teacher, targets, c=0.5, hard=0.5, tail=tail)
+        d = np32(d)
+        assert np.isnan(d[[0, 1, 2]]).all() and np.all(d[3] == 0) and np.isfinite(d[4]).all() and np.isnan(loss.item())
 
 
 def test_overflow_shows():
