@@ -6,8 +6,8 @@
 //     dx_j = S / rows (weight / temperature dL/dz_j + hard (softmax(x)_j - 1[j = target]))
 //
 // Bound by HBM: 2 bytes a class read, 2 written.  A workgroup holds a row in registers from its sums to its gradient; several of them
-// on a compute unit are in different parts of that (8192 x 32768 with 64 listed: 206 us, 5.2 TB/s).  Of rows beyond 65536 classes a unit's
-// registers hold one, and nothing is on its way while it is worked on (1021 x 131071 with 100 listed: 147 us, 3.6 TB/s, with the rest 166; in
+// on a compute unit are in different parts of that (8192 x 32768 with 64 listed: 202 us, 5.3 TB/s).  Of rows beyond 65536 classes a unit's
+// registers hold one, and nothing is on its way while it is worked on (1021 x 131071 with 100 listed: 147 us, 3.6 TB/s, with the rest 158; in
 // chunks, read twice, 194 and 208).
 // Outside A the gradient is one factor a row times the exponential.  The classes of A, at most 128, are one wave's work: their
 // gradients wait in LDS, and a map from pieces to entries tells each piece which of its elements to replace.  For r the sum over
@@ -66,10 +66,11 @@ struct Entries {
 
     __device__ __forceinline__ static int lane() { return threadIdx.x & 63; }
     __device__ __forceinline__ bool       there(int c) const { return c >= 0 && c < a.vocab; }
+    // f(slot, entry) for the lane's entries
     template <typename F>
     __device__ __forceinline__ void each(F&& f) const {
-#pragma unroll 1
-        for (int e = lane(); e < a.top; e += 64) f(e);
+        if (lane() < a.top) f(0, lane());
+        if (a.top > 64 && lane() + 64 < a.top) f(1, lane() + 64);
     }
     // word of the map for class c, or -1: another stretch's, or none
     __device__ __forceinline__ int word(const Stretch& z, int c) const { return c >= first && c < a.vocab && c - first < z.len ? (c - first + z.head) >> SHIFT : -1; }
@@ -91,12 +92,7 @@ struct Entries {
         return h;
     }
     __device__ __forceinline__ void settle(const List& h) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-            if (lane() + 64 * s < a.top) {
-                l.id[lane() + 64 * s] = h.id[s];
-                l.t[lane() + 64 * s]  = h.t[s];
-            }
+        each([&](int s, int e) { l.id[e] = h.id[s]; });
         target = h.target;
         if (lane() == 0) l.id[DI_TARGET] = target;
     }
@@ -104,69 +100,67 @@ struct Entries {
     struct Logits {
         uint16_t x[2], target;
     };
-    __device__ __forceinline__ Logits fetch_logits(long long row) const {
+    __device__ __forceinline__ Logits fetch_logits(long long row, const List& list) const {
         const uint16_t* z = a.logits + row * a.ld;
         Logits          h;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int c = l.id[min(lane() + 64 * s, a.top - 1)];
-            h.x[s]      = z[there(c) ? c : 0];
-        }
+        for (int s = 0; s < 2; ++s) h.x[s] = z[there(list.id[s]) ? list.id[s] : 0];
         h.target = z[there(target) ? target : 0];
         return h;
     }
     __device__ __forceinline__ void settle_logits(const Logits& h) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-            if (lane() + 64 * s < a.top) l.x[lane() + 64 * s] = h2f(h.x[s]);
+        each([&](int s, int e) { l.x[e] = h2f(h.x[s]); });
         if (lane() == 0) l.x[DI_TARGET] = h2f(h.target);
     }
     // into the map of the row's pieces, those that lie in the stretch
-    __device__ __forceinline__ void insert(const Stretch& z) {
+    __device__ __forceinline__ void insert(const Stretch& z, const List& h) {
         bool any = false, eq = false;
-        each([&](int e) {
-            any |= there(l.id[e]);
-            eq |= l.id[e] == target;
+        each([&](int s, int) {
+            any |= there(h.id[s]);
+            eq |= h.id[s] == target;
         });
         some   = __any(any);
         listed = __any(eq) && there(target);
         bool again = false;
         if (a.chunks > 1) {  // (entries of one class may all lie in another chunk: the map is a hash table of the whole list first)
-            each([&](int e) {
-                if (there(l.id[e])) l.info[e] = atomicExch(&map[l.id[e] & 255], (unsigned)e + 1);
+            each([&](int s, int e) {
+                if (there(h.id[s])) l.info[e] = atomicExch(&map[h.id[s] & 255], (unsigned)e + 1);
             });
             __builtin_amdgcn_wave_barrier();
-            each([&](int e) {
-                if (there(l.id[e]))
-                    for (unsigned o = l.info[e]; o; o = l.info[o - 1]) again |= l.id[o - 1] == l.id[e];
+            each([&](int s, int e) {
+                if (there(h.id[s]))
+                    for (unsigned o = l.info[e]; o; o = l.info[o - 1]) again |= l.id[o - 1] == h.id[s];
             });
-            each([&](int e) { map[l.id[e] & 255] = 0; });
+            __builtin_amdgcn_wave_barrier();
+            each([&](int s, int) { map[h.id[s] & 255] = 0; });
         }
-        const auto enter = [&](int e, unsigned flag) {
-            const int c = l.id[e], w = word(z, c);
-            if (w >= 0) l.info[e] = atomicExch(&map[w], (unsigned)e + 1) | (unsigned)((c - first + z.head) & ((1 << SHIFT) - 1)) << 8 | flag | MAP_THERE;
+        unsigned   info[2] = {0, 0}, info_t = 0;
+        int        at[2]   = {-1, -1}, at_t = -1;
+        const auto enter = [&](int c, int e, unsigned flag, int& w, unsigned& i) {
+            w = word(z, c);
+            if (w < 0) return;
+            i         = atomicExch(&map[w], (unsigned)e + 1) | (unsigned)((c - first + z.head) & ((1 << SHIFT) - 1)) << 8 | flag | MAP_THERE;
+            l.info[e] = i;
         };
-        each([&](int e) { enter(e, 0u); });
-        if (lane() == 0 && !listed) enter(DI_TARGET, MAP_TARGET);
+        each([&](int s, int e) { enter(h.id[s], e, 0u, at[s], info[s]); });
+        if (lane() == 0 && !listed) enter(target, DI_TARGET, MAP_TARGET, at_t, info_t);
         __builtin_amdgcn_wave_barrier();
-        each([&](int e) {
-            if (word(z, l.id[e]) >= 0)
-                for (unsigned o = l.info[e] & MAP_NEXT; o; o = l.info[o - 1] & MAP_NEXT) again |= l.id[o - 1] == l.id[e];
+        each([&](int s, int) {
+            for (unsigned o = info[s] & MAP_NEXT; o; o = l.info[o - 1] & MAP_NEXT) again |= l.id[o - 1] == h.id[s];
         });
         twice = __any(again);
         // the first one of a word moves into it; indices are below 256 and what moves in is above
-        const auto head = [&](int e) {
-            const int w = word(z, l.id[e]);
-            if (w >= 0 && map[w] == (unsigned)e + 1) map[w] = l.info[e] |= MAP_FIRST;
+        const auto head = [&](int e, int w, unsigned i) {
+            if (w >= 0 && map[w] == (unsigned)e + 1) map[w] = l.info[e] = i | MAP_FIRST;
         };
-        each(head);
-        if (lane() == 0 && !listed) head(DI_TARGET);
+        each([&](int s, int e) { head(e, at[s], info[s]); });
+        if (lane() == 0 && !listed) head(DI_TARGET, at_t, info_t);
     }
     // the entry's gradient, where its word of the map will find it
-    __device__ __forceinline__ void put(const Stretch& z, int e, float value) const {
-        const int w = word(z, l.id[e]);
+    __device__ __forceinline__ void put(const Stretch& z, int e, int c, unsigned info, float value) const {
+        const int w = word(z, c);
         if (w < 0) return;
-        const unsigned full = l.info[e] | (unsigned)f2h(value) << 16;
+        const unsigned full = info | (unsigned)f2h(value) << 16;
         if (full & MAP_FIRST) map[w] = full;
         else l.info[e] = full;
     }
@@ -186,54 +180,54 @@ struct RowWork {
     float                 sum_q, sum_r, r;     // Q, what 1 - Q leaves, and that or 0 where nothing outside A can be
     float                 wc, hs, u;           // S / rows times weight / temperature and hard; Q + r
     Sums<false>           one, all, at1;       // sums outside A (TAIL), over all, at temperature 1
-    float                 log_s;
+    int                   id[2];               // the lane's entries: class (-1: none), the student's logit, q
+    float                 x[2], q[2];
+    bool                  first[2];            // of its class
 
     __device__ __forceinline__ explicit RowWork(const Entries<SHIFT>& n_) : n(n_), one(1.f), all(1.f), at1(1.f) {}
-    __device__ __forceinline__ bool first(int e) const { return !n.twice || !n.l.again[e]; }
 
-    __device__ __forceinline__ void teacher() {
+    __device__ __forceinline__ void teacher(const typename Entries<SHIFT>::List& h) {
         EntryLds& l = n.l;
         sum_r       = 0.f;
         if (TAIL) {
             double sum = 0.0;
-            n.each([&](int e) {
-                const double q = n.there(l.id[e]) ? exp((double)l.t[e]) : 0.0;  // (64 bits: 1 minus their sum is often next to nothing)
-                l.q[e]         = (float)q;
-                sum += q;
+            n.each([&](int s, int e) {
+                const double v = n.there(h.id[s]) ? exp((double)h.t[s]) : 0.0;  // (64 bits: 1 minus their sum is often next to nothing)
+                l.q[e]         = (float)v;
+                sum += v;
             });
             sum   = wave_sum64(sum);
             sum_q = (float)sum;
             if (n.some && sum < 1.0) sum_r = (float)(1.0 - sum);
         } else {
-            float m = -INFINITY, sum = 0.f;
-            n.each([&](int e) { m = fmaxf(m, n.there(l.id[e]) ? l.t[e] : -INFINITY); });
+            float m = -INFINITY, sum = 0.f, v[2] = {0.f, 0.f};
+            n.each([&](int s, int) { m = fmaxf(m, n.there(h.id[s]) ? h.t[s] : -INFINITY); });
             m = wave_max(m);
             m = m == -INFINITY ? 0.f : m;
-            n.each([&](int e) {
-                const float q = n.there(l.id[e]) ? expf(l.t[e] - m) : 0.f;
-                l.q[e]        = q;
-                sum += q;
+            n.each([&](int s, int) {
+                v[s] = n.there(h.id[s]) ? expf(h.t[s] - m) : 0.f;
+                sum += v[s];
             });
             sum             = wave_sum(sum);
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            n.each([&](int e) { l.q[e] *= inv; });
+            n.each([&](int s, int e) { l.q[e] = v[s] * inv; });
             sum_q = sum * inv;
         }
         __builtin_amdgcn_wave_barrier();
         if (n.twice) {  // a class counts once, with the sum of its entries in their order
-            n.each([&](int e) {
-                float q     = 0.f;
-                bool  again = false;
+            float v[2];
+            n.each([&](int s, int e) {
+                bool again = false;
+                v[s]       = 0.f;
                 for (int j = 0; j < n.a.top; ++j)
-                    if (l.id[j] == l.id[e]) {
-                        q += l.q[j];
+                    if (l.id[j] == h.id[s]) {
+                        v[s] += l.q[j];
                         again |= j < e;
                     }
-                l.t[e]     = q;
                 l.again[e] = again;
             });
             __builtin_amdgcn_wave_barrier();
-            n.each([&](int e) { l.q[e] = l.t[e]; });
+            n.each([&](int s, int e) { l.q[e] = v[s]; });
         }
     }
     // s1, s2: sums at the temperature and (TWO) at 1, without A if TAIL
@@ -244,16 +238,24 @@ struct RowWork {
         const float        scale = (float)((double)a.st->scale / (double)a.rows);
         wc = n.some ? a.weight * a.inv_temperature * scale : 0.f, hs = real ? a.hard * scale : 0.f;
         one = all = s1, at1 = s2;
+        unsigned info[2];
+        n.each([&](int s, int e) {
+            id[s]    = l.id[e];
+            x[s]     = l.x[e];
+            q[s]     = l.q[e];
+            info[s]  = l.info[e];
+            first[s] = !n.twice || !l.again[e];
+        });
         r = one.s > 0.f ? sum_r : 0.f, u = sum_q + r;
         if (TAIL) {
             float top = -INFINITY;
-            n.each([&](int e) { top = fmaxf(top, n.there(l.id[e]) ? l.x[e] : -INFINITY); });
+            n.each([&](int s, int) { top = fmaxf(top, n.there(id[s]) ? x[s] : -INFINITY); });
             top                    = wave_max(top);
             const auto with_listed = [&](Sums<false>& t, float c2) {
                 t.move(fmaxf(t.ref, top * c2));
                 float sum = 0.f;
-                n.each([&](int e) {
-                    if (n.there(l.id[e]) && first(e)) sum += __builtin_amdgcn_exp2f(fmaf(l.x[e], c2, -t.ref));
+                n.each([&](int s, int) {
+                    if (n.there(id[s]) && first[s]) sum += __builtin_amdgcn_exp2f(fmaf(x[s], c2, -t.ref));
                 });
                 t.s += wave_sum(sum);
             };
@@ -271,16 +273,15 @@ struct RowWork {
             out = f;
             if (TWO == TWO_SQUARES) out.b = f.b * __builtin_amdgcn_exp2f(2.f * f.ref - f.ref2);  // (the other's reference may be a listed logit)
         }
-        n.each([&](int e) {
-            const int c = l.id[e];
-            if (!n.there(c)) return;
-            const float p  = __builtin_amdgcn_exp2f(fmaf(l.x[e], a.c2, -all.ref)) * inv_s;
-            const float p1 = TWO ? __builtin_amdgcn_exp2f(fmaf(l.x[e], LOG2E, -at1.ref)) * inv_1 : p;
-            n.put(z, e, wc * (p * u - l.q[e]) + (real ? hs * (p1 - (c == n.target ? 1.f : 0.f)) : 0.f));
+        n.each([&](int s, int e) {
+            if (!n.there(id[s])) return;
+            const float p  = __builtin_amdgcn_exp2f(fmaf(x[s], a.c2, -all.ref)) * inv_s;
+            const float p1 = TWO ? __builtin_amdgcn_exp2f(fmaf(x[s], LOG2E, -at1.ref)) * inv_1 : p;
+            n.put(z, e, id[s], info[s], wc * (p * u - q[s]) + (real ? hs * (p1 - (id[s] == n.target ? 1.f : 0.f)) : 0.f));
         });
         if (n.lane() == 0 && real && !n.listed) {
-            const float x = l.x[DI_TARGET];
-            n.put(z, DI_TARGET, f.a * __builtin_amdgcn_exp2f(fmaf(x, a.c2, -f.ref)) + (TWO ? f.b * __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -f.ref2)) : 0.f) - hs);
+            const float xt = l.x[DI_TARGET], e = __builtin_amdgcn_exp2f(fmaf(xt, a.c2, -f.ref));
+            n.put(z, DI_TARGET, n.target, l.info[DI_TARGET], f.a * e + (TWO ? f.b * __builtin_amdgcn_exp2f(fmaf(xt, LOG2E, -f.ref2)) : 0.f) - hs);
         }
     }
     __device__ __forceinline__ void loss(float* out) {
@@ -288,15 +289,14 @@ struct RowWork {
         EntryLds&          l     = n.l;
         const float        log_s = log2f(all.s);
         float              kl    = 0.f;
-        n.each([&](int e) {
-            const float q = l.q[e];
-            if (n.there(l.id[e]) && first(e) && q != 0.f) kl += q * (logf(q) - LN2 * (fmaf(l.x[e], a.c2, -all.ref) - log_s));
+        n.each([&](int s, int) {
+            if (n.there(id[s]) && first[s] && q[s] != 0.f) kl += q[s] * (logf(q[s]) - LN2 * (fmaf(x[s], a.c2, -all.ref) - log_s));
         });
         kl = wave_sum(kl);
         if (TAIL && r > 0.f) kl += r * (logf(r) - LN2 * ((one.ref - all.ref) + (log2f(one.s) - log_s)));
         float       sum = n.some ? a.weight * kl : 0.f;
-        const float x   = l.x[DI_TARGET];
-        if (n.there(n.target)) sum -= a.hard * (LN2 * (TWO ? fmaf(x, LOG2E, -at1.ref) - log2f(at1.s) : fmaf(x, a.c2, -all.ref) - log_s));
+        const float xt  = l.x[DI_TARGET];
+        if (n.there(n.target)) sum -= a.hard * (LN2 * (TWO ? fmaf(xt, LOG2E, -at1.ref) - log2f(at1.s) : fmaf(xt, a.c2, -all.ref) - log_s));
         if (n.lane() == 0) *out = sum;
     }
 };
@@ -336,8 +336,8 @@ __global__ __launch_bounds__(THREADS, THREADS == 768 ? 3 : 4) void distill_kerne
     lds_barrier();
     if (wave == 0) {
         n.settle(list);
-        n.insert(z);
-        if (MODE != DI_GRADIENT) logits = n.fetch_logits(row);
+        if (MODE != DI_GRADIENT) logits = n.fetch_logits(row, list);
+        n.insert(z, list);
     }
     // f(place in the piece, word of the map) for the entries of piece v
     const auto entries_of = [&](int v, auto&& f) {
@@ -346,7 +346,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 768 ? 3 : 4) void distill_kerne
                 if (SHIFT == 3 || (map_place(w) >> 3) == (v & 1)) f(map_place(w) & 7, w);
     };
     if (TAIL && MODE != DI_GRADIENT) lds_barrier();  // the map is there: sums without A
-    if (wave == 0 && MODE != DI_SUMS) work.teacher();
+    if (wave == 0 && MODE != DI_SUMS) work.teacher(list);
     int at = tid;
     asm("" : "+v"(at));  // (places of the pieces are formed again, not kept in registers)
     if (MODE != DI_GRADIENT) {
@@ -394,7 +394,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 768 ? 3 : 4) void distill_kerne
                 s1.add_sums(v[0], v[1], 0.f);
                 if (TWO) s2.add_sums(v[2], v[3], 0.f);
             }
-            n.each([&](int e) { l.x[e] = chosen[e]; });
+            n.each([&](int, int e) { l.x[e] = chosen[e]; });
             if (tid == 0) l.x[DI_TARGET] = chosen[DI_TARGET];
         } else {
             n.settle_logits(logits);
@@ -408,7 +408,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 768 ? 3 : 4) void distill_kerne
         if (MODE == DI_SUMS) {
             if (tid == 0) *reinterpret_cast<f32x4*>(a.sums + (row * a.chunks + chunk) * 4) = f32x4{s1.ref, s1.s, s2.ref, s2.s};
             if (chunk == 0) {
-                n.each([&](int e) { chosen[e] = l.x[e]; });
+                n.each([&](int, int e) { chosen[e] = l.x[e]; });
                 if (tid == 0) chosen[DI_TARGET] = l.x[DI_TARGET];
             }
         } else {
@@ -465,9 +465,8 @@ struct DistillPlan {
     int chunks, chunk;  // 0 chunks: rows in registers
 };
 // Chunks where rows do not fit, and where a long row would keep few compute units long: us, in registers / in chunks, 1, 64 and 128 rows of
-// 100000 classes 19.2 / 13.1, 20.7 / 17.7, 22.5 / 23.0, of 131071 21.6 / 13.2, 24.7 / 22.4, 27.4 / 31.4; of 50021 13.4 / 13.3, 14.6 / 17.7,
-// 15.6 / 19.7.  Chunks are at least 4096 classes, and no more than fill the chip.  even: rows start at 16-byte pieces.  (Others may take a
-// piece more.)
+// 100000 classes 19.7 / 12.0, 23.7 / 20.1, 25.3 / 26.2, of 131071 22.1 / 12.4, 26.9 / 21.3, 29.6 / 34.2; of 50021 13.5 / 12.2, 18.7 / 20.8, 19.5 / 23.3.
+// Chunks are at least 4096 classes, and no more than fill the chip.  even: rows start at 16-byte pieces.  (Others may take a piece more.)
 DistillPlan distill_plan(int rows, int vocab, bool even) {
     const int pieces = (vocab + (even ? 7 : 14)) / 8;
     if (pieces <= (rows <= 64 ? DI_FULL : DI_MOST)) return {0, vocab};
@@ -561,9 +560,9 @@ extern "C" int mp_distill_scaled_parts(const mp_distill_desc* d, const mp_half* 
     } else {
         const int  pieces = (d->vocab + (even ? 7 : 14)) / 8;
         const long long n = d->rows;
-        // Waves of a row, and pieces a lane: what was fastest of two to four forms each, us for 8192 rows with 64 classes listed, r 0 or with the
-        // rest as one: 4000 classes 4 a lane 41 / 48, 8 (half as many lanes) 50 / 55; 8192 classes 4 a lane 58 / 69, 2 73 / 87, 8 60 / 68; 16384: 8 111
-        // / 115, 4 105 / 122, 2 139 / 163; 32768: 16 207 / 223, 8 214 / 217, 4 203 / 234; 1024 x 65536: 16 59 / 64, 8 58 / 75.
+        // Waves of a row, and pieces a lane: what was fastest of two or three forms each, us for 8192 rows with 64 classes listed, r 0 or with the rest as
+        // one: 4000 classes 4 a lane 39 / 45, 8 (half as many lanes) 42 / 47; 8192 classes 4 a lane 56 / 63, 2 70 / 76, 8 57 / 63; 16384: 8 109 / 111, 4 108
+        // / 109, 2 131 / 148; 32768: 16 217 / 212, 8 207 / 198, 4 202 / 213; 1024 x 65536: 16 59 / 62, 8 63 / 69.
         if (pieces <= 64) rc = launch_distill<64, 1, DI_FUSED>(a, d, n, hs);
         else if (pieces <= 64 * 2) rc = launch_distill<64, 2, DI_FUSED>(a, d, n, hs);
         else if (pieces <= 64 * 4) rc = launch_distill<64, 4, DI_FUSED>(a, d, n, hs);
