@@ -38,7 +38,7 @@ struct DistillArgs {
 // The entries of a row, in LDS: one wave's work.  The last one is the target's.
 struct EntryLds {
     int      id[MP_TOP_MAX + 1];
-    float    t[MP_TOP_MAX], q[MP_TOP_MAX], x[MP_TOP_MAX + 1];  // the teacher's log probability, q, the student's logit
+    float    q[MP_TOP_MAX], x[MP_TOP_MAX + 1];                 // q, the student's logit
     unsigned info[MP_TOP_MAX + 1];                             // as in the map; there for those behind the first one of a word
     int      again[MP_TOP_MAX];                                // an earlier entry names the class too
 };
