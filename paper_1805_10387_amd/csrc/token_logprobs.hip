@@ -520,7 +520,7 @@ extern "C" size_t mp_token_logprobs_workspace_bytes(int rows, int vocab, int top
 extern "C" int mp_token_logprobs(int rows, int vocab, int top, const mp_half* logits, int ld, const int32_t* targets, float inv_temperature, float* logp,
                                  float* entropy, float* lse, int32_t* top_ids, float* top_logp, void* ws, size_t ws_bytes, mp_stream stream) {
     const char* const what = "mp_token_logprobs";
-    const int         rc   = logprobs_check(what, rows, vocab, ld, inv_temperature);
+    int               rc   = logprobs_check(what, rows, vocab, ld, inv_temperature);
     if (rc != MP_OK) return rc;
     MP_REQUIRE(top >= 0 && top <= vocab, "%s: %d alternatives of %d", what, top, vocab);
     if (top > MP_TOP_MAX) {
@@ -540,15 +540,17 @@ extern "C" int mp_token_logprobs(int rows, int vocab, int top, const mp_half* lo
         set_error("%s: 16-byte aligned workspace of %zu bytes needed, %zu given", what, need, ws_bytes);
         return MP_E_WORKSPACE;
     }
-    MP_REQUIRE(grid_fits((long long)rows * p.chunks, 512), "%s: too many rows", what);
     RowArgs a{vocab, ld, top, p.chunks, p.chunk, logits, targets, inv_temperature * LOG2E, logp, entropy, lse, top_logp, top_ids, static_cast<float*>(ws), nullptr};
     if (p.chunks > 1) a.lists = reinterpret_cast<u64*>(static_cast<char*>(ws) + lists_offset(rows, p));
     hipStream_t hs     = as_stream(stream);
-    const auto  launch = [&](auto threads, auto vecs) {
+    const auto  launch = [&](auto threads, auto vecs) -> int {
         constexpr int T = decltype(threads)::value, V = decltype(vecs)::value;
-        const dim3    grid((unsigned)(rows * p.chunks));
+        MP_REQUIRE(grid_fits((long long)rows * p.chunks, T), "%s: too many rows", what);
+        const dim3 grid((unsigned)(rows * p.chunks));
         if (top) hipLaunchKernelGGL((token_logprobs_kernel<T, V, true>), grid, dim3(T), 0, hs, a);
         else hipLaunchKernelGGL((token_logprobs_kernel<T, V, false>), grid, dim3(T), 0, hs, a);
+        MP_LAUNCH_CHECK("mp_token_logprobs");
+        return MP_OK;
     };
     const int pieces = (p.chunk + (even ? 7 : 14)) / 8;
     typedef std::integral_constant<int, 64>   W1;
@@ -563,17 +565,17 @@ extern "C" int mp_token_logprobs(int rows, int vocab, int top, const mp_half* lo
     // Waves of a row and pieces a lane, us with 8 alternatives, 8192 rows and 1: of 2000 64 x 4 14.9 and 5.7, 128 x 2 18.2 and 5.2; of 4000 128 x 4 22.8
     // and 5.3 (1024 rows 6.8, 512 6.7), 256 x 2 28.5 and 5.0 (7.3, 5.9); of 8192 128 x 8 32.3 and 6.0, 256 x 4 35.4 and 5.4; of 16384 256 x 8 51.7 and 6.1,
     // 512 x 4 74.7 and 6.2; of 32768 256 x 16 101 and 7.9, 512 x 8 118 and 7.3 (128 rows alike, 256 rows 9.2 and 9.4).
-    if (pieces <= 64) launch(W1{}, V1{});
-    else if (pieces <= 128) launch(W1{}, V2{});
-    else if (pieces <= 256) launch(W1{}, V4{});
-    else if (pieces <= 512 && rows >= 1024) launch(W2{}, V4{});
-    else if (pieces <= 512) launch(W4{}, V2{});
-    else if (pieces <= 1024) launch(W4{}, V4{});
-    else if (pieces <= 2048) launch(W4{}, V8{});
-    else if (pieces <= 4096 && rows <= 64) launch(W8{}, V8{});
-    else if (pieces <= 4096) launch(W4{}, V16{});
-    else launch(W8{}, V16{});
-    MP_LAUNCH_CHECK("mp_token_logprobs");
+    if (pieces <= 64) rc = launch(W1{}, V1{});
+    else if (pieces <= 128) rc = launch(W1{}, V2{});
+    else if (pieces <= 256) rc = launch(W1{}, V4{});
+    else if (pieces <= 512 && rows >= 1024) rc = launch(W2{}, V4{});
+    else if (pieces <= 512) rc = launch(W4{}, V2{});
+    else if (pieces <= 1024) rc = launch(W4{}, V4{});
+    else if (pieces <= 2048) rc = launch(W4{}, V8{});
+    else if (pieces <= 4096 && rows <= 64) rc = launch(W8{}, V8{});
+    else if (pieces <= 4096) rc = launch(W4{}, V16{});
+    else rc = launch(W8{}, V16{});
+    if (rc != MP_OK) return rc;
     if (p.chunks > 1) {
         hipLaunchKernelGGL(token_logprobs_join_kernel, dim3(rows), dim3(JOIN_THREADS), ((size_t)p.chunks * top + 8) * sizeof(u64), hs, a);
         MP_LAUNCH_CHECK("mp_token_logprobs(join)");
