@@ -523,16 +523,18 @@ class XentStep(_StepBase):
                        B.mp_softmax_xent_db_workspace_bytes(T, V) if self.db_with_loss else B.mp_loss_workspace_bytes(T, V))
 
     def set_batch(self, batch):
-        wl = self.wl
+        wl, lists = self.wl, ()
         if getattr(wl, "teacher_top", 0):
             lists = batch["teacher_ids"], batch["teacher_logp"]
             for x in lists:
                 if tuple(x.shape) != (wl.tokens, wl.teacher_top):
                     raise ValueError(f"a teacher's lists of shape {tuple(x.shape)} for {wl.tokens} tokens of {wl.teacher_top}")
-            for mine, x in zip((self.teacher_ids, self.teacher_logp), lists):
-                mine.copy_(torch.as_tensor(x))
-        self.h.copy_(_h16(batch["h"]))
-        self.targets.copy_(torch.from_numpy(np.asarray(batch["targets"], dtype=np.int32)).cuda())
+            lists = list(zip((self.teacher_ids, self.teacher_logp), map(torch.as_tensor, lists)))
+        new = [(self.h, _h16(batch["h"])), (self.targets, _i32(batch["targets"])), *lists]
+        for mine, x in new:
+            x.expand_as(mine)                       # (what does not fit raises before anything of the last batch is replaced)
+        for mine, x in new:
+            mine.copy_(x)
 
     def forward_backward(self):
         wl, w, g = self.wl, self.P.w16, self.P.g16
