@@ -529,7 +529,10 @@ class XentStep(_StepBase):
             for x in lists:
                 if tuple(x.shape) != (wl.tokens, wl.teacher_top):
                     raise ValueError(f"a teacher's lists of shape {tuple(x.shape)} for {wl.tokens} tokens of {wl.teacher_top}")
-            lists = list(zip((self.teacher_ids, self.teacher_logp), map(torch.as_tensor, lists)))
+            ids, logp = map(torch.as_tensor, lists)
+            if ids.dtype != torch.int32:            # (what is no class in 64 bits is none in 32)
+                ids = ids.long().clamp(-1, 2 ** 31 - 1)
+            lists = (self.teacher_ids, ids), (self.teacher_logp, logp)
         new = [(self.h, _h16(batch["h"])), (self.targets, _i32(batch["targets"])), *lists]
         for mine, x in new:
             x.expand_as(mine)                       # (what does not fit raises before anything of the last batch is replaced)

@@ -39,3 +39,14 @@ def test_a_batch_that_does_not_fit_replaces_nothing(step, bad):
     with pytest.raises((ValueError, RuntimeError, KeyError)):
         step.set_batch({k: v for k, v in dict(batch, **bad).items() if v is not None})
     assert all(torch.equal(a, b) for a, b in zip(kept, (step.h, step.targets, step.teacher_ids, step.teacher_logp)))
+
+
+def test_classes_of_lists_in_64_bits_keep_what_they_say(step):
+    """What is no class stays none: cut to 32 bits 2^32 + 3 would be class 3, and the least of all class 0."""
+    ids = np.array([[3, -1, 10], [2 ** 32 + 3, 2 ** 31, 2 ** 32], [-2 ** 63, 2 ** 63 - 1, -2 ** 32], [-2 ** 32 + 5, 2 ** 33 + 9, 0], [11, -100, 4], [-2 ** 31, 2 ** 31 - 1, 1],
+                    [7, 8, 9]], np.int64)
+    for given in (ids, torch.from_numpy(ids), torch.from_numpy(ids).t().contiguous().t()):
+        step.teacher_ids.fill_(6)
+        step.set_batch(dict(WL.batch(), teacher_ids=given))
+        got, there = step.teacher_ids.numpy(), (ids >= 0) & (ids < WL.vocab)
+        assert np.array_equal(got[there], ids[there]) and not ((got[~there] >= 0) & (got[~there] < WL.vocab)).any()
