@@ -377,7 +377,7 @@ int mp_token_logprobs_bwd(int rows, int vocab, const mp_half* logits, int ld, co
  *     loss = mean over rows of (weight L + hard_weight CE)
  *     dlogits = RNE16( float(S / rows) (weight inv_temperature ((Q + r) p - (j in A ? q : r p / p_rest)) + hard_weight (softmax(logits) -
  *               1[j = target])) ),  Q = sum q
- * Entries that name one class count as one with the sum of their q.  A row without entries has L = 0; without a target either, a zero
+ * Entries that name one class count as one with the sum of their q.  A list of which all entries are -inf has q = 0.  A row without entries has L = 0; without a target either, a zero
  * row of dlogits, whatever it holds.  (The factor temperature^2 that keeps gradients alike is the caller's, in weight.)  targets may be NULL
  * where hard_weight is 0.  dlogits shares ld and may be logits.
  *   ws    device, 16-byte aligned, mp_distill_workspace_bytes(desc) bytes (0 for a description that the calls refuse), of these rows or of more. */

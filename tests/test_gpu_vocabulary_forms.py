@@ -180,3 +180,24 @@ def test_the_same_rows_in_registers_and_in_chunks(tail):
         loss, d, _ = D.check(*part, hard=0.5, c=0.7, tail=tail, scale=scale)
         loss2, d2, _ = D.call(*part, hard=0.5, c=0.7, tail=tail, scale=scale, in_place=True)
         assert torch.equal(d, d2) and torch.equal(loss, loss2)
+
+
+@pytest.mark.parametrize("vocab", [500, 65537, 140000])
+def test_lists_to_which_the_teacher_gives_nothing(vocab):
+    """All entries -inf: q = 0.  Renormalised such a row has neither loss nor gradient; with the rest all of the teacher is there, L = -ln p_rest.
+    Tolerances as counted in the distillation's own tests: 2^-24 (480 + 16 |z|), times p r + r p / p_rest or what the logarithms are up to."""
+    rows, scale = 66, 2.0 ** 12
+    x, ids, teacher, targets = D.problem(14, rows, vocab, 5)
+    teacher[:] = -np.inf
+    loss, d, _ = D.call(x, ids, teacher, targets, scale=scale)
+    assert loss.item() == 0 and torch.all(d == 0)
+    loss, d, _ = D.call(x, ids, teacher, targets, scale=scale, tail=True)
+    x = x.astype(np.float64)
+    p = np.exp(x - np.log(np.exp(x).sum(1, keepdims=True)))
+    rest = p.copy()
+    np.put_along_axis(rest, ids, 0.0, 1)
+    p_rest = rest.sum(1, keepdims=True)
+    want, z = (p - rest / p_rest) * (scale / rows), np.abs(x).max(1, keepdims=True)
+    unit = 2.0 ** -24 * (480 + 16 * z)
+    assert np.all(np.abs(np32(d) - want) <= 2.0 ** -11 * np.abs(want) + 2.0 ** -25 + unit * (p + rest / p_rest) * (scale / rows))
+    assert abs(loss.item() + np.log(p_rest).mean()) <= (unit * (2 + 2 * z + np.log(vocab))).mean()
