@@ -6,9 +6,9 @@
 //     dx_j = S / rows (weight / temperature dL/dz_j + hard (softmax(x)_j - 1[j = target]))
 //
 // Bound by HBM: 2 bytes a class read, 2 written.  A workgroup holds a row in registers from its sums to its gradient; several of them
-// on a compute unit are in different parts of that (8192 x 32768 with 64 listed: 202 us, 5.3 TB/s).  Of rows beyond 65536 classes a unit's
-// registers hold one, and nothing is on its way while it is worked on (1021 x 131071 with 100 listed: 147 us, 3.6 TB/s, with the rest 158; in
-// chunks, read twice, 194 and 208).
+// on a compute unit are in different parts of that (8192 x 32768 with 64 listed and the rest: 204 us, 5.3 TB/s).  Of rows beyond 65536 classes a unit's
+// registers hold one, and nothing is on its way while it is worked on (1021 x 131071 with 100 listed: 146 us, 3.7 TB/s, with the rest 158; in
+// chunks, read twice, 194 and 208).  Times here are of calls in a row, captured and replayed over the same buffers.
 // Outside A the gradient is one factor a row times the exponential.  The classes of A, at most 128, are one wave's work: their
 // gradients wait in LDS, and a map from pieces to entries tells each piece which of its elements to replace.  For r the sum over
 // "all others" is formed without A, not as a difference of sums, which would lose it where the student is sure of A.
@@ -46,7 +46,7 @@ struct EntryLds {
 constexpr unsigned MAP_NEXT = 0xFFu, MAP_TARGET = 1u << 12, MAP_THERE = 1u << 13, MAP_FIRST = 1u << 14;
 __device__ __forceinline__ int map_place(unsigned w) { return (int)(w >> 8) & 15; }
 // Hard labels: TWO_NONE without these or at temperature 1; TWO_ANY: exponentials of their own; TWO_SQUARES, at temperature 2: squares of the
-// others (1021 x 131071 with 100 listed: without hard labels 147 us, with squares 153, with exponentials 171; 8192 x 32768 with 64 206, 221 and 248).
+// others (1021 x 131071 with 100 listed: without hard labels 146 us, with squares 151, with exponentials 170; 8192 x 32768 with 64 208, 212 and 240).
 enum { TWO_NONE, TWO_ANY, TWO_SQUARES };
 struct RowFactors {
     float a, ref, b, ref2;  // gradient outside A: a 2^(c2 x - ref) + b 2^(log2(e) x - ref2); TWO_SQUARES: e = 2^(c2 x - ref), e (a + b e)

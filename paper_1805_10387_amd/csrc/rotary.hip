@@ -4,8 +4,9 @@
 // (a cos t - b sin t, a sin t + b cos t).  Backward with u = the gradient turned back by -t: dg = sum u x^, v = u g,
 // dx = r (v - x^ mean(v x^)); r is formed again from x, so forward keeps nothing.
 //
-// Bound by HBM: forward moves 4 bytes, backward 6 bytes an element (16384 tokens of 16 + 4 heads of 128: 36 us, 4.6 TB/s, and 60 us, 4.2 TB/s;
-// without norms 36 us each way).  The angle depends on token and pair only, so a workgroup takes
+// Bound by HBM: forward moves 4 bytes, backward 6 bytes an element (16384 tokens of 16 + 4 heads of 128 in a row: 36 us, 4.6 TB/s, and 60 us, 4.2
+// TB/s, without norms 36 us each way; one launch by itself, whose last stores are still in a cache at its end, 28 and 51 + 5 us).  Times below are
+// of calls in a row, captured and replayed over buffers beyond the caches.  The angle depends on token and pair only, so a workgroup takes
 // some tokens, forms their cosines and sines once into LDS, and all heads of these tokens read them there.
 // A lane owns "units" of 2 W columns: W and their partners where halves are paired, 2 W neighbours where neighbours are; a head
 // is then d / (2 W) lanes, filled up to a power of two, whose sums go through lane permutations.
@@ -263,8 +264,8 @@ __global__ __launch_bounds__(RO_THREADS) void rope_fwd_kernel(const RopeArgs a) 
 
 // Queries, then keys: the sums for their weights are all that a lane keeps from item to item.  A workgroup has one block of tokens, several
 // only where there are more than some thousands of these, so that the weights' gradients are few partial rows: [workgroup][queries, keys][d].
-// The only workgroup writes the gradients themselves.  Three waves a SIMD for W 8 with norms: their values, sums and addresses take some 150
-// registers, and held to the 128 that four waves leave they spill (36.8 against 31.0 us for 8192 tokens of 16 + 16 heads of 64, 38.0 against 28.4
+// The only workgroup writes the gradients themselves.  Three waves a SIMD for W 8 with norms: their values, sums and addresses take 162 to
+// 165 registers, and held to the 128 that four waves leave they spill (36.8 against 31.0 us for 8192 tokens of 16 + 16 heads of 64, 38.0 against 28.4
 // for 12289 of 8 + 2 of 128); narrower ones fit.
 template <int W, bool ADJ, bool NORM, int LANES>
 __global__ __launch_bounds__(RO_THREADS, W == 8 && NORM ? 3 : 4) void rope_bwd_kernel(const RopeArgs a) {

@@ -2,9 +2,10 @@
 //
 // z = x / temperature, lse = log sum exp z, logp = z[target] - lse, entropy = lse - sum p z.  One pass: a workgroup holds a row (or a
 // chunk of one) in registers, sums against a running reference (vocab_rows.hpp), and picks the alternatives out of the
-// registers.  Bound by HBM with many rows of many classes (8192 x 32768: 97 us, 5.5 TB/s; with 64 alternatives 111 us), by the search for
-// the alternatives with short rows (8192 x 2000 with 20: 15.7 us, 9.3 without), by the chain of trips to memory and barriers with few
-// (1 x 32768 with 20: 6.5 us).
+// registers.  Bound by HBM with many rows of many classes (8192 x 32768: 101 to 105 us, 5.1 to 5.3 TB/s; with 64 alternatives 109 to 111 us), by the
+// search for the alternatives with short rows (8192 x 2000 with 20: 15.9 us, 8.8 without), by the chain of trips to memory and barriers with few
+// (1 x 32768 with 20: 7.7 us).  Times here are of calls in a row, captured and replayed over the same buffers; where forward and backward take
+// turns, forward (8192 x 32768) is 135 to 141 us, as it begins on the gradient's last stores, and backward 175.
 //
 // The top `k` of a chunk: the k-th largest of the lanes' own maxima (or the least of what each wave finds for its share of k) is a bound that at
 // least k elements reach, and with values that are spread over the lanes hardly more.  These are gathered in LDS, and each finds its place by
@@ -432,8 +433,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void token_logprobs_join_kernel(const
     }
 }
 
-// dx = RNE16(S c (g (1[target] - p) - h p (ln p + entropy))), S c = scale / temperature; bound by HBM (4 bytes an element; 8192 x 32768 205 us,
-// 5.2 TB/s).
+// dx = RNE16(S c (g (1[target] - p) - h p (ln p + entropy))), S c = scale / temperature; bound by HBM (4 bytes an element; 8192 x 32768 194 us,
+// 5.5 TB/s).
 constexpr int LPB_VECS = 4, LPB_THREADS = 256;
 __global__ __launch_bounds__(LPB_THREADS) void token_logprobs_bwd_kernel(const int vocab, const int ld, const int pieces, const uint16_t* logits,
                                                                         const int32_t* __restrict__ targets, const float c,

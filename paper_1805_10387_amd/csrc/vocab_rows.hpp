@@ -96,8 +96,9 @@ __device__ __forceinline__ float max_of_half(const u32x4 q, int h) {
 }
 
 // Sums over exponentials of base 2, y = c2 x - ref with c2 = log2(e) / temperature:  s = sum 2^y, t = sum 2^y y (for the entropy).
-// ref is the largest c2 x so far as rounded, so that y of the largest is 0 to its last bit; never below the floor, which is below
-// every finite logit, so that a row of -inf makes no NaN of differences.  +inf and NaN make s NaN.
+// ref is the largest c2 x so far, rounded: y of the largest is what that left, at most 2^-24 |c2 x| (1 where 1 / temperature is 256 and x near
+// 60000, so that its term is 2^y and not 1).  All sums of a row and all that is made of them have the same ref, so that it cancels.  Never below
+// the floor, which is below every finite logit, so that a row of -inf makes no NaN of differences.  +inf and NaN make s NaN.
 constexpr float REF_FLOOR = -70000.f;
 template <bool ENTROPY>
 struct Sums {
