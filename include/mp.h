@@ -363,7 +363,8 @@ int mp_token_logprobs(int rows, int vocab, int top, const mp_half* logits, int l
 /* Gradient of sum_r dlogp[r] logp[r] + dentropy[r] entropy[r], times the loss scale, p = exp(z - lse):
  *     dlogits = RNE16( S inv_temperature ( dlogp (1[j = target] - p) - dentropy p (ln p + entropy) ) )
  * from the forward call's logits, entropy and lse.  dlogp (with targets) or dentropy (with entropy) may be NULL, not both.  st NULL: S = 1.
- * A row whose dlogp (or target) and dentropy say 0 is zero, whatever it holds.  dlogits shares ld and may be logits. */
+ * A row whose dlogp (or target) and dentropy say 0 is zero, whatever it holds.  dlogits shares ld and may be logits.
+ * (lse is given in 32 bits, so that p is off by up to 2^-24 |lse| of itself.) */
 int mp_token_logprobs_bwd(int rows, int vocab, const mp_half* logits, int ld, const int32_t* targets, float inv_temperature,
                           const float* entropy, const float* lse, const float* dlogp, const float* dentropy, const mp_scale_state* st,
                           mp_half* dlogits, mp_stream stream);
